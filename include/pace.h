@@ -396,6 +396,66 @@ int pace_diagnostics(const double *score, const int64_t *gen_sum, const int64_t 
                      const int32_t *completion, int32_t current_version, const uint8_t *keep, int64_t n_traj,
                      const double *edges, int nbins, int64_t *hist_out, int64_t *totals_out, void *stream);
 
+/* ---- Around the step: log-probabilities, loss, products, updates --------------
+ * The step reads log-probabilities (Eq. (5)) and packs a training batch. The
+ * entry points below compute the former from a policy's logits and hidden
+ * states, and take the latter to a gradient and a weight update.
+ * Element types of matrices given as void*: */
+#define PACE_F32 0
+#define PACE_BF16 1
+#define PACE_F16 2
+/* Matrices are rows of contiguous elements, row_stride elements apart
+ * (row_stride >= the row's length), aligned to their element. Products, sums
+ * and softmax statistics are held in at least 32 bits and rounded to the
+ * output's type once, to nearest even. */
+
+/* pace_token_logprob -- log-probabilities of given tokens under the policy
+ * softmax(logits / temperature), with the entropy and the best alternatives of
+ * each row. For row i with z = logits[i, :] / temperature:
+ *   logp_out[i]    = z[token_ids[i]] - log sum exp z
+ *   entropy_out[i] = - sum p log p, p = softmax(z); a p of zero adds nothing
+ *   top_ids_out[i, 0 .. top_k), top_logp_out: the top_k tokens in the order
+ *     (logit descending, id ascending), -0 and +0 equal, and their
+ *     log-probabilities. Tokens whose logit is -inf are no alternatives;
+ *     places beyond the others hold id -1 and -inf.
+ * logits      [n_rows, vocab] of dtype, row_stride elements apart;
+ *             1 <= vocab < 2^31
+ * token_ids   int32 [n_rows]. -1 marks a row that is not scored: it is not
+ *             read, and its outputs are 0 (top: -1 and -inf). Another id
+ *             outside [0, vocab) gives a NaN logp.
+ * temperature [host] 1e-6 .. 1e6
+ * top_k       0 .. PACE_TOP_MAX, at most vocab
+ * logp_out    f32 [n_rows]; entropy_out f32 [n_rows] or NULL
+ * stats_out   f32 [n_rows, 2] or NULL: the row's largest logit and
+ *             sum exp((logits - largest) / temperature), which the backward
+ *             pass takes
+ * top_ids_out int32 [n_rows, top_k], top_logp_out f32 [n_rows, top_k] (NULL
+ *             when top_k = 0)
+ * A row of nothing but -inf has no distribution: logp -inf, entropy 0. A NaN
+ * or +inf logit makes its row's logp, entropy and top_logp NaN.
+ * workspace: pace_token_logprob_workspace_bytes() bytes. */
+#define PACE_TOP_MAX 64
+int pace_token_logprob_workspace_bytes(int64_t n_rows, int64_t vocab, int top_k, size_t *bytes_out);
+int pace_token_logprob(const void *logits, int dtype, int64_t n_rows, int64_t vocab, int64_t row_stride,
+                       const int32_t *token_ids, double temperature, int top_k, float *logp_out, float *entropy_out,
+                       float *stats_out, int32_t *top_ids_out, float *top_logp_out, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
+/* pace_token_logprob_backward -- gradient of sum_i (grad_logp[i] logp[i] +
+ * grad_entropy[i] entropy[i]) with respect to the logits:
+ *   dz_v = (g ([v = t] - p_v) - g_H p_v (log p_v + H)) / temperature
+ * logits .. temperature, stats, entropy: as given to and written by
+ * pace_token_logprob (entropy may be NULL without grad_entropy).
+ * grad_logp f32 [n_rows]; grad_entropy f32 [n_rows] or NULL (zero).
+ * grad_logits_out: [n_rows, vocab] of dtype, grad_row_stride elements apart;
+ * every element is written, zeros in rows that were not scored or had nothing
+ * left. It may be logits itself (with the same stride), which it then
+ * replaces; otherwise the two must not overlap. */
+int pace_token_logprob_backward(const void *logits, int dtype, int64_t n_rows, int64_t vocab, int64_t row_stride,
+                                const int32_t *token_ids, double temperature, const float *stats, const float *entropy,
+                                const float *grad_logp, const float *grad_entropy, void *grad_logits_out,
+                                int64_t grad_row_stride, void *stream);
+
 /* pace_time_next_kernel -- measurement hook, not part of the method.
  * Arms a one-shot timer for one phase of the device work of the NEXT call
  * made from the calling host thread to an entry point that enqueues device

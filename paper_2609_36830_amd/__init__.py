@@ -532,6 +532,99 @@ def pace_diagnostics(score, gen_sum, gen_count, completion, current_version, kee
     return hist_out, totals_out
 
 
+# ---- around the step: log-probabilities, loss, products, updates -------------
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+TOP_MAX = 64
+
+
+def _matrix(t, name: str):
+    """A device matrix with contiguous rows; returns its dtype code, rows, columns and row stride."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2:
+        raise ValueError("%s must be a device matrix" % name)
+    if t.dtype not in DTYPES:
+        raise ValueError("%s must be float32, bfloat16 or float16, got %s" % (name, t.dtype))
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError("%s must have contiguous rows" % name)
+    # a stride is only used between rows; torch leaves it free where there is one
+    return DTYPES[t.dtype], rows, cols, (t.stride(0) if rows > 1 else max(cols, 1))
+
+
+def _sized(t, dtype, shape, device, name: str):
+    """The caller's output (checked), or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if _dev(t, dtype, name).shape != torch.Size(shape) or t.device != device:
+        raise ValueError("%s must have shape %s on %s" % (name, tuple(shape), device))
+    return t
+
+
+def _vector(t, dtype, n: int, device, name: str):
+    if _dev(t, dtype, name).numel() != n or t.device != device:
+        raise ValueError("%s must hold %d elements on %s" % (name, n, device))
+    return t
+
+
+def pace_token_logprob_workspace_bytes(n_rows: int, vocab: int, top_k: int = 0) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().pace_token_logprob_workspace_bytes(int(n_rows), int(vocab), int(top_k), ctypes.byref(out)),
+           "pace_token_logprob_workspace_bytes")
+    return int(out.value)
+
+
+def token_logprob_buffers(n_rows: int, vocab: int, top_k: int, device):
+    """Outputs and workspace for repeated pace_token_logprob calls on n_rows rows
+    (pass as ``buffers``)."""
+    e = lambda shape, dt: torch.empty(shape, dtype=dt, device=device)
+    return dict(logp=e(n_rows, torch.float32), entropy=e(n_rows, torch.float32), stats=e((n_rows, 2), torch.float32),
+                top_ids=e((n_rows, top_k), torch.int32), top_logp=e((n_rows, top_k), torch.float32),
+                workspace=e(pace_token_logprob_workspace_bytes(n_rows, vocab, top_k), torch.uint8))
+
+
+def pace_token_logprob(logits, token_ids, temperature: float = 1.0, top_k: int = 0, buffers=None, stream=None):
+    """Log-probabilities of token_ids (int32, -1: row not scored) under softmax(logits / temperature).
+    Returns (logp f32[n], entropy f32[n], stats f32[n, 2], top_ids i32[n, k], top_logp f32[n, k])."""
+    dt, n, vocab, stride = _matrix(logits, "logits")
+    dev = logits.device
+    _vector(token_ids, torch.int32, n, dev, "token_ids")
+    if not 0 <= int(top_k) <= TOP_MAX:
+        raise ValueError("top_k must be in [0, %d]" % TOP_MAX)
+    b = token_logprob_buffers(n, vocab, int(top_k), dev) if buffers is None else buffers
+    logp, entropy = _sized(b["logp"], torch.float32, (n,), dev, "logp"), _sized(b["entropy"], torch.float32, (n,), dev, "entropy")
+    stats = _sized(b["stats"], torch.float32, (n, 2), dev, "stats")
+    ids, top = _sized(b["top_ids"], torch.int32, (n, top_k), dev, "top_ids"), _sized(b["top_logp"], torch.float32, (n, top_k), dev, "top_logp")
+    ws = b["workspace"]
+    _check(lib().pace_token_logprob(logits.data_ptr(), dt, n, vocab, stride, token_ids.data_ptr(), float(temperature),
+                                    int(top_k), logp.data_ptr(), entropy.data_ptr(), stats.data_ptr(), ids.data_ptr(),
+                                    top.data_ptr(), ws.data_ptr(), ws.numel(), _stream(dev, stream)), "pace_token_logprob")
+    return logp, entropy, stats, ids, top
+
+
+def pace_token_logprob_backward(logits, token_ids, stats, grad_logp, entropy=None, grad_entropy=None,
+                                temperature: float = 1.0, grad_logits_out=None, stream=None):
+    """Gradient of sum(grad_logp * logp + grad_entropy * entropy) with respect to the logits, in their type.
+    grad_logits_out may be logits itself."""
+    dt, n, vocab, stride = _matrix(logits, "logits")
+    dev = logits.device
+    _vector(token_ids, torch.int32, n, dev, "token_ids")
+    _vector(stats, torch.float32, 2 * n, dev, "stats")
+    _vector(grad_logp, torch.float32, n, dev, "grad_logp")
+    if entropy is not None:
+        _vector(entropy, torch.float32, n, dev, "entropy")
+    if grad_entropy is not None:
+        _vector(grad_entropy, torch.float32, n, dev, "grad_entropy")
+    if grad_logits_out is None:
+        grad_logits_out = torch.empty((n, vocab), dtype=logits.dtype, device=dev)
+    gdt, gn, gvocab, gstride = _matrix(grad_logits_out, "grad_logits_out")
+    if (gdt, gn, gvocab) != (dt, n, vocab) or grad_logits_out.device != dev:
+        raise ValueError("grad_logits_out must have the logits' type and shape")
+    _check(lib().pace_token_logprob_backward(logits.data_ptr(), dt, n, vocab, stride, token_ids.data_ptr(),
+                                             float(temperature), stats.data_ptr(), _ptr(entropy), grad_logp.data_ptr(),
+                                             _ptr(grad_entropy), grad_logits_out.data_ptr(), gstride, _stream(dev, stream)),
+           "pace_token_logprob_backward")
+    return grad_logits_out
+
+
 def pace_time_next_kernel(phase: int, start=None, stop=None):
     """Arm a one-shot timer on the next kernel of `phase` launched from this
     thread. start/stop are torch.cuda.Event(enable_timing=True) objects that

@@ -41,6 +41,9 @@ SIGNATURES = [
     ("pace_prefix_score", ctypes.c_int, [P, P, P, P, i64, i64, i64, i64, P, P]),
     ("pace_stale_k", ctypes.c_int, [P, P, P, i32, i64, i64, P, P, P]),
     ("pace_diagnostics", ctypes.c_int, [P, P, P, P, i32, P, i64, P, ctypes.c_int, P, P, P]),
+    ("pace_token_logprob_workspace_bytes", ctypes.c_int, [i64, i64, ctypes.c_int, P]),
+    ("pace_token_logprob", ctypes.c_int, [P, ctypes.c_int, i64, i64, i64, P, d, ctypes.c_int, P, P, P, P, P, P, sz, P]),
+    ("pace_token_logprob_backward", ctypes.c_int, [P, ctypes.c_int, i64, i64, i64, P, d, P, P, P, P, P, i64, P]),
     ("pace_time_next_kernel", ctypes.c_int, [ctypes.c_int, P, P]),
     ("pace_strerror", ctypes.c_char_p, [ctypes.c_int]),
 ]

@@ -318,6 +318,22 @@ hipError_t launch_diagnostics(const double *score, const int64_t *S, const int64
                               int32_t V, const uint8_t *keep, int64_t n, const double *edges, int nbins,
                               int64_t *hist, int64_t *totals, hipStream_t stream);
 
+// ---- log-probabilities of given tokens -----------------------------------------
+constexpr int kTopMax = 64;          // alternatives of a row, at most: one a lane
+struct LogprobOut {
+    float *logp, *entropy, *stats;   // entropy and stats may be null
+    int32_t *top_ids;
+    float *top_logp;
+};
+size_t logprob_ws_bytes(int64_t rows, int64_t vocab, int top_k);
+hipError_t launch_token_logprob(const void *logits, int dtype, int64_t rows, int64_t vocab, int64_t stride,
+                                const int32_t *ids, double temperature, int top_k, const LogprobOut &out, void *ws,
+                                hipStream_t stream);
+hipError_t launch_token_logprob_backward(const void *logits, int dtype, int64_t rows, int64_t vocab, int64_t stride,
+                                         const int32_t *ids, double temperature, const float *stats,
+                                         const float *entropy, const float *g_logp, const float *g_entropy, void *grad,
+                                         int64_t grad_stride, hipStream_t stream);
+
 // ---- validate --------------------------------------------------------------
 hipError_t launch_validate(const int32_t *tags, const int64_t *offsets, int64_t n, int64_t n_tokens,
                            const int32_t *completion, int32_t V, const double *window, int64_t W,

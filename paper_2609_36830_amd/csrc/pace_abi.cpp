@@ -9,6 +9,7 @@
 #include <hip/hip_runtime_api.h>
 
 #include "../../include/pace.h"
+#include "elem.hpp"
 #include "kernels.hpp"
 
 #pragma clang fp contract(off)
@@ -558,6 +559,63 @@ int pace_diagnostics(const double *score, const int64_t *gen_sum, const int64_t 
         return PACE_ERR_INVALID_ARG;
     return hip_status(launch_diagnostics(score, gen_sum, gen_count, completion, current_version, keep, n_traj,
                                          edges, nbins, hist_out, totals_out, (hipStream_t)stream));
+}
+
+static_assert(PACE_F32 == kF32 && PACE_BF16 == kBf16 && PACE_F16 == kF16, "element types");
+static_assert(PACE_TOP_MAX == kTopMax, "alternatives");
+
+// Rows of `cols` elements `stride` apart, as the operators on matrices take them.
+static bool rows_ok(const void *p, int dtype, int64_t rows, int64_t cols, int64_t stride) {
+    if (dtype < 0 || dtype >= kElemTypes || rows < 0 || rows >= INT32_MAX || cols < 1 || cols >= INT32_MAX) return false;
+    if (stride < cols || (rows > 0 && stride > INT64_MAX / 4 / rows)) return false;
+    return rows == 0 || (p != nullptr && aligned(p, elem_bytes_of(dtype)));
+}
+
+// c = log2(e) / temperature and its inverse stay normal binary32 numbers.
+static bool temperature_ok(double t) { return t >= 1e-6 && t <= 1e6; }
+
+int pace_token_logprob_workspace_bytes(int64_t n_rows, int64_t vocab, int top_k, size_t *bytes_out) {
+    if (!bytes_out || n_rows < 0 || n_rows >= INT32_MAX || vocab < 1 || vocab >= INT32_MAX || top_k < 0 || top_k > kTopMax)
+        return PACE_ERR_INVALID_ARG;
+    *bytes_out = logprob_ws_bytes(n_rows, vocab, top_k);
+    return PACE_OK;
+}
+
+int pace_token_logprob(const void *logits, int dtype, int64_t n_rows, int64_t vocab, int64_t row_stride,
+                       const int32_t *token_ids, double temperature, int top_k, float *logp_out, float *entropy_out,
+                       float *stats_out, int32_t *top_ids_out, float *top_logp_out, void *workspace,
+                       size_t workspace_bytes, void *stream) {
+    const TimerScope timers;
+    if (!rows_ok(logits, dtype, n_rows, vocab, row_stride) || !temperature_ok(temperature)) return PACE_ERR_INVALID_ARG;
+    if (top_k < 0 || top_k > kTopMax || top_k > vocab) return PACE_ERR_INVALID_ARG;
+    if (n_rows > 0 && (!token_ids || !logp_out || (top_k > 0 && (!top_ids_out || !top_logp_out)))) return PACE_ERR_INVALID_ARG;
+    if (!aligned(token_ids, 4) || !aligned(logp_out, 4) || !aligned(entropy_out, 4) || !aligned(stats_out, 4) ||
+        !aligned(top_ids_out, 4) || !aligned(top_logp_out, 4))
+        return PACE_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < logprob_ws_bytes(n_rows, vocab, top_k))
+        return PACE_ERR_WORKSPACE;
+    return hip_status(launch_token_logprob(logits, dtype, n_rows, vocab, row_stride, token_ids, temperature, top_k,
+                                           LogprobOut{logp_out, entropy_out, stats_out, top_ids_out, top_logp_out},
+                                           workspace, (hipStream_t)stream));
+}
+
+int pace_token_logprob_backward(const void *logits, int dtype, int64_t n_rows, int64_t vocab, int64_t row_stride,
+                                const int32_t *token_ids, double temperature, const float *stats, const float *entropy,
+                                const float *grad_logp, const float *grad_entropy, void *grad_logits_out,
+                                int64_t grad_row_stride, void *stream) {
+    const TimerScope timers;
+    if (!rows_ok(logits, dtype, n_rows, vocab, row_stride) || !rows_ok(grad_logits_out, dtype, n_rows, vocab, grad_row_stride) ||
+        !temperature_ok(temperature))
+        return PACE_ERR_INVALID_ARG;
+    if (n_rows > 0 && (!token_ids || !stats || !grad_logp || (grad_entropy && !entropy))) return PACE_ERR_INVALID_ARG;
+    // In place only element for element.
+    if (grad_logits_out == logits && grad_row_stride != row_stride) return PACE_ERR_INVALID_ARG;
+    if (!aligned(token_ids, 4) || !aligned(stats, 4) || !aligned(entropy, 4) || !aligned(grad_logp, 4) ||
+        !aligned(grad_entropy, 4))
+        return PACE_ERR_INVALID_ARG;
+    return hip_status(launch_token_logprob_backward(logits, dtype, n_rows, vocab, row_stride, token_ids, temperature, stats,
+                                                    entropy, grad_logp, grad_entropy, grad_logits_out, grad_row_stride,
+                                                    (hipStream_t)stream));
 }
 
 static_assert(PACE_PHASE_COUNT == kPhaseCount, "phase count");

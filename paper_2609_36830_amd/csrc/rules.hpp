@@ -87,4 +87,21 @@ inline bool small_step_ok(int64_t n, int64_t n_tokens, int n_cols, int64_t budge
     return n <= kSmallMaxN && expected_kept(n, n_tokens, n - budget) <= most;
 }
 
+// ---- log-probabilities (logprob.hip) --------------------------------------------
+// Workgroups that share a row of logits: enough rows' parts for the chip, each
+// of at least kLogprobPart logits, at most one part a lane of the joining wave.
+constexpr int64_t kLogprobFill = 2048;
+constexpr int64_t kLogprobPart = 8192;
+inline int64_t logprob_parts(int64_t rows, int64_t vocab) {
+    const int64_t want = rows > 0 ? (kLogprobFill + rows - 1) / rows : 1, most = vocab / kLogprobPart;
+    const int64_t parts = want < most ? want : most;
+    return parts < 1 ? 1 : (parts > 64 ? 64 : parts);
+}
+// The backward pass has nothing to join: parts of 16,384 logits as far as the
+// grid can number them.
+inline int64_t logprob_backward_parts(int64_t rows, int64_t vocab) {
+    const int64_t parts = (vocab + 16383) / 16384, most = rows > 0 ? INT32_MAX / rows : 1;
+    return parts < most ? parts : most;
+}
+
 }  // namespace pace

@@ -1,0 +1,321 @@
+"""GPU tests of pace_token_logprob and its backward pass against a plain
+implementation in binary64 on the CPU.
+
+Tolerances. u = 2^-24 is half a unit of binary32. A thread adds at most
+T = vocab / 512 + 32 terms one after another (each within 4u of its own value:
+one fused step, one exp2), and at most 16 joins follow, so the sum S and the
+weighted sum are within (T + 64) u relative of their terms' absolute sum. Hence
+  |logp error|    <= (T + 64) u + 8 u (|logp| + log S)
+  |entropy error| <= (T + 64) u (2 + H + mean |log p|) , mean |log p| = H
+  |dz error|      <= |p part| ((T + 64) u + 8 u (|log p| + 2)) + u |dz| + the output type's rounding."""
+import math
+import sys
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+HALF_ULP = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+TINY = {torch.float32: 1e-38, torch.bfloat16: 1e-38, torch.float16: 2.0 ** -25}
+
+
+def say(msg):
+    sys.stdout.write("[gpu] %s\n" % msg)
+    sys.stdout.flush()
+
+
+@pytest.fixture(scope="module")
+def pace():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import os
+    from paper_2609_36830_amd import _lib
+    if not os.path.exists(_lib.library_path):
+        from paper_2609_36830_amd import build
+        build.build()
+    import paper_2609_36830_amd as pace
+    return pace
+
+
+def reference(z, ids, temperature, k, g=None, gh=None):
+    """logp, entropy, top ids, top logp and dz of CPU logits z, in binary64."""
+    z = z.double()
+    n, vocab = z.shape
+    live, known = ids != -1, (ids >= 0) & (ids < vocab)
+    m = z.max(1, keepdim=True).values
+    none = m[:, 0] == -math.inf
+    d = torch.where(none[:, None], 0.0, z - torch.where(none[:, None], 0.0, m)) / temperature
+    e = torch.where(z == -math.inf, 0.0, torch.exp(d))
+    s = e.sum(1, keepdim=True)
+    p = torch.where(none[:, None], 0.0, e / s)
+    lp = torch.where(z == -math.inf, -math.inf, d - torch.log(s))
+    lp = torch.where(torch.isnan(z).any(1, keepdim=True), math.nan, lp)
+    plp = torch.where(p > 0, p * lp, torch.where(torch.isnan(p), p, 0.0))
+    h = torch.where(none, 0.0, -plp.sum(1))
+    t = ids.long().clamp(0, vocab - 1)[:, None]
+    logp = torch.where(known, lp.gather(1, t)[:, 0], math.nan)
+    out = {"logp": torch.where(live, logp, 0.0), "entropy": torch.where(live, h, 0.0), "lse": torch.log(s[:, 0])}
+    order = torch.from_numpy(np.stack([np.lexsort((np.arange(vocab), -(r + 0.0))) for r in z.numpy()]))[:, :k]
+    val = z.gather(1, order)
+    absent = (val == -math.inf) | ~live[:, None]
+    out["top_ids"] = torch.where(absent, -1, order).to(torch.int32)
+    out["top_logp"] = torch.where(absent, -math.inf, lp.gather(1, order))
+    if g is not None:
+        one = torch.zeros_like(z).scatter_(1, t, 1.0) * known[:, None]
+        dz = g.double()[:, None] * (one - p)
+        part = (g.double()[:, None] * p).abs()
+        if gh is not None:
+            dz = dz - gh.double()[:, None] * (plp + p * h[:, None])
+            part = part + (gh.double()[:, None] * p).abs() * (torch.where(p > 0, lp.abs(), 0.0) + h[:, None])
+        dead = none | ~live
+        out["dz"] = torch.where(dead[:, None], 0.0, dz / temperature)
+        out["part"] = torch.where(dead[:, None], 0.0, part / temperature)
+        out["lp"] = torch.where(p > 0, lp, 0.0)
+    return out
+
+
+def close(name, got, want, tol):
+    got, want = got.double().cpu(), want.double()
+    fin = torch.isfinite(want)
+    assert torch.equal(fin, torch.isfinite(got)), name
+    assert torch.equal(torch.isnan(want), torch.isnan(got)), name
+    inf = torch.isinf(want)
+    assert torch.equal(got[inf], want[inf]), name
+    over = (got - want).abs()[fin] - tol.expand_as(want)[fin]
+    assert over.numel() == 0 or float(over.max()) <= 0, (name, float(over.max()))
+
+
+def size(x):
+    """|x| where it is a finite number (infinities and NaN are compared as such)."""
+    return torch.nan_to_num(x.abs(), nan=0.0, posinf=0.0)
+
+
+def check(pace, z, ids, temperature=1.0, k=0, gh=False, seed=0, inplace=False):
+    """z, ids on the GPU; z may be a view with wider rows."""
+    n, vocab = z.shape
+    gen = torch.Generator().manual_seed(seed)
+    g = torch.randn(n, generator=gen)
+    ge = torch.randn(n, generator=gen) if gh else None
+    logp, ent, stats, top_ids, top_logp = pace.pace_token_logprob(z, ids, temperature, k)
+    zc = z.cpu()
+    ref = reference(zc, ids.cpu(), temperature, k, g, ge)
+    terms = (vocab / 512 + 96) * U
+    lse = size(ref["lse"])
+    close("logp", logp, ref["logp"], terms + 8 * U * (size(ref["logp"]) + lse))
+    close("entropy", ent, ref["entropy"], terms * (2 + 2 * torch.nan_to_num(ref["entropy"])) + 8 * U * lse)
+    if k:
+        nan = torch.isnan(zc).any(1)
+        assert torch.equal(top_ids.cpu()[~nan], ref["top_ids"][~nan])
+        assert bool(((top_ids.cpu() >= -1) & (top_ids.cpu() < vocab)).all())
+        near = size(ref["top_logp"])
+        close("top_logp", top_logp[~nan.to(DEV)], ref["top_logp"][~nan], (terms + 8 * U * (near + lse[:, None]))[~nan])
+    zin = z.clone() if inplace else z
+    dz = pace.pace_token_logprob_backward(zin, ids, stats, g.to(DEV), ent if gh else None, ge.to(DEV) if gh else None,
+                                          temperature, grad_logits_out=zin if inplace else None)
+    fine = torch.isfinite(zc).all(1) | (ids.cpu() == -1) | ~(torch.isnan(zc) | (zc == math.inf)).any(1)
+    tol = (ref["part"] * (terms + 8 * U * (ref["lp"].abs() + 2)) + (ref["dz"].abs() + ref["part"] * U) * 2 * HALF_ULP[z.dtype] + TINY[z.dtype])
+    close("dz", dz[fine.to(DEV)], ref["dz"][fine], tol[fine])
+    return logp, ent, stats, top_ids, top_logp, dz
+
+
+def make(n, vocab, dtype, seed, scale=2.5, stride=None, lead=0):
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    z = (scale * torch.randn(n, vocab, generator=gen, device=DEV)).to(dtype)
+    ids = torch.randint(0, vocab, (n,), generator=gen, device=DEV, dtype=torch.int32)
+    if stride or lead:
+        stride = stride or vocab
+        buf = torch.full((lead + n * stride,), float("nan"), dtype=dtype, device=DEV)
+        view = buf[lead:].view(n, stride)[:, :vocab]
+        view.copy_(z)
+        z = view
+    return z, ids
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("n,vocab,k,temperature", [
+    (1, 1, 1, 1.0), (1, 2, 2, 0.5), (2, 7, 7, 1.0), (3, 8, 1, 2.0), (5, 513, 64, 1.0), (4, 4096, 20, 0.7), (3, 16391, 5, 1.0),
+    (2, 65536, 64, 1.3), (3, 70001, 20, 1.0), (300, 1000, 20, 1.0), (257, 16384, 3, 1.0), (1, 150000, 20, 0.7)])
+def test_shapes(pace, dtype, n, vocab, k, temperature):
+    say("logprob %s n=%d vocab=%d k=%d" % (dtype, n, vocab, k))
+    z, ids = make(n, vocab, dtype, 7 * n + vocab)
+    check(pace, z, ids, temperature, k, gh=(n % 2 == 1), seed=n)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("vocab,stride,lead", [(1000, 1003, 0), (50021, 50021, 1), (4097, 4100, 3), (40000, 40001, 5)])
+def test_strides_and_starts(pace, dtype, vocab, stride, lead):
+    """Rows wider than the vocabulary and at odd starts: the elements between rows are NaN and not read."""
+    say("logprob strides %s vocab=%d stride=%d lead=%d" % (dtype, vocab, stride, lead))
+    z, ids = make(9, vocab, dtype, vocab, stride=stride, lead=lead)
+    check(pace, z, ids, 1.0, 20, gh=True)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [6, 2050])
+def test_backward_in_place_and_into_wider_rows(pace, dtype, n):
+    say("logprob backward in place %s n=%d" % (dtype, n))
+    z, ids = make(n, 777, dtype, 3)
+    dz = check(pace, z, ids, 0.9, 0, gh=True, inplace=True)[-1]
+    logp, ent, stats, _, _ = pace.pace_token_logprob(z, ids, 0.9)
+    gen = torch.Generator().manual_seed(0)
+    g, ge = torch.randn(n, generator=gen).to(DEV), torch.randn(n, generator=gen).to(DEV)
+    wide = torch.full((n, 801), 5.0, dtype=dtype, device=DEV)
+    pace.pace_token_logprob_backward(z, ids, stats, g, ent, ge, 0.9, grad_logits_out=wide[:, 3:780])
+    assert torch.equal(wide[:, 3:780], dz)
+    assert bool((wide[:, :3] == 5).all()) and bool((wide[:, 780:] == 5).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("vocab", [40, 3000, 40000])
+def test_masks_and_special_rows(pace, dtype, vocab):
+    """Rows not scored (full of NaN, not read), vocabulary entries masked by -inf and by the type's lowest value,
+    rows with nothing left, with one entry left, of equal logits, rising rows, unknown ids, NaN and +inf."""
+    say("logprob special rows %s vocab=%d" % (dtype, vocab))
+    z, ids = make(16, vocab, dtype, vocab)
+    low = torch.finfo(dtype).min
+    z[0] = float("nan"); ids[0] = -1
+    z[1, vocab // 2:] = -math.inf; ids[1] = 0
+    z[2, vocab // 3:] = low; ids[2] = 1
+    z[3] = -math.inf
+    z[4] = low
+    z[5] = -math.inf; z[5, 17] = 3.0; ids[5] = 17
+    z[6] = 1.5
+    z[7] = torch.linspace(-8, 8, vocab, device=DEV).to(dtype)
+    z[8] = torch.linspace(8, -8, vocab, device=DEV).to(dtype)
+    ids[9] = vocab; ids[10] = -7
+    z[11, 20] = float("nan")
+    z[12, 5] = math.inf
+    z[13, 3] = torch.finfo(dtype).max / 4
+    z[14, 1:] = -math.inf; ids[14] = 2                 # the given token itself is masked out
+    z[15, ::2] = 0.0; z[15, 1::2] = -0.0               # -0 and +0 are ties
+    # a +inf logit: only that its row is NaN is asserted
+    logp, ent, stats, top_ids, top_logp = pace.pace_token_logprob(z, ids, 1.0, 20)
+    assert bool(torch.isnan(logp[12])) and bool(torch.isnan(ent[12])) and bool(torch.isnan(top_logp[12]).any())
+    z[12] = 0.25
+    check(pace, z, ids, 1.0, 20, gh=True)
+    check(pace, z, ids, 1.0, 0)
+
+
+@pytest.mark.parametrize("temperature", [1e-6, 1e-3, 1e3, 1e6])
+def test_temperatures(pace, temperature):
+    say("logprob temperature %g" % temperature)
+    z, ids = make(5, 2001, torch.float32, 5)
+    z[1] = torch.finfo(torch.float32).min
+    ids[2] = int(z[2].argmax())
+    got = pace.pace_token_logprob(z, ids, temperature, 4)
+    ref = reference(z.cpu(), ids.cpu(), temperature, 4)
+    # relative to the largest |z| / temperature: z c - m c is rounded once at that size
+    tol = (2001 / 512 + 96) * U + 8 * U * (z[[0, 2, 3, 4]].abs().max().item() / temperature + 20) + 8 * U * ref["logp"].abs()
+    close("logp", got[0], ref["logp"], tol)
+    assert torch.equal(got[3].cpu(), ref["top_ids"])
+
+
+def test_rows_beyond_32_bits(pace):
+    """Rows that lie more than 2^31 elements apart."""
+    stride = (1 << 30) + 3
+    say("logprob rows %d elements apart" % stride)
+    buf = torch.empty(3 * stride, dtype=torch.bfloat16, device=DEV)
+    z = buf.view(3, stride)[:, :30011]
+    z.copy_(make(3, 30011, torch.bfloat16, 1)[0])
+    ids = torch.tensor([5, 30010, 77], dtype=torch.int32, device=DEV)
+    logp, ent, stats, top_ids, _ = pace.pace_token_logprob(z, ids, 1.0, 5)
+    ref = pace.pace_token_logprob(z.contiguous(), ids, 1.0, 5)
+    assert torch.equal(logp, ref[0]) and torch.equal(ent, ref[1]) and torch.equal(top_ids, ref[3])
+    g = torch.ones(3, device=DEV)
+    want = pace.pace_token_logprob_backward(z.contiguous(), ids, stats, g)
+    assert torch.equal(pace.pace_token_logprob_backward(z, ids, stats, g, grad_logits_out=z), want)
+
+
+def test_gradient_against_differences(pace):
+    """Central differences of the forward kernel along random directions. With step h the forward's error enters as
+    error / h, and the third derivative of a log-sum-exp along a direction of entries +-1 is at most 8 (of the entropy
+    at most 64 with H < 8): tolerance (weights' sum) (2 e / h + 64 h^2 / 6)."""
+    say("logprob gradient against differences")
+    n, vocab, h = 6, 900, 2.0 ** -7
+    z, ids = make(n, vocab, torch.float32, 11, scale=1.0)
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    g, ge = torch.randn(n, generator=gen, device=DEV), 0.1 * torch.randn(n, generator=gen, device=DEV)
+    logp, ent, stats, _, _ = pace.pace_token_logprob(z, ids)
+    dz = pace.pace_token_logprob_backward(z, ids, stats, g, ent, ge).double()
+
+    def f(zz):
+        a, b, _, _, _ = pace.pace_token_logprob(zz, ids)
+        return (g.double() * a.double() + ge.double() * b.double()).sum().item()
+
+    weight = float(g.abs().sum() + ge.abs().sum())
+    e = 110 * U * 20
+    for trial in range(4):
+        v = torch.randint(0, 2, (n, vocab), generator=gen, device=DEV).float() * 2 - 1
+        num = (f(z + h * v) - f(z - h * v)) / (2 * h)
+        # z + h v is rounded in binary32: a direction off by 2^-24 |z| / h at most
+        tol = weight * (2 * e / (2 * h) + 64 * h * h / 6 + 8 * U / h)
+        assert abs(num - float((dz * v.double()).sum())) <= tol
+
+
+def test_streams_graph_and_repeats(pace):
+    """Bit-identical on repeats, on another stream, and on replays of a captured graph with other work between them."""
+    say("logprob repeats, streams, graph")
+    z, ids = make(40, 60001, torch.bfloat16, 4)
+    g = torch.randn(40, device=DEV)
+    b = pace.token_logprob_buffers(40, 60001, 20, DEV)
+    grad = torch.empty_like(z)
+
+    def run(stream=None):
+        out = pace.pace_token_logprob(z, ids, 1.0, 20, buffers=b, stream=stream)
+        pace.pace_token_logprob_backward(z, ids, out[2], g, grad_logits_out=grad, stream=stream)
+
+    outs = lambda: [b[k].clone() for k in ("logp", "entropy", "stats", "top_ids", "top_logp")] + [grad.clone()]
+    run()
+    ref = outs()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for t in (b["logp"], grad):
+        t.zero_()
+    torch.cuda.synchronize()
+    run(side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(outs(), ref))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for _ in range(3):
+        for t in (b["logp"], b["top_ids"], grad, b["workspace"]):
+            t.fill_(7)
+        (z.float() @ torch.ones(60001, 3, device=DEV)).sum()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(outs(), ref))
+
+
+def test_no_rows(pace):
+    say("logprob no rows")
+    z = torch.empty(0, 500, device=DEV)
+    ids = torch.empty(0, dtype=torch.int32, device=DEV)
+    out = pace.pace_token_logprob(z, ids, 1.0, 3)
+    assert out[0].numel() == 0 and out[3].shape == (0, 3)
+    assert pace.pace_token_logprob_backward(z, ids, out[2], out[0]).shape == (0, 500)
+
+
+def test_refusals(pace):
+    say("logprob refusals")
+    z, ids = make(4, 100, torch.float32, 1)
+    ok = pace.pace_token_logprob(z, ids)
+    g = torch.ones(4, device=DEV)
+    for bad in (lambda: pace.pace_token_logprob(z.double(), ids), lambda: pace.pace_token_logprob(z.cpu(), ids),
+                lambda: pace.pace_token_logprob(z.t(), ids), lambda: pace.pace_token_logprob(z, ids.long()),
+                lambda: pace.pace_token_logprob(z, ids[:3]), lambda: pace.pace_token_logprob(z, ids, top_k=65),
+                lambda: pace.pace_token_logprob(z, ids, buffers=pace.token_logprob_buffers(3, 100, 0, DEV)),
+                lambda: pace.pace_token_logprob_backward(z, ids, ok[2], g[:2]),
+                lambda: pace.pace_token_logprob_backward(z, ids, ok[2], g, grad_logits_out=z[:, :50]),
+                lambda: pace.pace_token_logprob_backward(z, ids, ok[2], g, grad_logits_out=z.bfloat16())):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: pace.pace_token_logprob(z, ids, temperature=0.0), lambda: pace.pace_token_logprob(z, ids, temperature=float("nan")),
+                lambda: pace.pace_token_logprob(z[:, :10], ids, top_k=11),
+                lambda: pace.pace_token_logprob_backward(z, ids, ok[2], g, grad_entropy=g)):
+        with pytest.raises(pace.PaceError):
+            bad()

@@ -1,0 +1,48 @@
+"""CPU tests of the host checks of the operators around the filter step: every
+refusal returns before any launch, so no GPU is needed."""
+import os
+
+import pytest
+
+FAKE = 0x100000   # aligned, never dereferenced
+
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_2609_36830_amd import _lib
+    if not os.path.exists(_lib.library_path):
+        from paper_2609_36830_amd import build
+        build.build()
+    return _lib.lib()
+
+
+def test_token_logprob_host_argument_errors(L):
+    def call(z=FAKE, dt=0, n=4, v=100, st=100, ids=FAKE, t=1.0, k=0, lp=FAKE, ti=FAKE, tl=FAKE, ws=FAKE, wsb=1 << 30):
+        return L.pace_token_logprob(z, dt, n, v, st, ids, t, k, lp, FAKE, FAKE, ti, tl, ws, wsb, None)
+
+    for kw in (dict(z=None), dict(z=FAKE + 2), dict(dt=3), dict(dt=-1), dict(n=-1), dict(v=0), dict(v=2 ** 31), dict(st=99),
+               dict(n=2 ** 31 - 2, st=2 ** 40), dict(ids=None), dict(ids=FAKE + 2), dict(t=0.0), dict(t=-1.0), dict(t=1e-7),
+               dict(t=float("inf")), dict(t=float("nan")), dict(k=-1), dict(k=65), dict(v=10, st=10, k=11), dict(lp=None),
+               dict(k=3, ti=None), dict(k=3, tl=None), dict(lp=FAKE + 1)):
+        assert call(**kw) == -1, kw
+    for kw in (dict(ws=None), dict(ws=FAKE + 64), dict(wsb=64), dict(n=2, v=150000, st=150000, k=20, wsb=4096)):
+        assert call(**kw) == -2, kw
+    assert call(dt=1, z=FAKE + 2, wsb=0) == -2          # two-byte elements need two-byte alignment only
+
+
+def test_token_logprob_backward_host_argument_errors(L):
+    def call(z=FAKE, dt=0, n=4, v=100, st=100, ids=FAKE, t=1.0, stats=FAKE, ent=FAKE, g=FAKE, ge=None, out=FAKE * 2, ost=100):
+        return L.pace_token_logprob_backward(z, dt, n, v, st, ids, t, stats, ent, g, ge, out, ost, None)
+
+    for kw in (dict(z=None), dict(out=None), dict(ost=99), dict(dt=4), dict(t=0.0), dict(stats=None), dict(g=None), dict(ids=None),
+               dict(ent=None, ge=FAKE), dict(out=FAKE, ost=101), dict(g=FAKE + 2), dict(n=-1)):
+        assert call(**kw) == -1, kw
+
+
+def test_token_logprob_workspace(L):
+    import paper_2609_36830_amd as pace
+    assert pace.pace_token_logprob_workspace_bytes(0, 10) >= 256
+    assert pace.pace_token_logprob_workspace_bytes(10 ** 6, 150000, 64) < 1 << 20      # whole rows: nothing to join
+    for bad in ((-1, 10, 0), (1, 0, 0), (1, 10, 65)):
+        with pytest.raises(pace.PaceError):
+            pace.pace_token_logprob_workspace_bytes(*bad)
