@@ -456,6 +456,37 @@ int pace_token_logprob_backward(const void *logits, int dtype, int64_t n_rows, i
                                 const float *grad_logp, const float *grad_entropy, void *grad_logits_out,
                                 int64_t grad_row_stride, void *stream);
 
+/* pace_policy_loss -- the clipped policy objective of a packed batch, with its
+ * gradient. For a response token (tag != -1) of trajectory i with
+ * k = scale * weight[i] * advantage[i], d = lp_new - lp_behavior (a binary32
+ * difference) and r = exp(d):
+ *   k > 0: loss = -k min(r, 1 + clip_high)
+ *   k < 0: loss = -k min(max(r, 1 - clip_low), dual_clip)
+ *   gradient with respect to lp_new: -k r, or 0 where a bound holds, that is
+ *   where d is beyond the bound's logarithm rounded to binary32
+ * (k = 0: both are 0). With scale = 1 / (tokens of the batch) and no weights
+ * the total loss is the mean over tokens; weights 1 / T_i give means over
+ * trajectories.
+ * lp_new, lp_behavior f32 [n_tokens]; tags int32 [n_tokens] or NULL (every
+ *   token counts). What stands at masked tokens has no effect.
+ * offsets int64 [n_traj+1], non-decreasing; tokens outside every trajectory
+ *   (behind offsets[n_traj], where columns are wider than the batch) get a
+ *   gradient of 0 and are not read. n_tokens < 2^40.
+ * advantage f32 [n_traj]; weight f32 [n_traj] or NULL (1)
+ * scale [host] finite; clip_low in [0, 1); clip_high >= 0; dual_clip > 1
+ *   (either upper bound may be infinite)
+ * grad_out f32 [n_tokens], every element written
+ * loss_out f32 [n_traj]: sum of the trajectory's losses
+ * kl_out f32 [n_traj] or NULL: sum of exp(d) - 1 - d over its response tokens
+ * clipped_out int32 [n_traj] or NULL: how many of them a bound holds for
+ * Sums are binary64, in an order fixed by the arguments.
+ * workspace: pace_policy_loss_workspace_bytes() bytes. */
+int pace_policy_loss_workspace_bytes(int64_t n_traj, int64_t n_tokens, size_t *bytes_out);
+int pace_policy_loss(const float *lp_new, const float *lp_behavior, const int32_t *tags, const int64_t *offsets,
+                     int64_t n_traj, int64_t n_tokens, const float *advantage, const float *weight, double scale,
+                     double clip_low, double clip_high, double dual_clip, float *grad_out, float *loss_out, float *kl_out,
+                     int32_t *clipped_out, void *workspace, size_t workspace_bytes, void *stream);
+
 /* pace_time_next_kernel -- measurement hook, not part of the method.
  * Arms a one-shot timer for one phase of the device work of the NEXT call
  * made from the calling host thread to an entry point that enqueues device

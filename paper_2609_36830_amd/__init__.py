@@ -625,6 +625,44 @@ def pace_token_logprob_backward(logits, token_ids, stats, grad_logp, entropy=Non
     return grad_logits_out
 
 
+def pace_policy_loss_workspace_bytes(n_traj: int, n_tokens: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().pace_policy_loss_workspace_bytes(int(n_traj), int(n_tokens), ctypes.byref(out)),
+           "pace_policy_loss_workspace_bytes")
+    return int(out.value)
+
+
+def policy_loss_buffers(n_traj: int, n_tokens: int, device):
+    """Outputs and workspace for repeated pace_policy_loss calls (pass as ``buffers``)."""
+    e = lambda k, dt: torch.empty(k, dtype=dt, device=device)
+    return dict(grad=e(n_tokens, torch.float32), loss=e(n_traj, torch.float32), kl=e(n_traj, torch.float32),
+                clipped=e(n_traj, torch.int32), workspace=e(pace_policy_loss_workspace_bytes(n_traj, n_tokens), torch.uint8))
+
+
+def pace_policy_loss(lp_new, lp_behavior, offsets, advantage, tags=None, weight=None, scale: float = 1.0,
+                     clip_low: float = 0.2, clip_high: float = 0.28, dual_clip: float = 10.0, buffers=None, stream=None):
+    """Clipped policy loss of a packed batch (clips of the paper's App. B by default). Returns (gradient with respect to
+    lp_new f32[n_tokens], loss f32[n], kl f32[n], clipped i32[n]), the last three as sums by trajectory."""
+    _dev(lp_new, torch.float32, "lp_new")
+    _dev(offsets, torch.int64, "offsets")
+    dev, nt, n = lp_new.device, lp_new.numel(), offsets.numel() - 1
+    _vector(lp_behavior, torch.float32, nt, dev, "lp_behavior")
+    _vector(advantage, torch.float32, n, dev, "advantage")
+    if tags is not None:
+        _vector(tags, torch.int32, nt, dev, "tags")
+    if weight is not None:
+        _vector(weight, torch.float32, n, dev, "weight")
+    b = policy_loss_buffers(n, nt, dev) if buffers is None else buffers
+    grad, loss = _sized(b["grad"], torch.float32, (nt,), dev, "grad"), _sized(b["loss"], torch.float32, (n,), dev, "loss")
+    kl, clipped = _sized(b["kl"], torch.float32, (n,), dev, "kl"), _sized(b["clipped"], torch.int32, (n,), dev, "clipped")
+    ws = b["workspace"]
+    _check(lib().pace_policy_loss(lp_new.data_ptr(), lp_behavior.data_ptr(), _ptr(tags), offsets.data_ptr(), n, nt,
+                                  advantage.data_ptr(), _ptr(weight), float(scale), float(clip_low), float(clip_high),
+                                  float(dual_clip), grad.data_ptr(), loss.data_ptr(), kl.data_ptr(), clipped.data_ptr(),
+                                  ws.data_ptr(), ws.numel(), _stream(dev, stream)), "pace_policy_loss")
+    return grad, loss, kl, clipped
+
+
 def pace_time_next_kernel(phase: int, start=None, stop=None):
     """Arm a one-shot timer on the next kernel of `phase` launched from this
     thread. start/stop are torch.cuda.Event(enable_timing=True) objects that

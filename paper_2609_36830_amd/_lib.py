@@ -44,6 +44,8 @@ SIGNATURES = [
     ("pace_token_logprob_workspace_bytes", ctypes.c_int, [i64, i64, ctypes.c_int, P]),
     ("pace_token_logprob", ctypes.c_int, [P, ctypes.c_int, i64, i64, i64, P, d, ctypes.c_int, P, P, P, P, P, P, sz, P]),
     ("pace_token_logprob_backward", ctypes.c_int, [P, ctypes.c_int, i64, i64, i64, P, d, P, P, P, P, P, i64, P]),
+    ("pace_policy_loss_workspace_bytes", ctypes.c_int, [i64, i64, P]),
+    ("pace_policy_loss", ctypes.c_int, [P, P, P, P, i64, i64, P, P, d, d, d, d, P, P, P, P, P, sz, P]),
     ("pace_time_next_kernel", ctypes.c_int, [ctypes.c_int, P, P]),
     ("pace_strerror", ctypes.c_char_p, [ctypes.c_int]),
 ]

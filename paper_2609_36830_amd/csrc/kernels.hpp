@@ -334,6 +334,17 @@ hipError_t launch_token_logprob_backward(const void *logits, int dtype, int64_t 
                                          const float *entropy, const float *g_logp, const float *g_entropy, void *grad,
                                          int64_t grad_stride, hipStream_t stream);
 
+// ---- policy loss ----------------------------------------------------------------
+struct LossBounds {
+    float low, high, dual;                  // 1 - el, 1 + eh, c
+    float log_low, log_high, log_dual;      // and their logarithms, which d is compared with
+};
+size_t policy_loss_ws_bytes(int64_t n_tokens);
+hipError_t launch_policy_loss(const float *lp_new, const float *lp_beh, const int32_t *tags, const int64_t *offsets,
+                              int64_t n, int64_t n_tokens, const float *adv, const float *weight, double scale,
+                              const LossBounds &bounds, float *grad, float *loss, float *kl, int32_t *clipped, void *ws,
+                              hipStream_t stream);
+
 // ---- validate --------------------------------------------------------------
 hipError_t launch_validate(const int32_t *tags, const int64_t *offsets, int64_t n, int64_t n_tokens,
                            const int32_t *completion, int32_t V, const double *window, int64_t W,

@@ -564,6 +564,9 @@ int pace_diagnostics(const double *score, const int64_t *gen_sum, const int64_t 
 static_assert(PACE_F32 == kF32 && PACE_BF16 == kBf16 && PACE_F16 == kF16, "element types");
 static_assert(PACE_TOP_MAX == kTopMax, "alternatives");
 
+// Spans and their workgroups stay 32-bit numbers.
+constexpr int64_t kLossTokensMax = (int64_t)1 << 40;
+
 // Rows of `cols` elements `stride` apart, as the operators on matrices take them.
 static bool rows_ok(const void *p, int dtype, int64_t rows, int64_t cols, int64_t stride) {
     if (dtype < 0 || dtype >= kElemTypes || rows < 0 || rows >= INT32_MAX || cols < 1 || cols >= INT32_MAX) return false;
@@ -616,6 +619,36 @@ int pace_token_logprob_backward(const void *logits, int dtype, int64_t n_rows, i
     return hip_status(launch_token_logprob_backward(logits, dtype, n_rows, vocab, row_stride, token_ids, temperature, stats,
                                                     entropy, grad_logp, grad_entropy, grad_logits_out, grad_row_stride,
                                                     (hipStream_t)stream));
+}
+
+int pace_policy_loss_workspace_bytes(int64_t n_traj, int64_t n_tokens, size_t *bytes_out) {
+    if (!bytes_out || n_traj < 0 || n_traj >= INT32_MAX || n_tokens < 0 || n_tokens >= kLossTokensMax)
+        return PACE_ERR_INVALID_ARG;
+    *bytes_out = policy_loss_ws_bytes(n_tokens);
+    return PACE_OK;
+}
+
+int pace_policy_loss(const float *lp_new, const float *lp_behavior, const int32_t *tags, const int64_t *offsets,
+                     int64_t n_traj, int64_t n_tokens, const float *advantage, const float *weight, double scale,
+                     double clip_low, double clip_high, double dual_clip, float *grad_out, float *loss_out, float *kl_out,
+                     int32_t *clipped_out, void *workspace, size_t workspace_bytes, void *stream) {
+    const TimerScope timers;
+    if (n_traj < 0 || n_traj >= INT32_MAX || n_tokens < 0 || n_tokens >= kLossTokensMax || !offsets)
+        return PACE_ERR_INVALID_ARG;
+    if ((n_tokens > 0 && (!lp_new || !lp_behavior || !grad_out)) || (n_traj > 0 && (!advantage || !loss_out)))
+        return PACE_ERR_INVALID_ARG;
+    if (!aligned(lp_new, 4) || !aligned(lp_behavior, 4) || !aligned(tags, 4) || !aligned(offsets, 8) ||
+        !aligned(advantage, 4) || !aligned(weight, 4) || !aligned(grad_out, 4) || !aligned(loss_out, 4) ||
+        !aligned(kl_out, 4) || !aligned(clipped_out, 4))
+        return PACE_ERR_INVALID_ARG;
+    if (!isfinite(scale) || !(clip_low >= 0.0 && clip_low < 1.0) || !(clip_high >= 0.0) || !(dual_clip > 1.0))
+        return PACE_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < policy_loss_ws_bytes(n_tokens))
+        return PACE_ERR_WORKSPACE;
+    const LossBounds b{(float)(1.0 - clip_low), (float)(1.0 + clip_high), (float)dual_clip,
+                       (float)log1p(-clip_low), (float)log1p(clip_high), (float)log(dual_clip)};
+    return hip_status(launch_policy_loss(lp_new, lp_behavior, tags, offsets, n_traj, n_tokens, advantage, weight, scale, b,
+                                         grad_out, loss_out, kl_out, clipped_out, workspace, (hipStream_t)stream));
 }
 
 static_assert(PACE_PHASE_COUNT == kPhaseCount, "phase count");

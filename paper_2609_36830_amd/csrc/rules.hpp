@@ -87,6 +87,15 @@ inline bool small_step_ok(int64_t n, int64_t n_tokens, int n_cols, int64_t budge
     return n <= kSmallMaxN && expected_kept(n, n_tokens, n - budget) <= most;
 }
 
+// ---- policy loss (policy_loss.hip) ------------------------------------------------
+// Tokens a wave takes: 256 are one load a lane; at least two of them, at most
+// what leaves 8192 waves, which the chip holds at once.
+constexpr int64_t kLossSpanMin = 512;
+inline int64_t policy_loss_span(int64_t n_tokens) {
+    const int64_t per = (n_tokens / 8192 + 255) / 256 * 256;
+    return per > kLossSpanMin ? per : kLossSpanMin;
+}
+
 // ---- log-probabilities (logprob.hip) --------------------------------------------
 // Workgroups that share a row of logits: enough rows' parts for the chip, each
 // of at least kLogprobPart logits, at most one part a lane of the joining wave.

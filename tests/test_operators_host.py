@@ -46,3 +46,16 @@ def test_token_logprob_workspace(L):
     for bad in ((-1, 10, 0), (1, 0, 0), (1, 10, 65)):
         with pytest.raises(pace.PaceError):
             pace.pace_token_logprob_workspace_bytes(*bad)
+
+
+def test_policy_loss_host_argument_errors(L):
+    def call(new=FAKE, beh=FAKE, tags=None, off=FAKE, n=4, nt=100, adv=FAKE, w=None, scale=1.0, low=0.2, high=0.28, dual=10.0,
+             grad=FAKE, loss=FAKE, ws=FAKE, wsb=1 << 30):
+        return L.pace_policy_loss(new, beh, tags, off, n, nt, adv, w, scale, low, high, dual, grad, loss, None, None, ws, wsb, None)
+
+    for kw in (dict(new=None), dict(beh=None), dict(off=None), dict(off=FAKE + 4), dict(n=-1), dict(nt=-1), dict(nt=2 ** 40),
+               dict(adv=None), dict(scale=float("nan")), dict(low=1.0), dict(low=-0.1), dict(high=-0.1), dict(high=float("nan")),
+               dict(dual=1.0), dict(dual=float("nan")), dict(grad=None), dict(loss=None), dict(tags=FAKE + 2), dict(w=FAKE + 1)):
+        assert call(**kw) == -1, kw
+    for kw in (dict(ws=None), dict(ws=FAKE + 8), dict(wsb=128)):
+        assert call(**kw) == -2, kw
