@@ -487,6 +487,30 @@ int pace_policy_loss(const float *lp_new, const float *lp_behavior, const int32_
                      double clip_low, double clip_high, double dual_clip, float *grad_out, float *loss_out, float *kl_out,
                      int32_t *clipped_out, void *workspace, size_t workspace_bytes, void *stream);
 
+/* pace_quantize_rows -- rows in 8 bits with a scale each (tokens, or the output
+ * channels of a weight): with a the row's largest |x|,
+ *   scale_out[i] = a / 127,  q_out[i, :] = rint(x (127 / a)), half to even,
+ * each operation a binary32 step. A row with a < 2^-119 is zeros with scale 0; one
+ * with an infinity or a NaN is zeros with scale NaN.
+ * x: [n_rows, n_cols] of dtype, row_stride elements apart; 1 <= n_cols < 2^31
+ * q_out int8 [n_rows, n_cols], contiguous; scale_out f32 [n_rows] */
+int pace_quantize_rows(const void *x, int dtype, int64_t n_rows, int64_t n_cols, int64_t row_stride, int8_t *q_out,
+                       float *scale_out, void *stream);
+
+/* pace_matmul_i8 -- product in 8-bit integers with a scale for each token and
+ * channel: out[i, j] = (sum_k a[i, k] b[j, k]) * (a_scale[i] * b_scale[j]). The
+ * integer sum is exact (all of -128 .. 127 may occur), then converted to binary32,
+ * multiplied and rounded to out_dtype.
+ * a int8 [m, k], b int8 [n, k] (one row an output channel), strides in elements;
+ *   1 <= k < 131072. Any strides and starts are read; both being multiples of 16
+ *   bytes, with k, is the fast case.
+ * a_scale f32 [m], b_scale f32 [n]; out [m, n] of out_dtype, rows out_stride apart
+ * workspace: pace_matmul_i8_workspace_bytes() bytes. */
+int pace_matmul_i8_workspace_bytes(int64_t m, int64_t n, int64_t k, size_t *bytes_out);
+int pace_matmul_i8(const int8_t *a, int64_t a_stride, const float *a_scale, const int8_t *b, int64_t b_stride,
+                   const float *b_scale, int64_t m, int64_t n, int64_t k, void *out, int out_dtype, int64_t out_stride,
+                   void *workspace, size_t workspace_bytes, void *stream);
+
 /* pace_time_next_kernel -- measurement hook, not part of the method.
  * Arms a one-shot timer for one phase of the device work of the NEXT call
  * made from the calling host thread to an entry point that enqueues device

@@ -663,6 +663,61 @@ def pace_policy_loss(lp_new, lp_behavior, offsets, advantage, tags=None, weight=
     return grad, loss, kl, clipped
 
 
+def pace_quantize_rows(x, q_out=None, scale_out=None, stream=None):
+    """Rows in 8 bits: scale = max |x| / 127, q = rint(x (127 / max |x|)). Returns (q int8[n, k], scale f32[n])."""
+    dt, n, k, stride = _matrix(x, "x")
+    q_out = _sized(q_out, torch.int8, (n, k), x.device, "q_out")
+    scale_out = _sized(scale_out, torch.float32, (n,), x.device, "scale_out")
+    _check(lib().pace_quantize_rows(x.data_ptr(), dt, n, k, stride, q_out.data_ptr(), scale_out.data_ptr(),
+                                    _stream(x.device, stream)), "pace_quantize_rows")
+    return q_out, scale_out
+
+
+def pace_matmul_i8_workspace_bytes(m: int, n: int, k: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().pace_matmul_i8_workspace_bytes(int(m), int(n), int(k), ctypes.byref(out)), "pace_matmul_i8_workspace_bytes")
+    return int(out.value)
+
+
+def matmul_i8_buffers(m: int, n: int, k: int, out_dtype, device):
+    """Quantised rows, output and workspace for repeated products of m rows with an [n, k] weight."""
+    e = lambda shape, dt: torch.empty(shape, dtype=dt, device=device)
+    return dict(q=e((m, k), torch.int8), scale=e(m, torch.float32), out=e((m, n), out_dtype),
+                workspace=e(pace_matmul_i8_workspace_bytes(m, n, k), torch.uint8))
+
+
+def _int8_rows(t, name: str):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2 or t.dtype != torch.int8:
+        raise ValueError("%s must be an int8 device matrix" % name)
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError("%s must have contiguous rows" % name)
+    return rows, cols, (t.stride(0) if rows > 1 else max(cols, 1))
+
+
+def pace_matmul_i8(a, a_scale, b, b_scale, out=None, out_dtype=torch.bfloat16, workspace=None, stream=None):
+    """(a int8[m, k]) (b int8[n, k])^T with a scale for each row of both. Returns out [m, n] of out_dtype (of ``out``'s
+    type where it is given)."""
+    m, k, lda = _int8_rows(a, "a")
+    n, kb, ldb = _int8_rows(b, "b")
+    dev = a.device
+    if kb != k or b.device != dev:
+        raise ValueError("a and b must have rows of the same length on one device")
+    _vector(a_scale, torch.float32, m, dev, "a_scale")
+    _vector(b_scale, torch.float32, n, dev, "b_scale")
+    if out is None:
+        out = torch.empty((m, n), dtype=out_dtype, device=dev)
+    dt, om, on, ldo = _matrix(out, "out")
+    if (om, on) != (m, n) or out.device != dev:
+        raise ValueError("out must have shape (%d, %d) on %s" % (m, n, dev))
+    ws = workspace
+    if ws is None:
+        ws = torch.empty(pace_matmul_i8_workspace_bytes(m, n, k), dtype=torch.uint8, device=dev)
+    _check(lib().pace_matmul_i8(a.data_ptr(), lda, a_scale.data_ptr(), b.data_ptr(), ldb, b_scale.data_ptr(), m, n, k,
+                                out.data_ptr(), dt, ldo, ws.data_ptr(), ws.numel(), _stream(dev, stream)), "pace_matmul_i8")
+    return out
+
+
 def pace_time_next_kernel(phase: int, start=None, stop=None):
     """Arm a one-shot timer on the next kernel of `phase` launched from this
     thread. start/stop are torch.cuda.Event(enable_timing=True) objects that

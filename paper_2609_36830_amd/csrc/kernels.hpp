@@ -26,7 +26,7 @@ enum TimedPhase : int { kPhaseReduce = 0, kPhaseFinalize = 1, kPhaseSelect = 2, 
 bool take_phase_timer(int phase, hipEvent_t *start, hipEvent_t *stop);
 
 template <typename... P, typename... A>
-hipError_t launch(int phase, void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t stream, A... a) {
+hipError_t launch_lds(int phase, void (*kernel)(P...), dim3 grid, dim3 block, size_t lds, hipStream_t stream, A... a) {
     static_assert(sizeof...(P) == sizeof...(A), "kernel argument count");
     hipEvent_t t0 = nullptr, t1 = nullptr;
     if (phase >= 0 && take_phase_timer(phase, &t0, &t1)) {
@@ -36,10 +36,14 @@ hipError_t launch(int phase, void (*kernel)(P...), dim3 grid, dim3 block, hipStr
             int k = 0;
             ((argv[k++] = (void *)&x), ...);
         }, held);
-        return hipExtLaunchKernel((const void *)kernel, grid, block, argv, 0, stream, t0, t1, 0);
+        return hipExtLaunchKernel((const void *)kernel, grid, block, argv, lds, stream, t0, t1, 0);
     }
-    kernel<<<grid, block, 0, stream>>>(static_cast<P>(a)...);
+    kernel<<<grid, block, lds, stream>>>(static_cast<P>(a)...);
     return hipGetLastError();
+}
+template <typename... P, typename... A>
+hipError_t launch(int phase, void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t stream, A... a) {
+    return launch_lds(phase, kernel, grid, block, 0, stream, a...);
 }
 
 // ---- score: segmented reduction over token chunks --------------------------
@@ -344,6 +348,14 @@ hipError_t launch_policy_loss(const float *lp_new, const float *lp_beh, const in
                               int64_t n, int64_t n_tokens, const float *adv, const float *weight, double scale,
                               const LossBounds &bounds, float *grad, float *loss, float *kl, int32_t *clipped, void *ws,
                               hipStream_t stream);
+
+// ---- products in 8-bit integers ---------------------------------------------------
+hipError_t launch_quantize_rows(const void *x, int dtype, int64_t rows, int64_t cols, int64_t stride, int8_t *q,
+                                float *scale, hipStream_t stream);
+size_t matmul_i8_ws_bytes(int64_t m, int64_t n, int64_t k);
+hipError_t launch_matmul_i8(const int8_t *a, int64_t lda, const float *sa, const int8_t *b, int64_t ldb, const float *sb,
+                            int64_t m, int64_t n, int64_t k, void *out, int dtype, int64_t ldo, void *ws,
+                            hipStream_t stream);
 
 // ---- validate --------------------------------------------------------------
 hipError_t launch_validate(const int32_t *tags, const int64_t *offsets, int64_t n, int64_t n_tokens,

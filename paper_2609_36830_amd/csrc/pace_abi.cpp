@@ -564,6 +564,9 @@ int pace_diagnostics(const double *score, const int64_t *gen_sum, const int64_t 
 static_assert(PACE_F32 == kF32 && PACE_BF16 == kBf16 && PACE_F16 == kF16, "element types");
 static_assert(PACE_TOP_MAX == kTopMax, "alternatives");
 
+// 128 * 128 * k stays below 2^31: the integer sums are exact.
+constexpr int64_t kMatmulI8MaxK = 131072;
+
 // Spans and their workgroups stay 32-bit numbers.
 constexpr int64_t kLossTokensMax = (int64_t)1 << 40;
 
@@ -649,6 +652,38 @@ int pace_policy_loss(const float *lp_new, const float *lp_behavior, const int32_
                        (float)log1p(-clip_low), (float)log1p(clip_high), (float)log(dual_clip)};
     return hip_status(launch_policy_loss(lp_new, lp_behavior, tags, offsets, n_traj, n_tokens, advantage, weight, scale, b,
                                          grad_out, loss_out, kl_out, clipped_out, workspace, (hipStream_t)stream));
+}
+
+int pace_quantize_rows(const void *x, int dtype, int64_t n_rows, int64_t n_cols, int64_t row_stride, int8_t *q_out,
+                       float *scale_out, void *stream) {
+    const TimerScope timers;
+    if (!rows_ok(x, dtype, n_rows, n_cols, row_stride)) return PACE_ERR_INVALID_ARG;
+    if (n_rows > 0 && (!q_out || !scale_out || !aligned(scale_out, 4))) return PACE_ERR_INVALID_ARG;
+    return hip_status(launch_quantize_rows(x, dtype, n_rows, n_cols, row_stride, q_out, scale_out, (hipStream_t)stream));
+}
+
+int pace_matmul_i8_workspace_bytes(int64_t m, int64_t n, int64_t k, size_t *bytes_out) {
+    if (!bytes_out || m < 0 || m >= INT32_MAX || n < 0 || n >= INT32_MAX || k < 1 || k >= kMatmulI8MaxK)
+        return PACE_ERR_INVALID_ARG;
+    *bytes_out = matmul_i8_ws_bytes(m, n, k);
+    return PACE_OK;
+}
+
+int pace_matmul_i8(const int8_t *a, int64_t a_stride, const float *a_scale, const int8_t *b, int64_t b_stride,
+                   const float *b_scale, int64_t m, int64_t n, int64_t k, void *out, int out_dtype, int64_t out_stride,
+                   void *workspace, size_t workspace_bytes, void *stream) {
+    const TimerScope timers;
+    if (m < 0 || m >= INT32_MAX || n < 0 || n >= INT32_MAX || k < 1 || k >= kMatmulI8MaxK) return PACE_ERR_INVALID_ARG;
+    if (a_stride < k || b_stride < k || (m > 0 && a_stride > INT64_MAX / 4 / m) || (n > 0 && b_stride > INT64_MAX / 4 / n))
+        return PACE_ERR_INVALID_ARG;
+    if (n > 0 && !rows_ok(out, out_dtype, m, n, out_stride)) return PACE_ERR_INVALID_ARG;
+    // tiles are numbered in 32 bits
+    if (((m + 63) / 64) * ((n + 63) / 64) >= INT32_MAX) return PACE_ERR_INVALID_ARG;
+    if (m > 0 && n > 0 && (!a || !a_scale || !b || !b_scale)) return PACE_ERR_INVALID_ARG;
+    if (!aligned(a_scale, 4) || !aligned(b_scale, 4)) return PACE_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < matmul_i8_ws_bytes(m, n, k)) return PACE_ERR_WORKSPACE;
+    return hip_status(launch_matmul_i8(a, a_stride, a_scale, b, b_stride, b_scale, m, n, k, out, out_dtype, out_stride,
+                                       workspace, (hipStream_t)stream));
 }
 
 static_assert(PACE_PHASE_COUNT == kPhaseCount, "phase count");

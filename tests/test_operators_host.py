@@ -59,3 +59,21 @@ def test_policy_loss_host_argument_errors(L):
         assert call(**kw) == -1, kw
     for kw in (dict(ws=None), dict(ws=FAKE + 8), dict(wsb=128)):
         assert call(**kw) == -2, kw
+
+
+def test_quantize_and_matmul_i8_host_argument_errors(L):
+    def quant(x=FAKE, dt=0, n=4, k=100, st=100, q=FAKE, s=FAKE):
+        return L.pace_quantize_rows(x, dt, n, k, st, q, s, None)
+
+    for kw in (dict(x=None), dict(x=FAKE + 2), dict(dt=5), dict(n=-1), dict(k=0), dict(st=99), dict(q=None), dict(s=None), dict(s=FAKE + 2)):
+        assert quant(**kw) == -1, kw
+
+    def mul(a=FAKE, lda=64, sa=FAKE, b=FAKE, ldb=64, sb=FAKE, m=4, n=6, k=64, out=FAKE, dt=0, ldo=6, ws=FAKE, wsb=1 << 30):
+        return L.pace_matmul_i8(a, lda, sa, b, ldb, sb, m, n, k, out, dt, ldo, ws, wsb, None)
+
+    for kw in (dict(a=None), dict(b=None), dict(sa=None), dict(sb=None), dict(sa=FAKE + 1), dict(lda=63), dict(ldb=63), dict(m=-1),
+               dict(n=-1), dict(k=0), dict(k=131072, lda=131072, ldb=131072), dict(out=None), dict(dt=3), dict(ldo=5),
+               dict(out=FAKE + 2), dict(m=2 ** 30, n=2 ** 20, ldo=2 ** 20)):
+        assert mul(**kw) == -1, kw
+    for kw in (dict(ws=None), dict(ws=FAKE + 16), dict(wsb=8)):
+        assert mul(**kw) == -2, kw
