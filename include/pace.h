@@ -511,6 +511,26 @@ int pace_matmul_i8(const int8_t *a, int64_t a_stride, const float *a_scale, cons
                    const float *b_scale, int64_t m, int64_t n, int64_t k, void *out, int out_dtype, int64_t out_stride,
                    void *workspace, size_t workspace_bytes, void *stream);
 
+/* pace_orthogonalize -- the nearest semi-orthogonal direction of each update of
+ * a batch, by Newton-Schulz steps:
+ *   X = G / (|G|_F + eps);  steps times: A = X X^T, X <- (a I + b A + c A A) X
+ * on the orientation with rows <= columns (a taller update is turned and turned
+ * back). With coefs = {3.4445, -4.7750, 2.0315} five steps bring singular values
+ * from about 0.02 .. 1 of the norm into 0.7 .. 1.2; {1.5, -0.5, 0} converges to 1
+ * from nearer.
+ * update: [batch, rows, cols] of dtype, rows row_stride and matrices batch_stride
+ *   elements apart; rows, cols 1 .. 2^21, batch < 65536
+ * steps 0 .. 100; coefs [host] double[3], finite; eps > 0, finite
+ * out: bfloat16 [batch, rows, cols], contiguous. Between the products values are
+ *   binary16, scaled: X may reach 32 and A, C 128, far above what coefficients
+ *   that converge give. A zero update gives zeros; one with a NaN or an infinity
+ *   spoils its own matrix only.
+ * workspace: pace_orthogonalize_workspace_bytes() bytes. */
+int pace_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int64_t cols, size_t *bytes_out);
+int pace_orthogonalize(const void *update, int dtype, int64_t batch, int64_t rows, int64_t cols, int64_t row_stride,
+                       int64_t batch_stride, int steps, const double *coefs, double eps, void *out, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
 /* pace_time_next_kernel -- measurement hook, not part of the method.
  * Arms a one-shot timer for one phase of the device work of the NEXT call
  * made from the calling host thread to an entry point that enqueues device

@@ -718,6 +718,43 @@ def pace_matmul_i8(a, a_scale, b, b_scale, out=None, out_dtype=torch.bfloat16, w
     return out
 
 
+def pace_orthogonalize_workspace_bytes(batch: int, rows: int, cols: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().pace_orthogonalize_workspace_bytes(int(batch), int(rows), int(cols), ctypes.byref(out)),
+           "pace_orthogonalize_workspace_bytes")
+    return int(out.value)
+
+
+def orthogonalize_buffers(batch: int, rows: int, cols: int, device):
+    """Output and workspace for repeated pace_orthogonalize calls on updates of one shape."""
+    return dict(out=torch.empty((batch, rows, cols), dtype=torch.bfloat16, device=device),
+                workspace=torch.empty(pace_orthogonalize_workspace_bytes(batch, rows, cols), dtype=torch.uint8, device=device))
+
+
+def pace_orthogonalize(update, steps: int = 5, coefs=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, out=None, workspace=None,
+                       stream=None):
+    """Newton-Schulz steps on update [rows, cols] or [batch, rows, cols] (rows contiguous). Returns bfloat16 of its shape."""
+    if not isinstance(update, torch.Tensor) or not update.is_cuda or update.dim() not in (2, 3) or update.dtype not in DTYPES:
+        raise ValueError("update must be a float32, bfloat16 or float16 device matrix, or a batch of them")
+    u = update if update.dim() == 3 else update[None]
+    batch, rows, cols = u.shape
+    if cols > 1 and u.stride(2) != 1:
+        raise ValueError("update must have contiguous rows")
+    if len(coefs) != 3:
+        raise ValueError("coefs must be three numbers")
+    dev = update.device
+    out = _sized(out, torch.bfloat16, tuple(update.shape), dev, "out")
+    ws = workspace
+    if ws is None:
+        ws = torch.empty(pace_orthogonalize_workspace_bytes(batch, rows, cols), dtype=torch.uint8, device=dev)
+    stride = u.stride(1) if rows > 1 else max(cols, 1)
+    _check(lib().pace_orthogonalize(update.data_ptr(), DTYPES[update.dtype], batch, rows, cols, stride,
+                                    u.stride(0) if batch > 1 else rows * stride, int(steps),
+                                    (ctypes.c_double * 3)(*map(float, coefs)), float(eps), out.data_ptr(), ws.data_ptr(),
+                                    ws.numel(), _stream(dev, stream)), "pace_orthogonalize")
+    return out
+
+
 def pace_time_next_kernel(phase: int, start=None, stop=None):
     """Arm a one-shot timer on the next kernel of `phase` launched from this
     thread. start/stop are torch.cuda.Event(enable_timing=True) objects that

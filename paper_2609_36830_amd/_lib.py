@@ -49,6 +49,8 @@ SIGNATURES = [
     ("pace_quantize_rows", ctypes.c_int, [P, ctypes.c_int, i64, i64, i64, P, P, P]),
     ("pace_matmul_i8_workspace_bytes", ctypes.c_int, [i64, i64, i64, P]),
     ("pace_matmul_i8", ctypes.c_int, [P, i64, P, P, i64, P, i64, i64, i64, P, ctypes.c_int, i64, P, sz, P]),
+    ("pace_orthogonalize_workspace_bytes", ctypes.c_int, [i64, i64, i64, P]),
+    ("pace_orthogonalize", ctypes.c_int, [P, ctypes.c_int, i64, i64, i64, i64, i64, ctypes.c_int, P, d, P, P, sz, P]),
     ("pace_time_next_kernel", ctypes.c_int, [ctypes.c_int, P, P]),
     ("pace_strerror", ctypes.c_char_p, [ctypes.c_int]),
 ]

@@ -357,6 +357,12 @@ hipError_t launch_matmul_i8(const int8_t *a, int64_t lda, const float *sa, const
                             int64_t m, int64_t n, int64_t k, void *out, int dtype, int64_t ldo, void *ws,
                             hipStream_t stream);
 
+// ---- orthogonalised updates ---------------------------------------------------------
+size_t ortho_ws_bytes(int64_t batch, int64_t rows, int64_t cols);
+hipError_t launch_orthogonalize(const void *g, int dtype, int64_t batch, int64_t rows, int64_t cols, int64_t stride,
+                                int64_t batch_stride, int steps, const double *coefs, double eps, void *out, void *ws,
+                                hipStream_t stream);
+
 // ---- validate --------------------------------------------------------------
 hipError_t launch_validate(const int32_t *tags, const int64_t *offsets, int64_t n, int64_t n_tokens,
                            const int32_t *completion, int32_t V, const double *window, int64_t W,

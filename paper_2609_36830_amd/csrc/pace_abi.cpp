@@ -567,6 +567,9 @@ static_assert(PACE_TOP_MAX == kTopMax, "alternatives");
 // 128 * 128 * k stays below 2^31: the integer sums are exact.
 constexpr int64_t kMatmulI8MaxK = 131072;
 
+// Tiles of 64 of both sides are numbered in a grid's 16-bit axis, and a tile's rows by 32-bit byte offsets.
+constexpr int64_t kOrthoSideMax = (int64_t)1 << 21;
+
 // Spans and their workgroups stay 32-bit numbers.
 constexpr int64_t kLossTokensMax = (int64_t)1 << 40;
 
@@ -684,6 +687,32 @@ int pace_matmul_i8(const int8_t *a, int64_t a_stride, const float *a_scale, cons
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < matmul_i8_ws_bytes(m, n, k)) return PACE_ERR_WORKSPACE;
     return hip_status(launch_matmul_i8(a, a_stride, a_scale, b, b_stride, b_scale, m, n, k, out, out_dtype, out_stride,
                                        workspace, (hipStream_t)stream));
+}
+
+static bool ortho_sizes_ok(int64_t batch, int64_t rows, int64_t cols) {
+    return batch >= 0 && batch < 65536 && rows >= 1 && rows <= kOrthoSideMax && cols >= 1 && cols <= kOrthoSideMax &&
+           rows * cols <= INT64_MAX / 64 / (batch > 0 ? batch : 1);
+}
+
+int pace_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int64_t cols, size_t *bytes_out) {
+    if (!bytes_out || !ortho_sizes_ok(batch, rows, cols)) return PACE_ERR_INVALID_ARG;
+    *bytes_out = ortho_ws_bytes(batch, rows, cols);
+    return PACE_OK;
+}
+
+int pace_orthogonalize(const void *update, int dtype, int64_t batch, int64_t rows, int64_t cols, int64_t row_stride,
+                       int64_t batch_stride, int steps, const double *coefs, double eps, void *out, void *workspace,
+                       size_t workspace_bytes, void *stream) {
+    const TimerScope timers;
+    if (!ortho_sizes_ok(batch, rows, cols) || steps < 0 || steps > 100 || !coefs) return PACE_ERR_INVALID_ARG;
+    if (!rows_ok(update ? update : out, dtype, batch > 0 ? rows : 0, cols, row_stride)) return PACE_ERR_INVALID_ARG;
+    if (batch > 1 && (batch_stride < 0 || batch_stride > INT64_MAX / 4 / batch || batch_stride < (rows - 1) * row_stride + cols))
+        return PACE_ERR_INVALID_ARG;
+    if (batch > 0 && (!update || !out || !aligned(out, 2))) return PACE_ERR_INVALID_ARG;
+    if (!isfinite(coefs[0]) || !isfinite(coefs[1]) || !isfinite(coefs[2]) || !(eps > 0.0) || isinf(eps)) return PACE_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < ortho_ws_bytes(batch, rows, cols)) return PACE_ERR_WORKSPACE;
+    return hip_status(launch_orthogonalize(update, dtype, batch, rows, cols, row_stride, batch_stride, steps, coefs, eps, out,
+                                           workspace, (hipStream_t)stream));
 }
 
 static_assert(PACE_PHASE_COUNT == kPhaseCount, "phase count");

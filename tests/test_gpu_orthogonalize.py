@@ -1,0 +1,169 @@
+"""GPU tests of pace_orthogonalize against the same steps in binary64.
+
+Tolerance (2-norm of the difference over that of the result), for updates whose
+singular values are of one size: a step rounds X, A and C to binary16, each
+within 2^-12 root mean square of its own size, and a step passes errors on at
+most doubled where singular values stay near the fixed region; over `steps`
+steps 6 steps 2^-12. The result's rounding to bfloat16 adds 2^-9."""
+import sys
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+QUINTIC, CUBIC = (3.4445, -4.7750, 2.0315), (1.5, -0.5, 0.0)
+
+
+def say(msg):
+    sys.stdout.write("[gpu] %s\n" % msg)
+    sys.stdout.flush()
+
+
+@pytest.fixture(scope="module")
+def pace():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import os
+    from paper_2609_36830_amd import _lib
+    if not os.path.exists(_lib.library_path):
+        from paper_2609_36830_amd import build
+        build.build()
+    import paper_2609_36830_amd as pace
+    return pace
+
+
+def reference(g, steps=5, coefs=QUINTIC, eps=1e-7):
+    x = g.double()
+    turned = x.shape[1] > x.shape[2]
+    x = x.transpose(1, 2) if turned else x
+    x = x / (torch.linalg.vector_norm(x, dim=(1, 2), keepdim=True) + eps)
+    for _ in range(steps):
+        p = x @ x.transpose(1, 2)
+        x = coefs[0] * x + (coefs[1] * p + coefs[2] * (p @ p)) @ x
+    return x.transpose(1, 2) if turned else x
+
+
+def check(pace, g, steps=5, coefs=QUINTIC, eps=1e-7, **kw):
+    out = pace.pace_orthogonalize(g, steps=steps, coefs=coefs, eps=eps, **kw)
+    ref = reference(g if g.dim() == 3 else g[None], steps, coefs, eps)
+    got = (out if out.dim() == 3 else out[None]).double()
+    rel = torch.linalg.vector_norm(got - ref, dim=(1, 2)) / torch.linalg.vector_norm(ref, dim=(1, 2)).clamp(min=1e-300)
+    assert float(rel.max()) <= 6 * steps * 2.0 ** -12 + 2.0 ** -9, float(rel.max())
+    return out
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("batch,rows,cols", [(1, 1, 1), (2, 1, 300), (2, 300, 1), (3, 5, 7), (1, 63, 65), (2, 64, 64), (1, 200, 130),
+                                             (4, 128, 513), (1, 1000, 257), (7, 65, 64)])
+def test_shapes(pace, dtype, batch, rows, cols):
+    say("orthogonalize %s %d x %d x %d" % (dtype, batch, rows, cols))
+    g = torch.randn(batch, rows, cols, generator=torch.Generator(device=DEV).manual_seed(rows + cols), device=DEV).to(dtype)
+    check(pace, g)
+    check(pace, g, steps=3, coefs=CUBIC)
+
+
+@pytest.mark.parametrize("batch,rows,cols", [(1, 2900, 3001), (1, 4097, 2050), (24, 600, 700), (2, 2048, 2048)])
+def test_large_tiles(pace, batch, rows, cols):
+    say("orthogonalize %d x %d x %d" % (batch, rows, cols))
+    g = torch.randn(batch, rows, cols, generator=torch.Generator(device=DEV).manual_seed(3), device=DEV)
+    check(pace, g)
+
+
+def test_steps_and_coefficients(pace):
+    say("orthogonalize steps")
+    g = torch.randn(2, 90, 150, generator=torch.Generator(device=DEV).manual_seed(4), device=DEV)
+    for steps in (0, 1, 2, 7):
+        check(pace, g, steps=steps)
+        check(pace, g.transpose(1, 2).contiguous(), steps=steps, coefs=CUBIC)
+    check(pace, g, eps=0.5)
+    # twenty cubic steps: orthonormal rows to bfloat16's precision
+    x = pace.pace_orthogonalize(g, steps=20, coefs=CUBIC).double()
+    eye = x @ x.transpose(1, 2)
+    assert float((eye - torch.eye(90, device=DEV, dtype=torch.float64)).abs().max()) < 0.02
+
+
+def test_singular_values_come_together(pace):
+    """Singular values from 0.03 to 1 of the largest: five quintic steps bring all into 0.6 .. 1.3."""
+    say("orthogonalize singular values")
+    gen = torch.Generator(device=DEV).manual_seed(6)
+    n = 256
+    u, v = (torch.linalg.qr(torch.randn(n, n, generator=gen, device=DEV))[0] for _ in range(2))
+    s = torch.linspace(0.2, 1, n, device=DEV)
+    x = pace.pace_orthogonalize((u * s) @ v.t())
+    got = torch.linalg.svdvals(x.float())
+    assert 0.6 < float(got.min()) and float(got.max()) < 1.3
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-3, 1e30, 1e37])
+def test_sizes_of_values(pace, scale):
+    """The norm's squares leave binary32 at both ends; eps is below the norm throughout."""
+    say("orthogonalize values of %g" % scale)
+    g = torch.randn(1, 100, 180, generator=torch.Generator(device=DEV).manual_seed(5), device=DEV) * scale
+    check(pace, g, eps=1e-36)
+
+
+def test_special_matrices(pace):
+    """Zeros give zeros; NaN and infinities spoil their own matrix only."""
+    say("orthogonalize zeros, NaN, infinities")
+    g = torch.randn(5, 96, 70, generator=torch.Generator(device=DEV).manual_seed(7), device=DEV)
+    ref = pace.pace_orthogonalize(g)
+    g[1] = 0
+    g[2, 3, 4] = float("nan")
+    g[3, 0, 0] = float("inf")
+    out = pace.pace_orthogonalize(g)
+    assert not bool(out[1].any())
+    assert bool(torch.isnan(out[2]).all()) and bool(torch.isnan(out[3]).any())
+    assert torch.equal(out[[0, 4]], ref[[0, 4]])
+
+
+def test_strides(pace):
+    """Slices of wider rows and of larger batches, off any alignment; a single matrix without a batch."""
+    say("orthogonalize strides")
+    buf = torch.full((4, 70, 131), float("nan"), dtype=torch.bfloat16, device=DEV)
+    view = buf[::2, 3:63, 1:124]
+    view.copy_(torch.randn(2, 60, 123, generator=torch.Generator(device=DEV).manual_seed(8), device=DEV))
+    assert torch.equal(pace.pace_orthogonalize(view), pace.pace_orthogonalize(view.contiguous()))
+    assert torch.equal(pace.pace_orthogonalize(view[1]), pace.pace_orthogonalize(view.contiguous())[1])
+
+
+@pytest.mark.parametrize("shape", [(3, 100, 140), (1, 2500, 2600)])
+def test_repeats_streams_graph(pace, shape):
+    say("orthogonalize repeats, streams, graph %s" % (shape,))
+    g = torch.randn(shape, generator=torch.Generator(device=DEV).manual_seed(9), device=DEV)
+    b = pace.orthogonalize_buffers(*shape, DEV)
+    ref = pace.pace_orthogonalize(g, **b).clone()
+    b["out"].zero_()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    pace.pace_orthogonalize(g, stream=side, **b)
+    torch.cuda.synchronize()
+    assert torch.equal(b["out"], ref)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pace.pace_orthogonalize(g, **b)
+    for _ in range(3):
+        b["out"].zero_()
+        b["workspace"].fill_(255)                    # NaN in every binary16: nothing left by an earlier call is read
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(b["out"], ref)
+
+
+def test_refusals(pace):
+    say("orthogonalize refusals")
+    g = torch.randn(2, 30, 40, device=DEV)
+    for bad in (lambda: pace.pace_orthogonalize(g.double()), lambda: pace.pace_orthogonalize(g.cpu()), lambda: pace.pace_orthogonalize(g[0, 0]),
+                lambda: pace.pace_orthogonalize(g.transpose(1, 2)), lambda: pace.pace_orthogonalize(g, coefs=(1.0, 2.0)),
+                lambda: pace.pace_orthogonalize(g, out=torch.empty(2, 30, 41, dtype=torch.bfloat16, device=DEV)),
+                lambda: pace.pace_orthogonalize(g, out=torch.empty(2, 30, 40, device=DEV))):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: pace.pace_orthogonalize(g, steps=-1), lambda: pace.pace_orthogonalize(g, steps=101), lambda: pace.pace_orthogonalize(g, eps=0.0),
+                lambda: pace.pace_orthogonalize(g, coefs=(float("nan"), 0, 0)),
+                lambda: pace.pace_orthogonalize(g, workspace=torch.empty(64, dtype=torch.uint8, device=DEV)),
+                lambda: pace.pace_orthogonalize(g[0][:, :0])):
+        with pytest.raises(pace.PaceError):
+            bad()

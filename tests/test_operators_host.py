@@ -77,3 +77,19 @@ def test_quantize_and_matmul_i8_host_argument_errors(L):
         assert mul(**kw) == -1, kw
     for kw in (dict(ws=None), dict(ws=FAKE + 16), dict(wsb=8)):
         assert mul(**kw) == -2, kw
+
+
+def test_orthogonalize_host_argument_errors(L):
+    import ctypes
+    coefs = (ctypes.c_double * 3)(1.5, -0.5, 0.0)
+    nan = (ctypes.c_double * 3)(1.5, float("nan"), 0.0)
+
+    def call(g=FAKE, dt=0, batch=2, rows=30, cols=40, st=40, bst=1200, steps=5, co=coefs, eps=1e-7, out=FAKE, ws=FAKE, wsb=1 << 30):
+        return L.pace_orthogonalize(g, dt, batch, rows, cols, st, bst, steps, co, eps, out, ws, wsb, None)
+
+    for kw in (dict(g=None), dict(g=FAKE + 2), dict(dt=3), dict(batch=-1), dict(batch=65536), dict(rows=0), dict(cols=0),
+               dict(cols=2 ** 21 + 1, st=2 ** 22, bst=2 ** 40), dict(st=39), dict(bst=1199), dict(steps=-1), dict(steps=101), dict(co=None),
+               dict(co=nan), dict(eps=0.0), dict(eps=-1.0), dict(eps=float("inf")), dict(eps=float("nan")), dict(out=None), dict(out=FAKE + 1)):
+        assert call(**kw) == -1, kw
+    for kw in (dict(ws=None), dict(ws=FAKE + 32), dict(wsb=100)):
+        assert call(**kw) == -2, kw
