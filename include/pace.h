@@ -489,7 +489,7 @@ int pace_policy_loss(const float *lp_new, const float *lp_behavior, const int32_
 
 /* pace_quantize_rows -- rows in 8 bits with a scale each (tokens, or the output
  * channels of a weight): with a the row's largest |x|,
- *   scale_out[i] = a / 127,  q_out[i, :] = rint(x (127 / a)), half to even,
+ *   scale_out[i] = a / 127,  q_out[i, :] = rint(x (127 (1 / a))), half to even,
  * each operation a binary32 step. A row with a < 2^-119 is zeros with scale 0; one
  * with an infinity or a NaN is zeros with scale NaN.
  * x: [n_rows, n_cols] of dtype, row_stride elements apart; 1 <= n_cols < 2^31

@@ -664,7 +664,7 @@ def pace_policy_loss(lp_new, lp_behavior, offsets, advantage, tags=None, weight=
 
 
 def pace_quantize_rows(x, q_out=None, scale_out=None, stream=None):
-    """Rows in 8 bits: scale = max |x| / 127, q = rint(x (127 / max |x|)). Returns (q int8[n, k], scale f32[n])."""
+    """Rows in 8 bits: scale = max |x| / 127, q = rint(x (127 (1 / max |x|))). Returns (q int8[n, k], scale f32[n])."""
     dt, n, k, stride = _matrix(x, "x")
     q_out = _sized(q_out, torch.int8, (n, k), x.device, "q_out")
     scale_out = _sized(scale_out, torch.float32, (n,), x.device, "scale_out")

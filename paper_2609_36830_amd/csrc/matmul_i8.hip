@@ -1,7 +1,7 @@
 // Products in 8-bit integers for gfx950, with a scale for each row of both
 // sides (tokens and output channels), and the rows' quantisation.
 //
-//   s = max |x| / 127,  q = rint(x (127 / max |x|));   out = (sum_k a b) sa sb
+//   s = max |x| / 127,  q = rint(x (127 (1 / max |x|)));   out = (sum_k a b) sa sb
 //
 // The integer sums are exact in 32 bits (k < 131072). They are converted once,
 // multiplied by the product of the scales in binary32 and rounded once.
@@ -48,7 +48,7 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_rows_kernel(const T *_
     // A row below 2^-119 would have a scale that is no normal number: it is nothing.
     // One with an infinity or a NaN has a NaN scale and zeros.
     const bool bad = most >= 0x7f800000u, none = bad || amax < 1.5046327690525280e-36f;
-    const float inv = none ? 0.0f : 127.0f / amax;
+    const float inv = none ? 0.0f : 127.0f * (1.0f / amax);
     if (threadIdx.x == 0) scale[row_i] = bad ? __builtin_nanf("") : (none ? 0.0f : amax / 127.0f);
     auto code = [&](float v) { return none ? 0 : (int)__builtin_rintf(v * inv); };
     for (int64_t v = threadIdx.x; v < nv; v += kQuantThreads) {

@@ -43,7 +43,7 @@ def quantized(x):
         most = np.max(np.abs(x), axis=1)
         bad = ~np.isfinite(x).all(1)
         none = bad | (most < np.float32(2.0 ** -119))
-        inv = np.where(none, np.float32(0), np.float32(127) / most).astype(np.float32)
+        inv = np.where(none, np.float32(0), np.float32(127) * (np.float32(1) / most)).astype(np.float32)
         q = np.where(none[:, None], 0, np.rint(x * inv[:, None])).astype(np.int8)
         s = np.where(bad, np.float32("nan"), np.where(none, np.float32(0), most / np.float32(127))).astype(np.float32)
     return q, s
