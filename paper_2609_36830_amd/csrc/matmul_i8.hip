@@ -88,15 +88,30 @@ __global__ __launch_bounds__(kWM *kWN *kWave) void matmul_i8_kernel(Rows b, Rows
     tile_of<8>(blockIdx.x, (b.rows + kBN - 1) / kBN, (a.rows + kBM - 1) / kBM, tn, tm);
     TileProduct<MulI8, kBN, kBM, kWN, kWM, kDirect> t;
     t.run(b, tn * kBN, a, tm * kBM, lds, 0, a.bytes);
-    t.each4([&](int c, int r, const mfma_v4i &v) {
-        const int64_t row = tm * kBM + r, col = tn * kBN + c;
-        if (row >= a.rows || col >= b.rows) return;
-        const float s = sa[row];
-        float y[4];
+    // All scales first: a lane's channels are 4 kTM, its tokens kTN.
+    using P = decltype(t);
+    float s[P::kTM][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = (float)v[e] * (s * sb[col + e < b.rows ? col + e : col]);
-        store4(out + row * ldo, col, b.rows, y);
-    });
+    for (int i = 0; i < P::kTM; ++i) {
+        const int64_t c = tn * kBN + P::row4(i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[i][e] = sb[c + e < b.rows ? c + e : b.rows - 1];
+    }
+#pragma unroll
+    for (int j = 0; j < P::kTN; ++j) {
+        const int64_t row = tm * kBM + P::col(j);
+        if (row >= a.rows) continue;
+        const float sr = sa[row];
+        O *to = out + row * ldo;
+#pragma unroll
+        for (int i = 0; i < P::kTM; ++i) {
+            const int64_t c = tn * kBN + P::row4(i);
+            float y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = (float)t.acc[i][j][e] * (sr * s[i][e]);
+            store4(to, c, b.rows, y);
+        }
+    }
 }
 
 }  // namespace

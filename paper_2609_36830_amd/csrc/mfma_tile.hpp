@@ -107,14 +107,14 @@ struct TileProduct {
             return i < kMineA ? load_chunk(a, row_of(a, row_a, i), k + lane_chunk())
                               : load_chunk(b, row_of(b, row_b, i - kMineA), k + lane_chunk());
         };
-        // Begins to fetch the whole step k into buf, and ends it.
-        auto fetch = [&](int64_t k, char *buf) {
+        // Begins to fetch the whole step k (into `to`), and ends it.
+        auto fetch = [&](int64_t k, char *to) {
 #pragma unroll
             for (int i = 0; i < kMine; ++i) {
                 if constexpr (kDirect)
                     __builtin_amdgcn_global_load_lds(
                         (const __attribute__((address_space(1))) void *)((i < kMineA ? pa : pb) + k + from[i]),
-                        (__attribute__((address_space(3))) void *)piece(buf, i), 16, 0, 0);
+                        (__attribute__((address_space(3))) void *)piece(to, i), 16, 0, 0);
                 else
                     held[i] = staged(k, i);
             }
@@ -135,60 +135,110 @@ struct TileProduct {
                 for (int i = 0; i < kMine; ++i) *reinterpret_cast<uint4 *>(piece(buf, i) + lane * 16) = staged(k, i);
             }
         };
-        // The products of the step in `now`, with what is done after its first reads.
-        auto products = [&](const char *now, auto between) {
-            mfma_v4i fa[kTM], fb[kTN];
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const int c = s ? c1 : c0;
-#pragma unroll
-                for (int i = 0; i < kTM; ++i) fa[i] = *reinterpret_cast<const mfma_v4i *>(now + base_a + i * 16 * kStepBytes + c);
-#pragma unroll
-                for (int j = 0; j < kTN; ++j) fb[j] = *reinterpret_cast<const mfma_v4i *>(now + base_b + j * 16 * kStepBytes + c);
-                if (s == 0) between();
-#pragma unroll
-                for (int i = 0; i < kTM; ++i)
-#pragma unroll
-                    for (int j = 0; j < kTN; ++j) acc[i][j] = Mul::mul(fa[i], fb[j], acc[i][j]);
-            }
+        // The operands of half a step (64 bytes), and its products.
+        struct Half {
+            mfma_v4i a[kTM], b[kTN];
         };
-        // A step's bytes are there, and nobody reads the other buffer any more.
+        auto half = [&](const char *now, int s, Half &h) {
+            const int c = s ? c1 : c0;
+#pragma unroll
+            for (int i = 0; i < kTM; ++i) h.a[i] = *reinterpret_cast<const mfma_v4i *>(now + base_a + i * 16 * kStepBytes + c);
+#pragma unroll
+            for (int j = 0; j < kTN; ++j) h.b[j] = *reinterpret_cast<const mfma_v4i *>(now + base_b + j * 16 * kStepBytes + c);
+        };
+        auto products = [&](const Half &h) {
+#pragma unroll
+            for (int i = 0; i < kTM; ++i)
+#pragma unroll
+                for (int j = 0; j < kTN; ++j) acc[i][j] = Mul::mul(h.a[i], h.b[j], acc[i][j]);
+        };
+        // The bytes on their way are there, and nobody reads what was read before.
         auto ready = [&]() {
             __builtin_amdgcn_s_waitcnt(0);
             __syncthreads();
         };
-        int64_t k = k0;
+        int64_t k = k0, fetched = k0;
         int buf = 0;
-        if (k + 2 * kStepBytes <= k1) {
-            fetch(k, lds);
-            settle(lds);
-            for (; k + 2 * kStepBytes <= k1; k += kStepBytes) {
+        if constexpr (kDirect) {
+            // Half a step ahead: while one half's products run, the next half is
+            // read from LDS, and between the halves the buffer that has just
+            // been read is given to the step after the next.
+            if (k0 + 3 * kStepBytes <= k1) {
+                fetch(k0, lds);
                 ready();
-                products(lds + buf * kBuf, [&]() { fetch(k + kStepBytes, lds + (buf ^ 1) * kBuf); });
-                buf ^= 1;
-                settle(lds + buf * kBuf);
+                fetch(k0 + kStepBytes, lds + kBuf);
+                Half h0, h1;
+                half(lds, 0, h0);
+                for (; k + 3 * kStepBytes <= k1; k += kStepBytes) {
+                    half(lds + buf * kBuf, 1, h1);
+                    products(h0);
+                    interleave<kTM + kTN, 0>();
+                    ready();
+                    fetch(k + 2 * kStepBytes, lds + buf * kBuf);
+                    buf ^= 1;
+                    half(lds + buf * kBuf, 0, h0);
+                    products(h1);
+                    interleave<kTM + kTN, kMine>();
+                }
+                fetched = k + 2 * kStepBytes;
             }
         } else {
-            fetch_last(k, lds);
+            if (k0 + 2 * kStepBytes <= k1) {
+                fetch(k0, lds);
+                settle(lds);
+                for (; k + 2 * kStepBytes <= k1; k += kStepBytes) {
+                    ready();
+                    Half h;
+                    half(lds + buf * kBuf, 0, h);
+                    fetch(k + kStepBytes, nullptr);
+                    products(h);
+                    half(lds + buf * kBuf, 1, h);
+                    products(h);
+                    buf ^= 1;
+                    settle(lds + buf * kBuf);
+                }
+                fetched = k + kStepBytes;
+            }
         }
-        // The last whole step, fetched above, and what is behind it.
+        // The last steps, whole or not.
+        if (fetched == k0) {
+            fetch_last(k0, lds);
+            fetched += kStepBytes;
+        }
         for (; k < k1; k += kStepBytes) {
             ready();
-            if (k + kStepBytes < k1) fetch_last(k + kStepBytes, lds + (buf ^ 1) * kBuf);
-            products(lds + buf * kBuf, []() {});
+            if (fetched == k + kStepBytes && fetched < k1) {
+                fetch_last(fetched, lds + (buf ^ 1) * kBuf);
+                fetched += kStepBytes;
+            }
+            Half h;
+            half(lds + buf * kBuf, 0, h);
+            products(h);
+            half(lds + buf * kBuf, 1, h);
+            products(h);
             buf ^= 1;
         }
     }
 
-    // f(first of four rows in the tile, column in the tile, the four values) for all that this lane holds.
-    template <typename F>
-    __device__ __forceinline__ void each4(F f) const {
-        const int wave = threadIdx.x / kWave, lane = lane_id();
-        const int r0 = wave / kWN * (kBM / kWM) + (lane >> 4) * 4, c0 = wave % kWN * (kBN / kWN) + (lane & 15);
+    // Asks for an order of what stands before it: one read (and, while there
+    // are some, one fetch) for every few products.
+    template <int kReads, int kFetches>
+    static __device__ __forceinline__ void interleave() {
+        constexpr int kAll = kTM * kTN, kEach = kAll / kReads > 0 ? kAll / kReads : 1;
 #pragma unroll
-        for (int j = 0; j < kTN; ++j)
-#pragma unroll
-            for (int i = 0; i < kTM; ++i) f(r0 + i * 16, c0 + j * 16, acc[i][j]);
+        for (int i = 0; i < kReads; ++i) {
+            if (i < kFetches) __builtin_amdgcn_sched_group_barrier(0x10, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x8, kEach, 0);
+        }
+    }
+
+    // The first of the four consecutive rows in the tile of acc[i][..], and the column of acc[..][j].
+    static __device__ __forceinline__ int row4(int i) {
+        return (int)(threadIdx.x / kWave) / kWN * (kBM / kWM) + (lane_id() >> 4) * 4 + i * 16;
+    }
+    static __device__ __forceinline__ int col(int j) {
+        return (int)(threadIdx.x / kWave) % kWN * (kBN / kWN) + (lane_id() & 15) + j * 16;
     }
 };
 

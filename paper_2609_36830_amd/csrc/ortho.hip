@@ -128,17 +128,21 @@ __device__ __forceinline__ void lower_tile(int64_t id, int64_t &tm, int64_t &tn)
     tn = id - t * (t + 1) / 2;
 }
 
-// Element (r .. r + 3, c) of a symmetric matrix with zeros up to column mp, to
-// both of its places.
+struct alignas(8) Four {
+    f16_t e[4];
+};
+
+// Elements (r .. r + 3, c) of a symmetric matrix with zeros up to column mp, to
+// both of their places.
 __device__ __forceinline__ void store_both(f16_t *to, int64_t m, int64_t mp, int64_t r, int64_t c, const float (&v)[4],
                                            bool mirror) {
-    struct alignas(8) { f16_t e[4]; } w;
+    Four w;
 #pragma unroll
     for (int e = 0; e < 4; ++e) w.e[e] = (f16_t)(r + e < m ? v[e] : 0.0f);
-    if (mirror && c < m && r < mp) *reinterpret_cast<decltype(w) *>(to + c * mp + r) = w;
+    if (mirror && c < m && r < mp) *reinterpret_cast<Four *>(to + c * mp + r) = w;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-        if (r + e < m && c < mp) to[(r + e) * mp + c] = (f16_t)(c < m ? v[e] : 0.0f);
+        if (r + e < m && c < mp) to[(r + e) * mp + c] = c < m ? w.e[e] : (f16_t)0.0f;
 }
 
 // kSquare: C = a I + b A + c A A from A, else A = X X^T.
@@ -153,20 +157,33 @@ __global__ __launch_bounds__(kWM *kWN *kWave) void ortho_gram_kernel(OrthoShape 
     t.run(x, tm * kB, x, tn * kB, lds, 0, x.bytes);
     const f16_t *a = (const f16_t *)(w + s.a);
     f16_t *to = (f16_t *)(w + (kSquare ? s.c : s.a));
-    t.each4([&](int r, int c, const mfma_v4f &v) {
-        const int64_t row = tm * kB + r, col = tn * kB + c;
-        float y[4];
+    using P = decltype(t);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (kSquare) {
-                const float g = row + e < s.m && col < s.m ? (float)a[(row + e) * s.mp + col] : 0.0f;
-                y[e] = __builtin_fmaf(cc / kScaleA, v[e], cb * g) + (row + e == col ? ca * kScaleA : 0.0f);
-            } else {
-                y[e] = v[e] * (kScaleA / (kScaleX * kScaleX));
+    for (int j = 0; j < P::kTN; ++j) {
+        const int64_t col = tn * kB + P::col(j);
+        Four g[P::kTM];
+        if (kSquare) {
+            // A's elements of this column, by its row of the same number
+#pragma unroll
+            for (int i = 0; i < P::kTM; ++i) {
+                const int64_t row = tm * kB + P::row4(i);
+                g[i] = *reinterpret_cast<const Four *>(a + (col < s.m ? col : 0) * s.mp + (row < s.mp ? row : 0));
             }
         }
-        store_both(to, s.m, s.mp, row, col, y, tm != tn);
-    });
+#pragma unroll
+        for (int i = 0; i < P::kTM; ++i) {
+            const int64_t row = tm * kB + P::row4(i);
+            float y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (kSquare)
+                    y[e] = __builtin_fmaf(cc / kScaleA, t.acc[i][j][e], cb * (float)g[i].e[e]) + (row + e == col ? ca * kScaleA : 0.0f);
+                else
+                    y[e] = t.acc[i][j][e] * (kScaleA / (kScaleX * kScaleX));
+            }
+            store_both(to, s.m, s.mp, row, col, y, tm != tn);
+        }
+    }
 }
 
 // X <- C X by rows and by columns, or, in the last step, the result.
@@ -182,23 +199,30 @@ __global__ __launch_bounds__(kWM *kWN *kWave) void ortho_apply_kernel(OrthoShape
     t.run(c, tm * kB, x, tn * kB, lds, 0, c.bytes);
     f16_t *by_rows = (f16_t *)(w + s.x), *by_cols = (f16_t *)(w + xt_to);
     bf16_t *o = kLast ? out + blockIdx.y * s.m * s.n : nullptr;
-    t.each4([&](int r, int cl, const mfma_v4f &v) {
-        const int64_t row = tm * kB + r, col = tn * kB + cl;
-        if constexpr (kLast) {
+    using P = decltype(t);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (row + e < s.m && col < s.n)
-                    o[s.turned ? col * s.m + row + e : (row + e) * s.n + col] = from_f32<bf16_t>(v[e] * (1.0f / (kScaleA * kScaleX)));
-        } else {
-            struct alignas(8) { f16_t e[4]; } y;
+    for (int j = 0; j < P::kTN; ++j) {
+        const int64_t col = tn * kB + P::col(j);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y.e[e] = (f16_t)(row + e < s.m ? v[e] * (1.0f / kScaleA) : 0.0f);
-            if (col < s.n && row < s.mp) *reinterpret_cast<decltype(y) *>(by_cols + col * s.mp + row) = y;
+        for (int i = 0; i < P::kTM; ++i) {
+            const int64_t row = tm * kB + P::row4(i);
+            const mfma_v4f v = t.acc[i][j];
+            if constexpr (kLast) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (row + e < s.m && col < s.np) by_rows[(row + e) * s.np + col] = col < s.n ? y.e[e] : (f16_t)0.0f;
+                for (int e = 0; e < 4; ++e)
+                    if (row + e < s.m && col < s.n)
+                        o[s.turned ? col * s.m + row + e : (row + e) * s.n + col] = from_f32<bf16_t>(v[e] * (1.0f / (kScaleA * kScaleX)));
+            } else {
+                Four y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y.e[e] = (f16_t)(row + e < s.m ? v[e] * (1.0f / kScaleA) : 0.0f);
+                if (col < s.n && row < s.mp) *reinterpret_cast<Four *>(by_cols + col * s.mp + row) = y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (row + e < s.m && col < s.np) by_rows[(row + e) * s.np + col] = col < s.n ? y.e[e] : (f16_t)0.0f;
+            }
         }
-    });
+    }
 }
 
 // No steps: the normalised update itself.
