@@ -62,54 +62,76 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_rows_kernel(const T *_
     if (nv * V + threadIdx.x < cols) to[nv * V + threadIdx.x] = (int8_t)code(to_f32(row[nv * V + threadIdx.x]));
 }
 
-// Four values in consecutive columns of a row of the output, from column c on.
-template <typename O>
-__device__ __forceinline__ void store4(O *row, int64_t c, int64_t n, const float (&v)[4]) {
-    struct __attribute__((packed)) { O e[4]; } w;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w.e[e] = from_f32<O>(v[e]);
-    if (c + 4 <= n) {
-        *reinterpret_cast<decltype(w) *>(row + c) = w;
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (c + e < n) row[c + e] = w.e[e];
-    }
-}
-
 // The channels are the tile's rows, so that a lane holds four consecutive ones
-// of a token and stores them together.
+// of a token. A wave turns its part in LDS and stores each token's channels in
+// 16-byte pieces of one run; the scales, which the first bytes' wait covers, lie
+// behind.
+template <typename O, int kBN, int kBM, int kWN, int kWM, bool kDirect>
+struct I8Tile {
+    using P = TileProduct<MulI8, kBN, kBM, kWN, kWM, kDirect>;
+    static constexpr int kChan = kBN / kWN, kTok = kBM / kWM;      // of a wave
+    static constexpr int kPass = sizeof(O) == 4 ? kTok / 2 : kTok;  // tokens turned at a time
+    static constexpr int kRun = kChan * (int)sizeof(O) + 16;       // a token's bytes in LDS: 4 banks on from the last token's
+    static constexpr int kTurn = P::kWaves * kPass * kRun;
+    static constexpr int kScales = P::kLdsBytes > kTurn ? P::kLdsBytes : kTurn;
+    static constexpr int kLds = kScales + (kBN + kBM) * (int)sizeof(float);
+};
+
 template <typename O, int kBN, int kBM, int kWN, int kWM, bool kDirect>
 __global__ __launch_bounds__(kWM *kWN *kWave) void matmul_i8_kernel(Rows b, Rows a, const float *__restrict__ sb,
                                                                     const float *__restrict__ sa, O *__restrict__ out,
                                                                     int64_t ldo) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    int64_t tn, tm;
-    tile_of<8>(blockIdx.x, (b.rows + kBN - 1) / kBN, (a.rows + kBM - 1) / kBM, tn, tm);
-    TileProduct<MulI8, kBN, kBM, kWN, kWM, kDirect> t;
-    t.run(b, tn * kBN, a, tm * kBM, lds, 0, a.bytes);
-    // All scales first: a lane's channels are 4 kTM, its tokens kTN.
-    using P = decltype(t);
-    float s[P::kTM][4];
-#pragma unroll
-    for (int i = 0; i < P::kTM; ++i) {
-        const int64_t c = tn * kBN + P::row4(i);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[i][e] = sb[c + e < b.rows ? c + e : b.rows - 1];
+    using T = I8Tile<O, kBN, kBM, kWN, kWM, kDirect>;
+    using P = typename T::P;
+    int tn, tm;
+    tile_of<8>(blockIdx.x, (uint32_t)((b.rows + kBN - 1) / kBN), (uint32_t)((a.rows + kBM - 1) / kBM), tn, tm);
+    const int64_t n0 = (int64_t)tn * kBN, m0 = (int64_t)tm * kBM;
+    float *sn = reinterpret_cast<float *>(lds + T::kScales), *sm = sn + kBN;
+    for (int v = threadIdx.x; v < kBN + kBM; v += P::kThreads) {
+        const bool chan = v < kBN;
+        const int64_t at = chan ? n0 + v : m0 + v - kBN, n = chan ? b.rows : a.rows;
+        sn[v] = (chan ? sb : sa)[at < n ? at : n - 1];
     }
+    P t;
+    t.run(b, n0, a, m0, lds);
+    __syncthreads();                                 // nobody reads the operands any more
+    constexpr int kPer = 16 / (int)sizeof(O);        // channels of a piece
+    const int wave = threadIdx.x / kWave, lane = lane_id();
+    char *mine = lds + wave * (T::kPass * T::kRun);
+    const int c0 = wave / kWM * T::kChan, r0 = wave % kWM * T::kTok;
 #pragma unroll
-    for (int j = 0; j < P::kTN; ++j) {
-        const int64_t row = tm * kBM + P::col(j);
-        if (row >= a.rows) continue;
-        const float sr = sa[row];
-        O *to = out + row * ldo;
+    for (int pass = 0; pass < T::kTok / T::kPass; ++pass) {
+        constexpr int kJ = T::kPass / 16;
 #pragma unroll
-        for (int i = 0; i < P::kTM; ++i) {
-            const int64_t c = tn * kBN + P::row4(i);
-            float y[4];
+        for (int jj = 0; jj < kJ; ++jj) {
+            const int j = pass * kJ + jj;
+            const float sr = sm[P::col(j)];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = (float)t.acc[i][j][e] * (sr * s[i][e]);
-            store4(to, c, b.rows, y);
+            for (int i = 0; i < P::kTM; ++i) {
+                const float4 s = *reinterpret_cast<const float4 *>(sn + P::row4(i));
+                struct __attribute__((packed, aligned(4))) { O e[4]; } y = {{from_f32<O>((float)t.acc[i][j][0] * (sr * s.x)), from_f32<O>((float)t.acc[i][j][1] * (sr * s.y)),
+                                                        from_f32<O>((float)t.acc[i][j][2] * (sr * s.z)), from_f32<O>((float)t.acc[i][j][3] * (sr * s.w))}};
+                __builtin_memcpy(mine + (P::col(j) - r0 - pass * T::kPass) * T::kRun + (P::row4(i) - c0) * (int)sizeof(O), &y, sizeof(y));
+            }
+        }
+        // Only this wave's part of LDS: no barrier, the wave's own accesses are in order.
+        constexpr int kPieces = T::kChan / kPer, kRows = kWave / kPieces;      // of a token; tokens a round
+        const int64_t c = n0 + c0 + lane % kPieces * kPer;
+#pragma unroll
+        for (int r = lane / kPieces; r < T::kPass; r += kRows) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(mine + r * T::kRun + lane % kPieces * 16);
+            const int64_t row = m0 + r0 + pass * T::kPass + r;
+            if (row >= a.rows) continue;
+            O *to = out + row * ldo + c;
+            if (c + kPer <= b.rows) {
+                store_a1(to, v);
+            } else {
+                struct { O e[kPer]; } w = __builtin_bit_cast(decltype(w), v);
+#pragma unroll
+                for (int e = 0; e < kPer; ++e)
+                    if (c + e < b.rows) to[e] = w.e[e];
+            }
         }
     }
 }
@@ -131,10 +153,10 @@ namespace {
 template <typename O, int kBN, int kBM, int kWN, int kWM, bool kDirect>
 hipError_t launch_tiles(const Rows &b, const Rows &a, const float *sb, const float *sa, void *out, int64_t ldo,
                         hipStream_t stream) {
-    using T = TileProduct<MulI8, kBN, kBM, kWN, kWM, kDirect>;
+    using T = I8Tile<O, kBN, kBM, kWN, kWM, kDirect>;
     const int64_t tiles = ((a.rows + kBM - 1) / kBM) * ((b.rows + kBN - 1) / kBN);
-    return launch_lds(kPhaseAux, matmul_i8_kernel<O, kBN, kBM, kWN, kWM, kDirect>, dim3((unsigned)tiles), dim3(T::kThreads),
-                      T::kLdsBytes, stream, b, a, sb, sa, (O *)out, ldo);
+    return launch_lds(kPhaseAux, matmul_i8_kernel<O, kBN, kBM, kWN, kWM, kDirect>, dim3((unsigned)tiles), dim3(T::P::kThreads), T::kLds, stream,
+                      b, a, sb, sa, (O *)out, ldo);
 }
 
 }  // namespace
@@ -146,14 +168,14 @@ hipError_t launch_matmul_i8(const int8_t *a, int64_t lda, const float *sa, const
     if (m == 0 || n == 0) return hipSuccess;
     const Rows ra{(const char *)a, lda, m, k}, rb{(const char *)b, ldb, n, k};
     // a tile's rows are numbered by 32-bit byte offsets
-    const bool direct = (((uintptr_t)a | (uintptr_t)b | (uint64_t)lda | (uint64_t)ldb | (uint64_t)k) & 15) == 0 &&
+    const bool direct = (((uintptr_t)a | (uintptr_t)b | (uint64_t)lda | (uint64_t)ldb) & 15) == 0 && k % kStepBytes == 0 &&
                         lda < (1 << 23) && ldb < (1 << 23);
     return with_elem(dtype, [&](auto tag) {
         using O = decltype(tag);
         const int64_t big = ((m + 255) / 256) * ((n + 255) / 256);
         if (m > 128 && big >= 128)
             return direct ? launch_tiles<O, 256, 256, 2, 4, true>(rb, ra, sb, sa, out, ldo, stream)
-                          : launch_tiles<O, 256, 256, 2, 4, false>(rb, ra, sb, sa, out, ldo, stream);
+                          : launch_tiles<O, 128, 128, 2, 2, false>(rb, ra, sb, sa, out, ldo, stream);
         return direct ? launch_tiles<O, 64, 64, 2, 2, true>(rb, ra, sb, sa, out, ldo, stream)
                       : launch_tiles<O, 64, 64, 2, 2, false>(rb, ra, sb, sa, out, ldo, stream);
     });

@@ -22,6 +22,8 @@ typedef _Float16 mfma_v8h __attribute__((ext_vector_type(8)));
 
 // 16x16 products over 64 bytes of the summed axis: lane l holds 16 bytes of row
 // l & 15 of each side; result element i is (row 4 (l >> 4) + i, column l & 15).
+// (32x32 products are no faster, and their results lie in 16-byte pieces of 32
+// rows to a store where these lie in 32-byte pieces of 16.)
 struct MulI8 {
     using Acc = mfma_v4i;
     static __device__ __forceinline__ Acc mul(mfma_v4i a, mfma_v4i b, Acc c) {
@@ -44,14 +46,14 @@ struct Rows {
     int64_t stride, rows, bytes;
 };
 
-// kBM x kBN tiles by kWM x kWN waves. kDirect: rows and strides are whole,
-// aligned 16-byte chunks, fetched straight into LDS; otherwise, and for a last
-// step that is not whole, the bytes pass through registers.
+// kBM x kBN tiles by kWM x kWN waves. kDirect: rows are whole steps, their
+// starts and strides whole 16-byte chunks, and the bytes go straight into LDS;
+// otherwise they pass through registers.
 template <typename Mul, int kBM, int kBN, int kWM, int kWN, bool kDirect>
 struct TileProduct {
     static constexpr int kWaves = kWM * kWN, kThreads = kWaves * kWave;
     static constexpr int kTM = kBM / kWM / 16, kTN = kBN / kWN / 16;
-    static constexpr int kBuf = (kBM + kBN) * kStepBytes, kLdsBytes = 2 * kBuf;
+    static constexpr int kBuf = (kBM + kBN) * kStepBytes, kLdsBytes = 2 * kBuf, kB = kBM * kStepBytes;
     // Pieces of 8 rows, 1 KiB, an instruction; a wave takes every kWaves-th.
     static constexpr int kPieces = (kBM + kBN) / 8, kMine = kPieces / kWaves;
     static_assert(kPieces % kWaves == 0 && (kBM / 8) % kWaves == 0, "whole shares");
@@ -59,186 +61,143 @@ struct TileProduct {
     using Acc = typename Mul::Acc;
 
     Acc acc[kTM][kTN];
+    Rows a, b;
+    int64_t row_a, row_b;
+    const char *pa, *pb;                             // the tile's first rows
+    uint32_t from[kDirect ? kMine : 1];              // this lane's pieces, in bytes behind them
 
-    // The row of the operand that this lane fetches in its i-th piece. Rows
+    // The first of the four consecutive rows in the tile of acc[i][..], and the column of acc[..][j].
+    static __device__ __forceinline__ int row4(int i) {
+        return (int)(threadIdx.x / kWave) / kWN * (kBM / kWM) + i * 16 + (lane_id() >> 4) * 4;
+    }
+    static __device__ __forceinline__ int col(int j) {
+        return (int)(threadIdx.x / kWave) % kWN * (kBN / kWN) + j * 16 + (lane_id() & 15);
+    }
+
+    // The row of an operand that this lane fetches in its i-th piece. Rows
     // beyond the last are that one again: what they give is not kept.
     static __device__ __forceinline__ int64_t row_of(const Rows &m, int64_t row0, int i) {
         const int64_t row = row0 + (i * kWaves + threadIdx.x / kWave) * 8 + (lane_id() >> 3);
         return row < m.rows ? row : m.rows - 1;
     }
     static __device__ __forceinline__ int lane_chunk() { return ((lane_id() & 7) ^ (lane_id() >> 3)) << 4; }
+    static __device__ __forceinline__ char *piece(char *to, int i) { return to + (i * kWaves + threadIdx.x / kWave) * 1024; }
 
     static __device__ __forceinline__ uint4 load_chunk(const Rows &m, int64_t row, int64_t at) {
-        const char *from = m.p + row * m.stride + at;
-        if (at + 16 <= m.bytes) return load_a1(from);
+        const char *p = m.p + row * m.stride + at;
+        if (at + 16 <= m.bytes) return load_a1(p);
         uint32_t w[4] = {0, 0, 0, 0};
         if (at < m.bytes)
-            for (int b = 0; at + b < m.bytes; ++b) w[b >> 2] |= (uint32_t)(uint8_t)from[b] << (8 * (b & 3));
+            for (int k = 0; at + k < m.bytes; ++k) w[k >> 2] |= (uint32_t)(uint8_t)p[k] << (8 * (k & 3));
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
+    __device__ __forceinline__ uint4 staged(int64_t k, int i) const {
+        return i < kMineA ? load_chunk(a, row_of(a, row_a, i), k + lane_chunk())
+                          : load_chunk(b, row_of(b, row_b, i - kMineA), k + lane_chunk());
+    }
+    // Begins to fetch the whole step k.
+    __device__ __forceinline__ void fetch(int64_t k, char *to) const {
+#pragma unroll
+        for (int i = 0; i < kMine; ++i)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)((i < kMineA ? pa : pb) + k + from[i]),
+                                             (__attribute__((address_space(3))) void *)piece(to, i), 16, 0, 0);
+    }
+    // The bytes on their way are there, and nobody reads what was read before.
+    static __device__ __forceinline__ void ready() {
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+    }
 
-    __device__ __forceinline__ void run(const Rows &a, int64_t row_a, const Rows &b, int64_t row_b, char *lds, int64_t k0,
-                                        int64_t k1) {
-        const int wave = threadIdx.x / kWave, lane = lane_id();
-        const int wm = wave / kWN, wn = wave % kWN;
+    // The operands of half a step (64 bytes), and its products.
+    struct Half {
+        mfma_v4i a[kTM], b[kTN];
+    };
+    static __device__ __forceinline__ void half(const char *now, int s, Half &h) {
+        const int lane = lane_id(), wave = threadIdx.x / kWave;
+        const int at = (lane & 15) * kStepBytes + (((4 * s + (lane >> 4)) ^ (lane & 7)) << 4);
+        const char *ra = now + wave / kWN * (kBM / kWM) * kStepBytes + at;
+        const char *rb = now + kB + wave % kWN * (kBN / kWN) * kStepBytes + at;
+#pragma unroll
+        for (int i = 0; i < kTM; ++i) h.a[i] = *reinterpret_cast<const mfma_v4i *>(ra + i * 16 * kStepBytes);
+#pragma unroll
+        for (int j = 0; j < kTN; ++j) h.b[j] = *reinterpret_cast<const mfma_v4i *>(rb + j * 16 * kStepBytes);
+    }
+    __device__ __forceinline__ void products(const Half &h) {
 #pragma unroll
         for (int i = 0; i < kTM; ++i)
 #pragma unroll
-            for (int j = 0; j < kTN; ++j) acc[i][j] = Acc{0, 0, 0, 0};
-        if (k0 >= k1) return;
-        constexpr int kB = kBM * kStepBytes;
-        // Where this lane finds chunk 4 s + (lane >> 4) of row lane & 15 of a 16-row group.
-        const int row = (lane & 15) * kStepBytes;
-        const int c0 = row + ((((lane >> 4)) ^ (lane & 7)) << 4), c1 = row + (((4 + (lane >> 4)) ^ (lane & 7)) << 4);
-        const int base_a = wm * (kBM / kWM) * kStepBytes, base_b = kB + wn * (kBN / kWN) * kStepBytes;
-
-        // Where the lane's pieces come from, in bytes behind each tile's first row.
-        const char *pa = a.p + row_a * a.stride, *pb = b.p + row_b * b.stride;
-        uint32_t from[kDirect ? kMine : 1];
-        if constexpr (kDirect) {
-#pragma unroll
-            for (int i = 0; i < kMine; ++i)
-                from[i] = (i < kMineA ? (uint32_t)((row_of(a, row_a, i) - row_a) * a.stride)
-                                      : (uint32_t)((row_of(b, row_b, i - kMineA) - row_b) * b.stride)) + (uint32_t)lane_chunk();
-        }
-        uint4 held[kDirect ? 1 : kMine];
-        auto piece = [&](char *buf, int i) { return buf + (i * kWaves + wave) * 1024; };
-        auto staged = [&](int64_t k, int i) {
-            return i < kMineA ? load_chunk(a, row_of(a, row_a, i), k + lane_chunk())
-                              : load_chunk(b, row_of(b, row_b, i - kMineA), k + lane_chunk());
-        };
-        // Begins to fetch the whole step k (into `to`), and ends it.
-        auto fetch = [&](int64_t k, char *to) {
-#pragma unroll
-            for (int i = 0; i < kMine; ++i) {
-                if constexpr (kDirect)
-                    __builtin_amdgcn_global_load_lds(
-                        (const __attribute__((address_space(1))) void *)((i < kMineA ? pa : pb) + k + from[i]),
-                        (__attribute__((address_space(3))) void *)piece(to, i), 16, 0, 0);
-                else
-                    held[i] = staged(k, i);
-            }
-        };
-        auto settle = [&](char *buf) {
-            if constexpr (!kDirect) {
-#pragma unroll
-                for (int i = 0; i < kMine; ++i) *reinterpret_cast<uint4 *>(piece(buf, i) + lane * 16) = held[i];
-            }
-        };
-        // The step that ends at k1, whole or not.
-        auto fetch_last = [&](int64_t k, char *buf) {
-            if (k + kStepBytes <= k1) {
-                fetch(k, buf);
-                settle(buf);
-            } else {
-#pragma unroll 1
-                for (int i = 0; i < kMine; ++i) *reinterpret_cast<uint4 *>(piece(buf, i) + lane * 16) = staged(k, i);
-            }
-        };
-        // The operands of half a step (64 bytes), and its products.
-        struct Half {
-            mfma_v4i a[kTM], b[kTN];
-        };
-        auto half = [&](const char *now, int s, Half &h) {
-            const int c = s ? c1 : c0;
-#pragma unroll
-            for (int i = 0; i < kTM; ++i) h.a[i] = *reinterpret_cast<const mfma_v4i *>(now + base_a + i * 16 * kStepBytes + c);
-#pragma unroll
-            for (int j = 0; j < kTN; ++j) h.b[j] = *reinterpret_cast<const mfma_v4i *>(now + base_b + j * 16 * kStepBytes + c);
-        };
-        auto products = [&](const Half &h) {
-#pragma unroll
-            for (int i = 0; i < kTM; ++i)
-#pragma unroll
-                for (int j = 0; j < kTN; ++j) acc[i][j] = Mul::mul(h.a[i], h.b[j], acc[i][j]);
-        };
-        // The bytes on their way are there, and nobody reads what was read before.
-        auto ready = [&]() {
-            __builtin_amdgcn_s_waitcnt(0);
-            __syncthreads();
-        };
-        int64_t k = k0, fetched = k0;
-        int buf = 0;
-        if constexpr (kDirect) {
-            // Half a step ahead: while one half's products run, the next half is
-            // read from LDS, and between the halves the buffer that has just
-            // been read is given to the step after the next.
-            if (k0 + 3 * kStepBytes <= k1) {
-                fetch(k0, lds);
-                ready();
-                fetch(k0 + kStepBytes, lds + kBuf);
-                Half h0, h1;
-                half(lds, 0, h0);
-                for (; k + 3 * kStepBytes <= k1; k += kStepBytes) {
-                    half(lds + buf * kBuf, 1, h1);
-                    products(h0);
-                    interleave<kTM + kTN, 0>();
-                    ready();
-                    fetch(k + 2 * kStepBytes, lds + buf * kBuf);
-                    buf ^= 1;
-                    half(lds + buf * kBuf, 0, h0);
-                    products(h1);
-                    interleave<kTM + kTN, kMine>();
-                }
-                fetched = k + 2 * kStepBytes;
-            }
-        } else {
-            if (k0 + 2 * kStepBytes <= k1) {
-                fetch(k0, lds);
-                settle(lds);
-                for (; k + 2 * kStepBytes <= k1; k += kStepBytes) {
-                    ready();
-                    Half h;
-                    half(lds + buf * kBuf, 0, h);
-                    fetch(k + kStepBytes, nullptr);
-                    products(h);
-                    half(lds + buf * kBuf, 1, h);
-                    products(h);
-                    buf ^= 1;
-                    settle(lds + buf * kBuf);
-                }
-                fetched = k + kStepBytes;
-            }
-        }
-        // The last steps, whole or not.
-        if (fetched == k0) {
-            fetch_last(k0, lds);
-            fetched += kStepBytes;
-        }
-        for (; k < k1; k += kStepBytes) {
-            ready();
-            if (fetched == k + kStepBytes && fetched < k1) {
-                fetch_last(fetched, lds + (buf ^ 1) * kBuf);
-                fetched += kStepBytes;
-            }
-            Half h;
-            half(lds + buf * kBuf, 0, h);
-            products(h);
-            half(lds + buf * kBuf, 1, h);
-            products(h);
-            buf ^= 1;
-        }
+            for (int j = 0; j < kTN; ++j) acc[i][j] = Mul::mul(h.a[i], h.b[j], acc[i][j]);
     }
-
-    // Asks for an order of what stands before it: one read (and, while there
-    // are some, one fetch) for every few products.
-    template <int kReads, int kFetches>
+    // Asks for an order of what stands before it: one read for every few products.
+    template <int kReads>
     static __device__ __forceinline__ void interleave() {
         constexpr int kAll = kTM * kTN, kEach = kAll / kReads > 0 ? kAll / kReads : 1;
 #pragma unroll
         for (int i = 0; i < kReads; ++i) {
-            if (i < kFetches) __builtin_amdgcn_sched_group_barrier(0x10, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x8, kEach, 0);
         }
     }
 
-    // The first of the four consecutive rows in the tile of acc[i][..], and the column of acc[..][j].
-    static __device__ __forceinline__ int row4(int i) {
-        return (int)(threadIdx.x / kWave) / kWN * (kBM / kWM) + (lane_id() >> 4) * 4 + i * 16;
-    }
-    static __device__ __forceinline__ int col(int j) {
-        return (int)(threadIdx.x / kWave) % kWN * (kBN / kWN) + (lane_id() & 15) + j * 16;
+    // The tile of rows row_a_ .. of a_ and row_b_ .. of b_, into acc.
+    __device__ __forceinline__ void run(const Rows &a_, int64_t row_a_, const Rows &b_, int64_t row_b_, char *lds) {
+        a = a_, b = b_, row_a = row_a_, row_b = row_b_;
+        const int64_t bytes = a.bytes;
+        if constexpr (kDirect) {
+            pa = a.p + row_a * a.stride;
+            pb = b.p + row_b * b.stride;
+#pragma unroll
+            for (int i = 0; i < kMine; ++i)
+                from[i] = (i < kMineA ? (uint32_t)((row_of(a, row_a, i) - row_a) * a.stride)
+                                      : (uint32_t)((row_of(b, row_b, i - kMineA) - row_b) * b.stride)) + (uint32_t)lane_chunk();
+            fetch(0, lds);
+            if (bytes >= 2 * kStepBytes) fetch(kStepBytes, lds + kBuf);
+        }
+#pragma unroll
+        for (int i = 0; i < kTM; ++i)
+#pragma unroll
+            for (int j = 0; j < kTN; ++j) acc[i][j] = Acc{0, 0, 0, 0};
+        int64_t k = 0;
+        int buf = 0;
+        if constexpr (kDirect) {
+            // Half a step ahead: while one half's products run, the next half is
+            // read from LDS, and between the halves the buffer that has just
+            // been read is given to the step after the next.
+            Half h0, h1;
+            ready();
+            half(lds, 0, h0);
+            for (; k < bytes; k += kStepBytes) {
+                half(lds + buf * kBuf, 1, h1);
+                products(h0);
+                interleave<kTM + kTN>();
+                ready();
+                if (k + 2 * kStepBytes < bytes) fetch(k + 2 * kStepBytes, lds + buf * kBuf);
+                buf ^= 1;
+                half(lds + buf * kBuf, 0, h0);       // after the last step nothing that is used
+                products(h1);
+                interleave<kTM + kTN>();
+            }
+        } else {
+            // The next step's bytes are loaded while this one's products run.
+            uint4 held[kMine];
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) held[i] = staged(0, i);
+            for (; k < bytes; k += kStepBytes) {
+#pragma unroll
+                for (int i = 0; i < kMine; ++i) *reinterpret_cast<uint4 *>(piece(lds + buf * kBuf, i) + lane_id() * 16) = held[i];
+                ready();
+                Half h;
+                half(lds + buf * kBuf, 0, h);
+                if (k + kStepBytes < bytes) {
+#pragma unroll
+                    for (int i = 0; i < kMine; ++i) held[i] = staged(k + kStepBytes, i);
+                }
+                products(h);
+                half(lds + buf * kBuf, 1, h);
+                products(h);
+                buf ^= 1;
+            }
+        }
     }
 };
 
@@ -247,15 +206,16 @@ struct TileProduct {
 // down columns of kGroup row tiles, so that what its workgroups read at one
 // time is a block of few rows and columns.
 template <int kGroup>
-__device__ __forceinline__ void tile_of(int64_t id, int64_t tiles_m, int64_t tiles_n, int64_t &tm, int64_t &tn) {
-    const int64_t all = tiles_m * tiles_n, per = all / 8, rest = all % 8;
-    const int64_t x = id % 8, i = id / 8;
+__device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, int &tm, int &tn) {
+    const uint32_t all = tiles_m * tiles_n, per = all / 8, rest = all % 8;
+    const uint32_t x = id % 8, i = id / 8;
     id = x * per + (x < rest ? x : rest) + i;
-    const int64_t band = kGroup * tiles_n, g = id / band;
-    const int64_t rows = tiles_m - g * kGroup < kGroup ? tiles_m - g * kGroup : kGroup;
-    const int64_t in = id - g * band;
-    tm = g * kGroup + in % rows;
-    tn = in / rows;
+    const uint32_t band = kGroup * tiles_n, g = id / band;
+    const uint32_t rows = tiles_m - g * kGroup < kGroup ? tiles_m - g * kGroup : kGroup;
+    const uint32_t in = id - g * band;
+    // the same in every lane
+    tm = __builtin_amdgcn_readfirstlane((int)(g * kGroup + in % rows));
+    tn = __builtin_amdgcn_readfirstlane((int)(in / rows));
 }
 
 }  // namespace pace

@@ -120,12 +120,12 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(const T *__restrict__ 
 }
 
 // The id-th tile of a lower triangle of tiles, row by row.
-__device__ __forceinline__ void lower_tile(int64_t id, int64_t &tm, int64_t &tn) {
-    int64_t t = (int64_t)((sqrt((double)(8 * id + 1)) - 1.0) * 0.5);
+__device__ __forceinline__ void lower_tile(uint32_t id, int &tm, int &tn) {
+    int64_t t = (int64_t)((sqrt((double)(8 * (int64_t)id + 1)) - 1.0) * 0.5);
     while (t * (t + 1) / 2 > id) --t;
     while ((t + 1) * (t + 2) / 2 <= id) ++t;
-    tm = t;
-    tn = id - t * (t + 1) / 2;
+    tm = __builtin_amdgcn_readfirstlane((int)t);
+    tn = __builtin_amdgcn_readfirstlane((int)(id - t * (t + 1) / 2));
 }
 
 struct alignas(8) Four {
@@ -145,84 +145,92 @@ __device__ __forceinline__ void store_both(f16_t *to, int64_t m, int64_t mp, int
         if (r + e < m && c < mp) to[(r + e) * mp + c] = c < m ? w.e[e] : (f16_t)0.0f;
 }
 
+// A workgroup takes a tile of one matrix of the batch; a matrix's tiles are neighbours.
 // kSquare: C = a I + b A + c A A from A, else A = X X^T.
 template <bool kSquare, int kB, int kWM, int kWN>
-__global__ __launch_bounds__(kWM *kWN *kWave) void ortho_gram_kernel(OrthoShape s, char *ws, float ca, float cb, float cc) {
+__global__ __launch_bounds__(kWM *kWN *kWave) void ortho_gram_kernel(OrthoShape s, char *ws, uint32_t tiles, float ca,
+                                                                     float cb, float cc) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    char *w = ws + blockIdx.y * s.bytes;
-    int64_t tm, tn;
-    lower_tile(blockIdx.x, tm, tn);
+    using P = TileProduct<MulF16, kB, kB, kWM, kWN, true>;
+    P t;
+    const uint32_t mat = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / tiles));
+    char *w = ws + mat * s.bytes;
+    int tm, tn;
+    lower_tile(blockIdx.x - mat * tiles, tm, tn);
+    const int64_t r0 = (int64_t)tm * kB, c0 = (int64_t)tn * kB;
     const Rows x = kSquare ? Rows{w + s.a, s.mp * 2, s.m, s.mp * 2} : Rows{w + s.x, s.np * 2, s.m, s.np * 2};
-    TileProduct<MulF16, kB, kB, kWM, kWN, true> t;
-    t.run(x, tm * kB, x, tn * kB, lds, 0, x.bytes);
+    t.run(x, r0, x, c0, lds);
     const f16_t *a = (const f16_t *)(w + s.a);
     f16_t *to = (f16_t *)(w + (kSquare ? s.c : s.a));
-    using P = decltype(t);
 #pragma unroll
-    for (int j = 0; j < P::kTN; ++j) {
-        const int64_t col = tn * kB + P::col(j);
-        Four g[P::kTM];
-        if (kSquare) {
-            // A's elements of this column, by its row of the same number
+        for (int j = 0; j < P::kTN; ++j) {
+            const int64_t col = c0 + P::col(j);
+            Four g[P::kTM];
+            if (kSquare) {
+                // A's elements of this column, by its row of the same number
+#pragma unroll
+                for (int i = 0; i < P::kTM; ++i) {
+                    const int64_t row = r0 + P::row4(i);
+                    g[i] = *reinterpret_cast<const Four *>(a + (col < s.m ? col : 0) * s.mp + (row < s.mp ? row : 0));
+                }
+            }
 #pragma unroll
             for (int i = 0; i < P::kTM; ++i) {
-                const int64_t row = tm * kB + P::row4(i);
-                g[i] = *reinterpret_cast<const Four *>(a + (col < s.m ? col : 0) * s.mp + (row < s.mp ? row : 0));
+                const int64_t row = r0 + P::row4(i);
+                float y[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float v = t.acc[i][j][e];
+                    if (kSquare)
+                        y[e] = __builtin_fmaf(cc / kScaleA, v, cb * (float)g[i].e[e]) + (row + e == col ? ca * kScaleA : 0.0f);
+                    else
+                        y[e] = v * (kScaleA / (kScaleX * kScaleX));
+                }
+                store_both(to, s.m, s.mp, row, col, y, r0 != c0);
             }
         }
-#pragma unroll
-        for (int i = 0; i < P::kTM; ++i) {
-            const int64_t row = tm * kB + P::row4(i);
-            float y[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (kSquare)
-                    y[e] = __builtin_fmaf(cc / kScaleA, t.acc[i][j][e], cb * (float)g[i].e[e]) + (row + e == col ? ca * kScaleA : 0.0f);
-                else
-                    y[e] = t.acc[i][j][e] * (kScaleA / (kScaleX * kScaleX));
-            }
-            store_both(to, s.m, s.mp, row, col, y, tm != tn);
-        }
-    }
 }
 
 // X <- C X by rows and by columns, or, in the last step, the result.
 template <bool kLast, int kB, int kWM, int kWN>
 __global__ __launch_bounds__(kWM *kWN *kWave) void ortho_apply_kernel(OrthoShape s, char *ws, int64_t xt_from, int64_t xt_to,
+                                                                      uint32_t tiles_m, uint32_t tiles_n,
                                                                       bf16_t *__restrict__ out) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    char *w = ws + blockIdx.y * s.bytes;
-    int64_t tm, tn;
-    tile_of<8>(blockIdx.x, (s.m + kB - 1) / kB, (s.n + kB - 1) / kB, tm, tn);
+    using P = TileProduct<MulF16, kB, kB, kWM, kWN, true>;
+    P t;
+    const int mat = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / (tiles_m * tiles_n)));
+    int tm, tn;
+    tile_of<8>(blockIdx.x - mat * (tiles_m * tiles_n), tiles_m, tiles_n, tm, tn);
+    char *w = ws + mat * s.bytes;
+    const int64_t r0 = (int64_t)tm * kB, c0 = (int64_t)tn * kB;
     const Rows c{w + s.c, s.mp * 2, s.m, s.mp * 2}, x{w + xt_from, s.mp * 2, s.n, s.mp * 2};
-    TileProduct<MulF16, kB, kB, kWM, kWN, true> t;
-    t.run(c, tm * kB, x, tn * kB, lds, 0, c.bytes);
+    t.run(c, r0, x, c0, lds);
     f16_t *by_rows = (f16_t *)(w + s.x), *by_cols = (f16_t *)(w + xt_to);
-    bf16_t *o = kLast ? out + blockIdx.y * s.m * s.n : nullptr;
-    using P = decltype(t);
+    bf16_t *o = kLast ? out + mat * s.m * s.n : nullptr;
 #pragma unroll
-    for (int j = 0; j < P::kTN; ++j) {
-        const int64_t col = tn * kB + P::col(j);
+        for (int j = 0; j < P::kTN; ++j) {
+            const int64_t col = c0 + P::col(j);
 #pragma unroll
-        for (int i = 0; i < P::kTM; ++i) {
-            const int64_t row = tm * kB + P::row4(i);
-            const mfma_v4f v = t.acc[i][j];
-            if constexpr (kLast) {
+            for (int i = 0; i < P::kTM; ++i) {
+                const int64_t row = r0 + P::row4(i);
+                const mfma_v4f v = t.acc[i][j];
+                if constexpr (kLast) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (row + e < s.m && col < s.n)
-                        o[s.turned ? col * s.m + row + e : (row + e) * s.n + col] = from_f32<bf16_t>(v[e] * (1.0f / (kScaleA * kScaleX)));
-            } else {
-                Four y;
+                    for (int e = 0; e < 4; ++e)
+                        if (row + e < s.m && col < s.n)
+                            o[s.turned ? col * s.m + row + e : (row + e) * s.n + col] = from_f32<bf16_t>(v[e] * (1.0f / (kScaleA * kScaleX)));
+                } else {
+                    Four y;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y.e[e] = (f16_t)(row + e < s.m ? v[e] * (1.0f / kScaleA) : 0.0f);
-                if (col < s.n && row < s.mp) *reinterpret_cast<Four *>(by_cols + col * s.mp + row) = y;
+                    for (int e = 0; e < 4; ++e) y.e[e] = (f16_t)(row + e < s.m ? v[e] * (1.0f / kScaleA) : 0.0f);
+                    if (col < s.n && row < s.mp) *reinterpret_cast<Four *>(by_cols + col * s.mp + row) = y;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (row + e < s.m && col < s.np) by_rows[(row + e) * s.np + col] = col < s.n ? y.e[e] : (f16_t)0.0f;
+                    for (int e = 0; e < 4; ++e)
+                        if (row + e < s.m && col < s.np) by_rows[(row + e) * s.np + col] = col < s.n ? y.e[e] : (f16_t)0.0f;
+                }
             }
         }
-    }
 }
 
 // No steps: the normalised update itself.
@@ -239,16 +247,19 @@ hipError_t ortho_steps(const OrthoShape &s, char *ws, int64_t batch, int steps, 
                        hipStream_t stream) {
     using T = TileProduct<MulF16, kB, kB, kWM, kWN, true>;
     const int64_t tm = (s.m + kB - 1) / kB, tn = (s.n + kB - 1) / kB;
-    const dim3 lower((unsigned)(tm * (tm + 1) / 2), (unsigned)batch), all((unsigned)(tm * tn), (unsigned)batch), block(T::kThreads);
+    const int64_t lower = tm * (tm + 1) / 2;
+    const dim3 half((unsigned)(lower * batch)), all((unsigned)(tm * tn * batch)), block(T::kThreads);
     int64_t from = s.xt, to = s.xt2;
     hipError_t e = hipSuccess;
     for (int k = 0; k < steps && e == hipSuccess; ++k) {
-        e = launch_lds(-1, ortho_gram_kernel<false, kB, kWM, kWN>, lower, block, T::kLdsBytes, stream, s, ws, 0.0f, 0.0f, 0.0f);
+        e = launch_lds(-1, ortho_gram_kernel<false, kB, kWM, kWN>, half, block, T::kLdsBytes, stream, s, ws, lower, 0.0f, 0.0f, 0.0f);
         if (e == hipSuccess)
-            e = launch_lds(-1, ortho_gram_kernel<true, kB, kWM, kWN>, lower, block, T::kLdsBytes, stream, s, ws, coefs[0], coefs[1], coefs[2]);
+            e = launch_lds(-1, ortho_gram_kernel<true, kB, kWM, kWN>, half, block, T::kLdsBytes, stream, s, ws, lower, coefs[0], coefs[1], coefs[2]);
         if (e == hipSuccess)
-            e = k + 1 < steps ? launch_lds(kPhaseAux, ortho_apply_kernel<false, kB, kWM, kWN>, all, block, T::kLdsBytes, stream, s, ws, from, to, out)
-                              : launch_lds(kPhaseAux, ortho_apply_kernel<true, kB, kWM, kWN>, all, block, T::kLdsBytes, stream, s, ws, from, to, out);
+            e = k + 1 < steps ? launch_lds(kPhaseAux, ortho_apply_kernel<false, kB, kWM, kWN>, all, block, T::kLdsBytes, stream, s, ws,
+                                           from, to, tm, tn, out)
+                              : launch_lds(kPhaseAux, ortho_apply_kernel<true, kB, kWM, kWN>, all, block, T::kLdsBytes, stream, s, ws,
+                                           from, to, tm, tn, out);
         const int64_t x = from;
         from = to;
         to = x;
