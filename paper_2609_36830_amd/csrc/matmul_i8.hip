@@ -66,26 +66,26 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_rows_kernel(const T *_
 // of a token. A wave turns its part in LDS and stores each token's channels in
 // 16-byte pieces of one run; the scales, which the first bytes' wait covers, lie
 // behind.
-template <typename O, int kBN, int kBM, int kWN, int kWM, bool kDirect>
+template <typename O, typename P>
 struct I8Tile {
-    using P = TileProduct<MulI8, kBN, kBM, kWN, kWM, kDirect>;
-    static constexpr int kChan = kBN / kWN, kTok = kBM / kWM;      // of a wave
-    static constexpr int kPass = sizeof(O) == 4 ? kTok / 2 : kTok;  // tokens turned at a time
+    static constexpr int kChan = P::kRowsW, kTok = P::kColsW;      // of a wave
+    static constexpr int kPass = sizeof(O) == 2 ? kTok : (kTok % 32 ? 16 : kTok / 2);      // tokens turned at a time
+    static_assert(kTok % kPass == 0 && kPass % 16 == 0, "whole columns of products");
     static constexpr int kRun = kChan * (int)sizeof(O) + 16;       // a token's bytes in LDS: 4 banks on from the last token's
     static constexpr int kTurn = P::kWaves * kPass * kRun;
     static constexpr int kScales = P::kLdsBytes > kTurn ? P::kLdsBytes : kTurn;
-    static constexpr int kLds = kScales + (kBN + kBM) * (int)sizeof(float);
+    static constexpr int kLds = kScales + (P::kRows + P::kCols) * (int)sizeof(float);
 };
 
-template <typename O, int kBN, int kBM, int kWN, int kWM, bool kDirect>
-__global__ __launch_bounds__(kWM *kWN *kWave) void matmul_i8_kernel(Rows b, Rows a, const float *__restrict__ sb,
-                                                                    const float *__restrict__ sa, O *__restrict__ out,
-                                                                    int64_t ldo) {
+template <typename O, typename P>
+__global__ __launch_bounds__(P::kThreads) void matmul_i8_kernel(Rows b, Rows a, const float *__restrict__ sb,
+                                                                const float *__restrict__ sa, O *__restrict__ out,
+                                                                int64_t ldo) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    using T = I8Tile<O, kBN, kBM, kWN, kWM, kDirect>;
-    using P = typename T::P;
+    using T = I8Tile<O, P>;
+    constexpr int kBN = P::kRows, kBM = P::kCols;
     int tn, tm;
-    tile_of<8>(blockIdx.x, (uint32_t)((b.rows + kBN - 1) / kBN), (uint32_t)((a.rows + kBM - 1) / kBM), tn, tm);
+    tile_of<8>(xcd_run(blockIdx.x, gridDim.x), (uint32_t)((b.rows + kBN - 1) / kBN), (uint32_t)((a.rows + kBM - 1) / kBM), tn, tm);
     const int64_t n0 = (int64_t)tn * kBN, m0 = (int64_t)tm * kBM;
     float *sn = reinterpret_cast<float *>(lds + T::kScales), *sm = sn + kBN;
     for (int v = threadIdx.x; v < kBN + kBM; v += P::kThreads) {
@@ -99,7 +99,7 @@ __global__ __launch_bounds__(kWM *kWN *kWave) void matmul_i8_kernel(Rows b, Rows
     constexpr int kPer = 16 / (int)sizeof(O);        // channels of a piece
     const int wave = threadIdx.x / kWave, lane = lane_id();
     char *mine = lds + wave * (T::kPass * T::kRun);
-    const int c0 = wave / kWM * T::kChan, r0 = wave % kWM * T::kTok;
+    const int c0 = wave / P::kWavesN * T::kChan, r0 = wave % P::kWavesN * T::kTok;
 #pragma unroll
     for (int pass = 0; pass < T::kTok / T::kPass; ++pass) {
         constexpr int kJ = T::kPass / 16;
@@ -116,12 +116,13 @@ __global__ __launch_bounds__(kWM *kWN *kWave) void matmul_i8_kernel(Rows b, Rows
             }
         }
         // Only this wave's part of LDS: no barrier, the wave's own accesses are in order.
-        constexpr int kPieces = T::kChan / kPer, kRows = kWave / kPieces;      // of a token; tokens a round
-        const int64_t c = n0 + c0 + lane % kPieces * kPer;
+        constexpr int kPieces = T::kChan / kPer, kAll = kPieces * T::kPass;      // of a token; of the pass
 #pragma unroll
-        for (int r = lane / kPieces; r < T::kPass; r += kRows) {
-            const uint4 v = *reinterpret_cast<const uint4 *>(mine + r * T::kRun + lane % kPieces * 16);
-            const int64_t row = m0 + r0 + pass * T::kPass + r;
+        for (int p = 0; p < kAll; p += kWave) {
+            const int at = p + lane;
+            if (kAll % kWave != 0 && at >= kAll) break;
+            const uint4 v = *reinterpret_cast<const uint4 *>(mine + at / kPieces * T::kRun + at % kPieces * 16);
+            const int64_t row = m0 + r0 + pass * T::kPass + at / kPieces, c = n0 + c0 + at % kPieces * kPer;
             if (row >= a.rows) continue;
             O *to = out + row * ldo + c;
             if (c + kPer <= b.rows) {
@@ -150,13 +151,12 @@ hipError_t launch_quantize_rows(const void *x, int dtype, int64_t rows, int64_t 
 
 namespace {
 
-template <typename O, int kBN, int kBM, int kWN, int kWM, bool kDirect>
+template <typename O, typename P>
 hipError_t launch_tiles(const Rows &b, const Rows &a, const float *sb, const float *sa, void *out, int64_t ldo,
                         hipStream_t stream) {
-    using T = I8Tile<O, kBN, kBM, kWN, kWM, kDirect>;
-    const int64_t tiles = ((a.rows + kBM - 1) / kBM) * ((b.rows + kBN - 1) / kBN);
-    return launch_lds(kPhaseAux, matmul_i8_kernel<O, kBN, kBM, kWN, kWM, kDirect>, dim3((unsigned)tiles), dim3(T::P::kThreads), T::kLds, stream,
-                      b, a, sb, sa, (O *)out, ldo);
+    const int64_t tiles = ((a.rows + P::kCols - 1) / P::kCols) * ((b.rows + P::kRows - 1) / P::kRows);
+    return launch_lds(kPhaseAux, matmul_i8_kernel<O, P>, dim3((unsigned)tiles), dim3(P::kThreads), I8Tile<O, P>::kLds, stream, b, a, sb, sa,
+                      (O *)out, ldo);
 }
 
 }  // namespace
@@ -172,12 +172,16 @@ hipError_t launch_matmul_i8(const int8_t *a, int64_t lda, const float *sa, const
                         lda < (1 << 23) && ldb < (1 << 23);
     return with_elem(dtype, [&](auto tag) {
         using O = decltype(tag);
-        const int64_t big = ((m + 255) / 256) * ((n + 255) / 256);
-        if (m > 128 && big >= 128)
-            return direct ? launch_tiles<O, 256, 256, 2, 4, true>(rb, ra, sb, sa, out, ldo, stream)
-                          : launch_tiles<O, 128, 128, 2, 2, false>(rb, ra, sb, sa, out, ldo, stream);
-        return direct ? launch_tiles<O, 64, 64, 2, 2, true>(rb, ra, sb, sa, out, ldo, stream)
-                      : launch_tiles<O, 64, 64, 2, 2, false>(rb, ra, sb, sa, out, ldo, stream);
+        auto tiles = [&](int64_t side) { return ((m + side - 1) / side) * ((n + side - 1) / side); };
+        if (direct)
+            return with_tile(product_tile(k / kStepBytes, resident_waves() / 16, tiles), [&](auto shape) {
+                return launch_tiles<O, typename decltype(shape)::template Product<MulI8>>(rb, ra, sb, sa, out, ldo, stream);
+            });
+        // Off alignment the step's bytes pass through registers: 64 while that
+        // leaves no CU without a tile.
+        if (tiles(128) >= resident_waves() / 16)
+            return launch_tiles<O, TileProduct<MulI8, 128, 128, 2, 2, 2, false>>(rb, ra, sb, sa, out, ldo, stream);
+        return launch_tiles<O, TileProduct<MulI8, 64, 64, 2, 2, 2, false>>(rb, ra, sb, sa, out, ldo, stream);
     });
 }
 

@@ -2,8 +2,8 @@
 // are rows of bytes along the summed axis, 8-bit integers or 16-bit floats.
 //
 // Tiles of both go from memory to LDS without passing registers, 128 bytes of
-// the summed axis a step, two steps' buffers in turn: while the products of
-// one step run, the next one's bytes are in flight. A row's eight 16-byte
+// the summed axis a step, kDepth steps' buffers in turn: while the products of
+// one step run, the next ones' bytes are in flight. A row's eight 16-byte
 // chunks lie in LDS at chunk ^ (row & 7), so the eight lanes that read one chunk
 // of eight neighbouring rows touch all banks; since the memory side writes LDS
 // in lane order, each lane fetches the chunk that belongs in its place.
@@ -13,6 +13,7 @@
 #include <stdint.h>
 
 #include "elem.hpp"
+#include "rules.hpp"
 
 namespace pace {
 
@@ -49,11 +50,11 @@ struct Rows {
 // kBM x kBN tiles by kWM x kWN waves. kDirect: rows are whole steps, their
 // starts and strides whole 16-byte chunks, and the bytes go straight into LDS;
 // otherwise they pass through registers.
-template <typename Mul, int kBM, int kBN, int kWM, int kWN, bool kDirect>
+template <typename Mul, int kBM, int kBN, int kWM, int kWN, int kDepth, bool kDirect>
 struct TileProduct {
-    static constexpr int kWaves = kWM * kWN, kThreads = kWaves * kWave;
+    static constexpr int kRows = kBM, kCols = kBN, kWavesN = kWN, kWaves = kWM * kWN, kThreads = kWaves * kWave;
     static constexpr int kTM = kBM / kWM / 16, kTN = kBN / kWN / 16;
-    static constexpr int kBuf = (kBM + kBN) * kStepBytes, kLdsBytes = 2 * kBuf, kB = kBM * kStepBytes;
+    static constexpr int kBuf = (kBM + kBN) * kStepBytes, kLdsBytes = kDepth * kBuf, kB = kBM * kStepBytes;
     // Pieces of 8 rows, 1 KiB, an instruction; a wave takes every kWaves-th.
     static constexpr int kPieces = (kBM + kBN) / 8, kMine = kPieces / kWaves;
     static_assert(kPieces % kWaves == 0 && (kBM / 8) % kWaves == 0, "whole shares");
@@ -102,10 +103,20 @@ struct TileProduct {
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)((i < kMineA ? pa : pb) + k + from[i]),
                                              (__attribute__((address_space(3))) void *)piece(to, i), 16, 0, 0);
     }
-    // The bytes on their way are there, and nobody reads what was read before.
+    // All but the newest kLeft steps on their way are there, and nobody reads
+    // what was read before. (Fetches are counted in their order; a barrier with
+    // a fence would wait for all of them.)
+    template <int kLeft>
     static __device__ __forceinline__ void ready() {
-        __builtin_amdgcn_s_waitcnt(0);
-        __syncthreads();
+        static_assert(kLeft * kMine < 64, "the counter's range");
+        if constexpr (kLeft == 0) {
+            __builtin_amdgcn_s_waitcnt(0);
+            __syncthreads();
+            return;
+        }
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLeft * kMine) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
     }
 
     // The operands of half a step (64 bytes), and its products.
@@ -150,42 +161,50 @@ struct TileProduct {
             for (int i = 0; i < kMine; ++i)
                 from[i] = (i < kMineA ? (uint32_t)((row_of(a, row_a, i) - row_a) * a.stride)
                                       : (uint32_t)((row_of(b, row_b, i - kMineA) - row_b) * b.stride)) + (uint32_t)lane_chunk();
-            fetch(0, lds);
-            if (bytes >= 2 * kStepBytes) fetch(kStepBytes, lds + kBuf);
+#pragma unroll
+            for (int d = 0; d < kDepth; ++d)
+                if (d * kStepBytes < bytes) fetch(d * kStepBytes, lds + d * kBuf);
         }
 #pragma unroll
         for (int i = 0; i < kTM; ++i)
 #pragma unroll
             for (int j = 0; j < kTN; ++j) acc[i][j] = Acc{0, 0, 0, 0};
         int64_t k = 0;
-        int buf = 0;
         if constexpr (kDirect) {
             // Half a step ahead: while one half's products run, the next half is
             // read from LDS, and between the halves the buffer that has just
-            // been read is given to the step after the next.
+            // been read is given to the step kDepth further on.
             Half h0, h1;
-            ready();
+            if (kDepth * kStepBytes <= bytes)
+                ready<kDepth - 1>();
+            else
+                ready<0>();
             half(lds, 0, h0);
+            const char *now = lds;
             for (; k < bytes; k += kStepBytes) {
-                half(lds + buf * kBuf, 1, h1);
+                half(now, 1, h1);
                 products(h0);
                 interleave<kTM + kTN>();
-                ready();
-                if (k + 2 * kStepBytes < bytes) fetch(k + 2 * kStepBytes, lds + buf * kBuf);
-                buf ^= 1;
-                half(lds + buf * kBuf, 0, h0);       // after the last step nothing that is used
+                if (kDepth == 2 || k + kDepth * kStepBytes > bytes)
+                    ready<0>();
+                else
+                    ready<kDepth - 2>();
+                if (k + kDepth * kStepBytes < bytes) fetch(k + kDepth * kStepBytes, const_cast<char *>(now));
+                now = now + kBuf == lds + kLdsBytes ? lds : now + kBuf;
+                half(now, 0, h0);                    // after the last step nothing that is used
                 products(h1);
                 interleave<kTM + kTN>();
             }
         } else {
             // The next step's bytes are loaded while this one's products run.
             uint4 held[kMine];
+            int buf = 0;
 #pragma unroll
             for (int i = 0; i < kMine; ++i) held[i] = staged(0, i);
             for (; k < bytes; k += kStepBytes) {
 #pragma unroll
                 for (int i = 0; i < kMine; ++i) *reinterpret_cast<uint4 *>(piece(lds + buf * kBuf, i) + lane_id() * 16) = held[i];
-                ready();
+                ready<0>();
                 Half h;
                 half(lds + buf * kBuf, 0, h);
                 if (k + kStepBytes < bytes) {
@@ -199,23 +218,120 @@ struct TileProduct {
             }
         }
     }
+
+    // ---- results in 16 bits, by columns or by rows, through a wave's own part of LDS ----
+    static constexpr int kRowsW = kBM / kWM, kColsW = kBN / kWN;
+    static constexpr int kRunC = kRowsW * 2 + 16, kRunR = kColsW * 2 + 16;      // a line in LDS: 4 banks on from the last line's
+    static constexpr int kTurnW = kColsW * kRunC > kRowsW * kRunR ? kColsW * kRunC : kRowsW * kRunR;
+    static constexpr int kTurnBytes = kWaves * kTurnW;
+
+    // bits(i, j) packs the values of acc[i][j] as two words; put(column, first
+    // row, eight values) takes them along the rows. Coordinates are the tile's.
+    template <typename Bits, typename Put>
+    static __device__ __forceinline__ void by_columns(char *lds, Bits bits, Put put) {
+        const int wave = threadIdx.x / kWave, lane = lane_id();
+        char *mine = lds + wave * kTurnW;
+        const int r0 = wave / kWN * kRowsW, c0 = wave % kWN * kColsW;
+#pragma unroll
+        for (int j = 0; j < kTN; ++j)
+#pragma unroll
+            for (int i = 0; i < kTM; ++i) *reinterpret_cast<uint2 *>(mine + (col(j) - c0) * kRunC + (row4(i) - r0) * 2) = bits(i, j);
+        constexpr int kPieces = kRowsW / 8, kAll = kPieces * kColsW;
+#pragma unroll
+        for (int p = 0; p < kAll; p += kWave) {
+            const int at = p + lane;
+            if (kAll % kWave != 0 && at >= kAll) break;
+            put(c0 + at / kPieces, r0 + at % kPieces * 8, *reinterpret_cast<const uint4 *>(mine + at / kPieces * kRunC + at % kPieces * 16));
+        }
+    }
+    // The same by rows: neighbouring lanes, which hold neighbouring columns,
+    // exchange two of their four rows. put(row, first column, eight values).
+    template <typename Bits, typename Put>
+    static __device__ __forceinline__ void by_rows(char *lds, Bits bits, Put put) {
+        const int wave = threadIdx.x / kWave, lane = lane_id();
+        char *mine = lds + wave * kTurnW;
+        const int r0 = wave / kWN * kRowsW, c0 = wave % kWN * kColsW;
+        const bool odd = lane & 1;
+#pragma unroll
+        for (int j = 0; j < kTN; ++j)
+#pragma unroll
+            for (int i = 0; i < kTM; ++i) {
+                const uint2 b = bits(i, j);
+                const uint32_t got = dpp_u32<0xb1, 0xf>(0u, odd ? b.x : b.y);      // from the lane of the pair
+                const uint32_t left = odd ? got : b.x, right = odd ? b.y : got;    // two rows of the left and of the right column
+                char *to = mine + (row4(i) + (odd ? 2 : 0) - r0) * kRunR + (col(j) - (odd ? 1 : 0) - c0) * 2;
+                *reinterpret_cast<uint32_t *>(to) = (left & 0xffffu) | (right << 16);
+                *reinterpret_cast<uint32_t *>(to + kRunR) = (left >> 16) | (right & 0xffff0000u);
+            }
+        constexpr int kPieces = kColsW / 8, kAll = kPieces * kRowsW;
+#pragma unroll
+        for (int p = 0; p < kAll; p += kWave) {
+            const int at = p + lane;
+            if (kAll % kWave != 0 && at >= kAll) break;
+            put(r0 + at / kPieces, c0 + at % kPieces * 8, *reinterpret_cast<const uint4 *>(mine + at / kPieces * kRunR + at % kPieces * 16));
+        }
+    }
 };
 
+// Two 16-bit values of type T as a word.
+template <typename T>
+__device__ __forceinline__ uint32_t pair_bits(float a, float b) {
+    return (uint32_t)__builtin_bit_cast(uint16_t, from_f32<T>(a)) | ((uint32_t)__builtin_bit_cast(uint16_t, from_f32<T>(b)) << 16);
+}
+
 // Which tile a workgroup takes. Workgroups go round the eight XCDs, each with
-// an L2 of its own: each XCD takes a run of neighbouring tiles, and a run goes
-// down columns of kGroup row tiles, so that what its workgroups read at one
-// time is a block of few rows and columns.
+// an L2 of its own: xcd_run gives each XCD a run of neighbouring numbers, and
+// the tiles of a run go down columns of kGroup row tiles, so that what an XCD's
+// workgroups read at one time is a block of few rows and columns.
+__device__ __forceinline__ uint32_t xcd_run(uint32_t id, uint32_t all) {
+    const uint32_t per = all / 8, rest = all % 8, x = id % 8;
+    return x * per + (x < rest ? x : rest) + id / 8;
+}
 template <int kGroup>
 __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, int &tm, int &tn) {
-    const uint32_t all = tiles_m * tiles_n, per = all / 8, rest = all % 8;
-    const uint32_t x = id % 8, i = id / 8;
-    id = x * per + (x < rest ? x : rest) + i;
     const uint32_t band = kGroup * tiles_n, g = id / band;
     const uint32_t rows = tiles_m - g * kGroup < kGroup ? tiles_m - g * kGroup : kGroup;
     const uint32_t in = id - g * band;
     // the same in every lane
     tm = __builtin_amdgcn_readfirstlane((int)(g * kGroup + in % rows));
     tn = __builtin_amdgcn_readfirstlane((int)(in / rows));
+}
+// The same for the lower triangle of `tiles` x `tiles` tiles.
+template <int kGroup>
+__device__ __forceinline__ void lower_tile_of(uint32_t id, uint32_t tiles, int &tm, int &tn) {
+    int64_t t = (int64_t)((sqrt((double)(8 * (int64_t)id + 1)) - 1.0) * 0.5);      // the row it would be in, row by row
+    while (t * (t + 1) / 2 > id) --t;
+    while ((t + 1) * (t + 2) / 2 <= id) ++t;
+    const uint32_t r0 = (uint32_t)t / kGroup * kGroup, rows = tiles - r0 < kGroup ? tiles - r0 : kGroup;
+    uint32_t in = id - r0 * (r0 + 1) / 2, c = 0, r = 0;
+    if (in < rows * (r0 + 1)) {                      // columns that all rows of the band have
+        c = in / rows;
+        r = in % rows;
+    } else {                                         // the band's own triangle
+        in -= rows * (r0 + 1);
+        for (c = r0 + 1; in >= rows - (c - r0); ++c) in -= rows - (c - r0);
+        r = c - r0 + in;
+    }
+    tm = __builtin_amdgcn_readfirstlane((int)(r0 + r));
+    tn = __builtin_amdgcn_readfirstlane((int)c);
+}
+
+// Runs f with the tile of a side of product_tile: eight waves, and as many
+// steps in flight as the LDS of a CU holds (two workgroups of it for 64).
+template <int kBM, int kBN, int kWM, int kWN, int kDepth>
+struct TileShape {
+    template <typename Mul>
+    using Product = TileProduct<Mul, kBM, kBN, kWM, kWN, kDepth, true>;
+    static constexpr int kSide = kBM;
+};
+template <typename F>
+auto with_tile(int side, F f) {
+    switch (side) {
+        case 256: return f(TileShape<256, 256, 2, 4, 2>{});
+        case 192: return f(TileShape<192, 192, 2, 4, 2>{});
+        case 128: return f(TileShape<128, 128, 2, 4, 4>{});
+        default: return f(TileShape<64, 64, 4, 2, 4>{});
+    }
 }
 
 }  // namespace pace

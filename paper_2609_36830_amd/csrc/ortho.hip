@@ -21,9 +21,10 @@ namespace {
 
 constexpr float kScaleX = 1024.0f;                 // X up to 32 in binary16
 constexpr float kScaleA = 256.0f;                  // A and C up to 128
-constexpr int kNormThreads = 256;
-constexpr int kNormBlocks = 64;                    // partial sums of squares of a matrix, at most
+constexpr int kNormWaves = 4;                      // of a workgroup
+constexpr int kNormBlocks = 1024;                  // partial sums of squares of a matrix, at most
 constexpr int kTurn = 64;                          // side of the tiles that are turned
+constexpr int kTurnRun = 4;                        // of them by a workgroup
 
 // The m x n orientation of one matrix of the batch and its workspace; the rows'
 // ends up to a multiple of 64 elements are zeros, so that products have whole steps.
@@ -53,184 +54,215 @@ OrthoShape ortho_shape(int64_t rows, int64_t cols) {
     s.bytes = at;
     return s;
 }
+// Waves take pieces of kNormPiece elements of rows.
+constexpr int kNormPiece = 4096;
 int ortho_norm_blocks(int64_t rows, int64_t cols) {
-    const int64_t b = rows * cols / (kNormThreads * 32);
-    return (int)(b < 1 ? 1 : (b > kNormBlocks ? kNormBlocks : b));
+    const int64_t pieces = rows * ((cols + kNormPiece - 1) / kNormPiece), b = (pieces + kNormWaves - 1) / kNormWaves;
+    return (int)(b > kNormBlocks ? kNormBlocks : b);
 }
 
-// Sums of squares over every gridDim.x-th row, in binary64: no square of a
-// finite binary32 number leaves its range.
-template <typename T>
-__global__ __launch_bounds__(kNormThreads) void ortho_norm_kernel(const T *__restrict__ g, int64_t rows, int64_t cols,
-                                                                  int64_t stride, int64_t batch_stride, char *ws,
-                                                                  int64_t ws_stride) {
-    constexpr int V = kVecOf<T>;
-    __shared__ double part[kNormThreads / kWave];
-    const T *mat = g + blockIdx.y * batch_stride;
-    const int64_t nv = cols / V;
-    double sum = 0.0;
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        const T *row = mat + r * stride;
-        for (int64_t v = threadIdx.x; v < nv; v += kNormThreads) {
-            float z[V];
-            unpack16<T>(load_a1(row + v * V), z);
+// The sum over a workgroup of four waves, in thread order's tree, in every thread.
+__device__ __forceinline__ double block_total(double v, double *part) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) sum += (double)z[e] * (double)z[e];
-        }
-        if (nv * V + threadIdx.x < cols) {
-            const double x = (double)to_f32(row[nv * V + threadIdx.x]);
-            sum += x * x;
-        }
-    }
-#pragma unroll
-    for (int off = kWave / 2; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, kWave);
-    if (lane_id() == 0) part[threadIdx.x / kWave] = sum;
+    for (int off = kWave / 2; off >= 1; off >>= 1) v += __shfl_xor(v, off, kWave);
+    if (lane_id() == 0) part[threadIdx.x / kWave] = v;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int k = 1; k < kNormThreads / kWave; ++k) sum += part[k];
-        reinterpret_cast<double *>(ws + blockIdx.y * ws_stride)[blockIdx.x] = sum;
-    }
+    return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// X by rows and by columns from the update, a 64 x 64 tile a workgroup.
+// Sums of squares, in binary64: no square of a finite binary32 number leaves its range.
+template <typename T>
+__global__ __launch_bounds__(kNormWaves *kWave) void ortho_norm_kernel(const T *__restrict__ g, int64_t rows, int64_t cols,
+                                                                       int64_t stride, int64_t batch_stride, char *ws,
+                                                                       int64_t ws_stride) {
+    constexpr int V = kVecOf<T>;
+    __shared__ double part[kNormWaves];
+    const T *mat = g + blockIdx.y * batch_stride;
+    const int64_t pieces = (cols + kNormPiece - 1) / kNormPiece, all = rows * pieces;
+    double sum[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) sum[e] = 0.0;
+    for (int64_t p = (int64_t)blockIdx.x * kNormWaves + threadIdx.x / kWave; p < all; p += (int64_t)gridDim.x * kNormWaves) {
+        const int64_t r = pieces == 1 ? p : p / pieces, c0 = (p - r * pieces) * kNormPiece;
+        const int64_t c1 = c0 + kNormPiece < cols ? c0 + kNormPiece : cols;
+        const T *row = mat + r * stride;
+        int64_t c = c0 + lane_id() * V;
+#pragma unroll 4
+        for (; c + V <= c1; c += kWave * V) {
+            float z[V];
+            unpack16<T>(load_a1(row + c), z);
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum[e] += (double)z[e] * (double)z[e];
+        }
+        for (; c < c1; ++c) {                        // the one lane at a row's end
+            const double x = (double)to_f32(row[c]);
+            sum[0] += x * x;
+        }
+    }
+#pragma unroll
+    for (int e = 1; e < V; ++e) sum[0] += sum[e];
+    const double total = block_total(sum[0], part);
+    if (threadIdx.x == 0) reinterpret_cast<double *>(ws + blockIdx.y * ws_stride)[blockIdx.x] = total;
+}
+
+// X by rows and by columns from the update, a run of 64 x 64 tiles a workgroup.
 template <typename T>
 __global__ __launch_bounds__(256) void ortho_start_kernel(const T *__restrict__ g, int64_t rows, int64_t cols,
                                                           int64_t stride, int64_t batch_stride, int norm_blocks, double eps,
                                                           OrthoShape s, char *ws) {
-    __shared__ f16_t tile[kTurn][kTurn + 2];
+    constexpr int V = kVecOf<T>;
+    __shared__ f16_t tile[kTurn][kTurn + 8];
+    __shared__ double part[4];
     char *w = ws + blockIdx.z * s.bytes;
     double sum = 0.0;
-    for (int k = 0; k < norm_blocks; ++k) sum += reinterpret_cast<const double *>(w)[k];
-    const double inv = (double)kScaleX / (sqrt(sum) + eps);      // binary64: updates of any size
+    for (int k = threadIdx.x; k < norm_blocks; k += 256) sum += reinterpret_cast<const double *>(w)[k];
+    const double inv = (double)kScaleX / (sqrt(block_total(sum, part)) + eps);      // binary64: updates of any size
     const T *mat = g + blockIdx.z * batch_stride;
-    const int64_t r0 = (int64_t)blockIdx.y * kTurn, c0 = (int64_t)blockIdx.x * kTurn;      // in the update
-    const int x = threadIdx.x % kTurn, y0 = threadIdx.x / kTurn;
-    for (int y = y0; y < kTurn; y += 256 / kTurn) {
-        const bool in = r0 + y < rows && c0 + x < cols;
-        tile[y][x] = (f16_t)(float)(in ? (double)to_f32(mat[(r0 + y) * stride + c0 + x]) * inv : 0.0);
-    }
-    __syncthreads();
-    // by the update's rows, and by its columns; the ends of rows are zeros
     f16_t *by_rows = (f16_t *)(w + (s.turned ? s.xt : s.x)), *by_cols = (f16_t *)(w + (s.turned ? s.x : s.xt));
     const int64_t ld_rows = s.turned ? s.mp : s.np, ld_cols = s.turned ? s.np : s.mp;
-    for (int y = y0; y < kTurn; y += 256 / kTurn) {
-        if (r0 + y < rows && c0 + x < ld_rows) by_rows[(r0 + y) * ld_rows + c0 + x] = tile[y][x];
-        if (c0 + y < cols && r0 + x < ld_cols) by_cols[(c0 + y) * ld_cols + r0 + x] = tile[x][y];
+    const int64_t r0 = (int64_t)blockIdx.y * kTurn;             // in the update
+    for (int k = 0; k < kTurnRun; ++k) {
+        const int64_t c0 = ((int64_t)blockIdx.x * kTurnRun + k) * kTurn;
+        if (c0 >= cols) break;
+        if (k) __syncthreads();
+        constexpr int kAcross = kTurn / V;
+#pragma unroll
+        for (int p = threadIdx.x; p < kTurn * kAcross; p += 256) {
+            const int y = p / kAcross, x = p % kAcross * V;
+            const int64_t r = r0 + y, c = c0 + x;
+            float z[V];
+            if (r < rows && c + V <= cols) {
+                unpack16<T>(load_a1(mat + r * stride + c), z);
+            } else {
+#pragma unroll
+                for (int e = 0; e < V; ++e) z[e] = r < rows && c + e < cols ? to_f32(mat[r * stride + c + e]) : 0.0f;
+            }
+            // the rows' ends are zeros, also where the norm is no number
+#pragma unroll
+            for (int e = 0; e < V; ++e) tile[y][x + e] = r < rows && c + e < cols ? (f16_t)(float)((double)z[e] * inv) : (f16_t)0.0f;
+        }
+        __syncthreads();
+        struct alignas(16) Eight { f16_t e[8]; } v;
+#pragma unroll
+        for (int p = threadIdx.x; p < kTurn * kTurn / 8; p += 256) {
+            const int y = p / (kTurn / 8), x = p % (kTurn / 8) * 8;
+            if (r0 + y < rows && c0 + x < ld_rows) {
+                v = *reinterpret_cast<const Eight *>(&tile[y][x]);
+                *reinterpret_cast<Eight *>(by_rows + (r0 + y) * ld_rows + c0 + x) = v;
+            }
+            if (c0 + y < cols && r0 + x < ld_cols) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v.e[e] = tile[x + e][y];
+                *reinterpret_cast<Eight *>(by_cols + (c0 + y) * ld_cols + r0 + x) = v;
+            }
+        }
     }
 }
 
-// The id-th tile of a lower triangle of tiles, row by row.
-__device__ __forceinline__ void lower_tile(uint32_t id, int &tm, int &tn) {
-    int64_t t = (int64_t)((sqrt((double)(8 * (int64_t)id + 1)) - 1.0) * 0.5);
-    while (t * (t + 1) / 2 > id) --t;
-    while ((t + 1) * (t + 2) / 2 <= id) ++t;
-    tm = __builtin_amdgcn_readfirstlane((int)t);
-    tn = __builtin_amdgcn_readfirstlane((int)(id - t * (t + 1) / 2));
-}
-
-struct alignas(8) Four {
-    f16_t e[4];
-};
-
-// Elements (r .. r + 3, c) of a symmetric matrix with zeros up to column mp, to
-// both of their places.
-__device__ __forceinline__ void store_both(f16_t *to, int64_t m, int64_t mp, int64_t r, int64_t c, const float (&v)[4],
-                                           bool mirror) {
-    Four w;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w.e[e] = (f16_t)(r + e < m ? v[e] : 0.0f);
-    if (mirror && c < m && r < mp) *reinterpret_cast<Four *>(to + c * mp + r) = w;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (r + e < m && c < mp) to[(r + e) * mp + c] = c < m ? w.e[e] : (f16_t)0.0f;
-}
-
-// A workgroup takes a tile of one matrix of the batch; a matrix's tiles are neighbours.
-// kSquare: C = a I + b A + c A A from A, else A = X X^T.
-template <bool kSquare, int kB, int kWM, int kWN>
-__global__ __launch_bounds__(kWM *kWN *kWave) void ortho_gram_kernel(OrthoShape s, char *ws, uint32_t tiles, float ca,
-                                                                     float cb, float cc) {
+// kSquare: C = a I + b A + c A A from A, else A = X X^T: the lower tiles, each
+// to both of its places. A workgroup takes a tile of one matrix of the batch.
+template <bool kSquare, typename P>
+__global__ __launch_bounds__(P::kThreads) void ortho_gram_kernel(OrthoShape s, char *ws, uint32_t side, float ca, float cb, float cc) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    using P = TileProduct<MulF16, kB, kB, kWM, kWN, true>;
-    P t;
-    const uint32_t mat = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / tiles));
+    const uint32_t id = xcd_run(blockIdx.x, gridDim.x), tiles = side * (side + 1) / 2;
+    const uint32_t mat = __builtin_amdgcn_readfirstlane((int)(id / tiles));
     char *w = ws + mat * s.bytes;
     int tm, tn;
-    lower_tile(blockIdx.x - mat * tiles, tm, tn);
-    const int64_t r0 = (int64_t)tm * kB, c0 = (int64_t)tn * kB;
+    lower_tile_of<4>(id - mat * tiles, side, tm, tn);
+    const int64_t r0 = (int64_t)tm * P::kRows, c0 = (int64_t)tn * P::kCols;
     const Rows x = kSquare ? Rows{w + s.a, s.mp * 2, s.m, s.mp * 2} : Rows{w + s.x, s.np * 2, s.m, s.np * 2};
+    P t;
     t.run(x, r0, x, c0, lds);
     const f16_t *a = (const f16_t *)(w + s.a);
     f16_t *to = (f16_t *)(w + (kSquare ? s.c : s.a));
+    __syncthreads();                                 // nobody reads the operands any more
 #pragma unroll
-        for (int j = 0; j < P::kTN; ++j) {
-            const int64_t col = c0 + P::col(j);
-            Four g[P::kTM];
+    for (int j = 0; j < P::kTN; ++j) {
+        const int64_t col = c0 + P::col(j);
+#pragma unroll
+        for (int i = 0; i < P::kTM; ++i) {
+            const int64_t row = r0 + P::row4(i);
             if (kSquare) {
                 // A's elements of this column, by its row of the same number
+                struct alignas(8) { f16_t e[4]; } g;
+                g = *reinterpret_cast<const decltype(g) *>(a + (col < s.m ? col : 0) * s.mp + (row < s.mp ? row : 0));
 #pragma unroll
-                for (int i = 0; i < P::kTM; ++i) {
-                    const int64_t row = r0 + P::row4(i);
-                    g[i] = *reinterpret_cast<const Four *>(a + (col < s.m ? col : 0) * s.mp + (row < s.mp ? row : 0));
-                }
+                for (int e = 0; e < 4; ++e)
+                    t.acc[i][j][e] = __builtin_fmaf(cc / kScaleA, t.acc[i][j][e], cb * (float)g.e[e]) + (row + e == col ? ca * kScaleA : 0.0f);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t.acc[i][j][e] *= kScaleA / (kScaleX * kScaleX);
             }
 #pragma unroll
-            for (int i = 0; i < P::kTM; ++i) {
-                const int64_t row = r0 + P::row4(i);
-                float y[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float v = t.acc[i][j][e];
-                    if (kSquare)
-                        y[e] = __builtin_fmaf(cc / kScaleA, v, cb * (float)g[i].e[e]) + (row + e == col ? ca * kScaleA : 0.0f);
-                    else
-                        y[e] = v * (kScaleA / (kScaleX * kScaleX));
-                }
-                store_both(to, s.m, s.mp, row, col, y, r0 != c0);
-            }
+            for (int e = 0; e < 4; ++e)
+                if (row + e >= s.m || col >= s.m) t.acc[i][j][e] = 0.0f;       // the rows' ends
         }
+    }
+    auto bits = [&](int i, int j) {
+        const mfma_v4f v = t.acc[i][j];
+        return make_uint2(pair_bits<f16_t>(v[0], v[1]), pair_bits<f16_t>(v[2], v[3]));
+    };
+    auto put = [&](int64_t line, int64_t at, const uint4 &v) {
+        if (line < s.m && at < s.mp) *reinterpret_cast<uint4 *>(to + line * s.mp + at) = v;
+    };
+    if (tm != tn) P::by_columns(lds, bits, [&](int c, int r, const uint4 &v) { put(c0 + c, r0 + r, v); });
+    P::by_rows(lds, bits, [&](int r, int c, const uint4 &v) { put(r0 + r, c0 + c, v); });
 }
 
 // X <- C X by rows and by columns, or, in the last step, the result.
-template <bool kLast, int kB, int kWM, int kWN>
-__global__ __launch_bounds__(kWM *kWN *kWave) void ortho_apply_kernel(OrthoShape s, char *ws, int64_t xt_from, int64_t xt_to,
-                                                                      uint32_t tiles_m, uint32_t tiles_n,
-                                                                      bf16_t *__restrict__ out) {
+template <bool kLast, typename P>
+__global__ __launch_bounds__(P::kThreads) void ortho_apply_kernel(OrthoShape s, char *ws, int64_t xt_from, int64_t xt_to, uint32_t tiles_m,
+                                                                  uint32_t tiles_n, bf16_t *__restrict__ out) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    using P = TileProduct<MulF16, kB, kB, kWM, kWN, true>;
-    P t;
-    const int mat = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / (tiles_m * tiles_n)));
+    const uint32_t id = xcd_run(blockIdx.x, gridDim.x);
+    const uint32_t mat = __builtin_amdgcn_readfirstlane((int)(id / (tiles_m * tiles_n)));
     int tm, tn;
-    tile_of<8>(blockIdx.x - mat * (tiles_m * tiles_n), tiles_m, tiles_n, tm, tn);
+    tile_of<8>(id - mat * (tiles_m * tiles_n), tiles_m, tiles_n, tm, tn);
     char *w = ws + mat * s.bytes;
-    const int64_t r0 = (int64_t)tm * kB, c0 = (int64_t)tn * kB;
+    const int64_t r0 = (int64_t)tm * P::kRows, c0 = (int64_t)tn * P::kCols;
     const Rows c{w + s.c, s.mp * 2, s.m, s.mp * 2}, x{w + xt_from, s.mp * 2, s.n, s.mp * 2};
+    P t;
     t.run(c, r0, x, c0, lds);
-    f16_t *by_rows = (f16_t *)(w + s.x), *by_cols = (f16_t *)(w + xt_to);
-    bf16_t *o = kLast ? out + mat * s.m * s.n : nullptr;
+    __syncthreads();                                 // nobody reads the operands any more
+    if constexpr (kLast) {
+        constexpr float f = 1.0f / (kScaleA * kScaleX);
+        bf16_t *o = out + mat * s.m * s.n;
+        auto bits = [&](int i, int j) {
+            const mfma_v4f v = t.acc[i][j];
+            return make_uint2(pair_bits<bf16_t>(v[0] * f, v[1] * f), pair_bits<bf16_t>(v[2] * f, v[3] * f));
+        };
+        // lines of `len` elements
+        auto put = [&](int64_t line, int64_t lines, int64_t at, int64_t len, const uint4 &v) {
+            if (line >= lines) return;
+            bf16_t *to = o + line * len + at;
+            if (at + 8 <= len) {
+                store_a1(to, v);
+            } else {
+                struct { bf16_t e[8]; } y = __builtin_bit_cast(decltype(y), v);
 #pragma unroll
-        for (int j = 0; j < P::kTN; ++j) {
-            const int64_t col = c0 + P::col(j);
-#pragma unroll
-            for (int i = 0; i < P::kTM; ++i) {
-                const int64_t row = r0 + P::row4(i);
-                const mfma_v4f v = t.acc[i][j];
-                if constexpr (kLast) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (row + e < s.m && col < s.n)
-                            o[s.turned ? col * s.m + row + e : (row + e) * s.n + col] = from_f32<bf16_t>(v[e] * (1.0f / (kScaleA * kScaleX)));
-                } else {
-                    Four y;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) y.e[e] = (f16_t)(row + e < s.m ? v[e] * (1.0f / kScaleA) : 0.0f);
-                    if (col < s.n && row < s.mp) *reinterpret_cast<Four *>(by_cols + col * s.mp + row) = y;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (row + e < s.m && col < s.np) by_rows[(row + e) * s.np + col] = col < s.n ? y.e[e] : (f16_t)0.0f;
-                }
+                for (int e = 0; e < 8; ++e)
+                    if (at + e < len) to[e] = y.e[e];
             }
-        }
+        };
+        if (s.turned) P::by_columns(lds, bits, [&](int cl, int r, const uint4 &v) { put(c0 + cl, s.n, r0 + r, s.m, v); });
+        else P::by_rows(lds, bits, [&](int r, int cl, const uint4 &v) { put(r0 + r, s.m, c0 + cl, s.n, v); });
+    } else {
+        f16_t *by_rows = (f16_t *)(w + s.x), *by_cols = (f16_t *)(w + xt_to);
+        auto bits = [&](int i, int j) {
+            const int64_t row = r0 + P::row4(i);
+            const bool in = c0 + P::col(j) < s.n;
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = in && row + e < s.m ? t.acc[i][j][e] * (1.0f / kScaleA) : 0.0f;      // the rows' ends
+            return make_uint2(pair_bits<f16_t>(v[0], v[1]), pair_bits<f16_t>(v[2], v[3]));
+        };
+        P::by_columns(lds, bits, [&](int cl, int r, const uint4 &v) {
+            if (c0 + cl < s.n && r0 + r < s.mp) *reinterpret_cast<uint4 *>(by_cols + (c0 + cl) * s.mp + r0 + r) = v;
+        });
+        P::by_rows(lds, bits, [&](int r, int cl, const uint4 &v) {
+            if (r0 + r < s.m && c0 + cl < s.np) *reinterpret_cast<uint4 *>(by_rows + (r0 + r) * s.np + c0 + cl) = v;
+        });
+    }
 }
 
 // No steps: the normalised update itself.
@@ -242,24 +274,43 @@ __global__ __launch_bounds__(256) void ortho_copy_kernel(OrthoShape s, char *ws,
         for (int64_t c = threadIdx.x; c < cols; c += 256) o[r * cols + c] = from_f32<bf16_t>((float)x[r * ld + c] * (1.0f / kScaleX));
 }
 
-template <int kB, int kWM, int kWN>
-hipError_t ortho_steps(const OrthoShape &s, char *ws, int64_t batch, int steps, const float *coefs, bf16_t *out,
-                       hipStream_t stream) {
-    using T = TileProduct<MulF16, kB, kB, kWM, kWN, true>;
-    const int64_t tm = (s.m + kB - 1) / kB, tn = (s.n + kB - 1) / kB;
-    const int64_t lower = tm * (tm + 1) / 2;
-    const dim3 half((unsigned)(lower * batch)), all((unsigned)(tm * tn * batch)), block(T::kThreads);
+template <typename P>
+constexpr int ortho_lds() {
+    return P::kLdsBytes > P::kTurnBytes ? P::kLdsBytes : P::kTurnBytes;
+}
+
+template <bool kSquare>
+hipError_t launch_gram(const OrthoShape &s, char *ws, int64_t batch, const float *c, hipStream_t stream) {
+    auto tiles = [&](int64_t side) {
+        const int64_t t = (s.m + side - 1) / side;
+        return t * (t + 1) / 2 * batch;
+    };
+    const int side = product_tile((kSquare ? s.mp : s.np) * 2 / kStepBytes, resident_waves() / 16, tiles);
+    return with_tile(side, [&](auto shape) {
+        using P = typename decltype(shape)::template Product<MulF16>;
+        return launch_lds(-1, ortho_gram_kernel<kSquare, P>, dim3((unsigned)tiles(side)), dim3(P::kThreads), ortho_lds<P>(), stream, s, ws,
+                          (s.m + side - 1) / side, c[0], c[1], c[2]);
+    });
+}
+template <bool kLast>
+hipError_t launch_apply(const OrthoShape &s, char *ws, int64_t batch, int64_t from, int64_t to, bf16_t *out, hipStream_t stream) {
+    auto tiles = [&](int64_t side) { return ((s.m + side - 1) / side) * ((s.n + side - 1) / side) * batch; };
+    const int side = product_tile(s.mp * 2 / kStepBytes, resident_waves() / 16, tiles);
+    return with_tile(side, [&](auto shape) {
+        using P = typename decltype(shape)::template Product<MulF16>;
+        return launch_lds(kPhaseAux, ortho_apply_kernel<kLast, P>, dim3((unsigned)tiles(side)), dim3(P::kThreads), ortho_lds<P>(), stream, s, ws,
+                          from, to, (s.m + side - 1) / side, (s.n + side - 1) / side, out);
+    });
+}
+
+hipError_t ortho_steps(const OrthoShape &s, char *ws, int64_t batch, int steps, const float *coefs, bf16_t *out, hipStream_t stream) {
     int64_t from = s.xt, to = s.xt2;
     hipError_t e = hipSuccess;
     for (int k = 0; k < steps && e == hipSuccess; ++k) {
-        e = launch_lds(-1, ortho_gram_kernel<false, kB, kWM, kWN>, half, block, T::kLdsBytes, stream, s, ws, lower, 0.0f, 0.0f, 0.0f);
+        e = launch_gram<false>(s, ws, batch, coefs, stream);
+        if (e == hipSuccess) e = launch_gram<true>(s, ws, batch, coefs, stream);
         if (e == hipSuccess)
-            e = launch_lds(-1, ortho_gram_kernel<true, kB, kWM, kWN>, half, block, T::kLdsBytes, stream, s, ws, lower, coefs[0], coefs[1], coefs[2]);
-        if (e == hipSuccess)
-            e = k + 1 < steps ? launch_lds(kPhaseAux, ortho_apply_kernel<false, kB, kWM, kWN>, all, block, T::kLdsBytes, stream, s, ws,
-                                           from, to, tm, tn, out)
-                              : launch_lds(kPhaseAux, ortho_apply_kernel<true, kB, kWM, kWN>, all, block, T::kLdsBytes, stream, s, ws,
-                                           from, to, tm, tn, out);
+            e = k + 1 < steps ? launch_apply<false>(s, ws, batch, from, to, out, stream) : launch_apply<true>(s, ws, batch, from, to, out, stream);
         const int64_t x = from;
         from = to;
         to = x;
@@ -280,11 +331,10 @@ hipError_t launch_orthogonalize(const void *g, int dtype, int64_t batch, int64_t
     char *w = (char *)ws;
     hipError_t e = with_elem(dtype, [&](auto tag) {
         using T = decltype(tag);
-        hipError_t r = launch(-1, ortho_norm_kernel<T>, dim3((unsigned)blocks, (unsigned)batch), dim3(kNormThreads), stream, (const T *)g, rows,
+        hipError_t r = launch(-1, ortho_norm_kernel<T>, dim3((unsigned)blocks, (unsigned)batch), dim3(kNormWaves * kWave), stream, (const T *)g, rows,
                               cols, stride, batch_stride, w, s.bytes);
-        // the padded ends too: both sides up to a multiple of 64
         if (r == hipSuccess)
-            r = launch(-1, ortho_start_kernel<T>, dim3((unsigned)((cols + 63) / 64), (unsigned)((rows + 63) / 64), (unsigned)batch), dim3(256), stream,
+            r = launch(-1, ortho_start_kernel<T>, dim3((unsigned)((cols + kTurn * kTurnRun - 1) / (kTurn * kTurnRun)), (unsigned)((rows + kTurn - 1) / kTurn), (unsigned)batch), dim3(256), stream,
                        (const T *)g, rows, cols, stride, batch_stride, blocks, eps, s, w);
         return r;
     });
@@ -292,9 +342,7 @@ hipError_t launch_orthogonalize(const void *g, int dtype, int64_t batch, int64_t
     if (steps == 0)
         return launch(-1, ortho_copy_kernel, dim3((unsigned)(rows < 1024 ? rows : 1024), (unsigned)batch), dim3(256), stream, s, w, (bf16_t *)out);
     const float c[3] = {(float)coefs[0], (float)coefs[1], (float)coefs[2]};
-    const int64_t big = ((s.m + 255) / 256) * ((s.n + 255) / 256) * batch;
-    if (big >= 128) return ortho_steps<256, 2, 4>(s, w, batch, steps, c, (bf16_t *)out, stream);
-    return ortho_steps<64, 2, 2>(s, w, batch, steps, c, (bf16_t *)out, stream);
+    return ortho_steps(s, w, batch, steps, c, (bf16_t *)out, stream);
 }
 
 }  // namespace pace

@@ -112,6 +112,26 @@ def test_types(pace, dtype, m, n, k):
     check(pace, *operands(m, n, k, k), dtype=dtype)
 
 
+# Sizes that reach each of the tiles (test_operators_host.py holds them against the rule), with edges off every tile's side.
+TILES = [(40, 300, 256), (130, 3001, 1024), (701, 3000, 256), (1100, 1901, 128), (300, 20001, 384), (2001, 2100, 512), (2050, 4101, 1024),
+         (4097, 16385, 256), (1021, 70001, 640)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k", TILES)
+def test_tiles(pace, dtype, m, n, k):
+    say("i8 product tiles %s m=%d n=%d k=%d" % (dtype, m, n, k))
+    check(pace, *operands(m, n, k, k), dtype=dtype)
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 5, 7, 8])
+@pytest.mark.parametrize("m,n", [(40, 300), (701, 3000), (2001, 2100), (4097, 16385)])
+def test_few_steps(pace, m, n, steps):
+    """Fewer steps than are held in flight, as many, and more."""
+    say("i8 product m=%d n=%d, %d steps" % (m, n, steps))
+    check(pace, *operands(m, n, 128 * steps, steps), dtype=torch.bfloat16)
+
+
 @pytest.mark.parametrize("k", [1, 15, 17, 63, 65, 127, 129, 1000, 1023])
 @pytest.mark.parametrize("m,n", [(1, 300), (20, 50), (300, 20000)])
 def test_odd_lengths(pace, m, n, k):

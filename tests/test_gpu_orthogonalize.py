@@ -70,6 +70,18 @@ def test_large_tiles(pace, batch, rows, cols):
     check(pace, g)
 
 
+# Shapes whose three products reach each of the tiles (test_operators_host.py holds them against the rule).
+TILES = [(1, 2500, 2601), (1, 1000, 3001), (1, 2050, 4097), (2, 1700, 401), (24, 600, 700), (1, 4100, 4200), (3, 1500, 1501)]
+
+
+@pytest.mark.parametrize("batch,rows,cols", TILES)
+def test_tiles(pace, batch, rows, cols):
+    say("orthogonalize tiles %d x %d x %d" % (batch, rows, cols))
+    g = torch.randn(batch, rows, cols, generator=torch.Generator(device=DEV).manual_seed(rows), device=DEV)
+    check(pace, g, steps=2)
+    check(pace, g.transpose(1, 2).contiguous().bfloat16(), steps=2)
+
+
 def test_steps_and_coefficients(pace):
     say("orthogonalize steps")
     g = torch.randn(2, 90, 150, generator=torch.Generator(device=DEV).manual_seed(4), device=DEV)

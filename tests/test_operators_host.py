@@ -93,3 +93,32 @@ def test_orthogonalize_host_argument_errors(L):
         assert call(**kw) == -1, kw
     for kw in (dict(ws=None), dict(ws=FAKE + 32), dict(wsb=100)):
         assert call(**kw) == -2, kw
+
+
+def test_gpu_tests_reach_every_tile():
+    """The sizes of the GPU tests of tiles, by the library's own rule for a chip of 256 CUs."""
+    from tests.operator_rules import CUS, rules
+    from tests.test_gpu_matmul_i8 import TILES as I8
+    from tests.test_gpu_orthogonalize import TILES as ORTHO
+    R = rules()
+    every = {64, 128, 192, 256}
+    assert {R.full(m, n, 1, k // 128, CUS) for m, n, k in I8} == every
+    gram, square, apply = set(), set(), set()
+    for b, r, c in ORTHO:
+        m, n = min(r, c), max(r, c)
+        gram.add(R.lower(m, b, -(-n // 64), CUS))
+        square.add(R.lower(m, b, -(-m // 64), CUS))
+        apply.add(R.full(m, n, b, -(-m // 64), CUS))
+    assert apply == every and gram >= {64, 128, 192} and square >= {64, 128, 192}, (gram, square, apply)
+
+
+def test_logprob_parts_and_loss_spans():
+    from tests.operator_rules import rules
+    R = rules()
+    for rows in (1, 2, 48, 300, 2048, 5000):
+        for vocab in (1, 8191, 16384, 150000, 10 ** 6):
+            p = R.parts(rows, vocab)
+            assert 1 <= p <= 64 and (p == 1 or vocab // p >= 8192)
+    for nt in (0, 1, 10 ** 6, 10 ** 8, 2 ** 40 - 1):
+        s = R.span(nt)
+        assert s >= 512 and s % 256 == 0 and nt // s <= 2 ** 31 - 2
