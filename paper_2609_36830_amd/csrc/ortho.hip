@@ -24,7 +24,8 @@ constexpr float kScaleA = 256.0f;                  // A and C up to 128
 constexpr int kNormWaves = 4;                      // of a workgroup
 constexpr int kNormBlocks = 1024;                  // partial sums of squares of a matrix, at most
 constexpr int kTurn = 64;                          // side of the tiles that are turned
-constexpr int kTurnRun = 4;                        // of them by a workgroup
+constexpr int kTurnRun = 4;                        // of them by a workgroup, where there are kTurnMany
+constexpr int64_t kTurnMany = 8192;
 
 // The m x n orientation of one matrix of the batch and its workspace; the rows'
 // ends up to a multiple of 64 elements are zeros, so that products have whole steps.
@@ -109,7 +110,7 @@ __global__ __launch_bounds__(kNormWaves *kWave) void ortho_norm_kernel(const T *
 template <typename T>
 __global__ __launch_bounds__(256) void ortho_start_kernel(const T *__restrict__ g, int64_t rows, int64_t cols,
                                                           int64_t stride, int64_t batch_stride, int norm_blocks, double eps,
-                                                          OrthoShape s, char *ws) {
+                                                          int run, OrthoShape s, char *ws) {
     constexpr int V = kVecOf<T>;
     __shared__ f16_t tile[kTurn][kTurn + 8];
     __shared__ double part[4];
@@ -121,8 +122,8 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(const T *__restrict__ 
     f16_t *by_rows = (f16_t *)(w + (s.turned ? s.xt : s.x)), *by_cols = (f16_t *)(w + (s.turned ? s.x : s.xt));
     const int64_t ld_rows = s.turned ? s.mp : s.np, ld_cols = s.turned ? s.np : s.mp;
     const int64_t r0 = (int64_t)blockIdx.y * kTurn;             // in the update
-    for (int k = 0; k < kTurnRun; ++k) {
-        const int64_t c0 = ((int64_t)blockIdx.x * kTurnRun + k) * kTurn;
+    for (int k = 0; k < run; ++k) {
+        const int64_t c0 = ((int64_t)blockIdx.x * run + k) * kTurn;
         if (c0 >= cols) break;
         if (k) __syncthreads();
         constexpr int kAcross = kTurn / V;
@@ -333,9 +334,11 @@ hipError_t launch_orthogonalize(const void *g, int dtype, int64_t batch, int64_t
         using T = decltype(tag);
         hipError_t r = launch(-1, ortho_norm_kernel<T>, dim3((unsigned)blocks, (unsigned)batch), dim3(kNormWaves * kWave), stream, (const T *)g, rows,
                               cols, stride, batch_stride, w, s.bytes);
+        const int64_t across = (cols + kTurn - 1) / kTurn, down = (rows + kTurn - 1) / kTurn;
+        const int run = across * down * batch >= kTurnMany ? kTurnRun : 1;
         if (r == hipSuccess)
-            r = launch(-1, ortho_start_kernel<T>, dim3((unsigned)((cols + kTurn * kTurnRun - 1) / (kTurn * kTurnRun)), (unsigned)((rows + kTurn - 1) / kTurn), (unsigned)batch), dim3(256), stream,
-                       (const T *)g, rows, cols, stride, batch_stride, blocks, eps, s, w);
+            r = launch(-1, ortho_start_kernel<T>, dim3((unsigned)((across + run - 1) / run), (unsigned)down, (unsigned)batch), dim3(256), stream,
+                       (const T *)g, rows, cols, stride, batch_stride, blocks, eps, run, s, w);
         return r;
     });
     if (e != hipSuccess) return e;
