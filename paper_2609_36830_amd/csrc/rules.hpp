@@ -122,14 +122,27 @@ inline int64_t policy_loss_span(int64_t n_tokens) {
 }
 
 // ---- log-probabilities (logprob.hip) --------------------------------------------
-// Workgroups that share a row of logits: enough rows' parts for the chip, each
-// of at least kLogprobPart logits, at most one part a lane of the joining wave.
-constexpr int64_t kLogprobFill = 2048;
-constexpr int64_t kLogprobPart = 8192;
-inline int64_t logprob_parts(int64_t rows, int64_t vocab) {
-    const int64_t want = rows > 0 ? (kLogprobFill + rows - 1) / rows : 1, most = vocab / kLogprobPart;
-    const int64_t parts = want < most ? want : most;
-    return parts < 1 ? 1 : (parts > 64 ? 64 : parts);
+// A row of logits is taken by `parts` waves (waves = 1) or workgroups of eight
+// waves (8): enough of them for the chip, at most 64, one a lane of the joining
+// wave. A wave takes parts up to kLogprobWave logits, of at least
+// kLogprobWaveMin; a part's beginning and end cost a workgroup more than its
+// logits where these are few. A wave's 64 threads bound up to 32 alternatives
+// well; more are left to the workgroup's 512.
+struct LogprobPlan {
+    int waves;
+    int64_t parts;
+};
+constexpr int64_t kLogprobWaves = 4096, kLogprobWaveMin = 4096, kLogprobWave = 16384;
+constexpr int64_t kLogprobGroups = 2048, kLogprobGroupMin = 8192;
+inline LogprobPlan logprob_plan(int64_t rows, int64_t vocab, int top_k) {
+    auto parts = [&](int64_t fill, int64_t least) {
+        const int64_t want = rows > 0 ? (fill + rows - 1) / rows : 1, most = vocab / least;
+        const int64_t p = want < most ? want : most;
+        return p < 1 ? (int64_t)1 : (p > 64 ? (int64_t)64 : p);
+    };
+    const int64_t w = parts(kLogprobWaves, kLogprobWaveMin);
+    if (top_k <= 32 && vocab / w <= kLogprobWave) return {1, w};
+    return {8, parts(kLogprobGroups, kLogprobGroupMin)};
 }
 // The backward pass has nothing to join: parts of 16,384 logits as far as the
 // grid can number them.

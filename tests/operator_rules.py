@@ -17,7 +17,8 @@ int full(int64_t m, int64_t n, int64_t batch, int64_t steps, int64_t cus) {
 int lower(int64_t m, int64_t batch, int64_t steps, int64_t cus) {
     return product_tile(steps, cus, [=](int64_t s) { const int64_t t = (m + s - 1) / s; return t * (t + 1) / 2 * batch; });
 }
-int64_t parts(int64_t rows, int64_t vocab) { return logprob_parts(rows, vocab); }
+int64_t parts(int64_t rows, int64_t vocab, int k) { return logprob_plan(rows, vocab, k).parts; }
+int waves(int64_t rows, int64_t vocab, int k) { return logprob_plan(rows, vocab, k).waves; }
 int64_t span(int64_t n_tokens) { return policy_loss_span(n_tokens); }
 }
 """ % HEADER
@@ -36,7 +37,7 @@ def rules():
             subprocess.check_call(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", src, "-o", so])
             _lib = ctypes.CDLL(so)
         i64 = ctypes.c_int64
-        for name, res, args in (("full", ctypes.c_int, (i64,) * 5), ("lower", ctypes.c_int, (i64,) * 4), ("parts", i64, (i64, i64)),
+        for name, res, args in (("full", ctypes.c_int, (i64,) * 5), ("lower", ctypes.c_int, (i64,) * 4), ("parts", i64, (i64, i64, ctypes.c_int)), ("waves", ctypes.c_int, (i64, i64, ctypes.c_int)),
                                 ("span", i64, (i64,))):
             f = getattr(_lib, name)
             f.restype, f.argtypes = res, args

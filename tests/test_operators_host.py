@@ -117,8 +117,10 @@ def test_logprob_parts_and_loss_spans():
     R = rules()
     for rows in (1, 2, 48, 300, 2048, 5000):
         for vocab in (1, 8191, 16384, 150000, 10 ** 6):
-            p = R.parts(rows, vocab)
-            assert 1 <= p <= 64 and (p == 1 or vocab // p >= 8192)
+            for k in (0, 20, 64):
+                p, w = R.parts(rows, vocab, k), R.waves(rows, vocab, k)
+                assert w in (1, 8) and 1 <= p <= 64 and (p == 1 or vocab // p >= 4096)
+                assert w == 8 or (k <= 32 and vocab // p <= 16384)
     for nt in (0, 1, 10 ** 6, 10 ** 8, 2 ** 40 - 1):
         s = R.span(nt)
         assert s >= 512 and s % 256 == 0 and nt // s <= 2 ** 31 - 2
