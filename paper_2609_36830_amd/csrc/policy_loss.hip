@@ -8,12 +8,13 @@
 // a trajectory every loss has one sign: the sums by trajectory do not cancel.
 //
 // HBM-bound: 8 bytes read a token (12 with tags), 4 written. One wave takes one
-// span of consecutive tokens and walks the trajectories in it, 64 of their
-// ends, advantages and weights at a time. A trajectory inside a span is summed
-// and written there; one that crosses a span's end leaves its parts in the
-// spans' head and tail slots, which a second kernel adds in span order, one
-// wave a trajectory. Sums are binary64, so results repeat bit for bit and do
-// not depend on the span by more than its rounding.
+// span of consecutive tokens, 256 a round, four consecutive ones a lane; a
+// round's bytes are on their way while the trajectories of the one before are
+// summed. The trajectories' ends and factors are taken 64 at a time, one a lane;
+// a round that several trajectories meet in is summed once for each. A
+// trajectory inside a span is written there; one that crosses a span's end
+// leaves its parts in the spans' head and tail slots, which a second kernel adds
+// in span order, one wave a trajectory. Sums are binary64, in a fixed order.
 #include "elem.hpp"
 #include "kernels.hpp"
 
@@ -25,39 +26,59 @@ namespace {
 
 constexpr int kLossWaves = 4;          // waves of a workgroup
 constexpr int kLossPer = 4;            // consecutive tokens of a lane
+constexpr int kLossRound = kWave * kLossPer;
 
 struct LossSum {
     double loss, kl;
     int64_t clipped;
 };
 
-__device__ __forceinline__ LossSum wave_total(LossSum v) {
-#pragma unroll
-    for (int off = kWave / 2; off >= 1; off >>= 1) {
-        v.loss += __shfl_xor(v.loss, off, kWave);
-        v.kl += __shfl_xor(v.kl, off, kWave);
-        v.clipped += __shfl_xor((long long)v.clipped, off, kWave);
-    }
-    return v;
+// Sums in lane order's tree (row shifts and row broadcasts), in every lane.
+__device__ __forceinline__ double wave_total_f64(double v) {
+    auto step = [&](uint64_t got) { v += __builtin_bit_cast(double, got); };
+    step(dpp_u64<0x111, 0xf>(0ull, __builtin_bit_cast(uint64_t, v)));
+    step(dpp_u64<0x112, 0xf>(0ull, __builtin_bit_cast(uint64_t, v)));
+    step(dpp_u64<0x114, 0xf>(0ull, __builtin_bit_cast(uint64_t, v)));
+    step(dpp_u64<0x118, 0xf>(0ull, __builtin_bit_cast(uint64_t, v)));
+    step(dpp_u64<0x142, 0xa>(0ull, __builtin_bit_cast(uint64_t, v)));
+    step(dpp_u64<0x143, 0xc>(0ull, __builtin_bit_cast(uint64_t, v)));
+    return __builtin_bit_cast(double, readlane_i64(__builtin_bit_cast(int64_t, v), kWave - 1));
+}
+__device__ __forceinline__ LossSum wave_total(const LossSum &v) {
+    return {wave_total_f64(v.loss), wave_total_f64(v.kl), wave_sum_i64(v.clipped)};
 }
 
+// e^d within four units of 2^-24, by 2^(d log2 e) with what the product leaves:
+// a third of the library function's instructions, which bound the small batches.
+__device__ __forceinline__ float exp_of(float d) {
+    constexpr float hi = 1.44269502162933349609375f, lo = 1.92596299112661746887e-8f;      // log2 e
+    const float t = d * hi;
+    float rest = __builtin_fmaf(d, lo, __builtin_fmaf(d, hi, -t));
+    rest = __builtin_fabsf(t) < 126.0f ? rest : 0.0f;      // no number for infinities, nothing beyond the range
+    return __builtin_amdgcn_exp2f(t) * __builtin_fmaf(rest, 0.693147180559945309f, 1.0f);
+}
 // e^d - 1 - d. By its series for small d, where the difference would cancel
 // (at 0.7 the terms left out are below 2^-28 of the sum).
 __device__ __forceinline__ float exp_rest(float d, float r) {
-    if (!(__builtin_fabsf(d) < 0.7f)) return (r - 1.0f) - d;
-    float s = 1.0f;
-#pragma unroll
-    for (int k = 11; k >= 3; --k) s = __builtin_fmaf(d * (1.0f / (float)k), s, 1.0f);
-    return 0.5f * d * d * s;
+    float s = 1.0f / 39916800.0f;
+    s = __builtin_fmaf(s, d, 1.0f / 3628800.0f);
+    s = __builtin_fmaf(s, d, 1.0f / 362880.0f);
+    s = __builtin_fmaf(s, d, 1.0f / 40320.0f);
+    s = __builtin_fmaf(s, d, 1.0f / 5040.0f);
+    s = __builtin_fmaf(s, d, 1.0f / 720.0f);
+    s = __builtin_fmaf(s, d, 1.0f / 120.0f);
+    s = __builtin_fmaf(s, d, 1.0f / 24.0f);
+    s = __builtin_fmaf(s, d, 1.0f / 6.0f);
+    s = __builtin_fmaf(s, d, 0.5f);
+    return __builtin_fabsf(d) < 0.7f ? d * d * s : (r - 1.0f) - d;
 }
 
 struct TokenLoss {
-    float grad, loss, kl;
+    float grad, loss;
     bool cut;
 };
-__device__ __forceinline__ TokenLoss token_loss(float lp_new, float lp_beh, float k, const LossBounds &b) {
-    const float d = lp_new - lp_beh;
-    const float r = expf(d);
+// r = e^d.
+__device__ __forceinline__ TokenLoss token_loss(float d, float r, float k, const LossBounds &b) {
     TokenLoss t;
     const bool up = k > 0.0f && d > b.log_high, down = k < 0.0f && d < b.log_low, far = k < 0.0f && d > b.log_dual;
     t.cut = up || down || far;
@@ -65,8 +86,18 @@ __device__ __forceinline__ TokenLoss token_loss(float lp_new, float lp_beh, floa
     // No advantage, no gradient, whatever the ratio.
     t.loss = k == 0.0f ? 0.0f : -k * rc;
     t.grad = t.cut || k == 0.0f ? 0.0f : -k * r;
-    t.kl = exp_rest(d, r);
     return t;
+}
+
+// Four consecutive tokens from q on, those at or past `end` as zeros.
+__device__ __forceinline__ uint4 load_four(const void *a, int64_t q, int64_t end) {
+    const uint32_t *p = reinterpret_cast<const uint32_t *>(a) + q;
+    if (q + kLossPer <= end) return load_a4(p);
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (q < end) v.x = p[0];
+    if (q + 1 < end) v.y = p[1];
+    if (q + 2 < end) v.z = p[2];
+    return v;
 }
 
 template <bool kTags>
@@ -75,99 +106,126 @@ __global__ __launch_bounds__(kLossWaves * kWave) void policy_loss_kernel(
     const int64_t *__restrict__ off, int64_t n, int64_t nt, const float *__restrict__ adv,
     const float *__restrict__ weight, double scale, LossBounds bounds, int64_t span, float *__restrict__ grad,
     float *__restrict__ loss, float *__restrict__ kl, int32_t *__restrict__ clipped, LossSum *__restrict__ slots) {
-    const int64_t wave = (int64_t)blockIdx.x * kLossWaves + threadIdx.x / kWave;
+    const int64_t wave = (int64_t)blockIdx.x * kLossWaves + readlane_i32((int)threadIdx.x / kWave, 0);
     const int64_t p0 = wave * span;
     if (p0 >= nt) return;                            // whole waves; no barrier below
     const int64_t p1 = p0 + span < nt ? p0 + span : nt;
     const int lane = lane_id();
-    auto zero = [&](int64_t from, int64_t to) {       // tokens of no trajectory
-        for (int64_t q = from + lane; q < to; q += kWave) grad[q] = 0.0f;
+    const int64_t batch = readlane_i64(clamp64(off[n], 0, nt), 0), live1 = batch < p1 ? batch : p1;      // tokens behind it are not read
+    uint4 a, b, w = make_uint4(0, 0, 0, 0);
+    auto load = [&](int64_t base) {
+        const int64_t q = base + (int64_t)lane * kLossPer;
+        if (base + kLossRound <= live1) {            // the whole wave: no load behind a branch of its own
+            a = load_a4(lp_new + q);
+            b = load_a4(lp_beh + q);
+            if (kTags) w = load_a4(tags + q);
+        } else {
+            a = load_four(lp_new, q, live1);
+            b = load_four(lp_beh, q, live1);
+            if (kTags) w = load_four(tags, q, live1);
+        }
     };
-    int64_t i = wave_last_le(off, n, p0);
+    load(p0);
+
+    int64_t i = wave_last_le(off, n, p0);            // the trajectory at pos, or the first behind it
     int64_t pos = p0;
     if (i < 0) {
         i = 0;
-        const int64_t first = readlane_i64(clamp64(off[0], p0, p1), 0);
-        zero(p0, first);
-        pos = first;
+        pos = readlane_i64(clamp64(off[0], p0, p1), 0);      // tokens before the first trajectory
     }
-    bool inside = i < n && readlane_i64(off[i], 0) >= p0;      // trajectory i starts in this span
-    while (pos < p1 && i < n) {
-        // the next 64 trajectories, one a lane
+    bool inside = i < n && readlane_i64(off[i < n ? i : n], 0) >= p0;      // trajectory i starts in this span
+    // The next 64 trajectories from i on, one a lane, and where i is among them.
+    int64_t my_end = 0;
+    float my_k = 0.0f;
+    int at = 0;
+    auto take = [&]() {
         const int64_t mine = i + lane;
-        const int64_t my_end = mine < n ? clamp64(off[mine + 1], 0, nt) : nt;
-        float my_k = 0.0f;
-        if (mine < n) my_k = (float)(scale * (weight ? (double)weight[mine] : 1.0) * (double)adv[mine]);
-        const int64_t left = n - i;
-        const int most = left < kWave ? (int)left : kWave;
-        int j = 0;
-        for (; j < most && pos < p1; ++j) {
-            const int64_t end_all = readlane_i64(my_end, j);
-            const int64_t end = end_all < p1 ? end_all : p1;
-            if (end > pos) {
-                const float k = __builtin_bit_cast(float, readlane_i32(__builtin_bit_cast(int32_t, my_k), j));
-                LossSum sum = {0.0, 0.0, 0};
-                for (int64_t base = pos; base < end; base += kWave * kLossPer) {
-                    const int64_t q = base + (int64_t)lane * kLossPer;
-                    float a[kLossPer], b[kLossPer], g[kLossPer];
-                    bool live[kLossPer];
-                    const bool whole = q + kLossPer <= end;
-                    if (whole) {
-                        const uint4 x = load_a4(lp_new + q), y = load_a4(lp_beh + q);
-                        unpack16<float>(x, a);
-                        unpack16<float>(y, b);
-                        if (kTags) {
-                            const uint4 w = load_a4(tags + q);
-                            live[0] = (int32_t)w.x != -1, live[1] = (int32_t)w.y != -1;
-                            live[2] = (int32_t)w.z != -1, live[3] = (int32_t)w.w != -1;
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < kLossPer; ++e) live[e] = true;
-                        }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < kLossPer; ++e) {
-                            const bool in = q + e < end;
-                            a[e] = in ? lp_new[q + e] : 0.0f;
-                            b[e] = in ? lp_beh[q + e] : 0.0f;
-                            live[e] = in && (!kTags || tags[q + e] != -1);
-                        }
-                    }
-#pragma unroll
-                    for (int e = 0; e < kLossPer; ++e) {
-                        const TokenLoss t = token_loss(a[e], b[e], k, bounds);
-                        g[e] = live[e] ? t.grad : 0.0f;
-                        sum.loss += live[e] ? (double)t.loss : 0.0;
-                        sum.kl += live[e] ? (double)t.kl : 0.0;
-                        sum.clipped += live[e] && t.cut ? 1 : 0;
-                    }
-                    if (whole) {
-                        *reinterpret_cast<pace_v4u_a4 *>(grad + q) =
-                            pace_v4u_a4{__builtin_bit_cast(uint32_t, g[0]), __builtin_bit_cast(uint32_t, g[1]),
-                                        __builtin_bit_cast(uint32_t, g[2]), __builtin_bit_cast(uint32_t, g[3])};
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < kLossPer; ++e)
-                            if (q + e < end) grad[q + e] = g[e];
-                    }
-                }
-                sum = wave_total(sum);
-                if (lane == 0) {
-                    if (inside && end_all <= p1) {
-                        loss[i + j] = (float)sum.loss;
-                        if (kl) kl[i + j] = (float)sum.kl;
-                        if (clipped) clipped[i + j] = (int32_t)sum.clipped;
-                    } else {
-                        slots[2 * wave + (inside ? 1 : 0)] = sum;      // head slot for what began before
-                    }
-                }
-                pos = end;
+        my_end = mine < n ? clamp64(off[mine + 1], 0, nt) : nt;
+        my_k = mine < n ? (float)(scale * (weight ? (double)weight[mine] : 1.0) * (double)adv[mine]) : 0.0f;
+        at = 0;
+    };
+    int64_t end = nt;
+    float k = 0.0f;
+    // Trajectory i's end and factor, passing those that end at or before pos; behind the last, the span's end.
+    auto at_pos = [&]() {
+        for (;;) {
+            if (i >= n) {
+                end = p1;
+                return;
             }
-            if (pos < p1) inside = true;             // the next trajectory starts here
+            if (at == kWave) take();
+            end = readlane_i64(my_end, at);
+            k = __builtin_bit_cast(float, readlane_i32(__builtin_bit_cast(int32_t, my_k), at));
+            if (end > pos) return;
+            ++i;
+            ++at;
+            inside = true;
         }
-        i += j;
+    };
+    take();
+    at_pos();
+    LossSum sum = {0.0, 0.0, 0};
+    for (int64_t base = p0; base < p1; base += kLossRound) {
+        const int64_t q = base + (int64_t)lane * kLossPer, next = base + kLossRound;
+        float x[kLossPer], y[kLossPer], d[kLossPer], r[kLossPer], g[kLossPer];
+        bool live[kLossPer];
+        unpack16<float>(a, x);
+        unpack16<float>(b, y);
+        const uint32_t tag[kLossPer] = {w.x, w.y, w.z, w.w};
+        if (next < p1) load(next);
+#pragma unroll
+        for (int e = 0; e < kLossPer; ++e) {
+            live[e] = !kTags || (int32_t)tag[e] != -1;
+            d[e] = x[e] - y[e];
+            r[e] = exp_of(d[e]);
+            y[e] = exp_rest(d[e], r[e]);
+            g[e] = 0.0f;
+        }
+        const int64_t stop = next < p1 ? next : p1;
+        while (pos < stop) {
+            const int64_t to = end < stop ? end : stop;
+            if (i < n) {
+                const int from = (int)(pos - base) - lane * kLossPer, until = (int)(to - base) - lane * kLossPer;
+                // a lane's four terms in binary32, of one sign, then in binary64
+                float l[kLossPer], z[kLossPer];
+#pragma unroll
+                for (int e = 0; e < kLossPer; ++e) {
+                    const bool in = live[e] && e >= from && e < until;
+                    const TokenLoss t = token_loss(d[e], r[e], k, bounds);
+                    g[e] = in ? t.grad : g[e];
+                    l[e] = in ? t.loss : 0.0f;
+                    z[e] = in ? y[e] : 0.0f;
+                    sum.clipped += in && t.cut ? 1 : 0;
+                }
+                sum.loss += (double)((l[0] + l[1]) + (l[2] + l[3]));
+                sum.kl += (double)((z[0] + z[1]) + (z[2] + z[3]));
+            }
+            pos = to;
+            if (i < n && (end <= pos || pos == p1)) {      // ends here, or the span does
+                const LossSum all = wave_total(sum);
+                if (lane == 0) {
+                    if (inside && end <= pos) {
+                        loss[i] = (float)all.loss;
+                        if (kl) kl[i] = (float)all.kl;
+                        if (clipped) clipped[i] = (int32_t)all.clipped;
+                    } else {
+                        slots[2 * wave + (inside ? 1 : 0)] = all;      // head slot for what began before
+                    }
+                }
+                sum = {0.0, 0.0, 0};
+            }
+            if (pos < p1 && end <= pos) at_pos();
+        }
+        if (next <= p1 || q + kLossPer <= p1) {
+            *reinterpret_cast<pace_v4u_a4 *>(grad + q) =
+                pace_v4u_a4{__builtin_bit_cast(uint32_t, g[0]), __builtin_bit_cast(uint32_t, g[1]), __builtin_bit_cast(uint32_t, g[2]),
+                            __builtin_bit_cast(uint32_t, g[3])};
+        } else {
+#pragma unroll
+            for (int e = 0; e < kLossPer; ++e)
+                if (q + e < p1) grad[q + e] = g[e];
+        }
     }
-    zero(pos, p1);
 }
 
 // One wave a trajectory: zeros for an empty one, the slots' sum for one that

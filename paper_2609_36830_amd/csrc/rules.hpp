@@ -113,9 +113,9 @@ inline int product_tile(int64_t steps, int64_t cus, Tiles tiles) {
 }
 
 // ---- policy loss (policy_loss.hip) ------------------------------------------------
-// Tokens a wave takes: 256 are one load a lane; at least two of them, at most
+// Tokens a wave takes: 256 are one load a lane; at least that, at most
 // what leaves 8192 waves, which the chip holds at once.
-constexpr int64_t kLossSpanMin = 512;
+constexpr int64_t kLossSpanMin = 256;
 inline int64_t policy_loss_span(int64_t n_tokens) {
     const int64_t per = (n_tokens / 8192 + 255) / 256 * 256;
     return per > kLossSpanMin ? per : kLossSpanMin;

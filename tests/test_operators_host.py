@@ -123,4 +123,4 @@ def test_logprob_parts_and_loss_spans():
                 assert w == 8 or (k <= 32 and vocab // p <= 16384)
     for nt in (0, 1, 10 ** 6, 10 ** 8, 2 ** 40 - 1):
         s = R.span(nt)
-        assert s >= 512 and s % 256 == 0 and nt // s <= 2 ** 31 - 2
+        assert s >= 256 and s % 256 == 0 and nt // s <= 2 ** 31 - 2
