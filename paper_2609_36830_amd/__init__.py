@@ -541,27 +541,29 @@ def _matrix(t, name: str):
     """A device matrix with contiguous rows; returns its dtype code, rows, columns and row stride."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2:
         raise ValueError("%s must be a device matrix" % name)
-    if t.dtype not in DTYPES:
+    code = DTYPES.get(t.dtype)
+    if code is None:
         raise ValueError("%s must be float32, bfloat16 or float16, got %s" % (name, t.dtype))
-    rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+    (rows, cols), (stride, step) = t.shape, t.stride()
+    if step != 1 and cols > 1:
         raise ValueError("%s must have contiguous rows" % name)
     # a stride is only used between rows; torch leaves it free where there is one
-    return DTYPES[t.dtype], rows, cols, (t.stride(0) if rows > 1 else max(cols, 1))
+    return code, rows, cols, (stride if rows > 1 else max(cols, 1))
+
+
+def _vector(t, dtype, n: int, device, name: str):
+    """A contiguous device tensor of n elements (one test for all: these checks are a call's largest share of host time)."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of %d elements on %s" % (name, dtype, n, device))
+    return t
 
 
 def _sized(t, dtype, shape, device, name: str):
     """The caller's output (checked), or a new one."""
     if t is None:
         return torch.empty(shape, dtype=dtype, device=device)
-    if _dev(t, dtype, name).shape != torch.Size(shape) or t.device != device:
-        raise ValueError("%s must have shape %s on %s" % (name, tuple(shape), device))
-    return t
-
-
-def _vector(t, dtype, n: int, device, name: str):
-    if _dev(t, dtype, name).numel() != n or t.device != device:
-        raise ValueError("%s must hold %d elements on %s" % (name, n, device))
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape %s on %s" % (name, dtype, tuple(shape), device))
     return t
 
 
