@@ -173,15 +173,18 @@ hipError_t launch_matmul_i8(const int8_t *a, int64_t lda, const float *sa, const
     return with_elem(dtype, [&](auto tag) {
         using O = decltype(tag);
         auto tiles = [&](int64_t side) { return ((m + side - 1) / side) * ((n + side - 1) / side); };
-        if (direct)
-            return with_tile(product_tile(k / kStepBytes, resident_waves() / 16, tiles), [&](auto shape) {
+        if (direct) {
+            const int64_t cus = resident_waves() / 16;
+            const int side = product_tile(k / kStepBytes, cus, tiles);
+            return with_tile(side, tiles(side), cus, [&](auto shape) {
                 return launch_tiles<O, typename decltype(shape)::template Product<MulI8>>(rb, ra, sb, sa, out, ldo, stream);
             });
+        }
         // Off alignment the step's bytes pass through registers: 64 while that
         // leaves no CU without a tile.
         if (tiles(128) >= resident_waves() / 16)
-            return launch_tiles<O, TileProduct<MulI8, 128, 128, 2, 2, 2, false>>(rb, ra, sb, sa, out, ldo, stream);
-        return launch_tiles<O, TileProduct<MulI8, 64, 64, 2, 2, 2, false>>(rb, ra, sb, sa, out, ldo, stream);
+            return launch_tiles<O, TileProduct<MulI8, 128, 128, 2, 2, 2, 1, false>>(rb, ra, sb, sa, out, ldo, stream);
+        return launch_tiles<O, TileProduct<MulI8, 64, 64, 2, 2, 2, 1, false>>(rb, ra, sb, sa, out, ldo, stream);
     });
 }
 

@@ -50,7 +50,7 @@ struct Rows {
 // kBM x kBN tiles by kWM x kWN waves. kDirect: rows are whole steps, their
 // starts and strides whole 16-byte chunks, and the bytes go straight into LDS;
 // otherwise they pass through registers.
-template <typename Mul, int kBM, int kBN, int kWM, int kWN, int kDepth, bool kDirect>
+template <typename Mul, int kBM, int kBN, int kWM, int kWN, int kDepth, int kUnit, bool kDirect>
 struct TileProduct {
     static constexpr int kRows = kBM, kCols = kBN, kWavesN = kWN, kWaves = kWM * kWN, kThreads = kWaves * kWave;
     static constexpr int kTM = kBM / kWM / 16, kTN = kBN / kWN / 16;
@@ -59,6 +59,11 @@ struct TileProduct {
     static constexpr int kPieces = (kBM + kBN) / 8, kMine = kPieces / kWaves;
     static_assert(kPieces % kWaves == 0 && (kBM / 8) % kWaves == 0, "whole shares");
     static constexpr int kMineA = kBM / 8 / kWaves;
+    // A stage is kUnit steps between two barriers: one, or two where a step has
+    // few products to cover a barrier and the reads behind it.
+    static constexpr int kStages = kDepth / kUnit;
+    static_assert(kUnit == 1 || (kUnit == 2 && kDirect && kDepth % 2 == 0), "stages");
+    static constexpr int64_t kStageBytes = kUnit * kStepBytes;
     using Acc = typename Mul::Acc;
 
     Acc acc[kTM][kTN];
@@ -103,6 +108,18 @@ struct TileProduct {
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)((i < kMineA ? pa : pb) + k + from[i]),
                                              (__attribute__((address_space(3))) void *)piece(to, i), 16, 0, 0);
     }
+    // The stage from k on; a step that is not there is zeros.
+    __device__ __forceinline__ void fetch_stage(int64_t k, char *to) const {
+        fetch(k, to);
+        if constexpr (kUnit == 2) {
+            if (k + kStepBytes < a.bytes) {
+                fetch(k + kStepBytes, to + kBuf);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kMine; ++i) *reinterpret_cast<uint4 *>(piece(to + kBuf, i) + lane_id() * 16) = make_uint4(0, 0, 0, 0);
+            }
+        }
+    }
     // All but the newest kLeft steps on their way are there, and nobody reads
     // what was read before. (Fetches are counted in their order; a barrier with
     // a fence would wait for all of them.)
@@ -119,30 +136,36 @@ struct TileProduct {
         asm volatile("" ::: "memory");
     }
 
-    // The operands of half a step (64 bytes), and its products.
+    // The operands of half a stage (64 bytes times kUnit), and its products.
     struct Half {
-        mfma_v4i a[kTM], b[kTN];
+        mfma_v4i a[kUnit][kTM], b[kUnit][kTN];
     };
     static __device__ __forceinline__ void half(const char *now, int s, Half &h) {
         const int lane = lane_id(), wave = threadIdx.x / kWave;
-        const int at = (lane & 15) * kStepBytes + (((4 * s + (lane >> 4)) ^ (lane & 7)) << 4);
-        const char *ra = now + wave / kWN * (kBM / kWM) * kStepBytes + at;
-        const char *rb = now + kB + wave % kWN * (kBN / kWN) * kStepBytes + at;
+        if (kUnit == 2) now += s * kBuf;             // a whole step
 #pragma unroll
-        for (int i = 0; i < kTM; ++i) h.a[i] = *reinterpret_cast<const mfma_v4i *>(ra + i * 16 * kStepBytes);
+        for (int u = 0; u < kUnit; ++u) {
+            const int at = (lane & 15) * kStepBytes + (((4 * (kUnit == 2 ? u : s) + (lane >> 4)) ^ (lane & 7)) << 4);
+            const char *ra = now + wave / kWN * (kBM / kWM) * kStepBytes + at;
+            const char *rb = now + kB + wave % kWN * (kBN / kWN) * kStepBytes + at;
 #pragma unroll
-        for (int j = 0; j < kTN; ++j) h.b[j] = *reinterpret_cast<const mfma_v4i *>(rb + j * 16 * kStepBytes);
+            for (int i = 0; i < kTM; ++i) h.a[u][i] = *reinterpret_cast<const mfma_v4i *>(ra + i * 16 * kStepBytes);
+#pragma unroll
+            for (int j = 0; j < kTN; ++j) h.b[u][j] = *reinterpret_cast<const mfma_v4i *>(rb + j * 16 * kStepBytes);
+        }
     }
     __device__ __forceinline__ void products(const Half &h) {
 #pragma unroll
-        for (int i = 0; i < kTM; ++i)
+        for (int u = 0; u < kUnit; ++u)
 #pragma unroll
-            for (int j = 0; j < kTN; ++j) acc[i][j] = Mul::mul(h.a[i], h.b[j], acc[i][j]);
+            for (int i = 0; i < kTM; ++i)
+#pragma unroll
+                for (int j = 0; j < kTN; ++j) acc[i][j] = Mul::mul(h.a[u][i], h.b[u][j], acc[i][j]);
     }
     // Asks for an order of what stands before it: one read for every few products.
     template <int kReads>
     static __device__ __forceinline__ void interleave() {
-        constexpr int kAll = kTM * kTN, kEach = kAll / kReads > 0 ? kAll / kReads : 1;
+        constexpr int kAll = kUnit * kTM * kTN, kEach = kAll / kReads > 0 ? kAll / kReads : 1;
 #pragma unroll
         for (int i = 0; i < kReads; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
@@ -162,8 +185,8 @@ struct TileProduct {
                 from[i] = (i < kMineA ? (uint32_t)((row_of(a, row_a, i) - row_a) * a.stride)
                                       : (uint32_t)((row_of(b, row_b, i - kMineA) - row_b) * b.stride)) + (uint32_t)lane_chunk();
 #pragma unroll
-            for (int d = 0; d < kDepth; ++d)
-                if (d * kStepBytes < bytes) fetch(d * kStepBytes, lds + d * kBuf);
+            for (int d = 0; d < kStages; ++d)
+                if (d * kStageBytes < bytes) fetch_stage(d * kStageBytes, lds + d * kUnit * kBuf);
         }
 #pragma unroll
         for (int i = 0; i < kTM; ++i)
@@ -171,29 +194,29 @@ struct TileProduct {
             for (int j = 0; j < kTN; ++j) acc[i][j] = Acc{0, 0, 0, 0};
         int64_t k = 0;
         if constexpr (kDirect) {
-            // Half a step ahead: while one half's products run, the next half is
-            // read from LDS, and between the halves the buffer that has just
-            // been read is given to the step kDepth further on.
+            // Half a stage ahead: while one half's products run, the next half is
+            // read from LDS, and between the halves the buffers that have just
+            // been read are given to the stage kStages further on.
             Half h0, h1;
-            if (kDepth * kStepBytes <= bytes)
-                ready<kDepth - 1>();
+            if (kStages * kStageBytes <= bytes)
+                ready<(kStages - 1) * kUnit>();
             else
                 ready<0>();
             half(lds, 0, h0);
             const char *now = lds;
-            for (; k < bytes; k += kStepBytes) {
+            for (; k < bytes; k += kStageBytes) {
                 half(now, 1, h1);
                 products(h0);
-                interleave<kTM + kTN>();
-                if (kDepth == 2 || k + kDepth * kStepBytes > bytes)
+                interleave<kUnit *(kTM + kTN)>();
+                if (kStages == 2 || k + kStages * kStageBytes > bytes)
                     ready<0>();
                 else
-                    ready<kDepth - 2>();
-                if (k + kDepth * kStepBytes < bytes) fetch(k + kDepth * kStepBytes, const_cast<char *>(now));
-                now = now + kBuf == lds + kLdsBytes ? lds : now + kBuf;
-                half(now, 0, h0);                    // after the last step nothing that is used
+                    ready<(kStages - 2) * kUnit>();
+                if (k + kStages * kStageBytes < bytes) fetch_stage(k + kStages * kStageBytes, const_cast<char *>(now));
+                now = now + kUnit * kBuf == lds + kLdsBytes ? lds : now + kUnit * kBuf;
+                half(now, 0, h0);                    // after the last stage nothing that is used
                 products(h1);
-                interleave<kTM + kTN>();
+                interleave<kUnit *(kTM + kTN)>();
             }
         } else {
             // The next step's bytes are loaded while this one's products run.
@@ -317,20 +340,20 @@ __device__ __forceinline__ void lower_tile_of(uint32_t id, uint32_t tiles, int &
 }
 
 // Runs f with the tile of a side of product_tile: eight waves, and as many
-// steps in flight as the LDS of a CU holds (two workgroups of it for 64).
-template <int kBM, int kBN, int kWM, int kWN, int kDepth>
+// steps in flight as the LDS of a CU holds, for 64 of two workgroups where there
+// are tiles for more than one a CU.
+template <int kBM, int kBN, int kWM, int kWN, int kDepth, int kUnit>
 struct TileShape {
     template <typename Mul>
-    using Product = TileProduct<Mul, kBM, kBN, kWM, kWN, kDepth, true>;
-    static constexpr int kSide = kBM;
+    using Product = TileProduct<Mul, kBM, kBN, kWM, kWN, kDepth, kUnit, true>;
 };
 template <typename F>
-auto with_tile(int side, F f) {
+auto with_tile(int side, int64_t tiles, int64_t cus, F f) {
     switch (side) {
-        case 256: return f(TileShape<256, 256, 2, 4, 2>{});
-        case 192: return f(TileShape<192, 192, 2, 4, 2>{});
-        case 128: return f(TileShape<128, 128, 2, 4, 4>{});
-        default: return f(TileShape<64, 64, 4, 2, 4>{});
+        case 256: return f(TileShape<256, 256, 2, 4, 2, 1>{});
+        case 192: return f(TileShape<192, 192, 2, 4, 2, 1>{});
+        case 128: return f(TileShape<128, 128, 2, 4, 4, 1>{});
+        default: return tiles > cus ? f(TileShape<64, 64, 4, 2, 4, 2>{}) : f(TileShape<64, 64, 4, 2, 8, 2>{});
     }
 }
 

@@ -286,8 +286,9 @@ hipError_t launch_gram(const OrthoShape &s, char *ws, int64_t batch, const float
         const int64_t t = (s.m + side - 1) / side;
         return t * (t + 1) / 2 * batch;
     };
-    const int side = product_tile((kSquare ? s.mp : s.np) * 2 / kStepBytes, resident_waves() / 16, tiles);
-    return with_tile(side, [&](auto shape) {
+    const int64_t cus = resident_waves() / 16;
+    const int side = product_tile((kSquare ? s.mp : s.np) * 2 / kStepBytes, cus, tiles);
+    return with_tile(side, tiles(side), cus, [&](auto shape) {
         using P = typename decltype(shape)::template Product<MulF16>;
         return launch_lds(-1, ortho_gram_kernel<kSquare, P>, dim3((unsigned)tiles(side)), dim3(P::kThreads), ortho_lds<P>(), stream, s, ws,
                           (s.m + side - 1) / side, c[0], c[1], c[2]);
@@ -296,8 +297,9 @@ hipError_t launch_gram(const OrthoShape &s, char *ws, int64_t batch, const float
 template <bool kLast>
 hipError_t launch_apply(const OrthoShape &s, char *ws, int64_t batch, int64_t from, int64_t to, bf16_t *out, hipStream_t stream) {
     auto tiles = [&](int64_t side) { return ((s.m + side - 1) / side) * ((s.n + side - 1) / side) * batch; };
-    const int side = product_tile(s.mp * 2 / kStepBytes, resident_waves() / 16, tiles);
-    return with_tile(side, [&](auto shape) {
+    const int64_t cus = resident_waves() / 16;
+    const int side = product_tile(s.mp * 2 / kStepBytes, cus, tiles);
+    return with_tile(side, tiles(side), cus, [&](auto shape) {
         using P = typename decltype(shape)::template Product<MulF16>;
         return launch_lds(kPhaseAux, ortho_apply_kernel<kLast, P>, dim3((unsigned)tiles(side)), dim3(P::kThreads), ortho_lds<P>(), stream, s, ws,
                           from, to, (s.m + side - 1) / side, (s.n + side - 1) / side, out);

@@ -95,18 +95,18 @@ inline bool small_step_ok(int64_t n, int64_t n_tokens, int n_cols, int64_t budge
 // chip and waste less at the edges. Of 64 two workgroups share a CU from a tile
 // a CU on, which then cost more each. Measured in binary16: X X^T of 4096 x
 // 16384 342 / 281 / 406 / 484 us (256 / 192 / 128 / 64), of 2500 x 2600 56 / 42 /
-// 25 / 37, of 1000 x 3001 62 / 44 / 26 / 16; C X of 4096 x 16384 470 / 614 / 664 / 993.
+// 25 / 37, of 1000 x 3001 62 / 44 / 26 / 14; C X of 4096 x 16384 470 / 614 / 664 / 993.
 template <typename Tiles>
 inline int product_tile(int64_t steps, int64_t cus, Tiles tiles) {
     constexpr int side[4] = {256, 192, 128, 64};
-    constexpr double ends[4] = {5.0, 4.0, 3.0, 1.5}, step[4] = {1.65, 1.1, 0.55, 0.24};
+    constexpr double ends[4] = {5.0, 4.0, 3.0, 1.5}, step[4] = {1.65, 1.1, 0.55, 0.19};
     int best = 64;
     double least = 1e300;
     for (int k = 0; k < 4; ++k) {
         const int64_t n = tiles((int64_t)side[k]);
         const bool two = side[k] == 64 && n > cus;
         const int64_t rounds = two ? (n + 2 * cus - 1) / (2 * cus) : (n + cus - 1) / cus;
-        const double t = (double)rounds * (ends[k] + (double)steps * (two ? 0.45 : step[k]));
+        const double t = (double)rounds * (ends[k] + (double)steps * (two ? 0.43 : step[k]));
         if (t < least) least = t, best = side[k];
     }
     return best;
