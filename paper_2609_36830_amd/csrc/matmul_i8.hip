@@ -137,6 +137,100 @@ __global__ __launch_bounds__(P::kThreads) void matmul_i8_kernel(Rows b, Rows a, 
     }
 }
 
+// ---- a few tokens -----------------------------------------------------------------
+// The weights are read once and bound the time: no tiles, no LDS on their way. A
+// load of a wave is 8 channels by 128 bytes; a lane multiplies its 16 bytes with
+// the same bytes of each token, four products an instruction. The waves of a
+// workgroup take runs of the summed axis of the same channels.
+constexpr int kFewWaves = 4;
+constexpr int kFewSteps = 4;                         // steps of 128 bytes on their way together
+
+// 16 bytes from `at` on of a row of `bytes` bytes, zeros behind its end.
+__device__ __forceinline__ uint4 load_tail(const char *row, int64_t at, int64_t bytes) {
+    if (at + 16 <= bytes) return load_a1(row + at);
+    uint32_t w[4] = {0, 0, 0, 0};
+    for (int k = 0; k < 16 && at + k < bytes; ++k) w[k >> 2] |= (uint32_t)(uint8_t)row[at + k] << (8 * (k & 3));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ int dot16(const uint4 &a, const uint4 &b, int c) {
+    c = __builtin_amdgcn_sdot4((int)a.x, (int)b.x, c, false);
+    c = __builtin_amdgcn_sdot4((int)a.y, (int)b.y, c, false);
+    c = __builtin_amdgcn_sdot4((int)a.z, (int)b.z, c, false);
+    return __builtin_amdgcn_sdot4((int)a.w, (int)b.w, c, false);
+}
+
+// kTok tokens at most, kGroups groups of 8 channels a workgroup.
+template <typename O, int kTok, int kGroups>
+__global__ __launch_bounds__(kFewWaves *kWave) void matmul_i8_few_kernel(Rows b, Rows a, const float *__restrict__ sb,
+                                                                         const float *__restrict__ sa, O *__restrict__ out,
+                                                                         int64_t ldo) {
+    __shared__ int part[kFewWaves][kGroups * 8][kTok];
+    const int wave = threadIdx.x / kWave, lane = lane_id();
+    const int64_t n0 = (int64_t)blockIdx.x * (kGroups * 8);
+    const int64_t steps = (b.bytes + kStepBytes - 1) / kStepBytes, per = (steps + kFewWaves - 1) / kFewWaves;
+    const int64_t k1 = (wave + 1) * per < steps ? (wave + 1) * per : steps;
+    const char *rb[kGroups], *ra[kTok];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+        const int64_t r = n0 + g * 8 + (lane >> 3);
+        rb[g] = b.p + (r < b.rows ? r : b.rows - 1) * b.stride;
+    }
+#pragma unroll
+    for (int t = 0; t < kTok; ++t) ra[t] = a.p + (t < a.rows ? t : a.rows - 1) * a.stride;
+    int acc[kGroups][kTok];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+        for (int t = 0; t < kTok; ++t) acc[g][t] = 0;
+    const int chunk = (lane & 7) * 16;
+    int64_t k = wave * per;
+    for (; k + kFewSteps <= k1 && (k + kFewSteps) * kStepBytes <= b.bytes; k += kFewSteps) {
+        uint4 w[kFewSteps][kGroups];
+#pragma unroll
+        for (int s = 0; s < kFewSteps; ++s)
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) w[s][g] = load_a1(rb[g] + (k + s) * kStepBytes + chunk);
+#pragma unroll
+        for (int s = 0; s < kFewSteps; ++s)
+#pragma unroll
+            for (int t = 0; t < kTok; ++t) {
+                const uint4 x = load_a1(ra[t] + (k + s) * kStepBytes + chunk);
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) acc[g][t] = dot16(w[s][g], x, acc[g][t]);
+            }
+    }
+    for (; k < k1; ++k) {
+        uint4 w[kGroups];
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) w[g] = load_tail(rb[g], k * kStepBytes + chunk, b.bytes);
+#pragma unroll
+        for (int t = 0; t < kTok; ++t) {
+            const uint4 x = load_tail(ra[t], k * kStepBytes + chunk, b.bytes);
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) acc[g][t] = dot16(w[g], x, acc[g][t]);
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+        for (int t = 0; t < kTok; ++t) {
+            int v = acc[g][t];                       // over the eight lanes of a channel
+            v += (int)dpp_u32<0xb1, 0xf>(0u, (uint32_t)v);
+            v += (int)dpp_u32<0x4e, 0xf>(0u, (uint32_t)v);
+            v += (int)dpp_u32<0x141, 0xf>(0u, (uint32_t)v);
+            if ((lane & 7) == 0) part[wave][g * 8 + (lane >> 3)][t] = v;
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < kGroups * 8 * kTok; i += kFewWaves * kWave) {
+        const int c = i % (kGroups * 8), t = i / (kGroups * 8);
+        if (n0 + c >= b.rows || t >= a.rows) continue;
+        int v = 0;
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) v += part[w][c][t];
+        out[t * ldo + n0 + c] = from_f32<O>((float)v * (sa[t] * sb[n0 + c]));
+    }
+}
+
 }  // namespace
 
 hipError_t launch_quantize_rows(const void *x, int dtype, int64_t rows, int64_t cols, int64_t stride, int8_t *q,
@@ -159,6 +253,19 @@ hipError_t launch_tiles(const Rows &b, const Rows &a, const float *sb, const flo
                       (O *)out, ldo);
 }
 
+template <typename O, int kTok>
+hipError_t launch_few(const Rows &b, const Rows &a, const float *sb, const float *sa, void *out, int64_t ldo,
+                      hipStream_t stream) {
+    // as many channels a workgroup as leave a workgroup for every CU
+    const int64_t cus = resident_waves() / 16;
+    auto go = [&](auto kernel, int64_t channels) {
+        return launch(kPhaseAux, kernel, dim3((unsigned)((b.rows + channels - 1) / channels)), dim3(kFewWaves * kWave), stream, b, a, sb, sa, (O *)out, ldo);
+    };
+    if (b.rows >= 32 * cus) return go(matmul_i8_few_kernel<O, kTok, 4>, 32);
+    if (b.rows >= 16 * cus) return go(matmul_i8_few_kernel<O, kTok, 2>, 16);
+    return go(matmul_i8_few_kernel<O, kTok, 1>, 8);
+}
+
 }  // namespace
 
 size_t matmul_i8_ws_bytes(int64_t, int64_t, int64_t) { return 256; }
@@ -173,18 +280,30 @@ hipError_t launch_matmul_i8(const int8_t *a, int64_t lda, const float *sa, const
     return with_elem(dtype, [&](auto tag) {
         using O = decltype(tag);
         auto tiles = [&](int64_t side) { return ((m + side - 1) / side) * ((n + side - 1) / side); };
+        const int64_t cus = resident_waves() / 16;
+        // Up to 4 tokens the products on the vector units hide behind the weights'
+        // bytes at every size: 1 x 4096 x 4096 takes 7.9 us (tiles 10.5), 1 x 16384 x
+        // 4096 11.5 (12.7), 4 x 150000 x 2048 49 (55). With 5 to 8 they do where
+        // tiles leave CUs without work, 8 x 4096 x 4096 9.3 (11.1), or come through
+        // registers, 8 x 16385 x 4099 30 (37), and not elsewhere: 8 x 150000 x 2048
+        // 67 (55).
+        if (m == 1) return launch_few<O, 1>(rb, ra, sb, sa, out, ldo, stream);
+        if (m == 2) return launch_few<O, 2>(rb, ra, sb, sa, out, ldo, stream);
+        if (m <= 4) return launch_few<O, 4>(rb, ra, sb, sa, out, ldo, stream);
+        if (m <= 8 && (!direct || tiles(64) < cus)) return launch_few<O, 8>(rb, ra, sb, sa, out, ldo, stream);
         if (direct) {
-            const int64_t cus = resident_waves() / 16;
             const int side = product_tile(k / kStepBytes, cus, tiles);
             return with_tile(side, tiles(side), cus, [&](auto shape) {
                 return launch_tiles<O, typename decltype(shape)::template Product<MulI8>>(rb, ra, sb, sa, out, ldo, stream);
             });
         }
-        // Off alignment the step's bytes pass through registers: 64 while that
-        // leaves no CU without a tile.
-        if (tiles(128) >= resident_waves() / 16)
-            return launch_tiles<O, TileProduct<MulI8, 128, 128, 2, 2, 2, 1, false>>(rb, ra, sb, sa, out, ldo, stream);
-        return launch_tiles<O, TileProduct<MulI8, 64, 64, 2, 2, 2, 1, false>>(rb, ra, sb, sa, out, ldo, stream);
+        // Off alignment the step's bytes pass through registers. 170 x 150000 x 7097
+        // takes 569 us in tiles of 192 (3 a CU), 711 in tiles of 128 and 853 in tiles
+        // of 64; 2000 x 9000 x 3001 162 (2 a CU), 132 and 195; 1000 x 4000 x 1001 19 in
+        // tiles of 128 (one a CU) and 23 in tiles of 64.
+        if (tiles(192) >= 3 * cus) return launch_tiles<O, TileProduct<MulI8, 192, 192, 2, 4, 2, 1, false>>(rb, ra, sb, sa, out, ldo, stream);
+        if (tiles(128) >= cus) return launch_tiles<O, TileProduct<MulI8, 128, 128, 2, 4, 2, 1, false>>(rb, ra, sb, sa, out, ldo, stream);
+        return launch_tiles<O, TileProduct<MulI8, 64, 64, 4, 2, 2, 1, false>>(rb, ra, sb, sa, out, ldo, stream);
     });
 }
 

@@ -219,25 +219,45 @@ struct TileProduct {
                 interleave<kUnit *(kTM + kTN)>();
             }
         } else {
-            // The next step's bytes are loaded while this one's products run.
-            uint4 held[kMine];
-            int buf = 0;
+            // kAhead steps' bytes are on their way into registers while one step's products
+            // run: one for tiles with many registers of their own and many products a step.
+            constexpr int kAhead = kBM > 64 ? 1 : 2;
+            uint4 held[kAhead][kMine];
+            const char *from_row[kMine];
 #pragma unroll
-            for (int i = 0; i < kMine; ++i) held[i] = staged(0, i);
-            for (; k < bytes; k += kStepBytes) {
+            for (int i = 0; i < kMine; ++i)
+                from_row[i] = (i < kMineA ? a.p + row_of(a, row_a, i) * a.stride : b.p + row_of(b, row_b, i - kMineA) * b.stride) + lane_chunk();
+            auto load = [&](int64_t at, uint4 (&h)[kMine]) {
+                if (at + kStepBytes <= bytes) {
 #pragma unroll
-                for (int i = 0; i < kMine; ++i) *reinterpret_cast<uint4 *>(piece(lds + buf * kBuf, i) + lane_id() * 16) = held[i];
-                ready<0>();
-                Half h;
-                half(lds + buf * kBuf, 0, h);
-                if (k + kStepBytes < bytes) {
+                    for (int i = 0; i < kMine; ++i) h[i] = load_a1(from_row[i] + at);
+                } else if (at < bytes) {             // the last step, in part
 #pragma unroll
-                    for (int i = 0; i < kMine; ++i) held[i] = staged(k + kStepBytes, i);
+                    for (int i = 0; i < kMine; ++i) h[i] = staged(at, i);
                 }
-                products(h);
-                half(lds + buf * kBuf, 1, h);
-                products(h);
-                buf ^= 1;
+            };
+#pragma unroll
+            for (int d = 0; d < kAhead; ++d) load(d * kStepBytes, held[d]);
+            static_assert(kDepth % kAhead == 0, "whole turns of the register stages");
+            while (k < bytes) {
+#pragma unroll
+                for (int d = 0; d < kDepth; ++d) {
+                    char *now = lds + d * kBuf;
+#pragma unroll
+                    for (int i = 0; i < kMine; ++i) *reinterpret_cast<uint4 *>(piece(now, i) + lane_id() * 16) = held[d % kAhead][i];
+                    load(k + kAhead * kStepBytes, held[d % kAhead]);
+                    // waits for LDS only: the loads of the steps to come stay on their way
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                    Half h;
+                    half(now, 0, h);
+                    products(h);
+                    half(now, 1, h);
+                    products(h);
+                    k += kStepBytes;
+                    if (k >= bytes) break;
+                }
             }
         }
     }

@@ -132,11 +132,29 @@ def test_few_steps(pace, m, n, steps):
     check(pace, *operands(m, n, 128 * steps, steps), dtype=torch.bfloat16)
 
 
+@pytest.mark.parametrize("m", [1, 2, 3, 4, 5, 7, 8, 9])
+@pytest.mark.parametrize("n,k,pad,lead", [(1, 1, 0, 0), (7, 130, 0, 0), (700, 4096, 0, 0), (5003, 1000, 0, 0), (9001, 4515, 0, 0), (4097, 2048, 3, 5), (300, 131071, 0, 1)])
+def test_few_tokens(pace, m, n, k, pad, lead):
+    """One to eight tokens, over weights of every alignment, and the first number beyond them."""
+    say("i8 product of %d tokens n=%d k=%d" % (m, n, k))
+    a, sa, b, sb = operands(m, n, k, n + k + m, (pad, pad), lead)
+    for dtype in TYPES:
+        check(pace, a, sa, b, sb, dtype=dtype)
+
+
 @pytest.mark.parametrize("k", [1, 15, 17, 63, 65, 127, 129, 1000, 1023])
 @pytest.mark.parametrize("m,n", [(1, 300), (20, 50), (300, 20000)])
 def test_odd_lengths(pace, m, n, k):
     say("i8 product odd k=%d m=%d n=%d" % (k, m, n))
     check(pace, *operands(m, n, k, k))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k", [(30, 900, 259), (300, 20011, 400), (577, 40003, 130), (1000, 25100, 1001)])
+def test_tiles_off_alignment(pace, dtype, m, n, k):
+    """Each size of tile whose bytes come through registers."""
+    say("i8 product off alignment m=%d n=%d k=%d" % (m, n, k))
+    check(pace, *operands(m, n, k, m + k), dtype=dtype)
 
 
 @pytest.mark.parametrize("m,n,k,pad,lead", [(3, 500, 256, (16, 32), 16), (200, 300, 512, (5, 11), 3), (1, 700, 1024, (0, 1), 7),
