@@ -12,6 +12,16 @@ fails loudly.
     budget, r_hat    = pace_budget(occupancy, capacity, r_hat_prev=0.0)
     keep, reject_ids = pace_select(score, budget)
     off_out, ids, n_kept_tokens, packed = pace_compact(offsets, keep, [tags])
+
+Around the step, from a policy's hidden states to its log-probabilities, and from
+the packed batch to a weight update:
+
+    q, q_scale               = pace_quantize_rows(hidden)
+    logits                   = pace_matmul_i8(q, q_scale, head_q, head_scale)
+    logp, entropy, stats, *_ = pace_token_logprob(logits, token_ids)
+    grad_logp, loss, *_      = pace_policy_loss(logp, lp_behavior, offsets, advantage, tags)
+    grad_logits              = pace_token_logprob_backward(logits, token_ids, stats, grad_logp)
+    update                   = pace_orthogonalize(momentum)
 """
 from __future__ import annotations
 
@@ -26,6 +36,8 @@ __all__ = [
     "PaceError", "PaceParams", "default_params", "pace_workspace_bytes", "pace_score",
     "pace_budget", "pace_select", "pace_compact", "pace_validate", "pace_filter_step",
     "pace_filter_step_noalloc", "FilterStep",
+    "pace_token_logprob", "pace_token_logprob_backward", "token_logprob_buffers", "pace_policy_loss", "policy_loss_buffers",
+    "pace_quantize_rows", "pace_matmul_i8", "matmul_i8_buffers", "pace_orthogonalize", "orthogonalize_buffers",
     "library_path", "WS_SCORE", "WS_SELECT", "WS_COMPACT", "WS_FILTER_STEP",
     "BAD_OFFSETS", "BAD_COMPLETION", "BAD_TAG", "BAD_WINDOW",
 ]
@@ -567,6 +579,13 @@ def _sized(t, dtype, shape, device, name: str):
     return t
 
 
+def _scratch(ws, device):
+    """The caller's workspace: its pointer and size (which the library checks)."""
+    if not isinstance(ws, torch.Tensor) or ws.dtype != torch.uint8 or ws.device != device or not ws.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor on %s" % device)
+    return ws.data_ptr(), ws.numel()
+
+
 def pace_token_logprob_workspace_bytes(n_rows: int, vocab: int, top_k: int = 0) -> int:
     out = ctypes.c_size_t(0)
     _check(lib().pace_token_logprob_workspace_bytes(int(n_rows), int(vocab), int(top_k), ctypes.byref(out)),
@@ -595,10 +614,10 @@ def pace_token_logprob(logits, token_ids, temperature: float = 1.0, top_k: int =
     logp, entropy = _sized(b["logp"], torch.float32, (n,), dev, "logp"), _sized(b["entropy"], torch.float32, (n,), dev, "entropy")
     stats = _sized(b["stats"], torch.float32, (n, 2), dev, "stats")
     ids, top = _sized(b["top_ids"], torch.int32, (n, top_k), dev, "top_ids"), _sized(b["top_logp"], torch.float32, (n, top_k), dev, "top_logp")
-    ws = b["workspace"]
+    ws, ws_bytes = _scratch(b["workspace"], dev)
     _check(lib().pace_token_logprob(logits.data_ptr(), dt, n, vocab, stride, token_ids.data_ptr(), float(temperature),
                                     int(top_k), logp.data_ptr(), entropy.data_ptr(), stats.data_ptr(), ids.data_ptr(),
-                                    top.data_ptr(), ws.data_ptr(), ws.numel(), _stream(dev, stream)), "pace_token_logprob")
+                                    top.data_ptr(), ws, ws_bytes, _stream(dev, stream)), "pace_token_logprob")
     return logp, entropy, stats, ids, top
 
 
@@ -657,11 +676,11 @@ def pace_policy_loss(lp_new, lp_behavior, offsets, advantage, tags=None, weight=
     b = policy_loss_buffers(n, nt, dev) if buffers is None else buffers
     grad, loss = _sized(b["grad"], torch.float32, (nt,), dev, "grad"), _sized(b["loss"], torch.float32, (n,), dev, "loss")
     kl, clipped = _sized(b["kl"], torch.float32, (n,), dev, "kl"), _sized(b["clipped"], torch.int32, (n,), dev, "clipped")
-    ws = b["workspace"]
+    ws, ws_bytes = _scratch(b["workspace"], dev)
     _check(lib().pace_policy_loss(lp_new.data_ptr(), lp_behavior.data_ptr(), _ptr(tags), offsets.data_ptr(), n, nt,
                                   advantage.data_ptr(), _ptr(weight), float(scale), float(clip_low), float(clip_high),
                                   float(dual_clip), grad.data_ptr(), loss.data_ptr(), kl.data_ptr(), clipped.data_ptr(),
-                                  ws.data_ptr(), ws.numel(), _stream(dev, stream)), "pace_policy_loss")
+                                  ws, ws_bytes, _stream(dev, stream)), "pace_policy_loss")
     return grad, loss, kl, clipped
 
 
@@ -712,11 +731,11 @@ def pace_matmul_i8(a, a_scale, b, b_scale, out=None, out_dtype=torch.bfloat16, w
     dt, om, on, ldo = _matrix(out, "out")
     if (om, on) != (m, n) or out.device != dev:
         raise ValueError("out must have shape (%d, %d) on %s" % (m, n, dev))
-    ws = workspace
-    if ws is None:
-        ws = torch.empty(pace_matmul_i8_workspace_bytes(m, n, k), dtype=torch.uint8, device=dev)
+    if workspace is None:
+        workspace = torch.empty(pace_matmul_i8_workspace_bytes(m, n, k), dtype=torch.uint8, device=dev)
+    ws, ws_bytes = _scratch(workspace, dev)
     _check(lib().pace_matmul_i8(a.data_ptr(), lda, a_scale.data_ptr(), b.data_ptr(), ldb, b_scale.data_ptr(), m, n, k,
-                                out.data_ptr(), dt, ldo, ws.data_ptr(), ws.numel(), _stream(dev, stream)), "pace_matmul_i8")
+                                out.data_ptr(), dt, ldo, ws, ws_bytes, _stream(dev, stream)), "pace_matmul_i8")
     return out
 
 
@@ -746,14 +765,14 @@ def pace_orthogonalize(update, steps: int = 5, coefs=(3.4445, -4.7750, 2.0315), 
         raise ValueError("coefs must be three numbers")
     dev = update.device
     out = _sized(out, torch.bfloat16, tuple(update.shape), dev, "out")
-    ws = workspace
-    if ws is None:
-        ws = torch.empty(pace_orthogonalize_workspace_bytes(batch, rows, cols), dtype=torch.uint8, device=dev)
+    if workspace is None:
+        workspace = torch.empty(pace_orthogonalize_workspace_bytes(batch, rows, cols), dtype=torch.uint8, device=dev)
+    ws, ws_bytes = _scratch(workspace, dev)
     stride = u.stride(1) if rows > 1 else max(cols, 1)
     _check(lib().pace_orthogonalize(update.data_ptr(), DTYPES[update.dtype], batch, rows, cols, stride,
                                     u.stride(0) if batch > 1 else rows * stride, int(steps),
-                                    (ctypes.c_double * 3)(*map(float, coefs)), float(eps), out.data_ptr(), ws.data_ptr(),
-                                    ws.numel(), _stream(dev, stream)), "pace_orthogonalize")
+                                    (ctypes.c_double * 3)(*map(float, coefs)), float(eps), out.data_ptr(), ws,
+                                    ws_bytes, _stream(dev, stream)), "pace_orthogonalize")
     return out
 
 

@@ -319,3 +319,11 @@ def test_refusals(pace):
                 lambda: pace.pace_token_logprob_backward(z, ids, ok[2], g, grad_entropy=g)):
         with pytest.raises(pace.PaceError):
             bad()
+
+
+def test_workspace_of_another_place_or_type(pace):
+    """A workspace in host memory, or counted in another unit than bytes, is refused before anything runs."""
+    for bad in (torch.empty(1 << 20, dtype=torch.uint8), torch.empty(1 << 18, dtype=torch.float32, device=DEV)):
+        b = pace.token_logprob_buffers(3, 50, 0, torch.device(DEV))
+        with pytest.raises(ValueError):
+            pace.pace_token_logprob(torch.zeros(3, 50, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV), buffers=dict(b, workspace=bad))

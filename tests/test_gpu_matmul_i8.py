@@ -291,3 +291,12 @@ def test_refusals(pace):
         pace.pace_matmul_i8(long, sa[:1], long, sb[:1])
     with pytest.raises(pace.PaceError):
         pace.pace_matmul_i8(a, sa, b, sb, workspace=torch.empty(8, dtype=torch.uint8, device=DEV))
+
+
+def test_workspace_of_another_place_or_type(pace):
+    """A workspace in host memory, or counted in another unit than bytes, is refused before anything runs."""
+    a = torch.zeros(3, 64, dtype=torch.int8, device=DEV)
+    s = torch.ones(3, device=DEV)
+    for bad in (torch.empty(1 << 20, dtype=torch.uint8), torch.empty(1 << 18, dtype=torch.float32, device=DEV)):
+        with pytest.raises(ValueError):
+            pace.pace_matmul_i8(a, s, a, s, workspace=bad)

@@ -179,3 +179,10 @@ def test_refusals(pace):
                 lambda: pace.pace_orthogonalize(g[0][:, :0])):
         with pytest.raises(pace.PaceError):
             bad()
+
+
+def test_workspace_of_another_place_or_type(pace):
+    """A workspace in host memory, or counted in another unit than bytes, is refused before anything runs."""
+    for bad in (torch.empty(1 << 20, dtype=torch.uint8), torch.empty(1 << 18, dtype=torch.float32, device=DEV)):
+        with pytest.raises(ValueError):
+            pace.pace_orthogonalize(torch.zeros(8, 8, device=DEV), workspace=bad)

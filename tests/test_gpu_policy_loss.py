@@ -254,3 +254,12 @@ def test_refusals(pace):
     for kw in (dict(scale=float("inf")), dict(clip_low=1.0), dict(clip_low=-0.1), dict(clip_high=-1.0), dict(dual_clip=1.0)):
         with pytest.raises(pace.PaceError):
             pace.pace_policy_loss(**a, **kw)
+
+
+def test_workspace_of_another_place_or_type(pace):
+    """A workspace in host memory, or counted in another unit than bytes, is refused before anything runs."""
+    f = lambda n: torch.zeros(n, device=DEV)
+    for bad in (torch.empty(1 << 20, dtype=torch.uint8), torch.empty(1 << 18, dtype=torch.float32, device=DEV)):
+        b = pace.policy_loss_buffers(1, 9, torch.device(DEV))
+        with pytest.raises(ValueError):
+            pace.pace_policy_loss(f(9), f(9), torch.tensor([0, 9], device=DEV), f(1), buffers=dict(b, workspace=bad))
