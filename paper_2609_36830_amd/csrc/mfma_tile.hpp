@@ -47,6 +47,15 @@ struct Rows {
     int64_t stride, rows, bytes;
 };
 
+// What a workgroup does with a tile: all of its steps, one of several runs of them,
+// whose sums it leaves in memory, or adding those up.
+enum TileWork { kWhole, kPart, kJoin };
+// The part-th of `parts` runs of an operand's steps, by rows of whole steps.
+__device__ __forceinline__ Rows part_of(Rows m, uint32_t part, int parts) {
+    const int64_t run = (m.bytes / kStepBytes + parts - 1) / parts * kStepBytes, at = part * run;
+    return Rows{m.p + at, m.stride, m.rows, m.bytes - at < run ? m.bytes - at : run};
+}
+
 // kBM x kBN tiles by kWM x kWN waves. kDirect: rows are whole steps, their
 // starts and strides whole 16-byte chunks, and the bytes go straight into LDS;
 // otherwise they pass through registers.
@@ -78,6 +87,24 @@ struct TileProduct {
     }
     static __device__ __forceinline__ int col(int j) {
         return (int)(threadIdx.x / kWave) % kWN * (kBN / kWN) + j * 16 + (lane_id() & 15);
+    }
+
+    // The sums of a part: each thread's, 16 bytes by 16 bytes.
+    static constexpr int64_t kSumBytes = (int64_t)kBM * kBN * 4;
+    __device__ __forceinline__ void leave_sums(char *to) const {
+        Acc *mine = reinterpret_cast<Acc *>(to) + threadIdx.x;
+#pragma unroll
+        for (int k = 0; k < kTM * kTN; ++k) mine[k * kThreads] = acc[k / kTN][k % kTN];
+    }
+    // The parts' sums, in the order of the parts.
+    __device__ __forceinline__ void add_sums(const char *from, int parts) {
+        const Acc *mine = reinterpret_cast<const Acc *>(from) + threadIdx.x;
+#pragma unroll
+        for (int k = 0; k < kTM * kTN; ++k) acc[k / kTN][k % kTN] = mine[k * kThreads];
+#pragma unroll 4
+        for (int p = 1; p < parts; ++p)
+#pragma unroll
+            for (int k = 0; k < kTM * kTN; ++k) acc[k / kTN][k % kTN] += mine[(p * kTM * kTN + k) * kThreads];
     }
 
     // The row of an operand that this lane fetches in its i-th piece. Rows

@@ -32,6 +32,7 @@ constexpr int64_t kTurnMany = 8192;
 struct OrthoShape {
     int64_t m, n, mp, np;                          // mp, np: m and n up to 64
     int64_t x, xt, xt2, a, c, bytes;               // byte offsets in a matrix's workspace, and its size
+    int64_t split;                                 // behind all matrices': the split products' parts (0: none)
     bool turned;                                   // the update has more rows than columns
 };
 OrthoShape ortho_shape(int64_t rows, int64_t cols) {
@@ -53,6 +54,7 @@ OrthoShape ortho_shape(int64_t rows, int64_t cols) {
     s.a = take(s.m * s.mp);
     s.c = take(s.m * s.mp);
     s.bytes = at;
+    s.split = 0;
     return s;
 }
 // Waves take pieces of kNormPiece elements of rows.
@@ -60,6 +62,13 @@ constexpr int kNormPiece = 4096;
 int ortho_norm_blocks(int64_t rows, int64_t cols) {
     const int64_t pieces = rows * ((cols + kNormPiece - 1) / kNormPiece), b = (pieces + kNormWaves - 1) / kNormWaves;
     return (int)(b > kNormBlocks ? kNormBlocks : b);
+}
+
+// The workspace of the parts of X X^T.
+size_t ortho_split_bytes(const OrthoShape &s, int64_t batch) {
+    const int64_t t = (s.m + 63) / 64, tiles = t * (t + 1) / 2 * batch;
+    const int parts = product_parts(s.np / 64, tiles);
+    return parts == 1 ? 0 : (size_t)(tiles * parts) * 64 * 64 * sizeof(float);
 }
 
 // The sum over a workgroup of four waves, in thread order's tree, in every thread.
@@ -161,22 +170,34 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(const T *__restrict__ 
 }
 
 // kSquare: C = a I + b A + c A A from A, else A = X X^T: the lower tiles, each
-// to both of its places. A workgroup takes a tile of one matrix of the batch.
-template <bool kSquare, typename P>
-__global__ __launch_bounds__(P::kThreads) void ortho_gram_kernel(OrthoShape s, char *ws, uint32_t side, float ca, float cb, float cc) {
+// to both of its places. A workgroup takes a tile of one matrix of the batch, or a
+// part of its steps.
+template <bool kSquare, TileWork kWork, typename P>
+__global__ __launch_bounds__(P::kThreads) void ortho_gram_kernel(OrthoShape s, char *ws, uint32_t side, float ca, float cb, float cc, int parts) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const uint32_t id = xcd_run(blockIdx.x, gridDim.x), tiles = side * (side + 1) / 2;
+    const uint32_t job = xcd_run(blockIdx.x, gridDim.x), tiles = side * (side + 1) / 2;
+    const uint32_t id = kWork == kPart ? job / parts : job;
     const uint32_t mat = __builtin_amdgcn_readfirstlane((int)(id / tiles));
     char *w = ws + mat * s.bytes;
     int tm, tn;
     lower_tile_of<4>(id - mat * tiles, side, tm, tn);
     const int64_t r0 = (int64_t)tm * P::kRows, c0 = (int64_t)tn * P::kCols;
-    const Rows x = kSquare ? Rows{w + s.a, s.mp * 2, s.m, s.mp * 2} : Rows{w + s.x, s.np * 2, s.m, s.np * 2};
+    Rows x = kSquare ? Rows{w + s.a, s.mp * 2, s.m, s.mp * 2} : Rows{w + s.x, s.np * 2, s.m, s.np * 2};
     P t;
-    t.run(x, r0, x, c0, lds);
+    char *sums = ws + s.split + (int64_t)(kWork == kPart ? job : id * parts) * P::kSumBytes;
+    if constexpr (kWork == kPart) x = part_of(x, job - id * parts, parts);
+    if constexpr (kWork == kJoin) {
+        t.add_sums(sums, parts);
+    } else {
+        t.run(x, r0, x, c0, lds);
+        __syncthreads();                             // nobody reads the operands any more
+    }
+    if constexpr (kWork == kPart) {
+        t.leave_sums(sums);
+        return;
+    }
     const f16_t *a = (const f16_t *)(w + s.a);
     f16_t *to = (f16_t *)(w + (kSquare ? s.c : s.a));
-    __syncthreads();                                 // nobody reads the operands any more
 #pragma unroll
     for (int j = 0; j < P::kTN; ++j) {
         const int64_t col = c0 + P::col(j);
@@ -287,11 +308,25 @@ hipError_t launch_gram(const OrthoShape &s, char *ws, int64_t batch, const float
         return t * (t + 1) / 2 * batch;
     };
     const int64_t cus = resident_waves() / 16;
-    const int side = product_tile((kSquare ? s.mp : s.np) * 2 / kStepBytes, cus, tiles);
+    int side = product_tile((kSquare ? s.mp : s.np) * 2 / kStepBytes, cus, tiles);
+    auto go = [&](auto kernel, auto p, int64_t jobs, int parts) {
+        using P = decltype(p);
+        return launch_lds(-1, kernel, dim3((unsigned)jobs), dim3(P::kThreads), ortho_lds<P>(), stream, s, ws, (s.m + side - 1) / side, c[0], c[1], c[2], parts);
+    };
+    if constexpr (!kSquare) {
+        if (s.split) {
+            side = 64;
+            const int parts = product_parts(s.np / 64, tiles(64));
+            return with_tile(64, tiles(64) * parts, cus, [&](auto shape) {
+                using P = typename decltype(shape)::template Product<MulF16>;
+                const hipError_t e = go(ortho_gram_kernel<false, kPart, P>, P{}, tiles(64) * parts, parts);
+                return e == hipSuccess ? go(ortho_gram_kernel<false, kJoin, P>, P{}, tiles(64), parts) : e;
+            });
+        }
+    }
     return with_tile(side, tiles(side), cus, [&](auto shape) {
         using P = typename decltype(shape)::template Product<MulF16>;
-        return launch_lds(-1, ortho_gram_kernel<kSquare, P>, dim3((unsigned)tiles(side)), dim3(P::kThreads), ortho_lds<P>(), stream, s, ws,
-                          (s.m + side - 1) / side, c[0], c[1], c[2]);
+        return go(ortho_gram_kernel<kSquare, kWhole, P>, P{}, tiles(side), 1);
     });
 }
 template <bool kLast>
@@ -323,13 +358,17 @@ hipError_t ortho_steps(const OrthoShape &s, char *ws, int64_t batch, int steps, 
 
 }  // namespace
 
-size_t ortho_ws_bytes(int64_t batch, int64_t rows, int64_t cols) { return (size_t)(batch * ortho_shape(rows, cols).bytes) + 256; }
+size_t ortho_ws_bytes(int64_t batch, int64_t rows, int64_t cols) {
+    const OrthoShape s = ortho_shape(rows, cols);
+    return (size_t)(batch * s.bytes) + ortho_split_bytes(s, batch) + 256;
+}
 
 hipError_t launch_orthogonalize(const void *g, int dtype, int64_t batch, int64_t rows, int64_t cols, int64_t stride,
                                 int64_t batch_stride, int steps, const double *coefs, double eps, void *out, void *ws,
                                 hipStream_t stream) {
     if (batch == 0) return hipSuccess;
-    const OrthoShape s = ortho_shape(rows, cols);
+    OrthoShape s = ortho_shape(rows, cols);
+    if (ortho_split_bytes(s, batch)) s.split = batch * s.bytes;
     const int blocks = ortho_norm_blocks(rows, cols);
     char *w = (char *)ws;
     hipError_t e = with_elem(dtype, [&](auto tag) {

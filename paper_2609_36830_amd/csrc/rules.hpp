@@ -112,6 +112,23 @@ inline int product_tile(int64_t steps, int64_t cus, Tiles tiles) {
     return best;
 }
 
+// The runs that a product's steps are split into where there are few tiles of 64
+// and many steps: a second launch, which adds the parts, costs 3 to 5 us, a step
+// 0.19. At least 8 steps a part, and three parts that the chip holds at once (two
+// of 24 to 64 steps gave nothing: 200.8 us for 199.7). Five steps on an update of
+// 256 x 8192 take 138 us in 16 parts (237 whole), of 64 x 4096 92 in 8 (131), of
+// 900 x 8000 283 in 4 (336), of 3001 x 1000 193 in 3 (200), of 512 x 2048 121 in 4
+// (129); but of 300 x 1000, with 16 steps, 103 in 2 (97).
+constexpr int64_t kPartSteps = 8, kPartsMost = 16, kPartJobs = 512;
+inline int product_parts(int64_t steps, int64_t tiles) {
+    int64_t parts = steps / kPartSteps;
+    if (parts > kPartsMost) parts = kPartsMost;
+    if (parts * tiles > kPartJobs) parts = kPartJobs / tiles;
+    if (parts < 3) return 1;
+    const int64_t run = (steps + parts - 1) / parts;
+    return (int)((steps + run - 1) / run);           // no part without a step
+}
+
 // ---- policy loss (policy_loss.hip) ------------------------------------------------
 // Tokens a wave takes: 256 are one load a lane; at least that, at most
 // what leaves 8192 waves, which the chip holds at once.

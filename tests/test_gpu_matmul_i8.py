@@ -124,6 +124,20 @@ def test_tiles(pace, dtype, m, n, k):
     check(pace, *operands(m, n, k, k), dtype=dtype)
 
 
+# Few tiles of many steps, whose sums are formed in parts (test_operators_host.py holds them against the rule).
+PARTS = [(16, 300, 8192), (100, 4097, 6272), (9, 64, 16384), (200, 1001, 8064)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k", PARTS)
+def test_parts(pace, dtype, m, n, k):
+    say("i8 product in parts %s m=%d n=%d k=%d" % (dtype, m, n, k))
+    a, sa, b, sb = operands(m, n, k, k, extreme=True)
+    ws = torch.full((pace.pace_matmul_i8_workspace_bytes(m, n, k),), 255, dtype=torch.uint8, device=DEV)
+    got = pace.pace_matmul_i8(a, sa, b, sb, out_dtype=dtype, workspace=ws)
+    assert torch.equal(got, check(pace, a, sa, b, sb, dtype=dtype))
+
+
 @pytest.mark.parametrize("steps", [1, 2, 3, 4, 5, 7, 8])
 @pytest.mark.parametrize("m,n", [(40, 300), (701, 3000), (2001, 2100), (4097, 16385)])
 def test_few_steps(pace, m, n, steps):

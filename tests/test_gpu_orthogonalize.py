@@ -82,6 +82,22 @@ def test_tiles(pace, batch, rows, cols):
     check(pace, g.transpose(1, 2).contiguous().bfloat16(), steps=2)
 
 
+# Few tiles of many steps in X X^T, whose sums are formed in parts (test_operators_host.py holds them against the rule).
+PARTS = [(1, 64, 4096), (2, 128, 2000), (1, 3001, 1000), (1, 8000, 40)]
+
+
+@pytest.mark.parametrize("batch,rows,cols", PARTS)
+def test_parts(pace, batch, rows, cols):
+    say("orthogonalize in parts %d x %d x %d" % (batch, rows, cols))
+    g = torch.randn(batch, rows, cols, generator=torch.Generator(device=DEV).manual_seed(cols), device=DEV)
+    check(pace, g, steps=3)
+    b = pace.orthogonalize_buffers(batch, rows, cols, torch.device(DEV))
+    b["workspace"].fill_(255)
+    first = pace.pace_orthogonalize(g, **b).clone()
+    for _ in range(3):
+        assert torch.equal(pace.pace_orthogonalize(g, **b), first)
+
+
 def test_steps_and_coefficients(pace):
     say("orthogonalize steps")
     g = torch.randn(2, 90, 150, generator=torch.Generator(device=DEV).manual_seed(4), device=DEV)

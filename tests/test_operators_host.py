@@ -124,3 +124,24 @@ def test_logprob_parts_and_loss_spans():
     for nt in (0, 1, 10 ** 6, 10 ** 8, 2 ** 40 - 1):
         s = R.span(nt)
         assert s >= 256 and s % 256 == 0 and nt // s <= 2 ** 31 - 2
+
+
+def test_product_parts():
+    """Splitting a product's steps: no part without a step, no more workgroups than the chip holds, and the GPU tests reach
+    parts of one length and of two, in both kinds of workgroup."""
+    from tests.operator_rules import CUS, rules
+    from tests.test_gpu_matmul_i8 import PARTS as I8
+    from tests.test_gpu_orthogonalize import PARTS as ORTHO
+    R = rules()
+    for steps in (1, 23, 24, 31, 47, 64, 125, 1000, 2 ** 15):
+        for tiles in (1, 3, 10, 64, 136, 170, 171, 512, 10 ** 6):
+            p = R.product(steps, tiles)
+            run = -(-steps // p)
+            assert p == 1 or (3 <= p <= 16 and p * tiles <= 512 and run >= 8 and (p - 1) * run < steps <= p * run)
+            assert p == 1 or steps >= 24
+    for jobs in ([(k // 128, -(-m // 64) * -(-n // 64)) for m, n, k in I8],
+                 [(-(-max(r, c) // 64), (-(-min(r, c) // 64)) * (-(-min(r, c) // 64) + 1) // 2 * b) for b, r, c in ORTHO]):
+        parts = [R.product(s, t) for s, t in jobs]
+        assert min(parts) > 1
+        assert {s % p == 0 for (s, _), p in zip(jobs, parts)} == {True, False}
+        assert {t * p > CUS for (_, t), p in zip(jobs, parts)} == {True, False}
