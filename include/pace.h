@@ -11,6 +11,11 @@
  *   pace_validate check the data preconditions of Lemma 1     Sec. 2, Lemma 1
  *   pace_filter_step  all four steps above in one call        Algorithm 1
  *
+ * Around the step: log-probabilities of tokens from logits (pace_token_logprob),
+ * logits from states in 8 bits (pace_quantize_rows, pace_matmul_i8), the packed
+ * batch's loss and gradient (pace_policy_loss, pace_token_logprob_backward), and
+ * orthogonalised weight updates (pace_orthogonalize).
+ *
  * Conventions shared by every call
  * --------------------------------
  * - Pool layout (CSR over tokens): trajectory i owns tokens
@@ -505,7 +510,8 @@ int pace_quantize_rows(const void *x, int dtype, int64_t n_rows, int64_t n_cols,
  *   1 <= k < 131072. Any strides and starts are read; both being multiples of 16
  *   bytes, with k, is the fast case.
  * a_scale f32 [m], b_scale f32 [n]; out [m, n] of out_dtype, rows out_stride apart
- * workspace: pace_matmul_i8_workspace_bytes() bytes. */
+ * workspace: pace_matmul_i8_workspace_bytes() bytes (sums of parts of k, where
+ *   there are few tiles; else 256). */
 int pace_matmul_i8_workspace_bytes(int64_t m, int64_t n, int64_t k, size_t *bytes_out);
 int pace_matmul_i8(const int8_t *a, int64_t a_stride, const float *a_scale, const int8_t *b, int64_t b_stride,
                    const float *b_scale, int64_t m, int64_t n, int64_t k, void *out, int out_dtype, int64_t out_stride,
@@ -553,7 +559,10 @@ int pace_orthogonalize(const void *update, int dtype, int64_t batch, int64_t row
  *   PACE_PHASE_COMPACT (the compaction copy kernel; in small filter steps it
  *   selects too, and there is no select phase), PACE_PHASE_PREFIX (the
  *   Prefix Forgetting Score kernel), PACE_PHASE_AUX (the single kernel of
- *   pace_group_score, pace_group_expand, pace_stale_k or pace_diagnostics,
+ *   pace_group_score, pace_group_expand, pace_stale_k or pace_diagnostics;
+ *   the kernel that reads the logits, the tokens or the operands in
+ *   pace_token_logprob, its backward pass, pace_policy_loss, pace_quantize_rows
+ *   and pace_matmul_i8; the first product C X of pace_orthogonalize;
  *   the window-cutoff kernel of the streaming rule, or in
  *   pace_group_filter_step the kernel that expands the group flags),
  *   PACE_PHASE_CLASSIFY

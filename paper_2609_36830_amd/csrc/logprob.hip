@@ -7,13 +7,21 @@
 //
 // Forward: one pass over the logits with the running maximum, sum and weighted
 // sum of each thread, joined over the workgroup and, where a row is split over
-// several workgroups, by a second small kernel. Everything is held in binary32
-// in units of log2: u = z c - m c with c = log2(e)/tau, one fused step and one
-// exp2 an element. The rounding of m c is the same for every u of a row, so it
-// leaves S and u_t by the same factor and cancels in logp.
+// several waves or workgroups, by a second small kernel. Everything is held in
+// binary32 in units of log2: u = (z - m) c with c = log2(e)/tau and one exp2 an
+// element. The difference is taken first: z c - m c would be one step less, but
+// its rounding grows with |m c|, and logits of the type's lowest value leave the
+// range. The exponents are rounded by 2^-24 of |u|, where p is at most 2^u.
 //
 // A part of a row (all of it where there are rows enough) is taken by one wave
-// or by a workgroup of eight, by its length.
+// or by a workgroup of eight, by its length; the parts are as many as fill the
+// chip. Bound by HBM, with 12 vector instructions an element close behind: 3074
+// scored rows of 150000 bfloat16 take 171 us (5.4 TB/s; a device copy 4.8), 4096
+// with the backward pass 250 + 445 (4.9 and 5.5 TB/s: the logits, 1.2 GB, are read
+// again from HBM), 1023 of 50021 in binary32 with an entropy
+// gradient 49 + 71. 48 rows with 20 alternatives take 15.8 us, of which two
+// launches' beginnings and the dependent reads of the second (bound, holders,
+// list, rank) are all but 3.
 //
 // Best alternatives: keys (logit in order, ~index), all different, so the set
 // and its order do not depend on the order of arrival. The pass over the logits

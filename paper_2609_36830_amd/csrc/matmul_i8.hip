@@ -5,6 +5,14 @@
 //
 // The integer sums are exact in 32 bits (k < 131072). They are converted once,
 // multiplied by the product of the scales in binary32 and rounded once.
+//
+// Many tokens are bound by the matrix cores, in tiles of 256 where there are
+// enough: 4096 tokens x 16384 channels x 4096 take 227 us (2.4 PTOP/s; a library's
+// large product 2.07), with the quantisation 240. There the cores are busy 66% of
+// the time at 1.8 GHz: the tile's LDS reads take as long as its products, and the
+// clock falls with the power. 1021 x 150000 x 2048 take 355 (1.8 PTOP/s): 16 steps
+// a tile, whose store of 309 MB nothing else covers. Few tokens are bound by the
+// weights' bytes: 1 x 16384 x 4096 takes 11.5 us (5.8 TB/s).
 #include "elem.hpp"
 #include "kernels.hpp"
 #include "mfma_tile.hpp"
@@ -15,6 +23,8 @@ namespace pace {
 
 namespace {
 
+// A workgroup a row, read twice (the second time from the cache): 4096 rows of 4096
+// bfloat16 take 11.7 us (4.3 TB/s), one row 3, a launch's least.
 constexpr int kQuantThreads = 256;
 
 template <typename T>

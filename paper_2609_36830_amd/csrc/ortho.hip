@@ -9,6 +9,14 @@
 // lose eight times less than bfloat16 (the result's type) would; the products'
 // sums are binary32. X is kept by rows for X X^T and by columns for C X, so that
 // every product reads both sides along the summed axis.
+//
+// Large updates are bound by the matrix cores: five steps on 4096 x 16384 take
+// 4.35 ms for 4.47e12 operations (1.03 PFLOP/s; a library's large product in
+// binary16 1.43), X X^T 280 us, A A 77, C X 480 each, with the cores busy 52% to
+// 62% of the time at 1.85 to 2.0 GHz, behind their tiles' LDS reads; the norm and
+// the turning are 70 + 94 us at 3.8 and 5.7 TB/s. Small ones are bound by their 17
+// launches: 24 updates of 256 x 256 take 83 us, 4.9 a launch. Between, tiles do not
+// fill the chip: 3001 x 1000 takes 193 us (X X^T in parts 10 + 4, A A 8, C X 16).
 #include "elem.hpp"
 #include "kernels.hpp"
 #include "mfma_tile.hpp"
