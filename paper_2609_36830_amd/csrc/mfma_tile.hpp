@@ -168,13 +168,16 @@ struct TileProduct {
         mfma_v4i a[kUnit][kTM], b[kUnit][kTN];
     };
     static __device__ __forceinline__ void half(const char *now, int s, Half &h) {
-        const int lane = lane_id(), wave = threadIdx.x / kWave;
         if (kUnit == 2) now += s * kBuf;             // a whole step
+        half_of(now, now + kB, s, h);
+    }
+    static __device__ __forceinline__ void half_of(const char *now_a, const char *now_b, int s, Half &h) {
+        const int lane = lane_id(), wave = threadIdx.x / kWave;
 #pragma unroll
         for (int u = 0; u < kUnit; ++u) {
             const int at = (lane & 15) * kStepBytes + (((4 * (kUnit == 2 ? u : s) + (lane >> 4)) ^ (lane & 7)) << 4);
-            const char *ra = now + wave / kWN * (kBM / kWM) * kStepBytes + at;
-            const char *rb = now + kB + wave % kWN * (kBN / kWN) * kStepBytes + at;
+            const char *ra = now_a + wave / kWN * (kBM / kWM) * kStepBytes + at;
+            const char *rb = now_b + wave % kWN * (kBN / kWN) * kStepBytes + at;
 #pragma unroll
             for (int i = 0; i < kTM; ++i) h.a[u][i] = *reinterpret_cast<const mfma_v4i *>(ra + i * 16 * kStepBytes);
 #pragma unroll
@@ -188,6 +191,21 @@ struct TileProduct {
             for (int i = 0; i < kTM; ++i)
 #pragma unroll
                 for (int j = 0; j < kTN; ++j) acc[i][j] = Mul::mul(h.a[u][i], h.b[u][j], acc[i][j]);
+    }
+    // kSteps steps of operands that are in LDS already, each step's rows together and
+    // the next's so many bytes on, into acc.
+    template <int kSteps>
+    __device__ __forceinline__ void run_held(const char *held_a, int next_a, const char *held_b, int next_b) {
+#pragma unroll
+        for (int i = 0; i < kTM; ++i)
+#pragma unroll
+            for (int j = 0; j < kTN; ++j) acc[i][j] = Acc{0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < 2 * kSteps; ++k) {
+            Half h;
+            half_of(held_a + k / 2 * next_a, held_b + k / 2 * next_b, k % 2, h);
+            products(h);
+        }
     }
     // Asks for an order of what stands before it: one read for every few products.
     template <int kReads>

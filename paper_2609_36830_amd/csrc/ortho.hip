@@ -14,8 +14,8 @@
 // 4.35 ms for 4.47e12 operations (1.03 PFLOP/s; a library's large product in
 // binary16 1.43), X X^T 280 us, A A 77, C X 480 each, with the cores busy 52% to
 // 62% of the time at 1.85 to 2.0 GHz, behind their tiles' LDS reads; the norm and
-// the turning are 70 + 94 us at 3.8 and 5.7 TB/s. Small ones are bound by their 17
-// launches: 24 updates of 256 x 256 take 83 us, 4.9 a launch. Between, tiles do not
+// the turning are 70 + 94 us at 3.8 and 5.7 TB/s. Small ones are bound by their 12 to
+// 17 launches: 24 updates of 256 x 256 take 78 us, 24 of 64 x 64 40. Between, tiles do not
 // fill the chip: 3001 x 1000 takes 193 us (X X^T in parts 10 + 4, A A 8, C X 16).
 #include "elem.hpp"
 #include "kernels.hpp"
@@ -239,24 +239,11 @@ __global__ __launch_bounds__(P::kThreads) void ortho_gram_kernel(OrthoShape s, c
     P::by_rows(lds, bits, [&](int r, int c, const uint4 &v) { put(r0 + r, c0 + c, v); });
 }
 
-// X <- C X by rows and by columns, or, in the last step, the result.
+// A tile of C X, from r0 and c0 on: X by rows and by columns, or, in the last step, the result.
 template <bool kLast, typename P>
-__global__ __launch_bounds__(P::kThreads) void ortho_apply_kernel(OrthoShape s, char *ws, int64_t xt_from, int64_t xt_to, uint32_t tiles_m,
-                                                                  uint32_t tiles_n, bf16_t *__restrict__ out) {
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    const uint32_t id = xcd_run(blockIdx.x, gridDim.x);
-    const uint32_t mat = __builtin_amdgcn_readfirstlane((int)(id / (tiles_m * tiles_n)));
-    int tm, tn;
-    tile_of<8>(id - mat * (tiles_m * tiles_n), tiles_m, tiles_n, tm, tn);
-    char *w = ws + mat * s.bytes;
-    const int64_t r0 = (int64_t)tm * P::kRows, c0 = (int64_t)tn * P::kCols;
-    const Rows c{w + s.c, s.mp * 2, s.m, s.mp * 2}, x{w + xt_from, s.mp * 2, s.n, s.mp * 2};
-    P t;
-    t.run(c, r0, x, c0, lds);
-    __syncthreads();                                 // nobody reads the operands any more
+__device__ __forceinline__ void store_applied(const P &t, const OrthoShape &s, char *w, int64_t r0, int64_t c0, int64_t xt_to, bf16_t *o, char *lds) {
     if constexpr (kLast) {
         constexpr float f = 1.0f / (kScaleA * kScaleX);
-        bf16_t *o = out + mat * s.m * s.n;
         auto bits = [&](int i, int j) {
             const mfma_v4f v = t.acc[i][j];
             return make_uint2(pair_bits<bf16_t>(v[0] * f, v[1] * f), pair_bits<bf16_t>(v[2] * f, v[3] * f));
@@ -293,6 +280,99 @@ __global__ __launch_bounds__(P::kThreads) void ortho_apply_kernel(OrthoShape s, 
             if (r0 + r < s.m && c0 + cl < s.np) *reinterpret_cast<uint4 *>(by_rows + (r0 + r) * s.np + c0 + cl) = v;
         });
     }
+}
+
+// X <- C X by rows and by columns, or, in the last step, the result.
+template <bool kLast, typename P>
+__global__ __launch_bounds__(P::kThreads) void ortho_apply_kernel(OrthoShape s, char *ws, int64_t xt_from, int64_t xt_to, uint32_t tiles_m,
+                                                                  uint32_t tiles_n, bf16_t *__restrict__ out) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const uint32_t id = xcd_run(blockIdx.x, gridDim.x);
+    const uint32_t mat = __builtin_amdgcn_readfirstlane((int)(id / (tiles_m * tiles_n)));
+    int tm, tn;
+    tile_of<8>(id - mat * (tiles_m * tiles_n), tiles_m, tiles_n, tm, tn);
+    char *w = ws + mat * s.bytes;
+    const int64_t r0 = (int64_t)tm * P::kRows, c0 = (int64_t)tn * P::kCols;
+    const Rows c{w + s.c, s.mp * 2, s.m, s.mp * 2}, x{w + xt_from, s.mp * 2, s.n, s.mp * 2};
+    P t;
+    t.run(c, r0, x, c0, lds);
+    __syncthreads();                                 // nobody reads the operands any more
+    store_applied<kLast>(t, s, w, r0, c0, xt_to, out + mat * s.m * s.n, lds);
+}
+
+// kRows rows of kSteps steps of a row operand on their way from memory to LDS, each
+// step's rows together as TileProduct reads them; zeros for rows that it does not have.
+template <int kRows, int kSteps>
+struct Held {
+    static constexpr int kMine = kRows / 8 * kSteps / 8;      // pieces of 8 rows by 128 bytes, for each of eight waves
+    uint4 v[kMine];
+    __device__ __forceinline__ void load(const Rows &m, int64_t row0) {
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int p = i * 8 + threadIdx.x / kWave, chunk = (lane_id() & 7) ^ (lane_id() >> 3);
+            const int64_t row = row0 + p % (kRows / 8) * 8 + (lane_id() >> 3);
+            v[i] = make_uint4(0, 0, 0, 0);
+            if (row < m.rows) v[i] = *reinterpret_cast<const uint4 *>(m.p + row * m.stride + p / (kRows / 8) * kStepBytes + chunk * 16);
+        }
+    }
+    __device__ __forceinline__ void put(char *to) const {
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) *reinterpret_cast<uint4 *>(to + (i * 8 + threadIdx.x / kWave) * 1024 + lane_id() * 16) = v[i];
+    }
+};
+
+// C and C X in one launch, for updates of at most kMP rows: a workgroup forms 64 rows
+// of C in LDS, from all of A, and multiplies them with kCols columns of X. The sums are
+// those of the two kernels, in their order.
+template <int kMP, int kCols>
+struct SmallStep {
+    static constexpr int kSteps = kMP / 64, kNext = kMP * kStepBytes, kNextC = 64 * kStepBytes, kNextX = kCols * kStepBytes;
+    using Square = TileProduct<MulF16, kMP, 64, 4, 2, 1, 1, true>;      // columns of C, which are its rows
+    using Apply = TileProduct<MulF16, 64, kCols, 2, 4, 1, 1, true>;
+    static constexpr int kC = kNext * kSteps, kLds = kC + kNextC * kSteps;      // X comes where A was
+    static_assert(kCols <= kMP && Apply::kTurnBytes <= kLds, "and is turned where the operands were");
+};
+template <bool kLast, int kMP, int kCols>
+__global__ __launch_bounds__(512) void ortho_small_step_kernel(OrthoShape s, char *ws, int64_t xt_from, int64_t xt_to, uint32_t tiles_m,
+                                                               uint32_t tiles_n, float ca, float cb, float cc, bf16_t *__restrict__ out) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    using S = SmallStep<kMP, kCols>;
+    const uint32_t id = xcd_run(blockIdx.x, gridDim.x), mat = id / (tiles_m * tiles_n), tile = id - mat * (tiles_m * tiles_n);
+    const int r0 = (int)(tile % tiles_m) * 64;
+    const int64_t c0 = (int64_t)(tile / tiles_m) * kCols;
+    char *w = ws + mat * s.bytes;
+    Held<kMP, S::kSteps> a;
+    Held<kCols, S::kSteps> x;
+    a.load(Rows{w + s.a, s.mp * 2, s.m, s.mp * 2}, 0);
+    x.load(Rows{w + xt_from, s.mp * 2, s.n, s.mp * 2}, c0);
+    a.put(lds);
+    __syncthreads();
+    typename S::Square q;
+    q.template run_held<S::kSteps>(lds, S::kNext, lds + r0 * kStepBytes, S::kNext);
+#pragma unroll
+    for (int j = 0; j < S::Square::kTN; ++j) {
+        const int to = S::Square::col(j);            // row of C, and of A, in the strip
+#pragma unroll
+        for (int i = 0; i < S::Square::kTM; ++i) {
+            const int k = S::Square::row4(i);        // four columns of C from here on
+            const int chunk = (((k % 64 / 8) ^ (to & 7)) << 4) + (k & 4) * 2;
+            struct alignas(8) { f16_t e[4]; } g;
+            g = *reinterpret_cast<const decltype(g) *>(lds + k / 64 * S::kNext + (r0 + to) * kStepBytes + chunk);
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = __builtin_fmaf(cc / kScaleA, q.acc[i][j][e], cb * (float)g.e[e]) + (k + e == r0 + to && k + e < s.m ? ca * kScaleA : 0.0f);
+            *reinterpret_cast<uint2 *>(lds + S::kC + k / 64 * S::kNextC + to * kStepBytes + chunk) =
+                make_uint2(pair_bits<f16_t>(v[0], v[1]), pair_bits<f16_t>(v[2], v[3]));
+        }
+    }
+    __syncthreads();                                 // nobody reads A any more
+    x.put(lds);
+    __syncthreads();
+    typename S::Apply t;
+    t.template run_held<S::kSteps>(lds + S::kC, S::kNextC, lds, S::kNextX);
+    __syncthreads();                                 // nobody reads the operands any more
+    store_applied<kLast>(t, s, w, r0, c0, xt_to, out + mat * s.m * s.n, lds);
 }
 
 // No steps: the normalised update itself.
@@ -349,14 +429,32 @@ hipError_t launch_apply(const OrthoShape &s, char *ws, int64_t batch, int64_t fr
     });
 }
 
+template <bool kLast>
+hipError_t launch_small(const OrthoShape &s, char *ws, int64_t batch, int cols, int64_t from, int64_t to, const float *c, bf16_t *out, hipStream_t stream) {
+    auto go = [&](auto kernel, auto shape) {
+        const int64_t tiles_m = s.mp / 64, tiles_n = (s.n + cols - 1) / cols;
+        return launch_lds(kPhaseAux, kernel, dim3((unsigned)(tiles_m * tiles_n * batch)), dim3(512), decltype(shape)::kLds, stream, s, ws, from, to,
+                          tiles_m, tiles_n, c[0], c[1], c[2], out);
+    };
+    if (s.mp == 64) return go(ortho_small_step_kernel<kLast, 64, 64>, SmallStep<64, 64>{});
+    if (s.mp == 128) return go(ortho_small_step_kernel<kLast, 128, 64>, SmallStep<128, 64>{});
+    if (s.mp == 192) return cols == 64 ? go(ortho_small_step_kernel<kLast, 192, 64>, SmallStep<192, 64>{}) : go(ortho_small_step_kernel<kLast, 192, 128>, SmallStep<192, 128>{});
+    return cols == 64 ? go(ortho_small_step_kernel<kLast, 256, 64>, SmallStep<256, 64>{}) : go(ortho_small_step_kernel<kLast, 256, 128>, SmallStep<256, 128>{});
+}
+
 hipError_t ortho_steps(const OrthoShape &s, char *ws, int64_t batch, int steps, const float *coefs, bf16_t *out, hipStream_t stream) {
     int64_t from = s.xt, to = s.xt2;
+    const int cols = ortho_step_cols(s.mp, s.n, batch, resident_waves() / 16);
     hipError_t e = hipSuccess;
     for (int k = 0; k < steps && e == hipSuccess; ++k) {
         e = launch_gram<false>(s, ws, batch, coefs, stream);
-        if (e == hipSuccess) e = launch_gram<true>(s, ws, batch, coefs, stream);
-        if (e == hipSuccess)
-            e = k + 1 < steps ? launch_apply<false>(s, ws, batch, from, to, out, stream) : launch_apply<true>(s, ws, batch, from, to, out, stream);
+        const bool last = k + 1 == steps;
+        if (e == hipSuccess && cols) {
+            e = last ? launch_small<true>(s, ws, batch, cols, from, to, coefs, out, stream) : launch_small<false>(s, ws, batch, cols, from, to, coefs, out, stream);
+        } else {
+            if (e == hipSuccess) e = launch_gram<true>(s, ws, batch, coefs, stream);
+            if (e == hipSuccess) e = last ? launch_apply<true>(s, ws, batch, from, to, out, stream) : launch_apply<false>(s, ws, batch, from, to, out, stream);
+        }
         const int64_t x = from;
         from = to;
         to = x;

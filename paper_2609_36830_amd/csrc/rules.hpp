@@ -129,6 +129,23 @@ inline int product_parts(int64_t steps, int64_t tiles) {
     return (int)((steps + run - 1) / run);           // no part without a step
 }
 
+// Columns of X that a workgroup takes where C and C X go in one launch, 0 where they
+// do not. A launch and C's round trip through memory cost 4 to 5 us, but each
+// workgroup forms its 64 rows of C again: with one strip (mp = 64) that is as much as
+// the product, with two it pays while the chip holds most workgroups, with three and
+// four, whose operands fill a CU's LDS, while it holds them all. Five steps in us,
+// one launch / two: 24 updates of 64 x 64 40 / 60, 256 of 64 x 512 107 / 143, 24 of
+// 128 x 512 65 / 78, 128 of them 143 / 149, 256 of 128 x 1024 485 / 441, 4 of 256 x
+// 1000 87 / 94 (64 columns), 24 of 256 x 256 78 / 85 (128; with 64 103), 24 of 256 x 512
+// 125 / 102.
+inline int ortho_step_cols(int64_t mp, int64_t n, int64_t batch, int64_t cus) {
+    auto jobs = [&](int64_t cols) { return mp / 64 * ((n + cols - 1) / cols) * batch; };
+    if (mp == 64) return 64;
+    if (mp == 128) return jobs(64) <= 8 * cus ? 64 : 0;
+    if (mp > 256) return 0;
+    return jobs(64) <= cus ? 64 : jobs(128) <= cus ? 128 : 0;
+}
+
 // ---- policy loss (policy_loss.hip) ------------------------------------------------
 // Tokens a wave takes: 256 are one load a lane; at least that, at most
 // what leaves 8192 waves, which the chip holds at once.

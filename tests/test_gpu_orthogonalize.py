@@ -98,6 +98,31 @@ def test_parts(pace, batch, rows, cols):
         assert torch.equal(pace.pace_orthogonalize(g, **b), first)
 
 
+# Updates of few rows, whose C and C X go in one launch (test_operators_host.py holds them against the rule).
+SMALL = [(3, 30, 200), (1, 64, 64), (2, 65, 127), (1, 1001, 100), (1, 129, 500), (12, 192, 701), (2, 250, 193), (1, 600, 256), (20, 201, 256)]
+
+
+@pytest.mark.parametrize("batch,rows,cols", SMALL)
+def test_small_steps(pace, batch, rows, cols):
+    say("orthogonalize small %d x %d x %d" % (batch, rows, cols))
+    g = torch.randn(batch, rows, cols, generator=torch.Generator(device=DEV).manual_seed(rows), device=DEV)
+    check(pace, g)
+    check(pace, g.half(), steps=1, coefs=CUBIC)
+    g[0, 0, 0] = float("nan")                        # its own matrix only
+    out = pace.pace_orthogonalize(g)
+    assert bool(out[0].isnan().any()) and not bool(out[1:].isnan().any())
+
+
+@pytest.mark.parametrize("batch,rows,cols", [(160, 128, 1000), (80, 256, 300), (80, 290, 180)])
+def test_alone_as_in_a_batch(pace, batch, rows, cols):
+    """A batch that takes C and C X apart gives each update the bits that it has alone, where they go together."""
+    say("orthogonalize alone and in a batch %d x %d x %d" % (batch, rows, cols))
+    g = torch.randn(batch, rows, cols, generator=torch.Generator(device=DEV).manual_seed(rows), device=DEV)
+    out = pace.pace_orthogonalize(g)
+    for k in (0, batch // 2, batch - 1):
+        assert torch.equal(pace.pace_orthogonalize(g[k]), out[k])
+
+
 def test_steps_and_coefficients(pace):
     say("orthogonalize steps")
     g = torch.randn(2, 90, 150, generator=torch.Generator(device=DEV).manual_seed(4), device=DEV)

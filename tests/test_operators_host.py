@@ -145,3 +145,15 @@ def test_product_parts():
         assert min(parts) > 1
         assert {s % p == 0 for (s, _), p in zip(jobs, parts)} == {True, False}
         assert {t * p > CUS for (_, t), p in zip(jobs, parts)} == {True, False}
+
+
+def test_gpu_tests_reach_every_small_step():
+    from tests.operator_rules import CUS, rules
+    from tests.test_gpu_orthogonalize import SMALL
+    R = rules()
+    got = set()
+    for b, r, c in SMALL:
+        mp = -(-min(r, c) // 64) * 64
+        got.add((mp, R.cols(mp, max(r, c), b, CUS)))
+    assert got == {(64, 64), (128, 64), (192, 64), (192, 128), (256, 64), (256, 128)}
+    assert R.cols(128, 1000, 160, CUS) == 0 and R.cols(256, 300, 80, CUS) == 0 and R.cols(320, 320, 1, CUS) == 0
