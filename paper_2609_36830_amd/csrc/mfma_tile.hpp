@@ -192,18 +192,18 @@ struct TileProduct {
 #pragma unroll
                 for (int j = 0; j < kTN; ++j) acc[i][j] = Mul::mul(h.a[u][i], h.b[u][j], acc[i][j]);
     }
-    // kSteps steps of operands that are in LDS already, each step's rows together and
-    // the next's so many bytes on, into acc.
-    template <int kSteps>
-    __device__ __forceinline__ void run_held(const char *held_a, int next_a, const char *held_b, int next_b) {
+    // The products of a step of operands that are in LDS already, onto acc.
+    __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int i = 0; i < kTM; ++i)
 #pragma unroll
             for (int j = 0; j < kTN; ++j) acc[i][j] = Acc{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ void step(const char *now_a, const char *now_b) {
 #pragma unroll
-        for (int k = 0; k < 2 * kSteps; ++k) {
+        for (int k = 0; k < 2; ++k) {
             Half h;
-            half_of(held_a + k / 2 * next_a, held_b + k / 2 * next_b, k % 2, h);
+            half_of(now_a, now_b, k, h);
             products(h);
         }
     }
@@ -233,10 +233,7 @@ struct TileProduct {
             for (int d = 0; d < kStages; ++d)
                 if (d * kStageBytes < bytes) fetch_stage(d * kStageBytes, lds + d * kUnit * kBuf);
         }
-#pragma unroll
-        for (int i = 0; i < kTM; ++i)
-#pragma unroll
-            for (int j = 0; j < kTN; ++j) acc[i][j] = Acc{0, 0, 0, 0};
+        clear();
         int64_t k = 0;
         if constexpr (kDirect) {
             // Half a stage ahead: while one half's products run, the next half is

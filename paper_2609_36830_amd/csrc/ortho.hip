@@ -15,7 +15,8 @@
 // binary16 1.43), X X^T 280 us, A A 77, C X 480 each, with the cores busy 52% to
 // 62% of the time at 1.85 to 2.0 GHz, behind their tiles' LDS reads; the norm and
 // the turning are 70 + 94 us at 3.8 and 5.7 TB/s. Small ones are bound by their 12 to
-// 17 launches: 24 updates of 256 x 256 take 78 us, 24 of 64 x 64 40. Between, tiles do not
+// 17 launches: 24 updates of 256 x 256 take 77 us; the smallest, in one launch, are
+// bound by one workgroup's LDS: 24 of 64 x 64 take 12 us, 128 x 256 44. Between, tiles do not
 // fill the chip: 3001 x 1000 takes 193 us (X X^T in parts 10 + 4, A A 8, C X 16).
 #include "elem.hpp"
 #include "kernels.hpp"
@@ -321,6 +322,22 @@ struct Held {
     }
 };
 
+// Where a row's element k lies in LDS, in steps of `next` bytes; four from a multiple
+// of four on lie together.
+__device__ __forceinline__ int held_at(int row, int k, int next) {
+    return k / 64 * next + row * kStepBytes + (((k % 64 / 8) ^ (row & 7)) << 4) + (k & 7) * 2;
+}
+// Four columns of C's row from k on, of the square's sums and A's elements there.
+__device__ __forceinline__ uint2 four_of_c(const mfma_v4f &square, const char *a, int64_t row, int k, int64_t m, float ca, float cb, float cc) {
+    struct alignas(8) { f16_t e[4]; } g;
+    g = *reinterpret_cast<const decltype(g) *>(a);
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        v[e] = __builtin_fmaf(cc / kScaleA, square[e], cb * (float)g.e[e]) + (k + e == row && row < m ? ca * kScaleA : 0.0f);
+    return make_uint2(pair_bits<f16_t>(v[0], v[1]), pair_bits<f16_t>(v[2], v[3]));
+}
+
 // C and C X in one launch, for updates of at most kMP rows: a workgroup forms 64 rows
 // of C in LDS, from all of A, and multiplies them with kCols columns of X. The sums are
 // those of the two kernels, in their order.
@@ -348,31 +365,193 @@ __global__ __launch_bounds__(512) void ortho_small_step_kernel(OrthoShape s, cha
     a.put(lds);
     __syncthreads();
     typename S::Square q;
-    q.template run_held<S::kSteps>(lds, S::kNext, lds + r0 * kStepBytes, S::kNext);
+    q.clear();
+#pragma unroll
+    for (int k = 0; k < S::kSteps; ++k) q.step(lds + k * S::kNext, lds + k * S::kNext + r0 * kStepBytes);
 #pragma unroll
     for (int j = 0; j < S::Square::kTN; ++j) {
         const int to = S::Square::col(j);            // row of C, and of A, in the strip
 #pragma unroll
         for (int i = 0; i < S::Square::kTM; ++i) {
             const int k = S::Square::row4(i);        // four columns of C from here on
-            const int chunk = (((k % 64 / 8) ^ (to & 7)) << 4) + (k & 4) * 2;
-            struct alignas(8) { f16_t e[4]; } g;
-            g = *reinterpret_cast<const decltype(g) *>(lds + k / 64 * S::kNext + (r0 + to) * kStepBytes + chunk);
-            float v[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[e] = __builtin_fmaf(cc / kScaleA, q.acc[i][j][e], cb * (float)g.e[e]) + (k + e == r0 + to && k + e < s.m ? ca * kScaleA : 0.0f);
-            *reinterpret_cast<uint2 *>(lds + S::kC + k / 64 * S::kNextC + to * kStepBytes + chunk) =
-                make_uint2(pair_bits<f16_t>(v[0], v[1]), pair_bits<f16_t>(v[2], v[3]));
+            *reinterpret_cast<uint2 *>(lds + S::kC + held_at(to, k, S::kNextC)) =
+                four_of_c(q.acc[i][j], lds + held_at(r0 + to, k, S::kNext), (int64_t)r0 + to, k, s.m, ca, cb, cc);
         }
     }
     __syncthreads();                                 // nobody reads A any more
     x.put(lds);
     __syncthreads();
     typename S::Apply t;
-    t.template run_held<S::kSteps>(lds + S::kC, S::kNextC, lds, S::kNextX);
+    t.clear();
+#pragma unroll
+    for (int k = 0; k < S::kSteps; ++k) t.step(lds + S::kC + k * S::kNextC, lds + k * S::kNextX);
     __syncthreads();                                 // nobody reads the operands any more
     store_applied<kLast>(t, s, w, r0, c0, xt_to, out + mat * s.m * s.n, lds);
+}
+
+// Whole updates in LDS, one a workgroup, for the smallest: X by rows and by columns
+// and A, then C in its place. Products and sums are those of the other kernels.
+template <typename T, int kMP>
+__global__ __launch_bounds__(512) void ortho_whole_kernel(const T *__restrict__ g, int rows, int cols, int64_t stride, int64_t batch_stride,
+                                                          double eps, int steps, float ca, float cb, float cc, OrthoShape s,
+                                                          bf16_t *__restrict__ out) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    constexpr int V = kVecOf<T>, kHold = 64 / V;     // 512 threads hold kMP x np elements, of which there are at most 2^15
+    constexpr int kNextX = kMP * kStepBytes, kNextA = kNextX;
+    const int np = (int)s.np, m = (int)s.m, next_t = np * kStepBytes;
+    char *x = lds, *xt = lds + kMP * np * 2, *a = xt + kMP * np * 2;
+    double *part = reinterpret_cast<double *>(a);     // before there is an A
+    const T *mat = g + blockIdx.x * batch_stride;
+    // The update, in vectors of its rows, and its norm.
+    const uint32_t across = (cols + V - 1) / V, all = rows * across;
+    uint4 held[kHold];
+    double sum = 0.0;
+#pragma unroll
+    for (int k = 0; k < kHold; ++k) {
+        const uint32_t at = k * 512 + threadIdx.x, r = at / across, c = (at - r * across) * V;
+        held[k] = make_uint4(0, 0, 0, 0);
+        if (at < all) {
+            const T *from = mat + r * stride + c;
+            if (c + V <= (uint32_t)cols) {
+                held[k] = load_a1(from);
+            } else {
+                struct { T e[V]; } w = __builtin_bit_cast(decltype(w), held[k]);
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    if (c + e < (uint32_t)cols) w.e[e] = from[e];
+                held[k] = __builtin_bit_cast(uint4, w);
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kHold; ++k) {
+        float z[V];
+        unpack16<T>(held[k], z);
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum += (double)z[e] * (double)z[e];
+    }
+#pragma unroll
+    for (int off = kWave / 2; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, kWave);
+    if (lane_id() == 0) part[threadIdx.x / kWave] = sum;
+    // The update's own order first, with zeros at the lines' ends and behind them; the
+    // other one is read from it, by lanes on neighbouring lines.
+    char *own = s.turned ? xt : x, *other = s.turned ? x : xt;
+    const int lines = s.turned ? np : kMP, len = s.turned ? kMP : np, next_own = lines * kStepBytes, next_other = len * kStepBytes;
+    for (int k = threadIdx.x; k < kMP * np * 2 / 16; k += 512) reinterpret_cast<uint4 *>(own)[k] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+    const double inv = (double)kScaleX / (sqrt(((part[0] + part[1]) + (part[2] + part[3])) + ((part[4] + part[5]) + (part[6] + part[7]))) + eps);
+#pragma unroll
+    for (int k = 0; k < kHold; ++k) {
+        const uint32_t at = k * 512 + threadIdx.x, r = at / across, c = (at - r * across) * V;
+        if (at >= all) continue;
+        float z[V];
+        unpack16<T>(held[k], z);
+        struct alignas(2 * V) { f16_t e[V]; } y;
+#pragma unroll
+        for (int e = 0; e < V; ++e) y.e[e] = c + e < (uint32_t)cols ? (f16_t)(float)((double)z[e] * inv) : (f16_t)0.0f;
+        *reinterpret_cast<decltype(y) *>(own + held_at(r, c, next_own)) = y;
+    }
+    __syncthreads();
+    for (int p = threadIdx.x; p < len * lines / 8; p += 512) {
+        const int line = p % len, at = p / len * 8;
+        struct alignas(16) { uint16_t e[8]; } y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y.e[e] = *reinterpret_cast<const uint16_t *>(own + held_at(at + e, line, next_own));
+        *reinterpret_cast<decltype(y) *>(other + held_at(line, at, next_other)) = y;
+    }
+    constexpr int kWM = kMP == 64 ? 4 : 2, kWN = 8 / kWM, kSteps = kMP / 64;
+    using Square = TileProduct<MulF16, kMP, kMP, kWM, kWN, 1, 1, true>;
+    constexpr int kCols = kMP / 4, kTM = kMP / 16, kTN = kCols / 16;      // of X a wave at a time
+    const int wave = threadIdx.x / kWave, lane = lane_id();
+    for (int step = 0; step < steps; ++step) {
+        const bool last = step + 1 == steps;
+        __syncthreads();
+        Square q;
+        q.clear();
+#pragma unroll 2
+        for (int k = 0; k < np / 64; ++k) q.step(x + k * kNextX, x + k * kNextX);
+#pragma unroll
+        for (int j = 0; j < Square::kTN; ++j)
+#pragma unroll
+            for (int i = 0; i < Square::kTM; ++i) {
+                const mfma_v4f v = q.acc[i][j] * (kScaleA / (kScaleX * kScaleX));
+                *reinterpret_cast<uint2 *>(a + held_at(Square::col(j), Square::row4(i), kNextA)) = make_uint2(pair_bits<f16_t>(v[0], v[1]), pair_bits<f16_t>(v[2], v[3]));
+            }
+        __syncthreads();
+        q.clear();
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) q.step(a + k * kNextA, a + k * kNextA);
+        __syncthreads();                             // nobody reads A any more but in its own places
+#pragma unroll
+        for (int j = 0; j < Square::kTN; ++j)
+#pragma unroll
+            for (int i = 0; i < Square::kTM; ++i) {
+                char *at = a + held_at(Square::col(j), Square::row4(i), kNextA);
+                *reinterpret_cast<uint2 *>(at) = four_of_c(q.acc[i][j], at, Square::col(j), Square::row4(i), m, ca, cb, cc);
+            }
+        __syncthreads();
+        // C X: a wave takes columns of X, which no other reads, and writes them where they were
+        for (int c0 = wave * kCols; c0 < np; c0 += 8 * kCols) {
+            mfma_v4f y[kTM][kTN];
+#pragma unroll
+            for (int i = 0; i < kTM; ++i)
+#pragma unroll
+                for (int j = 0; j < kTN; ++j) y[i][j] = mfma_v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < 2 * kSteps; ++k) {
+                const int at = (lane & 15) * kStepBytes + (((4 * (k % 2) + (lane >> 4)) ^ (lane & 7)) << 4);
+                mfma_v4i b[kTN];
+#pragma unroll
+                for (int j = 0; j < kTN; ++j) b[j] = *reinterpret_cast<const mfma_v4i *>(xt + k / 2 * next_t + (c0 + j * 16) * kStepBytes + at);
+#pragma unroll
+                for (int i = 0; i < kTM; ++i) {
+                    const mfma_v4i f = *reinterpret_cast<const mfma_v4i *>(a + k / 2 * kNextA + i * 16 * kStepBytes + at);
+#pragma unroll
+                    for (int j = 0; j < kTN; ++j) y[i][j] = MulF16::mul(f, b[j], y[i][j]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kTN; ++j)
+#pragma unroll
+                for (int i = 0; i < kTM; ++i) {
+                    const int col = c0 + j * 16 + (lane & 15), row = i * 16 + (lane >> 4) * 4;
+                    uint2 w;
+                    if (last) {
+                        const mfma_v4f v = y[i][j] * (1.0f / (kScaleA * kScaleX));
+                        w = make_uint2(pair_bits<bf16_t>(v[0], v[1]), pair_bits<bf16_t>(v[2], v[3]));
+                    } else {
+                        const mfma_v4f v = y[i][j] * (1.0f / kScaleA);
+                        w = make_uint2(pair_bits<f16_t>(v[0], v[1]), pair_bits<f16_t>(v[2], v[3]));
+                    }
+                    if (!last || s.turned) *reinterpret_cast<uint2 *>(xt + held_at(col, row, next_t)) = w;
+                    if (!last || !s.turned) {
+                        // lanes on neighbouring columns exchange two of their rows
+                        const bool odd = lane & 1;
+                        const uint32_t got = dpp_u32<0xb1, 0xf>(0u, odd ? w.x : w.y), l = odd ? got : w.x, r = odd ? w.y : got;
+                        const int to = row + (odd ? 2 : 0), pair = col - (odd ? 1 : 0);
+                        *reinterpret_cast<uint32_t *>(x + held_at(to, pair, kNextX)) = (l & 0xffffu) | (r << 16);
+                        *reinterpret_cast<uint32_t *>(x + held_at(to + 1, pair, kNextX)) = (l >> 16) | (r & 0xffff0000u);
+                    }
+                }
+        }
+    }
+    __syncthreads();
+    // the result's lines, in pieces of eight
+    const int pieces = (cols + 7) / 8;
+    bf16_t *o = out + blockIdx.x * s.m * s.n;
+    for (int p = threadIdx.x; p < rows * pieces; p += 512) {
+        const int line = p / pieces, at = (p - line * pieces) * 8;
+        const uint4 v = *reinterpret_cast<const uint4 *>(own + held_at(line, at, next_own));
+        bf16_t *to = o + line * cols + at;
+        if (at + 8 <= cols) {
+            store_a1(to, v);
+        } else {
+            struct { bf16_t e[8]; } w = __builtin_bit_cast(decltype(w), v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (at + e < cols) to[e] = w.e[e];
+        }
+    }
 }
 
 // No steps: the normalised update itself.
@@ -475,6 +654,15 @@ hipError_t launch_orthogonalize(const void *g, int dtype, int64_t batch, int64_t
     if (batch == 0) return hipSuccess;
     OrthoShape s = ortho_shape(rows, cols);
     if (ortho_split_bytes(s, batch)) s.split = batch * s.bytes;
+    if (steps > 0 && ortho_whole(s.mp, s.np))
+        return with_elem(dtype, [&](auto tag) {
+            using T = decltype(tag);
+            auto go = [&](auto kernel) {
+                return launch_lds(kPhaseAux, kernel, dim3((unsigned)batch), dim3(512), (size_t)(4 * s.mp * s.np + 2 * s.mp * s.mp), stream, (const T *)g, rows,
+                                  cols, stride, batch_stride, eps, steps, (float)coefs[0], (float)coefs[1], (float)coefs[2], s, (bf16_t *)out);
+            };
+            return s.mp == 64 ? go(ortho_whole_kernel<T, 64>) : go(ortho_whole_kernel<T, 128>);
+        });
     const int blocks = ortho_norm_blocks(rows, cols);
     char *w = (char *)ws;
     hipError_t e = with_elem(dtype, [&](auto tag) {

@@ -134,7 +134,7 @@ inline int product_parts(int64_t steps, int64_t tiles) {
 // workgroup forms its 64 rows of C again: with one strip (mp = 64) that is as much as
 // the product, with two it pays while the chip holds most workgroups, with three and
 // four, whose operands fill a CU's LDS, while it holds them all. Five steps in us,
-// one launch / two: 24 updates of 64 x 64 40 / 60, 256 of 64 x 512 107 / 143, 24 of
+// one launch / two: 1 update of 64 x 4096 69 / 87, 256 of 64 x 512 107 / 143, 24 of
 // 128 x 512 65 / 78, 128 of them 143 / 149, 256 of 128 x 1024 485 / 441, 4 of 256 x
 // 1000 87 / 94 (64 columns), 24 of 256 x 256 78 / 85 (128; with 64 103), 24 of 256 x 512
 // 125 / 102.
@@ -145,6 +145,13 @@ inline int ortho_step_cols(int64_t mp, int64_t n, int64_t batch, int64_t cus) {
     if (mp > 256) return 0;
     return jobs(64) <= cus ? 64 : jobs(128) <= cus ? 128 : 0;
 }
+
+// Updates that a workgroup of 512 threads takes whole, in one launch: X twice and A in
+// LDS, 64 elements a thread on the way in. As far as that fits it is faster than the
+// launches on the whole chip, alone and in batches; five steps in us: 1 of 64 x 64
+// 12 (38), 1 of 64 x 512 34 (48), 1 of 128 x 256 44 (52), 24 of 64 x 64 12 (40),
+// 256 of 64 x 512 38 (109), 2000 of 128 x 256 375 (1159).
+inline bool ortho_whole(int64_t mp, int64_t np) { return (mp == 64 && np <= 512) || (mp == 128 && np <= 256); }
 
 // ---- policy loss (policy_loss.hip) ------------------------------------------------
 // Tokens a wave takes: 256 are one load a lane; at least that, at most

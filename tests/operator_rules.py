@@ -21,6 +21,7 @@ int64_t parts(int64_t rows, int64_t vocab, int k) { return logprob_plan(rows, vo
 int waves(int64_t rows, int64_t vocab, int k) { return logprob_plan(rows, vocab, k).waves; }
 int product(int64_t steps, int64_t tiles) { return product_parts(steps, tiles); }
 int cols(int64_t mp, int64_t n, int64_t batch, int64_t cus) { return ortho_step_cols(mp, n, batch, cus); }
+int whole(int64_t mp, int64_t np) { return ortho_whole(mp, np); }
 int64_t span(int64_t n_tokens) { return policy_loss_span(n_tokens); }
 }
 """ % HEADER
@@ -40,7 +41,7 @@ def rules():
             _lib = ctypes.CDLL(so)
         i64 = ctypes.c_int64
         for name, res, args in (("full", ctypes.c_int, (i64,) * 5), ("lower", ctypes.c_int, (i64,) * 4), ("parts", i64, (i64, i64, ctypes.c_int)), ("waves", ctypes.c_int, (i64, i64, ctypes.c_int)),
-                                ("product", ctypes.c_int, (i64, i64)), ("cols", ctypes.c_int, (i64,) * 4), ("span", i64, (i64,))):
+                                ("product", ctypes.c_int, (i64, i64)), ("cols", ctypes.c_int, (i64,) * 4), ("whole", ctypes.c_int, (i64, i64)), ("span", i64, (i64,))):
             f = getattr(_lib, name)
             f.restype, f.argtypes = res, args
     return _lib

@@ -99,7 +99,7 @@ def test_parts(pace, batch, rows, cols):
 
 
 # Updates of few rows, whose C and C X go in one launch (test_operators_host.py holds them against the rule).
-SMALL = [(3, 30, 200), (1, 64, 64), (2, 65, 127), (1, 1001, 100), (1, 129, 500), (12, 192, 701), (2, 250, 193), (1, 600, 256), (20, 201, 256)]
+SMALL = [(3, 30, 700), (1, 64, 513), (2, 65, 300), (1, 1001, 100), (1, 129, 500), (12, 192, 701), (2, 250, 193), (1, 600, 256), (20, 201, 256)]
 
 
 @pytest.mark.parametrize("batch,rows,cols", SMALL)
@@ -111,6 +111,30 @@ def test_small_steps(pace, batch, rows, cols):
     g[0, 0, 0] = float("nan")                        # its own matrix only
     out = pace.pace_orthogonalize(g)
     assert bool(out[0].isnan().any()) and not bool(out[1:].isnan().any())
+
+
+# Updates that a workgroup holds whole, up to the largest of both kinds (test_operators_host.py holds them against the rule).
+WHOLE = [(3, 30, 200), (1, 1, 512), (2, 64, 449), (2, 512, 64), (1, 64, 512), (2, 65, 127), (5, 128, 256), (1, 256, 127), (2, 193, 65), (300, 20, 33)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("batch,rows,cols", WHOLE)
+def test_whole(pace, dtype, batch, rows, cols):
+    """Rows apart, off alignment and with other numbers between them; one update's NaN spoils no other."""
+    say("orthogonalize whole %s %d x %d x %d" % (dtype, batch, rows, cols))
+    gen = torch.Generator(device=DEV).manual_seed(rows + cols)
+    room = torch.randn(batch * (rows + 1) * (cols + 5) + 1, generator=gen, device=DEV).to(dtype)
+    g = room[1:].view(batch, rows + 1, cols + 5)[:, :rows, 2:cols + 2]
+    out = check(pace, g)
+    for k in range(0, batch, 2):
+        assert torch.equal(pace.pace_orthogonalize(g[k].contiguous()), out[k])
+    check(pace, g, steps=1, coefs=CUBIC)
+    check(pace, g, steps=8, coefs=CUBIC, eps=0.5)
+    if batch > 1:
+        g = g.clone()
+        g[1, rows - 1, cols - 1] = float("inf")
+        bad = pace.pace_orthogonalize(g)
+        assert bool(bad[1].isnan().any()) and torch.equal(bad[0], out[0]) and torch.equal(bad[2:], out[2:])
 
 
 @pytest.mark.parametrize("batch,rows,cols", [(160, 128, 1000), (80, 256, 300), (80, 290, 180)])

@@ -149,11 +149,17 @@ def test_product_parts():
 
 def test_gpu_tests_reach_every_small_step():
     from tests.operator_rules import CUS, rules
-    from tests.test_gpu_orthogonalize import SMALL
+    from tests.test_gpu_orthogonalize import SMALL, WHOLE
     R = rules()
     got = set()
     for b, r, c in SMALL:
-        mp = -(-min(r, c) // 64) * 64
+        mp, np = -(-min(r, c) // 64) * 64, -(-max(r, c) // 64) * 64
+        assert not R.whole(mp, np)
         got.add((mp, R.cols(mp, max(r, c), b, CUS)))
     assert got == {(64, 64), (128, 64), (192, 64), (192, 128), (256, 64), (256, 128)}
+    whole = {(-(-min(r, c) // 64) * 64, -(-max(r, c) // 64) * 64) for b, r, c in WHOLE}
+    assert all(R.whole(*k) for k in whole) and {(64, 64), (64, 512), (128, 128), (128, 256)} <= whole
+    # what a workgroup's threads and LDS hold
+    assert all(mp * np <= 2 ** 15 and 4 * mp * np + 2 * mp * mp <= 160 * 1024
+               for mp in range(64, 2049, 64) for np in range(mp, 4097, 64) if R.whole(mp, np))
     assert R.cols(128, 1000, 160, CUS) == 0 and R.cols(256, 300, 80, CUS) == 0 and R.cols(320, 320, 1, CUS) == 0
