@@ -192,13 +192,13 @@ struct TileProduct {
 #pragma unroll
                 for (int j = 0; j < kTN; ++j) acc[i][j] = Mul::mul(h.a[u][i], h.b[u][j], acc[i][j]);
     }
-    // The products of a step of operands that are in LDS already, onto acc.
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int i = 0; i < kTM; ++i)
 #pragma unroll
             for (int j = 0; j < kTN; ++j) acc[i][j] = Acc{0, 0, 0, 0};
     }
+    // The products of a step of operands that are in LDS already, onto acc.
     __device__ __forceinline__ void step(const char *now_a, const char *now_b) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
