@@ -710,10 +710,10 @@ def matmul_i8_buffers(m: int, n: int, k: int, out_dtype, device):
 def _int8_rows(t, name: str):
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2 or t.dtype != torch.int8:
         raise ValueError("%s must be an int8 device matrix" % name)
-    rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+    (rows, cols), (stride, step) = t.shape, t.stride()
+    if step != 1 and cols > 1:
         raise ValueError("%s must have contiguous rows" % name)
-    return rows, cols, (t.stride(0) if rows > 1 else max(cols, 1))
+    return rows, cols, (stride if rows > 1 else max(cols, 1))
 
 
 def pace_matmul_i8(a, a_scale, b, b_scale, out=None, out_dtype=torch.bfloat16, workspace=None, stream=None):
