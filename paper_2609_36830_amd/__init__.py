@@ -6,7 +6,8 @@ tensor dtypes/devices, allocates output tensors that were not supplied, and
 passes raw device pointers plus the current HIP stream. Every step of the
 filter runs in the library's HIP kernels; there is no CPU or PyTorch
 fallback, and importing this package on a machine without the built library
-fails loudly.
+fails loudly. With ``stream`` (a stream or its handle) a call runs there in
+place of the current stream, and what it allocates is that stream's memory.
 
     score, S, T      = pace_score(tags, offsets, completion, V, prefix, window)
     budget, r_hat    = pace_budget(occupancy, capacity, r_hat_prev=0.0)
@@ -95,6 +96,21 @@ def _stream(device: torch.device, stream=None) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _allocator(device, stream=None):
+    """empty(shape, dtype) on `device`. With `stream`, in that stream's memory: the caching allocator orders
+    the reuse of a block with the stream it was allocated on only, and a call's workspace is free again when
+    the call returns, while its kernels still run."""
+    if stream is None:
+        return lambda shape, dtype: torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_stream(device, stream), device=device)
+
+    def empty(shape, dtype):
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=dtype, device=device)
+    return empty
+
+
 def _first(t: torch.Tensor, k: int) -> torch.Tensor:
     """The first k entries of a 1-d buffer (the buffer itself when it has k)."""
     return t if t.shape[0] == k else t[:k]
@@ -116,10 +132,10 @@ def pace_workspace_bytes(which: int, n_traj: int, n_tokens: int) -> int:
     return int(out.value)
 
 
-def _workspace(which, n, nt, device, ws):
+def _workspace(which, n, nt, empty, ws):
     """The caller's workspace (the library checks its size), or a new one."""
     if ws is None:
-        ws = torch.empty(max(pace_workspace_bytes(which, n, nt), 256), dtype=torch.uint8, device=device)
+        ws = empty(max(pace_workspace_bytes(which, n, nt), 256), torch.uint8)
     return ws
 
 
@@ -139,14 +155,15 @@ def pace_score(tags, offsets, completion, current_version, prefix_score=None, wi
     if window_sorted is not None:
         _dev(window_sorted, torch.float64, "window_sorted")
         W = window_sorted.numel()
+    e = _allocator(dev, stream)
     if score_out is None:
-        score_out = torch.empty(n, dtype=torch.float64, device=dev)
+        score_out = e(n, torch.float64)
     if with_counts:
         if gen_sum_out is None:
-            gen_sum_out = torch.empty(n, dtype=torch.int64, device=dev)
+            gen_sum_out = e(n, torch.int64)
         if gen_count_out is None:
-            gen_count_out = torch.empty(n, dtype=torch.int64, device=dev)
-    ws = _workspace(WS_SCORE, n, nt, dev, workspace)
+            gen_count_out = e(n, torch.int64)
+    ws = _workspace(WS_SCORE, n, nt, e, workspace)
     _check(lib().pace_score(_ptr(tags), _ptr(offsets), n, nt, _ptr(completion), int(current_version),
                             _ptr(prefix_score), _ptr(window_sorted), W,
                             ctypes.byref(params) if params is not None else None,
@@ -172,11 +189,12 @@ def pace_select(score, budget: int, keep_out=None, reject_ids_out=None, workspac
     _dev(score, torch.float64, "score")
     n = score.numel()
     dev = score.device
+    e = _allocator(dev, stream)
     if keep_out is None:
-        keep_out = torch.empty(n, dtype=torch.uint8, device=dev)
+        keep_out = e(n, torch.uint8)
     if reject_ids_out is None:
-        reject_ids_out = torch.empty(max(int(budget), 1), dtype=torch.int32, device=dev)
-    ws = _workspace(WS_SELECT, n, 0, dev, workspace)
+        reject_ids_out = e(max(int(budget), 1), torch.int32)
+    ws = _workspace(WS_SELECT, n, 0, e, workspace)
     _check(lib().pace_select(_ptr(score), n, int(budget), _ptr(keep_out), _ptr(reject_ids_out),
                              _ptr(ws), ws.numel(), _stream(dev, stream)), "pace_select")
     return keep_out, reject_ids_out[: int(budget)]
@@ -198,15 +216,16 @@ def pace_compact(offsets, keep, cols: Sequence[torch.Tensor], cols_out=None, off
     for k, c in enumerate(cols):
         if not c.is_cuda or not c.is_contiguous() or c.numel() != n_tokens:
             raise ValueError("column %d must be a contiguous device tensor of n_tokens elements" % k)
+    e = _allocator(dev, stream)
     if cols_out is None:
-        cols_out = [torch.empty_like(c) for c in cols]
+        cols_out = [e(c.shape, c.dtype) for c in cols]
     if offsets_out is None:
-        offsets_out = torch.empty(n + 1, dtype=torch.int64, device=dev)
+        offsets_out = e(n + 1, torch.int64)
     if kept_ids_out is None:
-        kept_ids_out = torch.empty(max(n, 1), dtype=torch.int32, device=dev)
+        kept_ids_out = e(max(n, 1), torch.int32)
     if n_kept_tokens_out is None:
-        n_kept_tokens_out = torch.empty(1, dtype=torch.int64, device=dev)
-    ws = _workspace(WS_COMPACT, n, n_tokens, dev, workspace)
+        n_kept_tokens_out = e(1, torch.int64)
+    ws = _workspace(WS_COMPACT, n, n_tokens, e, workspace)
     nc, cin, eb, cout = _col_args(cols, cols_out)
     _check(lib().pace_compact(_ptr(offsets), n, int(n_tokens), _ptr(keep), nc, cin, eb, cout,
                               _ptr(offsets_out), _ptr(kept_ids_out), _ptr(n_kept_tokens_out),
@@ -226,7 +245,7 @@ def pace_validate(tags, offsets, completion, current_version, window_sorted=None
         _dev(window_sorted, torch.float64, "window_sorted")
         W = window_sorted.numel()
     if err_out is None:
-        err_out = torch.empty(1, dtype=torch.int32, device=dev)
+        err_out = _allocator(dev, stream)(1, torch.int32)
     _check(lib().pace_validate(_ptr(tags), _ptr(offsets), offsets.numel() - 1, tags.numel(),
                                _ptr(completion), int(current_version), _ptr(window_sorted), W,
                                _ptr(err_out), _stream(dev, stream)), "pace_validate")
@@ -245,14 +264,14 @@ def pace_filter_step(tags, offsets, completion, current_version, occupancy, capa
     cols = list(cols)
     _filter_step_inputs(tags, offsets, completion, prefix_score, window_sorted, cols)
     n, dev = offsets.numel() - 1, tags.device
-    e = lambda k, dt: torch.empty(k, dtype=dt, device=dev)
+    e = _allocator(dev, stream)
     score_out = e(n, torch.float64) if score_out is None else score_out
     if with_counts:
         gen_sum_out = e(n, torch.int64) if gen_sum_out is None else gen_sum_out
         gen_count_out = e(n, torch.int64) if gen_count_out is None else gen_count_out
     keep_out = e(n, torch.uint8) if keep_out is None else keep_out
     reject_ids_out = e(max(n, 1), torch.int32) if reject_ids_out is None else reject_ids_out
-    cols_out = [torch.empty_like(c) for c in cols] if cols_out is None else cols_out
+    cols_out = [e(c.shape, c.dtype) for c in cols] if cols_out is None else cols_out
     offsets_out = e(n + 1, torch.int64) if offsets_out is None else offsets_out
     kept_ids_out = e(max(n, 1), torch.int32) if kept_ids_out is None else kept_ids_out
     n_kept_tokens_out = e(1, torch.int64) if n_kept_tokens_out is None else n_kept_tokens_out
@@ -296,7 +315,7 @@ def _filter_step_call(tags, offsets, completion, current_version, occupancy, cap
     if noalloc:
         _check(lib().pace_filter_step_noalloc(*args, _stream(dev, stream)), "pace_filter_step_noalloc")
     else:
-        ws = _workspace(WS_FILTER_STEP, n, nt, dev, workspace)
+        ws = workspace if workspace is not None else _workspace(WS_FILTER_STEP, n, nt, _allocator(dev, stream), None)
         _check(lib().pace_filter_step(*args, ws.data_ptr(), ws.numel(), _stream(dev, stream)), "pace_filter_step")
     return b.value, rh.value
 
@@ -321,7 +340,7 @@ def pace_group_score(score, group_offsets, group_score_out=None, stream=None):
     _dev(group_offsets, torch.int64, "group_offsets")
     ng = group_offsets.numel() - 1
     if group_score_out is None:
-        group_score_out = torch.empty(ng, dtype=torch.float64, device=score.device)
+        group_score_out = _allocator(score.device, stream)(ng, torch.float64)
     _check(lib().pace_group_score(_ptr(score), score.numel(), _ptr(group_offsets), ng, _ptr(group_score_out),
                                   _stream(score.device, stream)), "pace_group_score")
     return group_score_out
@@ -333,7 +352,7 @@ def pace_group_expand(group_offsets, group_keep, n_traj: int, keep_out=None, str
     _dev(group_keep, torch.uint8, "group_keep")
     ng = group_offsets.numel() - 1
     if keep_out is None:
-        keep_out = torch.empty(int(n_traj), dtype=torch.uint8, device=group_keep.device)
+        keep_out = _allocator(group_keep.device, stream)(int(n_traj), torch.uint8)
     _check(lib().pace_group_expand(_ptr(group_offsets), ng, int(n_traj), _ptr(group_keep), _ptr(keep_out),
                                    _stream(group_keep.device, stream)), "pace_group_expand")
     return keep_out
@@ -344,21 +363,21 @@ def pace_validate_groups(group_offsets, n_traj: int, err_out=None, stream=None):
     _dev(group_offsets, torch.int64, "group_offsets")
     dev = group_offsets.device
     if err_out is None:
-        err_out = torch.empty(1, dtype=torch.int32, device=dev)
+        err_out = _allocator(dev, stream)(1, torch.int32)
     _check(lib().pace_validate_groups(_ptr(group_offsets), group_offsets.numel() - 1, int(n_traj),
                                       _ptr(err_out), _stream(dev, stream)), "pace_validate_groups")
     return err_out
 
 
-def group_step_buffers(n: int, n_groups: int, cols, device):
+def group_step_buffers(n: int, n_groups: int, cols, device, stream=None):
     """Output buffers for repeated pace_group_filter_step calls on pools of at
     most n trajectories, n_groups groups and the columns' sizes (pass as
     ``out``): no allocation inside the calls."""
-    e = lambda k, dt: torch.empty(k, dtype=dt, device=device)
+    e = _allocator(device, stream)
     return dict(score=e(max(n, 1), torch.float64), gen_sum=e(max(n, 1), torch.int64),
                 gen_count=e(max(n, 1), torch.int64), group_score=e(max(n_groups, 1), torch.float64),
                 group_keep=e(max(n_groups, 1), torch.uint8), reject_group_ids=e(max(n_groups, 1), torch.int32),
-                keep=e(max(n, 1), torch.uint8), cols_out=[torch.empty_like(c) for c in cols],
+                keep=e(max(n, 1), torch.uint8), cols_out=[e(c.shape, c.dtype) for c in cols],
                 offsets_out=e(n + 1, torch.int64), kept_ids=e(max(n, 1), torch.int32),
                 n_kept_tokens=e(1, torch.int64))
 
@@ -388,7 +407,7 @@ def pace_group_filter_step(tags, offsets, completion, current_version, group_off
     for k, c in enumerate(cols):
         if not c.is_cuda or not c.is_contiguous() or c.numel() != nt:
             raise ValueError("column %d must be a contiguous device tensor of n_tokens elements" % k)
-    o = out if out is not None else group_step_buffers(n, ng, cols, dev)
+    o = out if out is not None else group_step_buffers(n, ng, cols, dev, stream)
     if (o["score"].numel() < max(n, 1) or o["group_score"].numel() < max(ng, 1)
             or o["offsets_out"].numel() < n + 1 or len(o["cols_out"]) != len(cols)
             or any(a.numel() < c.numel() or a.dtype != c.dtype or not a.is_contiguous()
@@ -401,7 +420,7 @@ def pace_group_filter_step(tags, offsets, completion, current_version, group_off
     cols_out = [_first(a, nt) for a in o["cols_out"]]
     offsets_out, kept_ids_out = _first(o["offsets_out"], n + 1), o["kept_ids"]
     n_kept_tokens_out = o["n_kept_tokens"]
-    ws = _workspace(WS_FILTER_STEP, max(n, ng), nt, dev, workspace)
+    ws = _workspace(WS_FILTER_STEP, max(n, ng), nt, _allocator(dev, stream), workspace)
     nc, cin, eb, cout = _col_args(cols, cols_out)
     rh = ctypes.c_double(float(r_hat_prev))
     b = ctypes.c_int64(0)
@@ -437,7 +456,7 @@ def pace_stream_admit(score, r_hat: float, window: StreamWindow, batch_size: int
     _dev(score, torch.float64, "score")
     n = score.numel()
     dev = score.device
-    e = lambda k, dt: torch.empty(k, dtype=dt, device=dev)
+    e = _allocator(dev, stream)
     status_out = e(max(n, 1), torch.uint8) if status_out is None else status_out
     keep_out = e(max(n, 1), torch.uint8) if keep_out is None else keep_out
     reject_ids_out = e(max(n, 1), torch.int32) if reject_ids_out is None else reject_ids_out
@@ -450,9 +469,9 @@ def pace_stream_admit(score, r_hat: float, window: StreamWindow, batch_size: int
     return _first(status_out, n), _first(keep_out, n), reject_ids_out, kappa_out, counts_out
 
 
-def stream_step_buffers(n: int, n_tokens: int, col_dtypes: Sequence[torch.dtype], device):
+def stream_step_buffers(n: int, n_tokens: int, col_dtypes: Sequence[torch.dtype], device, stream=None):
     """Preallocated outputs for repeated pace_stream_step calls."""
-    e = lambda k, dt: torch.empty(k, dtype=dt, device=device)
+    e = _allocator(device, stream)
     return dict(score=e(max(n, 1), torch.float64), gen_sum=e(max(n, 1), torch.int64),
                 gen_count=e(max(n, 1), torch.int64), status=e(max(n, 1), torch.uint8),
                 keep=e(max(n, 1), torch.uint8), reject_ids=e(max(n, 1), torch.int32),
@@ -480,7 +499,7 @@ def pace_stream_step(tags, offsets, completion, current_version, occupancy, capa
         _dev(window_sorted, torch.float64, "window_sorted")
         W = window_sorted.numel()
     cols = list(cols)
-    b = buffers if buffers is not None else stream_step_buffers(n, nt, [c.dtype for c in cols], dev)
+    b = buffers if buffers is not None else stream_step_buffers(n, nt, [c.dtype for c in cols], dev, stream)
     nc, cin, eb, cout = _col_args(cols, b["cols_out"])
     rh = ctypes.c_double(float(r_hat_prev))
     ws = b["workspace"]
@@ -504,7 +523,7 @@ def pace_prefix_score(lp_new, lp_behavior, prefix_offsets, tags=None, cap: int =
         _dev(tags, torch.int32, "tags")
     n = prefix_offsets.numel() - 1
     if s_pre_out is None:
-        s_pre_out = torch.empty(max(n, 1), dtype=torch.float64, device=lp_new.device)
+        s_pre_out = _allocator(lp_new.device, stream)(max(n, 1), torch.float64)
     _check(lib().pace_prefix_score(_ptr(lp_new), _ptr(lp_behavior), _ptr(tags), _ptr(prefix_offsets), n,
                                    lp_new.numel(), int(cap), int(min_tokens), _ptr(s_pre_out),
                                    _stream(lp_new.device, stream)), "pace_prefix_score")
@@ -519,9 +538,10 @@ def pace_stale_k(gen_sum, gen_count, completion, current_version, k: int, keep_o
     _dev(completion, torch.int32, "completion")
     n = completion.numel()
     dev = completion.device
-    keep_out = torch.empty(max(n, 1), dtype=torch.uint8, device=dev) if keep_out is None else keep_out
+    e = _allocator(dev, stream)
+    keep_out = e(max(n, 1), torch.uint8) if keep_out is None else keep_out
     if with_lag and lag_out is None:
-        lag_out = torch.empty(max(n, 1), dtype=torch.float64, device=dev)
+        lag_out = e(max(n, 1), torch.float64)
     _check(lib().pace_stale_k(_ptr(gen_sum), _ptr(gen_count), _ptr(completion), int(current_version), n, int(k),
                               _ptr(keep_out), _ptr(lag_out), _stream(dev, stream)), "pace_stale_k")
     return _first(keep_out, n), (_first(lag_out, n) if lag_out is not None else None)
@@ -536,8 +556,9 @@ def pace_diagnostics(score, gen_sum, gen_count, completion, current_version, kee
     n = score.numel()
     nbins = edges.shape[1] - 1
     dev = score.device
-    hist_out = torch.empty((3, 2, nbins + 2), dtype=torch.int64, device=dev) if hist_out is None else hist_out
-    totals_out = torch.empty((2, 4), dtype=torch.int64, device=dev) if totals_out is None else totals_out
+    e = _allocator(dev, stream)
+    hist_out = e((3, 2, nbins + 2), torch.int64) if hist_out is None else hist_out
+    totals_out = e((2, 4), torch.int64) if totals_out is None else totals_out
     _check(lib().pace_diagnostics(_ptr(score), _ptr(gen_sum), _ptr(gen_count), _ptr(completion),
                                   int(current_version), _ptr(keep), n, _ptr(edges), int(nbins), _ptr(hist_out),
                                   _ptr(totals_out), _stream(dev, stream)), "pace_diagnostics")
@@ -570,10 +591,10 @@ def _vector(t, dtype, n: int, device, name: str):
     return t
 
 
-def _sized(t, dtype, shape, device, name: str):
+def _sized(t, dtype, shape, device, name: str, stream=None):
     """The caller's output (checked), or a new one."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return _allocator(device, stream)(shape, dtype)
     if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of shape %s on %s" % (name, dtype, tuple(shape), device))
     return t
@@ -593,10 +614,10 @@ def pace_token_logprob_workspace_bytes(n_rows: int, vocab: int, top_k: int = 0) 
     return int(out.value)
 
 
-def token_logprob_buffers(n_rows: int, vocab: int, top_k: int, device):
+def token_logprob_buffers(n_rows: int, vocab: int, top_k: int, device, stream=None):
     """Outputs and workspace for repeated pace_token_logprob calls on n_rows rows
     (pass as ``buffers``)."""
-    e = lambda shape, dt: torch.empty(shape, dtype=dt, device=device)
+    e = _allocator(device, stream)
     return dict(logp=e(n_rows, torch.float32), entropy=e(n_rows, torch.float32), stats=e((n_rows, 2), torch.float32),
                 top_ids=e((n_rows, top_k), torch.int32), top_logp=e((n_rows, top_k), torch.float32),
                 workspace=e(pace_token_logprob_workspace_bytes(n_rows, vocab, top_k), torch.uint8))
@@ -610,7 +631,7 @@ def pace_token_logprob(logits, token_ids, temperature: float = 1.0, top_k: int =
     _vector(token_ids, torch.int32, n, dev, "token_ids")
     if not 0 <= int(top_k) <= TOP_MAX:
         raise ValueError("top_k must be in [0, %d]" % TOP_MAX)
-    b = token_logprob_buffers(n, vocab, int(top_k), dev) if buffers is None else buffers
+    b = token_logprob_buffers(n, vocab, int(top_k), dev, stream) if buffers is None else buffers
     logp, entropy = _sized(b["logp"], torch.float32, (n,), dev, "logp"), _sized(b["entropy"], torch.float32, (n,), dev, "entropy")
     stats = _sized(b["stats"], torch.float32, (n, 2), dev, "stats")
     ids, top = _sized(b["top_ids"], torch.int32, (n, top_k), dev, "top_ids"), _sized(b["top_logp"], torch.float32, (n, top_k), dev, "top_logp")
@@ -635,7 +656,7 @@ def pace_token_logprob_backward(logits, token_ids, stats, grad_logp, entropy=Non
     if grad_entropy is not None:
         _vector(grad_entropy, torch.float32, n, dev, "grad_entropy")
     if grad_logits_out is None:
-        grad_logits_out = torch.empty((n, vocab), dtype=logits.dtype, device=dev)
+        grad_logits_out = _allocator(dev, stream)((n, vocab), logits.dtype)
     gdt, gn, gvocab, gstride = _matrix(grad_logits_out, "grad_logits_out")
     if (gdt, gn, gvocab) != (dt, n, vocab) or grad_logits_out.device != dev:
         raise ValueError("grad_logits_out must have the logits' type and shape")
@@ -653,9 +674,9 @@ def pace_policy_loss_workspace_bytes(n_traj: int, n_tokens: int) -> int:
     return int(out.value)
 
 
-def policy_loss_buffers(n_traj: int, n_tokens: int, device):
+def policy_loss_buffers(n_traj: int, n_tokens: int, device, stream=None):
     """Outputs and workspace for repeated pace_policy_loss calls (pass as ``buffers``)."""
-    e = lambda k, dt: torch.empty(k, dtype=dt, device=device)
+    e = _allocator(device, stream)
     return dict(grad=e(n_tokens, torch.float32), loss=e(n_traj, torch.float32), kl=e(n_traj, torch.float32),
                 clipped=e(n_traj, torch.int32), workspace=e(pace_policy_loss_workspace_bytes(n_traj, n_tokens), torch.uint8))
 
@@ -673,7 +694,7 @@ def pace_policy_loss(lp_new, lp_behavior, offsets, advantage, tags=None, weight=
         _vector(tags, torch.int32, nt, dev, "tags")
     if weight is not None:
         _vector(weight, torch.float32, n, dev, "weight")
-    b = policy_loss_buffers(n, nt, dev) if buffers is None else buffers
+    b = policy_loss_buffers(n, nt, dev, stream) if buffers is None else buffers
     grad, loss = _sized(b["grad"], torch.float32, (nt,), dev, "grad"), _sized(b["loss"], torch.float32, (n,), dev, "loss")
     kl, clipped = _sized(b["kl"], torch.float32, (n,), dev, "kl"), _sized(b["clipped"], torch.int32, (n,), dev, "clipped")
     ws, ws_bytes = _scratch(b["workspace"], dev)
@@ -687,8 +708,8 @@ def pace_policy_loss(lp_new, lp_behavior, offsets, advantage, tags=None, weight=
 def pace_quantize_rows(x, q_out=None, scale_out=None, stream=None):
     """Rows in 8 bits: scale = max |x| / 127, q = rint(x (127 (1 / max |x|))). Returns (q int8[n, k], scale f32[n])."""
     dt, n, k, stride = _matrix(x, "x")
-    q_out = _sized(q_out, torch.int8, (n, k), x.device, "q_out")
-    scale_out = _sized(scale_out, torch.float32, (n,), x.device, "scale_out")
+    q_out = _sized(q_out, torch.int8, (n, k), x.device, "q_out", stream)
+    scale_out = _sized(scale_out, torch.float32, (n,), x.device, "scale_out", stream)
     _check(lib().pace_quantize_rows(x.data_ptr(), dt, n, k, stride, q_out.data_ptr(), scale_out.data_ptr(),
                                     _stream(x.device, stream)), "pace_quantize_rows")
     return q_out, scale_out
@@ -700,9 +721,9 @@ def pace_matmul_i8_workspace_bytes(m: int, n: int, k: int) -> int:
     return int(out.value)
 
 
-def matmul_i8_buffers(m: int, n: int, k: int, out_dtype, device):
+def matmul_i8_buffers(m: int, n: int, k: int, out_dtype, device, stream=None):
     """Quantised rows, output and workspace for repeated products of m rows with an [n, k] weight."""
-    e = lambda shape, dt: torch.empty(shape, dtype=dt, device=device)
+    e = _allocator(device, stream)
     return dict(q=e((m, k), torch.int8), scale=e(m, torch.float32), out=e((m, n), out_dtype),
                 workspace=e(pace_matmul_i8_workspace_bytes(m, n, k), torch.uint8))
 
@@ -727,12 +748,12 @@ def pace_matmul_i8(a, a_scale, b, b_scale, out=None, out_dtype=torch.bfloat16, w
     _vector(a_scale, torch.float32, m, dev, "a_scale")
     _vector(b_scale, torch.float32, n, dev, "b_scale")
     if out is None:
-        out = torch.empty((m, n), dtype=out_dtype, device=dev)
+        out = _allocator(dev, stream)((m, n), out_dtype)
     dt, om, on, ldo = _matrix(out, "out")
     if (om, on) != (m, n) or out.device != dev:
         raise ValueError("out must have shape (%d, %d) on %s" % (m, n, dev))
     if workspace is None:
-        workspace = torch.empty(pace_matmul_i8_workspace_bytes(m, n, k), dtype=torch.uint8, device=dev)
+        workspace = _allocator(dev, stream)(pace_matmul_i8_workspace_bytes(m, n, k), torch.uint8)
     ws, ws_bytes = _scratch(workspace, dev)
     _check(lib().pace_matmul_i8(a.data_ptr(), lda, a_scale.data_ptr(), b.data_ptr(), ldb, b_scale.data_ptr(), m, n, k,
                                 out.data_ptr(), dt, ldo, ws, ws_bytes, _stream(dev, stream)), "pace_matmul_i8")
@@ -746,10 +767,11 @@ def pace_orthogonalize_workspace_bytes(batch: int, rows: int, cols: int) -> int:
     return int(out.value)
 
 
-def orthogonalize_buffers(batch: int, rows: int, cols: int, device):
+def orthogonalize_buffers(batch: int, rows: int, cols: int, device, stream=None):
     """Output and workspace for repeated pace_orthogonalize calls on updates of one shape."""
-    return dict(out=torch.empty((batch, rows, cols), dtype=torch.bfloat16, device=device),
-                workspace=torch.empty(pace_orthogonalize_workspace_bytes(batch, rows, cols), dtype=torch.uint8, device=device))
+    e = _allocator(device, stream)
+    return dict(out=e((batch, rows, cols), torch.bfloat16),
+                workspace=e(pace_orthogonalize_workspace_bytes(batch, rows, cols), torch.uint8))
 
 
 def pace_orthogonalize(update, steps: int = 5, coefs=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, out=None, workspace=None,
@@ -764,9 +786,9 @@ def pace_orthogonalize(update, steps: int = 5, coefs=(3.4445, -4.7750, 2.0315), 
     if len(coefs) != 3:
         raise ValueError("coefs must be three numbers")
     dev = update.device
-    out = _sized(out, torch.bfloat16, tuple(update.shape), dev, "out")
+    out = _sized(out, torch.bfloat16, tuple(update.shape), dev, "out", stream)
     if workspace is None:
-        workspace = torch.empty(pace_orthogonalize_workspace_bytes(batch, rows, cols), dtype=torch.uint8, device=dev)
+        workspace = _allocator(dev, stream)(pace_orthogonalize_workspace_bytes(batch, rows, cols), torch.uint8)
     ws, ws_bytes = _scratch(workspace, dev)
     stride = u.stride(1) if rows > 1 else max(cols, 1)
     _check(lib().pace_orthogonalize(update.data_ptr(), DTYPES[update.dtype], batch, rows, cols, stride,
