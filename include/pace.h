@@ -562,7 +562,8 @@ int pace_orthogonalize(const void *update, int dtype, int64_t batch, int64_t row
  *   pace_group_score, pace_group_expand, pace_stale_k or pace_diagnostics;
  *   the kernel that reads the logits, the tokens or the operands in
  *   pace_token_logprob, its backward pass, pace_policy_loss, pace_quantize_rows
- *   and pace_matmul_i8; the first product C X of pace_orthogonalize, or its only
+ *   and pace_matmul_i8 (its first launch, where rows or channels are more than
+ *   one launch holds); the first product C X of pace_orthogonalize, or its only
  *   kernel;
  *   the window-cutoff kernel of the streaming rule, or in
  *   pace_group_filter_step the kernel that expands the group flags),

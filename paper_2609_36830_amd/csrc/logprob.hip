@@ -478,8 +478,6 @@ __global__ __launch_bounds__(kTop ? kLpThreads : kWave) void logprob_join_kernel
     }
 }
 
-constexpr int kLpbThreads = 256;
-
 template <typename T, bool kEntropy>
 __global__ __launch_bounds__(kLpbThreads) void logprob_backward_kernel(
     const T *logits, int64_t vocab, int64_t stride, const int32_t *__restrict__ ids, float c, double inv_t,
@@ -551,9 +549,15 @@ hipError_t launch_token_logprob(const void *logits, int dtype, int64_t rows, int
     const float c = (float)(1.44269504088896340736 / temperature), inv_t = (float)(1.0 / temperature);
     return with_elem(dtype, [&](auto tag) {
         using T = decltype(tag);
+        // Rows in parts are few, and go in one launch.
         auto first = [&](auto kernel, int64_t groups) {
-            return launch(kPhaseAux, kernel, dim3((unsigned)((rows * parts + groups - 1) / groups)), dim3(kLpThreads), stream, (const T *)logits,
-                          vocab, rows, stride, ids, c, inv_t, top_k, parts, out, sum, most);
+            return in_launches((rows * parts + groups - 1) / groups, kLpThreads, [&](int64_t b, int64_t blocks) {
+                const int64_t r = b * groups / parts;
+                const LogprobOut o{out.logp + r, out.entropy ? out.entropy + r : nullptr, out.stats ? out.stats + 2 * r : nullptr,
+                                   out.top_ids ? out.top_ids + r * top_k : nullptr, out.top_logp ? out.top_logp + r * top_k : nullptr};
+                return launch(kPhaseAux, kernel, dim3((unsigned)blocks), dim3(kLpThreads), stream, (const T *)logits + r * stride, vocab,
+                              rows - r, stride, ids + r, c, inv_t, top_k, parts, o, sum, most);
+            });
         };
         auto join = [&](auto kernel, int threads) {
             return launch(-1, kernel, dim3((unsigned)rows), dim3(threads), stream, (const T *)logits, vocab, stride, ids, c, inv_t, top_k, parts,
@@ -578,13 +582,13 @@ hipError_t launch_token_logprob_backward(const void *logits, int dtype, int64_t 
     const double inv_t = 1.0 / temperature;
     return with_elem(dtype, [&](auto tag) {
         using T = decltype(tag);
-        const dim3 grid((unsigned)(rows * parts));
-        return g_entropy ? launch(kPhaseAux, logprob_backward_kernel<T, true>, grid, dim3(kLpbThreads), stream,
-                                  (const T *)logits, vocab, stride, ids, c, inv_t, stats, entropy, g_logp, g_entropy,
-                                  (T *)grad, grad_stride, parts)
-                         : launch(kPhaseAux, logprob_backward_kernel<T, false>, grid, dim3(kLpbThreads), stream,
-                                  (const T *)logits, vocab, stride, ids, c, inv_t, stats, entropy, g_logp, g_entropy,
-                                  (T *)grad, grad_stride, parts);
+        const auto kernel = g_entropy ? logprob_backward_kernel<T, true> : logprob_backward_kernel<T, false>;
+        return in_launches(rows * parts, kLpbThreads, [&](int64_t b, int64_t blocks) {      // several only of whole rows
+            const int64_t r = b / parts;
+            return launch(kPhaseAux, kernel, dim3((unsigned)blocks), dim3(kLpbThreads), stream, (const T *)logits + r * stride, vocab,
+                          stride, ids + r, c, inv_t, stats + 2 * r, entropy ? entropy + r : nullptr, g_logp + r,
+                          g_entropy ? g_entropy + r : nullptr, (T *)grad + r * grad_stride, grad_stride, parts);
+        });
     });
 }
 

@@ -255,19 +255,33 @@ hipError_t launch_quantize_rows(const void *x, int dtype, int64_t rows, int64_t 
     if (rows == 0) return hipSuccess;
     return with_elem(dtype, [&](auto tag) {
         using T = decltype(tag);
-        return launch(kPhaseAux, quantize_rows_kernel<T>, dim3((unsigned)rows), dim3(kQuantThreads), stream, (const T *)x, cols,
-                      stride, q, scale);
+        return in_launches(rows, kQuantThreads, [&](int64_t r, int64_t count) {
+            return launch(kPhaseAux, quantize_rows_kernel<T>, dim3((unsigned)count), dim3(kQuantThreads), stream, (const T *)x + r * stride, cols,
+                          stride, q + r * cols, scale + r);
+        });
     });
 }
 
 namespace {
 
+// `count` rows of an operand from `first` on, or what is there of them.
+Rows rows_from(const Rows &m, int64_t first, int64_t count) {
+    return Rows{m.p + first * m.stride, m.stride, m.rows - first < count ? m.rows - first : count, m.bytes};
+}
+
 template <typename O, typename P>
 hipError_t launch_tiles(const Rows &b, const Rows &a, const float *sb, const float *sa, void *out, int64_t ldo,
                         hipStream_t stream) {
-    const int64_t tiles = ((a.rows + P::kCols - 1) / P::kCols) * ((b.rows + P::kRows - 1) / P::kRows);
-    return launch_lds(kPhaseAux, matmul_i8_kernel<O, kWhole, P>, dim3((unsigned)tiles), dim3(P::kThreads), I8Tile<O, P>::kLds, stream, b, a, sb, sa,
-                      (O *)out, ldo, nullptr, 1);
+    // Runs of whole columns of tiles, or, of one beyond a launch, of its rows.
+    const int64_t tm = (a.rows + P::kCols - 1) / P::kCols, tn = (b.rows + P::kRows - 1) / P::kRows;
+    return in_launches(tm, P::kThreads, [&](int64_t i, int64_t ni) {
+        const Rows ai = rows_from(a, i * P::kCols, ni * P::kCols);
+        return in_launches(tn, P::kThreads * ni, [&](int64_t j, int64_t nj) {
+            const Rows bj = rows_from(b, j * P::kRows, nj * P::kRows);
+            return launch_lds(kPhaseAux, matmul_i8_kernel<O, kWhole, P>, dim3((unsigned)(ni * nj)), dim3(P::kThreads), I8Tile<O, P>::kLds, stream,
+                              bj, ai, sb + j * P::kRows, sa + i * P::kCols, (O *)out + i * P::kCols * ldo + j * P::kRows, ldo, nullptr, 1);
+        });
+    });
 }
 // Parts of the steps, then their sums.
 template <typename O, typename P>
@@ -286,7 +300,11 @@ hipError_t launch_few(const Rows &b, const Rows &a, const float *sb, const float
     // as many channels a workgroup as leave a workgroup for every CU
     const int64_t cus = resident_waves() / 16;
     auto go = [&](auto kernel, int64_t channels) {
-        return launch(kPhaseAux, kernel, dim3((unsigned)((b.rows + channels - 1) / channels)), dim3(kFewWaves * kWave), stream, b, a, sb, sa, (O *)out, ldo);
+        return in_launches((b.rows + channels - 1) / channels, kFewWaves * kWave, [&](int64_t g, int64_t groups) {
+            const int64_t n = g * channels;
+            return launch(kPhaseAux, kernel, dim3((unsigned)groups), dim3(kFewWaves * kWave), stream, rows_from(b, n, groups * channels), a, sb + n,
+                          sa, (O *)out + n, ldo);
+        });
     };
     if (b.rows >= 32 * cus) return go(matmul_i8_few_kernel<O, kTok, 4>, 32);
     if (b.rows >= 16 * cus) return go(matmul_i8_few_kernel<O, kTok, 2>, 16);

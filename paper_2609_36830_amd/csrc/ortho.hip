@@ -641,17 +641,9 @@ hipError_t ortho_steps(const OrthoShape &s, char *ws, int64_t batch, int steps, 
     return e;
 }
 
-}  // namespace
-
-size_t ortho_ws_bytes(int64_t batch, int64_t rows, int64_t cols) {
-    const OrthoShape s = ortho_shape(rows, cols);
-    return (size_t)(batch * s.bytes) + ortho_split_bytes(s, batch) + 256;
-}
-
-hipError_t launch_orthogonalize(const void *g, int dtype, int64_t batch, int64_t rows, int64_t cols, int64_t stride,
-                                int64_t batch_stride, int steps, const double *coefs, double eps, void *out, void *ws,
-                                hipStream_t stream) {
-    if (batch == 0) return hipSuccess;
+// As many updates as one launch of each product takes.
+hipError_t orthogonalize_some(const void *g, int dtype, int64_t batch, int64_t rows, int64_t cols, int64_t stride, int64_t batch_stride,
+                              int steps, const double *coefs, double eps, void *out, void *ws, hipStream_t stream) {
     OrthoShape s = ortho_shape(rows, cols);
     if (ortho_split_bytes(s, batch)) s.split = batch * s.bytes;
     if (steps > 0 && ortho_whole(s.mp, s.np))
@@ -681,6 +673,25 @@ hipError_t launch_orthogonalize(const void *g, int dtype, int64_t batch, int64_t
         return launch(-1, ortho_copy_kernel, dim3((unsigned)(rows < 1024 ? rows : 1024), (unsigned)batch), dim3(256), stream, s, w, (bf16_t *)out);
     const float c[3] = {(float)coefs[0], (float)coefs[1], (float)coefs[2]};
     return ortho_steps(s, w, batch, steps, c, (bf16_t *)out, stream);
+}
+
+}  // namespace
+
+size_t ortho_ws_bytes(int64_t batch, int64_t rows, int64_t cols) {
+    const OrthoShape s = ortho_shape(rows, cols);
+    return (size_t)(batch * s.bytes) + ortho_split_bytes(s, batch) + 256;
+}
+
+hipError_t launch_orthogonalize(const void *g, int dtype, int64_t batch, int64_t rows, int64_t cols, int64_t stride,
+                                int64_t batch_stride, int steps, const double *coefs, double eps, void *out, void *ws,
+                                hipStream_t stream) {
+    const int64_t most = ortho_batch_most(rows, cols);
+    hipError_t e = hipSuccess;
+    // Runs of the batch one after another, in the same workspace.
+    for (int64_t k = 0; k < batch && e == hipSuccess; k += most)
+        e = orthogonalize_some((const char *)g + k * batch_stride * elem_bytes_of(dtype), dtype, batch - k < most ? batch - k : most, rows, cols,
+                               stride, batch_stride, steps, coefs, eps, (bf16_t *)out + k * rows * cols, ws, stream);
+    return e;
 }
 
 }  // namespace pace

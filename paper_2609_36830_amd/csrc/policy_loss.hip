@@ -282,8 +282,11 @@ hipError_t launch_policy_loss(const float *lp_new, const float *lp_beh, const in
                           adv, weight, scale, bounds, span, grad, loss, kl, clipped, slots);
     }
     if (e == hipSuccess && n > 0)
-        e = launch(-1, policy_loss_join_kernel, dim3((unsigned)((n + kLossWaves - 1) / kLossWaves)),
-                   dim3(kLossWaves * kWave), stream, offsets, n, n_tokens, span, (const LossSum *)slots, loss, kl, clipped);
+        e = in_launches((n + kLossWaves - 1) / kLossWaves, kLossWaves * kWave, [&](int64_t b, int64_t blocks) {
+            const int64_t i = b * kLossWaves;
+            return launch(-1, policy_loss_join_kernel, dim3((unsigned)blocks), dim3(kLossWaves * kWave), stream, offsets + i, n - i, n_tokens,
+                          span, (const LossSum *)slots, loss + i, kl ? kl + i : nullptr, clipped ? clipped + i : nullptr);
+        });
     return e;
 }
 

@@ -87,6 +87,22 @@ inline bool small_step_ok(int64_t n, int64_t n_tokens, int n_cols, int64_t budge
     return n <= kSmallMaxN && expected_kept(n, n_tokens, n - budget) <= most;
 }
 
+// ---- launches of the operators' kernels -----------------------------------------------
+// A dimension of a grid holds fewer than 2^32 threads.
+constexpr int64_t kGridThreads = ((int64_t)1 << 32) - 1;
+// n workgroups in as many launches as that takes: f(first, count) returns 0, or an
+// error that ends it.
+template <typename F>
+inline auto in_launches(int64_t n, int64_t threads, F f) {
+    const int64_t most = kGridThreads / threads;
+    for (int64_t first = 0;;) {
+        const int64_t count = n - first < most ? n - first : most;
+        const auto e = f(first, count);
+        first += count;
+        if ((int)e != 0 || first >= n) return e;
+    }
+}
+
 // ---- tiles of matrix products (mfma_tile.hpp) --------------------------------------
 // The side of a product's square tiles, by the time that each would take, in
 // microseconds: a launch, and for every round of workgroups a beginning and an
@@ -153,6 +169,13 @@ inline int ortho_step_cols(int64_t mp, int64_t n, int64_t batch, int64_t cus) {
 // 256 of 64 x 512 38 (109), 2000 of 128 x 256 375 (1159).
 inline bool ortho_whole(int64_t mp, int64_t np) { return (mp == 64 && np <= 512) || (mp == 128 && np <= 256); }
 
+// Updates of a batch that one launch of a product's 64 x 64 tiles takes (512 threads
+// each): all but of the longest and lowest, of which 256 of 1 x 2^21 are too many.
+inline int64_t ortho_batch_most(int64_t m, int64_t n) {
+    const int64_t most = kGridThreads / 512 / (((m + 63) / 64) * ((n + 63) / 64));
+    return most < 1 ? 1 : most;
+}
+
 // ---- policy loss (policy_loss.hip) ------------------------------------------------
 // Tokens a wave takes: 256 are one load a lane; at least that, at most
 // what leaves 8192 waves, which the chip holds at once.
@@ -185,11 +208,12 @@ inline LogprobPlan logprob_plan(int64_t rows, int64_t vocab, int top_k) {
     if (top_k <= 32 && vocab / w <= kLogprobWave) return {1, w};
     return {8, parts(kLogprobGroups, kLogprobGroupMin)};
 }
-// The backward pass has nothing to join: parts of 16,384 logits as far as the
-// grid can number them.
+// The backward pass has nothing to join: parts of 16,384 logits, as far as one
+// launch of workgroups of kLpbThreads holds them.
+constexpr int kLpbThreads = 256;
 inline int64_t logprob_backward_parts(int64_t rows, int64_t vocab) {
-    const int64_t parts = (vocab + 16383) / 16384, most = rows > 0 ? INT32_MAX / rows : 1;
-    return parts < most ? parts : most;
+    const int64_t parts = (vocab + 16383) / 16384, most = rows > 0 ? kGridThreads / kLpbThreads / rows : 1;
+    return most < 1 ? 1 : (parts < most ? parts : most);
 }
 
 }  // namespace pace
