@@ -15,8 +15,8 @@
 // trajectory inside a span is written there; one that crosses a span's end
 // leaves its parts in the spans' head and tail slots, which a second kernel adds
 // in span order, one wave a trajectory. Sums are binary64, in a fixed order.
-// 16.8M tokens with tags take 64.5 us (4.2 TB/s, 50 of them the first kernel's
-// where nothing else holds the caches; a device copy 4.8 TB/s), 2.5M without 14.3:
+// 16.8M tokens with tags take 64.8 us (4.2 TB/s, 50 of them the first kernel's
+// where nothing else holds the caches; a device copy 4.8 TB/s), 2.5M without 14.6:
 // there two launches and one round's dependent chain (bytes, exponentials, sums,
 // slots) are 8 us.
 #include "elem.hpp"
@@ -190,19 +190,15 @@ __global__ __launch_bounds__(kLossWaves * kWave) void policy_loss_kernel(
             const int64_t to = end < stop ? end : stop;
             if (i < n) {
                 const int from = (int)(pos - base) - lane * kLossPer, until = (int)(to - base) - lane * kLossPer;
-                // a lane's four terms in binary32, of one sign, then in binary64
-                float l[kLossPer], z[kLossPer];
 #pragma unroll
                 for (int e = 0; e < kLossPer; ++e) {
                     const bool in = live[e] && e >= from && e < until;
                     const TokenLoss t = token_loss(d[e], r[e], k, bounds);
                     g[e] = in ? t.grad : g[e];
-                    l[e] = in ? t.loss : 0.0f;
-                    z[e] = in ? y[e] : 0.0f;
+                    sum.loss += (double)(in ? t.loss : 0.0f);
+                    sum.kl += (double)(in ? y[e] : 0.0f);
                     sum.clipped += in && t.cut ? 1 : 0;
                 }
-                sum.loss += (double)((l[0] + l[1]) + (l[2] + l[3]));
-                sum.kl += (double)((z[0] + z[1]) + (z[2] + z[3]));
             }
             pos = to;
             if (i < n && (end <= pos || pos == p1)) {      // ends here, or the span does
