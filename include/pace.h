@@ -469,7 +469,7 @@ int pace_token_logprob_backward(const void *logits, int dtype, int64_t n_rows, i
  *   k < 0: loss = -k min(max(r, 1 - clip_low), dual_clip)
  *   gradient with respect to lp_new: -k r, or 0 where a bound holds, that is
  *   where d is beyond the bound's logarithm rounded to binary32
- * (k = 0: both are 0). With scale = 1 / (tokens of the batch) and no weights
+ * (k = 0: both are 0; an r below 2^-126 counts as 0). With scale = 1 / (tokens of the batch) and no weights
  * the total loss is the mean over tokens; weights 1 / T_i give means over
  * trajectories.
  * lp_new, lp_behavior f32 [n_tokens]; tags int32 [n_tokens] or NULL (every

@@ -52,13 +52,14 @@ __device__ __forceinline__ LossSum wave_total(const LossSum &v) {
     return {wave_total_f64(v.loss), wave_total_f64(v.kl), wave_sum_i64(v.clipped)};
 }
 
-// e^d within four units of 2^-24, by 2^(d log2 e) with what the product leaves:
-// a third of the library function's instructions, which bound the small batches.
+// e^d within four units of 2^-24 up to the largest number, zero below 2^-126, by
+// 2^(d log2 e) with what the product leaves: a third of the library function's
+// instructions, which bound the small batches.
 __device__ __forceinline__ float exp_of(float d) {
     constexpr float hi = 1.44269502162933349609375f, lo = 1.92596299112661746887e-8f;      // log2 e
     const float t = d * hi;
     float rest = __builtin_fmaf(d, lo, __builtin_fmaf(d, hi, -t));
-    rest = __builtin_fabsf(t) < 126.0f ? rest : 0.0f;      // no number for infinities, nothing beyond the range
+    rest = __builtin_fabsf(t) < 192.0f ? rest : 0.0f;      // no number for infinities, too much far beyond the range
     return __builtin_amdgcn_exp2f(t) * __builtin_fmaf(rest, 0.693147180559945309f, 1.0f);
 }
 // e^d - 1 - d. By its series for small d, where the difference would cancel
