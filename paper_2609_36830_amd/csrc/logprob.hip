@@ -44,7 +44,7 @@ constexpr int kLpThreads = 512;                    // of a workgroup: eight wave
 constexpr int kLpAgain = 4;                        // vectors a thread reads again at a time
 constexpr int kLpUnroll = 4;                       // 16-byte vectors a thread takes of a chunk
 constexpr float kLowest = -3.402823466e+38f;       // below no finite logit
-constexpr float kFarLog2 = -1e30f;                 // stands for the logarithm of nothing, finite
+constexpr float kFarLog2 = -256.0f;                // stands for the logarithm of what 2^u has as 0; its products with factors stay finite
 constexpr float kLn2 = 0.693147180559945309f;
 
 // log2 of the factor that brings sums against the maximum `from` to `to`; finite.
