@@ -80,6 +80,13 @@ size_t ortho_split_bytes(const OrthoShape &s, int64_t batch) {
     return parts == 1 ? 0 : (size_t)(tiles * parts) * 64 * 64 * sizeof(float);
 }
 
+// The factor of an update whose squares add up to `squares`, in binary64: updates of
+// any size. A zero update's, with an eps near 0, is no number that leaves it 0.
+__device__ __forceinline__ double ortho_factor(double squares, double eps) {
+    const double f = (double)kScaleX / (sqrt(squares) + eps);
+    return f == __builtin_inf() ? 0.0 : f;
+}
+
 // The sum over a workgroup of four waves, in thread order's tree, in every thread.
 __device__ __forceinline__ double block_total(double v, double *part) {
 #pragma unroll
@@ -135,7 +142,7 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(const T *__restrict__ 
     char *w = ws + blockIdx.z * s.bytes;
     double sum = 0.0;
     for (int k = threadIdx.x; k < norm_blocks; k += 256) sum += reinterpret_cast<const double *>(w)[k];
-    const double inv = (double)kScaleX / (sqrt(block_total(sum, part)) + eps);      // binary64: updates of any size
+    const double inv = ortho_factor(block_total(sum, part), eps);
     const T *mat = g + blockIdx.z * batch_stride;
     f16_t *by_rows = (f16_t *)(w + (s.turned ? s.xt : s.x)), *by_cols = (f16_t *)(w + (s.turned ? s.x : s.xt));
     const int64_t ld_rows = s.turned ? s.mp : s.np, ld_cols = s.turned ? s.np : s.mp;
@@ -439,7 +446,7 @@ __global__ __launch_bounds__(512) void ortho_whole_kernel(const T *__restrict__ 
     const int lines = s.turned ? np : kMP, len = s.turned ? kMP : np, next_own = lines * kStepBytes, next_other = len * kStepBytes;
     for (int k = threadIdx.x; k < kMP * np * 2 / 16; k += 512) reinterpret_cast<uint4 *>(own)[k] = make_uint4(0, 0, 0, 0);
     __syncthreads();
-    const double inv = (double)kScaleX / (sqrt(((part[0] + part[1]) + (part[2] + part[3])) + ((part[4] + part[5]) + (part[6] + part[7]))) + eps);
+    const double inv = ortho_factor(((part[0] + part[1]) + (part[2] + part[3])) + ((part[4] + part[5]) + (part[6] + part[7])), eps);
 #pragma unroll
     for (int k = 0; k < kHold; ++k) {
         const uint32_t at = k * 512 + threadIdx.x, r = at / across, c = (at - r * across) * V;
