@@ -438,7 +438,9 @@ int pace_diagnostics(const double *score, const int64_t *gen_sum, const int64_t 
  *             when top_k = 0)
  * A row of nothing but -inf has no distribution: logp -inf, entropy 0. A NaN
  * or +inf logit makes its row's logp, entropy and top_logp NaN.
- * workspace: pace_token_logprob_workspace_bytes() bytes. */
+ * workspace: pace_token_logprob_workspace_bytes() bytes, of these sizes: fewer
+ * rows, whose parts are joined, need more than many, which are taken whole. One
+ * that is kept for several sizes takes the largest of theirs. */
 #define PACE_TOP_MAX 64
 int pace_token_logprob_workspace_bytes(int64_t n_rows, int64_t vocab, int top_k, size_t *bytes_out);
 int pace_token_logprob(const void *logits, int dtype, int64_t n_rows, int64_t vocab, int64_t row_stride,
@@ -487,7 +489,8 @@ int pace_token_logprob_backward(const void *logits, int dtype, int64_t n_rows, i
  * kl_out f32 [n_traj] or NULL: sum of exp(d) - 1 - d over its response tokens
  * clipped_out int32 [n_traj] or NULL: how many of them a bound holds for
  * Sums are binary64, in an order fixed by the arguments.
- * workspace: pace_policy_loss_workspace_bytes() bytes. */
+ * workspace: pace_policy_loss_workspace_bytes() bytes, which do for every
+ * smaller batch too. */
 int pace_policy_loss_workspace_bytes(int64_t n_traj, int64_t n_tokens, size_t *bytes_out);
 int pace_policy_loss(const float *lp_new, const float *lp_behavior, const int32_t *tags, const int64_t *offsets,
                      int64_t n_traj, int64_t n_tokens, const float *advantage, const float *weight, double scale,
@@ -512,8 +515,9 @@ int pace_quantize_rows(const void *x, int dtype, int64_t n_rows, int64_t n_cols,
  *   1 <= k < 131072. Any strides and starts are read; both being multiples of 16
  *   bytes, with k, is the fast case.
  * a_scale f32 [m], b_scale f32 [n]; out [m, n] of out_dtype, rows out_stride apart
- * workspace: pace_matmul_i8_workspace_bytes() bytes (sums of parts of k, where
- *   there are few tiles; else 256). */
+ * workspace: pace_matmul_i8_workspace_bytes() bytes, which do for every smaller
+ *   m, n and k too (sums of parts of k, where there are few tiles: at most 8 MiB;
+ *   256 for k below 6144 or m up to 4). */
 int pace_matmul_i8_workspace_bytes(int64_t m, int64_t n, int64_t k, size_t *bytes_out);
 int pace_matmul_i8(const int8_t *a, int64_t a_stride, const float *a_scale, const int8_t *b, int64_t b_stride,
                    const float *b_scale, int64_t m, int64_t n, int64_t k, void *out, int out_dtype, int64_t out_stride,
@@ -533,7 +537,8 @@ int pace_matmul_i8(const int8_t *a, int64_t a_stride, const float *a_scale, cons
  *   binary16, scaled: X may reach 32 and A, C 128, far above what coefficients
  *   that converge give. A zero update gives zeros; one with a NaN or an infinity
  *   spoils its own matrix only.
- * workspace: pace_orthogonalize_workspace_bytes() bytes. */
+ * workspace: pace_orthogonalize_workspace_bytes() bytes, which do for every
+ *   smaller batch of smaller updates too. */
 int pace_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int64_t cols, size_t *bytes_out);
 int pace_orthogonalize(const void *update, int dtype, int64_t batch, int64_t rows, int64_t cols, int64_t row_stride,
                        int64_t batch_stride, int steps, const double *coefs, double eps, void *out, void *workspace,

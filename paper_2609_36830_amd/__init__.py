@@ -616,7 +616,7 @@ def pace_token_logprob_workspace_bytes(n_rows: int, vocab: int, top_k: int = 0) 
 
 def token_logprob_buffers(n_rows: int, vocab: int, top_k: int, device, stream=None):
     """Outputs and workspace for repeated pace_token_logprob calls on n_rows rows
-    (pass as ``buffers``)."""
+    (pass as ``buffers``). Of exactly this size: fewer rows need a larger workspace."""
     e = _allocator(device, stream)
     return dict(logp=e(n_rows, torch.float32), entropy=e(n_rows, torch.float32), stats=e((n_rows, 2), torch.float32),
                 top_ids=e((n_rows, top_k), torch.int32), top_logp=e((n_rows, top_k), torch.float32),

@@ -343,7 +343,8 @@ struct LossBounds {
     float low, high, dual;                  // 1 - el, 1 + eh, c
     float log_low, log_high, log_dual;      // and their logarithms, which d is compared with
 };
-size_t policy_loss_ws_bytes(int64_t n_tokens);
+size_t policy_loss_ws_bytes(int64_t n_tokens);      // of a call
+size_t policy_loss_ws_most(int64_t n_tokens);       // of every call up to this size
 hipError_t launch_policy_loss(const float *lp_new, const float *lp_beh, const int32_t *tags, const int64_t *offsets,
                               int64_t n, int64_t n_tokens, const float *adv, const float *weight, double scale,
                               const LossBounds &bounds, float *grad, float *loss, float *kl, int32_t *clipped, void *ws,
@@ -352,13 +353,15 @@ hipError_t launch_policy_loss(const float *lp_new, const float *lp_beh, const in
 // ---- products in 8-bit integers ---------------------------------------------------
 hipError_t launch_quantize_rows(const void *x, int dtype, int64_t rows, int64_t cols, int64_t stride, int8_t *q,
                                 float *scale, hipStream_t stream);
-size_t matmul_i8_ws_bytes(int64_t m, int64_t n, int64_t k);
+size_t matmul_i8_ws_bytes(const int8_t *a, int64_t lda, const int8_t *b, int64_t ldb, int64_t m, int64_t n, int64_t k);
+size_t matmul_i8_ws_most(int64_t m, int64_t n, int64_t k);
 hipError_t launch_matmul_i8(const int8_t *a, int64_t lda, const float *sa, const int8_t *b, int64_t ldb, const float *sb,
                             int64_t m, int64_t n, int64_t k, void *out, int dtype, int64_t ldo, void *ws,
                             hipStream_t stream);
 
 // ---- orthogonalised updates ---------------------------------------------------------
 size_t ortho_ws_bytes(int64_t batch, int64_t rows, int64_t cols);
+size_t ortho_ws_most(int64_t batch, int64_t rows, int64_t cols);
 hipError_t launch_orthogonalize(const void *g, int dtype, int64_t batch, int64_t rows, int64_t cols, int64_t stride,
                                 int64_t batch_stride, int steps, const double *coefs, double eps, void *out, void *ws,
                                 hipStream_t stream);

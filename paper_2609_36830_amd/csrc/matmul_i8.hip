@@ -313,26 +313,23 @@ hipError_t launch_few(const Rows &b, const Rows &a, const float *sb, const float
 
 }  // namespace
 
-// The parts that a product's steps are split into, where its rows are whole steps,
-// 48 or more: 16 x 4096 x 8192 takes 14.3 us in 8 parts (17.6 whole), 16 x 300 x 8192
-// 10.8 in 8 (17.1), 128 x 4096 x 8192 16.9 in 4 (20.1), but 20 x 1024 x 3968, of 31
-// steps, 11.0 in 3 (10.2).
-int i8_parts(int64_t m, int64_t n, int64_t k) {
-    return k % kStepBytes || k < 48 * kStepBytes ? 1 : product_parts(k / kStepBytes, ((m + 63) / 64) * ((n + 63) / 64));
+// Rows of whole steps and 16-byte chunks go straight into LDS; a tile's are numbered by
+// 32-bit byte offsets.
+static bool i8_direct(const int8_t *a, int64_t lda, const int8_t *b, int64_t ldb, int64_t k) {
+    return (((uintptr_t)a | (uintptr_t)b | (uint64_t)lda | (uint64_t)ldb) & 15) == 0 && k % kStepBytes == 0 && lda < (1 << 23) && ldb < (1 << 23);
 }
-
-size_t matmul_i8_ws_bytes(int64_t m, int64_t n, int64_t k) {
-    const int parts = i8_parts(m, n, k);
-    return parts == 1 ? 256 : (size_t)(((m + 63) / 64) * ((n + 63) / 64) * parts) * 64 * 64 * sizeof(int32_t);
+static size_t i8_ws_of(int64_t jobs) { return jobs ? (size_t)jobs * 64 * 64 * sizeof(int32_t) : 256; }
+size_t matmul_i8_ws_bytes(const int8_t *a, int64_t lda, const int8_t *b, int64_t ldb, int64_t m, int64_t n, int64_t k) {
+    const int parts = i8_parts(m, n, k, i8_direct(a, lda, b, ldb, k), resident_waves() / 16);
+    return i8_ws_of(parts == 1 ? 0 : ((m + 63) / 64) * ((n + 63) / 64) * parts);
 }
+size_t matmul_i8_ws_most(int64_t m, int64_t n, int64_t k) { return i8_ws_of(i8_jobs_most(m, n, k, resident_waves() / 16)); }
 
 hipError_t launch_matmul_i8(const int8_t *a, int64_t lda, const float *sa, const int8_t *b, int64_t ldb, const float *sb,
                             int64_t m, int64_t n, int64_t k, void *out, int dtype, int64_t ldo, void *ws, hipStream_t stream) {
     if (m == 0 || n == 0) return hipSuccess;
     const Rows ra{(const char *)a, lda, m, k}, rb{(const char *)b, ldb, n, k};
-    // a tile's rows are numbered by 32-bit byte offsets
-    const bool direct = (((uintptr_t)a | (uintptr_t)b | (uint64_t)lda | (uint64_t)ldb) & 15) == 0 && k % kStepBytes == 0 &&
-                        lda < (1 << 23) && ldb < (1 << 23);
+    const bool direct = i8_direct(a, lda, b, ldb, k);
     return with_elem(dtype, [&](auto tag) {
         using O = decltype(tag);
         auto tiles = [&](int64_t side) { return ((m + side - 1) / side) * ((n + side - 1) / side); };
@@ -346,9 +343,12 @@ hipError_t launch_matmul_i8(const int8_t *a, int64_t lda, const float *sa, const
         if (m == 1) return launch_few<O, 1>(rb, ra, sb, sa, out, ldo, stream);
         if (m == 2) return launch_few<O, 2>(rb, ra, sb, sa, out, ldo, stream);
         if (m <= 4) return launch_few<O, 4>(rb, ra, sb, sa, out, ldo, stream);
-        if (m <= 8 && (!direct || tiles(64) < cus)) return launch_few<O, 8>(rb, ra, sb, sa, out, ldo, stream);
+        if (i8_few(m, n, direct, cus)) return launch_few<O, 8>(rb, ra, sb, sa, out, ldo, stream);
         if (direct) {
-            if (const int parts = i8_parts(m, n, k); parts > 1)
+            // 16 x 4096 x 8192 takes 14.3 us in 8 parts (17.6 whole), 16 x 300 x 8192
+            // 10.8 in 8 (17.1), 128 x 4096 x 8192 16.9 in 4 (20.1), but 20 x 1024 x 3968,
+            // of 31 steps, 11.0 in 3 (10.2).
+            if (const int parts = i8_parts(m, n, k, direct, cus); parts > 1)
                 return with_tile(64, tiles(64) * parts, cus, [&](auto shape) {
                     return launch_parts<O, typename decltype(shape)::template Product<MulI8>>(rb, ra, sb, sa, out, ldo, tiles(64), parts, (char *)ws, stream);
                 });

@@ -688,6 +688,11 @@ size_t ortho_ws_bytes(int64_t batch, int64_t rows, int64_t cols) {
     const OrthoShape s = ortho_shape(rows, cols);
     return (size_t)(batch * s.bytes) + ortho_split_bytes(s, batch) + 256;
 }
+size_t ortho_ws_most(int64_t batch, int64_t rows, int64_t cols) {
+    const OrthoShape s = ortho_shape(rows, cols);
+    const int64_t t = (s.m + 63) / 64;
+    return (size_t)(batch * s.bytes) + (size_t)product_jobs_most(s.np / 64, t * (t + 1) / 2 * batch) * 64 * 64 * sizeof(float) + 256;
+}
 
 hipError_t launch_orthogonalize(const void *g, int dtype, int64_t batch, int64_t rows, int64_t cols, int64_t stride,
                                 int64_t batch_stride, int steps, const double *coefs, double eps, void *out, void *ws,

@@ -630,7 +630,7 @@ int pace_token_logprob_backward(const void *logits, int dtype, int64_t n_rows, i
 int pace_policy_loss_workspace_bytes(int64_t n_traj, int64_t n_tokens, size_t *bytes_out) {
     if (!bytes_out || n_traj < 0 || n_traj >= INT32_MAX || n_tokens < 0 || n_tokens >= kLossTokensMax)
         return PACE_ERR_INVALID_ARG;
-    *bytes_out = policy_loss_ws_bytes(n_tokens);
+    *bytes_out = policy_loss_ws_most(n_tokens);
     return PACE_OK;
 }
 
@@ -668,7 +668,7 @@ int pace_quantize_rows(const void *x, int dtype, int64_t n_rows, int64_t n_cols,
 int pace_matmul_i8_workspace_bytes(int64_t m, int64_t n, int64_t k, size_t *bytes_out) {
     if (!bytes_out || m < 0 || m >= INT32_MAX || n < 0 || n >= INT32_MAX || k < 1 || k >= kMatmulI8MaxK)
         return PACE_ERR_INVALID_ARG;
-    *bytes_out = matmul_i8_ws_bytes(m, n, k);
+    *bytes_out = matmul_i8_ws_most(m, n, k);
     return PACE_OK;
 }
 
@@ -684,7 +684,8 @@ int pace_matmul_i8(const int8_t *a, int64_t a_stride, const float *a_scale, cons
     if (((m + 63) / 64) * ((n + 63) / 64) >= INT32_MAX) return PACE_ERR_INVALID_ARG;
     if (m > 0 && n > 0 && (!a || !a_scale || !b || !b_scale)) return PACE_ERR_INVALID_ARG;
     if (!aligned(a_scale, 4) || !aligned(b_scale, 4)) return PACE_ERR_INVALID_ARG;
-    if (!workspace || !aligned(workspace, 256) || workspace_bytes < matmul_i8_ws_bytes(m, n, k)) return PACE_ERR_WORKSPACE;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < matmul_i8_ws_bytes(a, a_stride, b, b_stride, m, n, k))
+        return PACE_ERR_WORKSPACE;
     return hip_status(launch_matmul_i8(a, a_stride, a_scale, b, b_stride, b_scale, m, n, k, out, out_dtype, out_stride,
                                        workspace, (hipStream_t)stream));
 }
@@ -696,7 +697,7 @@ static bool ortho_sizes_ok(int64_t batch, int64_t rows, int64_t cols) {
 
 int pace_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int64_t cols, size_t *bytes_out) {
     if (!bytes_out || !ortho_sizes_ok(batch, rows, cols)) return PACE_ERR_INVALID_ARG;
-    *bytes_out = ortho_ws_bytes(batch, rows, cols);
+    *bytes_out = ortho_ws_most(batch, rows, cols);
     return PACE_OK;
 }
 

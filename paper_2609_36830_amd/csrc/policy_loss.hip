@@ -259,10 +259,12 @@ __global__ __launch_bounds__(kLossWaves * kWave) void policy_loss_join_kernel(
 
 }  // namespace
 
+static size_t loss_ws_of(int64_t spans) { return align256((size_t)spans * 2 * sizeof(LossSum)) + 256; }
 size_t policy_loss_ws_bytes(int64_t n_tokens) {
-    const int64_t span = policy_loss_span(n_tokens), spans = (n_tokens + span - 1) / span;
-    return align256((size_t)spans * 2 * sizeof(LossSum)) + 256;
+    const int64_t span = policy_loss_span(n_tokens);
+    return loss_ws_of((n_tokens + span - 1) / span);
 }
+size_t policy_loss_ws_most(int64_t n_tokens) { return loss_ws_of(policy_loss_spans_most(n_tokens)); }
 
 hipError_t launch_policy_loss(const float *lp_new, const float *lp_beh, const int32_t *tags, const int64_t *offsets,
                               int64_t n, int64_t n_tokens, const float *adv, const float *weight, double scale,

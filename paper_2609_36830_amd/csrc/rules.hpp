@@ -144,6 +144,26 @@ inline int product_parts(int64_t steps, int64_t tiles) {
     const int64_t run = (steps + parts - 1) / parts;
     return (int)((steps + run - 1) / run);           // no part without a step
 }
+// No fewer parts times tiles than any product of at most these steps and tiles has.
+inline int64_t product_jobs_most(int64_t steps, int64_t tiles) {
+    int64_t parts = steps / kPartSteps;
+    if (parts < 3) return 0;
+    if (parts > kPartsMost) parts = kPartsMost;
+    return tiles > kPartJobs / parts ? kPartJobs : parts * tiles;
+}
+// The parts of an 8-bit product's steps: of rows of whole steps that go straight to LDS
+// (direct), 48 or more, and not where the kernel for few tokens takes them (matmul_i8.hip).
+inline bool i8_few(int64_t m, int64_t n, bool direct, int64_t cus) { return m <= 4 || (m <= 8 && (!direct || (n + 63) / 64 < cus)); }
+constexpr int64_t kI8PartSteps = 48;
+inline int i8_parts(int64_t m, int64_t n, int64_t k, bool direct, int64_t cus) {
+    if (!direct || k < kI8PartSteps * 128 || i8_few(m, n, direct, cus)) return 1;
+    return product_parts(k / 128, ((m + 63) / 64) * ((n + 63) / 64));
+}
+// As many as any product of at most this size has, times its tiles.
+inline int64_t i8_jobs_most(int64_t m, int64_t n, int64_t k, int64_t cus) {
+    if (k < kI8PartSteps * 128 || i8_few(m, n, true, cus)) return 0;
+    return product_jobs_most(k / 128, ((m + 63) / 64) * ((n + 63) / 64));
+}
 
 // Columns of X that a workgroup takes where C and C X go in one launch, 0 where they
 // do not. A launch and C's round trip through memory cost 4 to 5 us, but each
@@ -183,6 +203,12 @@ constexpr int64_t kLossSpanMin = 256;
 inline int64_t policy_loss_span(int64_t n_tokens) {
     const int64_t per = (n_tokens / 8192 + 255) / 256 * 256;
     return per > kLossSpanMin ? per : kLossSpanMin;
+}
+// No fewer spans than any batch of at most n_tokens has: a span is at least
+// n_tokens / 8192, rounded down, and that at least 256 where it is not the least.
+inline int64_t policy_loss_spans_most(int64_t n_tokens) {
+    const int64_t spans = (n_tokens + kLossSpanMin - 1) / kLossSpanMin;
+    return spans < 8192 + 32 ? spans : 8192 + 32;
 }
 
 // ---- log-probabilities (logprob.hip) --------------------------------------------
