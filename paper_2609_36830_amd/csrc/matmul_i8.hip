@@ -91,6 +91,7 @@ template <typename O, TileWork kWork, typename P>
 __global__ __launch_bounds__(P::kThreads) void matmul_i8_kernel(Rows b, Rows a, const float *__restrict__ sb,
                                                                 const float *__restrict__ sa, O *__restrict__ out,
                                                                 int64_t ldo, char *__restrict__ sums, int parts) {
+    static_assert(kWork == kWhole || P::kRows == 64, "no other tile's steps are split");
     extern __shared__ __attribute__((aligned(16))) char lds[];
     using T = I8Tile<O, P>;
     constexpr int kBN = P::kRows, kBM = P::kCols;
@@ -349,7 +350,7 @@ hipError_t launch_matmul_i8(const int8_t *a, int64_t lda, const float *sa, const
             // 10.8 in 8 (17.1), 128 x 4096 x 8192 16.9 in 4 (20.1), but 20 x 1024 x 3968,
             // of 31 steps, 11.0 in 3 (10.2).
             if (const int parts = i8_parts(m, n, k, direct, cus); parts > 1)
-                return with_tile(64, tiles(64) * parts, cus, [&](auto shape) {
+                return with_tile_of_64(tiles(64) * parts, cus, [&](auto shape) {
                     return launch_parts<O, typename decltype(shape)::template Product<MulI8>>(rb, ra, sb, sa, out, ldo, tiles(64), parts, (char *)ws, stream);
                 });
             const int side = product_tile(k / kStepBytes, cus, tiles);

@@ -402,20 +402,24 @@ __device__ __forceinline__ void lower_tile_of(uint32_t id, uint32_t tiles, int &
 }
 
 // Runs f with the tile of a side of product_tile: eight waves, and as many
-// steps in flight as the LDS of a CU holds, for 64 of two workgroups where there
-// are tiles for more than one a CU.
+// steps in flight as the LDS of a CU holds, for 64 (the only side whose steps are
+// split into parts) of two workgroups where there is work for more than one a CU.
 template <int kBM, int kBN, int kWM, int kWN, int kDepth, int kUnit>
 struct TileShape {
     template <typename Mul>
     using Product = TileProduct<Mul, kBM, kBN, kWM, kWN, kDepth, kUnit, true>;
 };
 template <typename F>
+auto with_tile_of_64(int64_t jobs, int64_t cus, F f) {
+    return jobs > cus ? f(TileShape<64, 64, 4, 2, 4, 2>{}) : f(TileShape<64, 64, 4, 2, 8, 2>{});
+}
+template <typename F>
 auto with_tile(int side, int64_t tiles, int64_t cus, F f) {
     switch (side) {
         case 256: return f(TileShape<256, 256, 2, 4, 2, 1>{});
         case 192: return f(TileShape<192, 192, 2, 4, 2, 1>{});
         case 128: return f(TileShape<128, 128, 2, 4, 4, 1>{});
-        default: return tiles > cus ? f(TileShape<64, 64, 4, 2, 4, 2>{}) : f(TileShape<64, 64, 4, 2, 8, 2>{});
+        default: return with_tile_of_64(tiles, cus, f);
     }
 }
 

@@ -190,6 +190,7 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(const T *__restrict__ 
 // part of its steps.
 template <bool kSquare, TileWork kWork, typename P>
 __global__ __launch_bounds__(P::kThreads) void ortho_gram_kernel(OrthoShape s, char *ws, uint32_t side, float ca, float cb, float cc, int parts) {
+    static_assert(kWork == kWhole || P::kRows == 64, "no other tile's steps are split");
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const uint32_t job = xcd_run(blockIdx.x, gridDim.x), tiles = side * (side + 1) / 2;
     const uint32_t id = kWork == kPart ? job / parts : job;
@@ -591,7 +592,7 @@ hipError_t launch_gram(const OrthoShape &s, char *ws, int64_t batch, const float
         if (s.split) {
             side = 64;
             const int parts = product_parts(s.np / 64, tiles(64));
-            return with_tile(64, tiles(64) * parts, cus, [&](auto shape) {
+            return with_tile_of_64(tiles(64) * parts, cus, [&](auto shape) {
                 using P = typename decltype(shape)::template Product<MulF16>;
                 const hipError_t e = go(ortho_gram_kernel<false, kPart, P>, P{}, tiles(64) * parts, parts);
                 return e == hipSuccess ? go(ortho_gram_kernel<false, kJoin, P>, P{}, tiles(64), parts) : e;
