@@ -512,8 +512,8 @@ int pace_quantize_rows(const void *x, int dtype, int64_t n_rows, int64_t n_cols,
  * integer sum is exact (all of -128 .. 127 may occur), then converted to binary32,
  * multiplied and rounded to out_dtype.
  * a int8 [m, k], b int8 [n, k] (one row an output channel), strides in elements;
- *   1 <= k < 131072. Any strides and starts are read; both being multiples of 16
- *   bytes, with k, is the fast case.
+ *   1 <= k < 131072. Any strides and starts are read; the fast case is both being
+ *   multiples of 16 bytes and k one of 128. Others pass through registers.
  * a_scale f32 [m], b_scale f32 [n]; out [m, n] of out_dtype, rows out_stride apart
  * workspace: pace_matmul_i8_workspace_bytes() bytes, which do for every smaller
  *   m, n and k too (sums of parts of k, where there are few tiles: at most 8 MiB;
