@@ -452,7 +452,7 @@ int pace_token_logprob(const void *logits, int dtype, int64_t n_rows, int64_t vo
  * grad_entropy[i] entropy[i]) with respect to the logits:
  *   dz_v = (g ([v = t] - p_v) - g_H p_v (log p_v + H)) / temperature
  * (an id outside the vocabulary is no v: its logp is NaN, its row's gradient
- * that of the other terms).
+ * that of the other terms; a p below 2^-126 counts as 0).
  * logits .. temperature, stats, entropy: as given to and written by
  * pace_token_logprob (entropy may be NULL without grad_entropy).
  * grad_logp f32 [n_rows]; grad_entropy f32 [n_rows] or NULL (zero).
