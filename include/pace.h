@@ -531,12 +531,16 @@ int pace_matmul_i8(const int8_t *a, int64_t a_stride, const float *a_scale, cons
  * from about 0.02 .. 1 of the norm into 0.7 .. 1.2; {1.5, -0.5, 0} converges to 1
  * from nearer.
  * update: [batch, rows, cols] of dtype, rows row_stride and matrices batch_stride
- *   elements apart; rows, cols 1 .. 2^21, batch < 65536
+ *   elements apart, one behind the other; rows, cols 1 .. 2^21, batch < 65536
  * steps 0 .. 100; coefs [host] double[3], finite; eps > 0, finite
  * out: bfloat16 [batch, rows, cols], contiguous. Between the products values are
- *   binary16, scaled: X may reach 32 and A, C 128, far above what coefficients
- *   that converge give. A zero update gives zeros; one with a NaN or an infinity
- *   spoils its own matrix only.
+ *   binary16, scaled, whatever the update's type: X may reach 32 and A, C 128, far
+ *   above what coefficients that converge give, and elements are held to 2^-11 of
+ *   their size or, where that is more, X's to 2^-35 and A's and C's to 2^-33.
+ *   Five quintic steps come within 2.3e-3 of binary64's result (2-norm of the
+ *   difference over that of the result), of which the rounding to bfloat16 alone
+ *   is 1.7e-3. A zero update gives zeros; one with a NaN or an infinity spoils its
+ *   own matrix only.
  * workspace: pace_orthogonalize_workspace_bytes() bytes, which do for every
  *   smaller batch of smaller updates too. */
 int pace_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int64_t cols, size_t *bytes_out);
