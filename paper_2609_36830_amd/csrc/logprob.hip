@@ -21,7 +21,8 @@
 // again from HBM), 1023 of 50021 in binary32 with an entropy
 // gradient 49 + 71. 48 rows with 20 alternatives take 15.8 us, of which two
 // launches' beginnings and the dependent reads of the second (bound, holders,
-// list, rank) are all but 3.
+// list, rank) are all but 3. Many short rows with alternatives are bound by vector
+// instructions, issued in 82% of the cycles: 8000 of 5000 with 20 take 30 us, without 19.
 //
 // Best alternatives: keys (logit in order, ~index), all different, so the set
 // and its order do not depend on the order of arrival. The pass over the logits

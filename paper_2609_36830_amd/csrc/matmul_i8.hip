@@ -10,9 +10,13 @@
 // enough: 4096 tokens x 16384 channels x 4096 take 227 us (2.4 PTOP/s; a library's
 // large product 2.07), with the quantisation 240. There the cores are busy 66% of
 // the time at 1.8 GHz: the tile's LDS reads take as long as its products, and the
-// clock falls with the power. 1021 x 150000 x 2048 take 355 (1.8 PTOP/s): 16 steps
+// clock falls with the power. 1021 x 150000 x 2048 take 360 (1.7 PTOP/s): 16 steps
 // a tile, whose store of 309 MB nothing else covers. Few tokens are bound by the
-// weights' bytes: 1 x 16384 x 4096 takes 11.5 us (5.8 TB/s).
+// weights' bytes: 1 x 16384 x 4096 takes 11.5 us (5.8 TB/s), 64 x 16384 x 4096 12.9. Less
+// than a tile a CU is bound by its steps' latency and, in parts, a second launch: 16 x
+// 4096 x 8192 take 10 + 4 us, the waves waiting 55% of them. Off the step (see the rule
+// below) it is the way through registers: waves wait 56% to 61%, the matrix cores are
+// busy 21%.
 #include "elem.hpp"
 #include "kernels.hpp"
 #include "mfma_tile.hpp"

@@ -112,6 +112,10 @@ inline auto in_launches(int64_t n, int64_t threads, F f) {
 // a CU on, which then cost more each. Measured in binary16: X X^T of 4096 x
 // 16384 342 / 281 / 406 / 484 us (256 / 192 / 128 / 64), of 2500 x 2600 56 / 42 /
 // 25 / 37, of 1000 x 3001 62 / 44 / 26 / 14; C X of 4096 x 16384 470 / 614 / 664 / 993.
+// In 8 bits, where a step has the same bytes and products, it takes the fastest of the
+// four in 20 of 21 products of 40 to 4096 tokens, 2048 to 150000 channels and 512 to 5120
+// bytes (4096 x 16384 x 4096 224 / 292 / 335 / 439, 512 x 16384 x 2048 28 / 39 / 27 / 34, 64
+// x 16384 x 4096 44 / 32 / 20 / 13), and 2000 x 9000 x 2944 in 79 us for 75.
 template <typename Tiles>
 inline int product_tile(int64_t steps, int64_t cus, Tiles tiles) {
     constexpr int side[4] = {256, 192, 128, 64};
@@ -173,7 +177,10 @@ inline int64_t i8_jobs_most(int64_t m, int64_t n, int64_t k, int64_t cus) {
 // one launch / two: 1 update of 64 x 4096 69 / 87, 256 of 64 x 512 107 / 143, 24 of
 // 128 x 512 65 / 78, 128 of them 143 / 149, 256 of 128 x 1024 485 / 441, 4 of 256 x
 // 1000 87 / 94 (64 columns), 24 of 256 x 256 78 / 85 (128; with 64 103), 24 of 256 x 512
-// 125 / 102.
+// 125 / 102. Of 25 batches of 1 to 80 updates of 192 and 256 rows and up to 4096 columns it
+// takes the fastest of the three forms in 23: 8 of 192 x 1000 104 (two launches) / 102 (64
+// columns) / 85 (128), 16 of 192 x 192 86 / 67 / 70, 48 of 256 x 256 116 / 149 / 127; but 40 of
+// 192 x 400 116 / 148 / 109 and 64 of 192 x 192 111 / 125 / 107.
 inline int ortho_step_cols(int64_t mp, int64_t n, int64_t batch, int64_t cus) {
     auto jobs = [&](int64_t cols) { return mp / 64 * ((n + cols - 1) / cols) * batch; };
     if (mp == 64) return 64;
