@@ -6,9 +6,11 @@
 // symmetric, so only their lower tiles are formed and both halves written.
 // Between products X, A and C are held as binary16, scaled by powers of two:
 // the singular values are at most about 1.2, so their range is known, and 11 bits
-// lose eight times less than bfloat16 (the result's type) would: five steps end
-// 2.0e-3 to 2.3e-3 from binary64's (2-norm, relative), the rounding of the result
-// alone 1.7e-3. Elements of X below 2^-24 of the norm, which lie far below the
+// lose eight times less than bfloat16 (the result's type) would: five steps on noise,
+// alone or over strong directions, end 1.9e-3 to 2.6e-3 from binary64's (2-norm,
+// relative), the rounding of the result alone 1.7e-3. In directions that the update
+// lacks the roundings grow as a small singular value would, 485 times in five
+// quintic steps: an update of rank k ends some 0.2 / sqrt(k) away. Elements of X below 2^-24 of the norm, which lie far below the
 // typical one's 1 / sqrt(m n), are held to 2^-35 of it. The products' sums are
 // binary32. X is kept by rows for X X^T and by columns for C X, so that
 // every product reads both sides along the summed axis.
