@@ -7,7 +7,8 @@ passes raw device pointers plus the current HIP stream. Every step of the
 filter runs in the library's HIP kernels; there is no CPU or PyTorch
 fallback, and importing this package on a machine without the built library
 fails loudly. With ``stream`` (a stream or its handle) a call runs there in
-place of the current stream, and what it allocates is that stream's memory.
+place of the current stream, and what it allocates is that stream's memory;
+the functions that make buffers for repeated calls take their stream too.
 
     score, S, T      = pace_score(tags, offsets, completion, V, prefix, window)
     budget, r_hat    = pace_budget(occupancy, capacity, r_hat_prev=0.0)

@@ -325,6 +325,7 @@ static bool i8_direct(const int8_t *a, int64_t lda, const int8_t *b, int64_t ldb
 }
 static size_t i8_ws_of(int64_t jobs) { return jobs ? (size_t)jobs * 64 * 64 * sizeof(int32_t) : 256; }
 size_t matmul_i8_ws_bytes(const int8_t *a, int64_t lda, const int8_t *b, int64_t ldb, int64_t m, int64_t n, int64_t k) {
+    if (m <= 4 || k < kI8PartSteps * kStepBytes) return i8_ws_of(0);      // most calls, without asking for the device
     const int parts = i8_parts(m, n, k, i8_direct(a, lda, b, ldb, k), resident_waves() / 16);
     return i8_ws_of(parts == 1 ? 0 : ((m + 63) / 64) * ((n + 63) / 64) * parts);
 }
