@@ -174,14 +174,14 @@ def _prepare_adamw(c, g):
 
 def _encode(m, v):
     """Moments [blocks, 256] in binary64 as codes and scales: m as c |c| M / 127^2, v as c^4 V / 255^4."""
-    most = torch.stack([m.abs().amax(1), v.amax(1)], 1).float()
-    most = torch.where(most < 2.0 ** -126, 0.0, most)
-    to = most.double().clamp(min=2.0 ** -126)
-    cm = torch.round(127.0 * torch.sqrt(m.abs() / to[:, :1])).clamp(max=127.0)
-    cv = torch.round(255.0 * torch.sqrt(torch.sqrt(v / to[:, 1:]))).clamp(max=255.0)
+    most = torch.stack([m.abs().amax(1), v.amax(1)], 1)      # codes go by the largest itself, its rounding is kept beside them
+    scale = torch.where(most < 2.0 ** -126, 0.0, most).float()
+    to = most.clamp(min=2.0 ** -126)
+    cm = torch.round(127.0 * torch.sqrt(m.abs() / to[:, :1]))
+    cv = torch.round(255.0 * torch.sqrt(torch.sqrt(v / to[:, 1:])))
     cv = torch.where(v > 0, cv.clamp(min=1.0), 0.0)
-    cm, cv = torch.where(most[:, :1] > 0, cm, 0.0), torch.where(most[:, 1:] > 0, cv, 0.0)
-    return (torch.sign(m) * cm).to(torch.int8), cv.to(torch.uint8), most
+    cm, cv = torch.where(scale[:, :1] > 0, cm, 0.0), torch.where(scale[:, 1:] > 0, cv, 0.0)
+    return (torch.sign(m) * cm).to(torch.int8), cv.to(torch.uint8), scale
 
 
 def _decode(mc, vc, scale):
@@ -351,8 +351,9 @@ def _exact_adamw(s):
         return {**out, "m": m, "v": v}
     del keep, unbiased
     m, v = m.view(-1, BLOCK), v.view(-1, BLOCK)
-    most = torch.stack([torch.linalg.vector_norm(m, math.inf, 1), v.max(1).values], 1).float().double()   # binary32 by definition
+    most = torch.stack([torch.linalg.vector_norm(m, math.inf, 1), v.max(1).values], 1)
     cm, cv = _nearest(m.abs(), most[:, :1], (127, 2)), _nearest(v, most[:, 1:], (255, 4))
     cm, cv = cm.double(), torch.where((v > 0) & (cv == 0), 1, cv).double()
-    return {**out, "scale": most, "m": (torch.sign(m) * (cm / 127).square() * most[:, :1]).view(-1),
-            "v": ((cv / 255).square().square() * most[:, 1:]).view(-1)}
+    scale = most.float().double()                            # kept in binary32
+    return {**out, "scale": most, "m": (torch.sign(m) * (cm / 127).square() * scale[:, :1]).view(-1),
+            "v": ((cv / 255).square().square() * scale[:, 1:]).view(-1)}
