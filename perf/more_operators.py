@@ -323,7 +323,7 @@ def _nearest(values, most, levels):
     """The index of the code nearest to each value, in the root in which codes stand evenly: a search among the borders."""
     borders = ((torch.arange(levels[0], dtype=torch.float64, device=DEV) + 0.5) / levels[0]) ** levels[1]
     share = torch.where(most > 0, values / torch.where(most > 0, most, 1.0), 0.0)
-    return torch.searchsorted(borders, share.contiguous())
+    return torch.searchsorted(borders, share.contiguous(), right=True)      # a quarter of the largest is halfway: it goes up
 
 
 def _exact_adamw(s):
