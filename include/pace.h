@@ -551,6 +551,104 @@ int pace_orthogonalize(const void *update, int dtype, int64_t batch, int64_t row
                        int64_t batch_stride, int steps, const double *coefs, double eps, void *out, void *workspace,
                        size_t workspace_bytes, void *stream);
 
+/* pace_layer_norm -- each row at mean 0 and variance 1, then weighted:
+ *   mu = mean x,  rstd = 1 / sqrt(mean (x - mu)^2 + eps),  out = (x - mu) rstd weight + bias
+ * x, out      [n_rows, n_cols] of dtype, rows row_stride and out_stride elements
+ *             apart; 1 <= n_cols <= 2^24
+ * weight, bias [n_cols] of weight_dtype, which is dtype or PACE_F32; either may be
+ *             NULL (ones, zeros)
+ * eps         [host] 1e-30 .. 1e30
+ * stats_out   f32 [n_rows, 2] or NULL: mu and rstd, which the backward pass takes
+ * Statistics are binary32, the variance from differences to the mean, with the
+ * mean's own rounding made good. An infinity or a NaN spoils its own row; so may
+ * elements beyond 2^60, whose squares' sum leaves binary32. */
+int pace_layer_norm(const void *x, int dtype, int64_t n_rows, int64_t n_cols, int64_t row_stride, const void *weight,
+                    const void *bias, int weight_dtype, double eps, void *out, int64_t out_stride, float *stats_out,
+                    void *stream);
+
+/* pace_layer_norm_backward -- gradients of pace_layer_norm: with h = (x - mu) rstd
+ * and a = grad_out weight,
+ *   grad_x = rstd (a - mean a - h mean(a h))
+ *   grad_weight = sum over rows of grad_out h,  grad_bias = sum over rows of grad_out
+ * x .. weight_dtype, stats: as given to and written by pace_layer_norm.
+ * grad_out, grad_x_out: [n_rows, n_cols] of dtype, with strides of their own.
+ *   grad_x_out may be grad_out itself (with the same stride), which it then
+ *   replaces; otherwise the two must not overlap.
+ * grad_weight_out, grad_bias_out: f32 [n_cols] or NULL; overwritten, zeros without
+ *   rows. Sums down the columns are binary32, in an order fixed by the sizes, at
+ *   most 1024 rows one after the other.
+ * workspace: pace_layer_norm_backward_workspace_bytes() bytes, which do for every
+ *   smaller problem too; none is needed where both sums are NULL. */
+int pace_layer_norm_backward_workspace_bytes(int64_t n_rows, int64_t n_cols, size_t *bytes_out);
+int pace_layer_norm_backward(const void *x, int dtype, int64_t n_rows, int64_t n_cols, int64_t row_stride, const void *weight,
+                             int weight_dtype, const float *stats, const void *grad_out, int64_t grad_out_stride,
+                             void *grad_x_out, int64_t grad_x_stride, float *grad_weight_out, float *grad_bias_out,
+                             void *workspace, size_t workspace_bytes, void *stream);
+
+/* Calls on many tensors take [host] arrays with an entry for each: device
+ * pointers to contiguous elements (aligned to their element), their types and
+ * sizes. Tensors may be empty (their pointers are not looked at), have at most
+ * 2^35 elements, and none may overlap another that a call writes: no tensor twice. The
+ * arrays are read before the call returns. */
+
+/* pace_grad_norm -- the 2-norm of all gradients together, and the factor that
+ * clips it: 1 up to max_norm, else max_norm / norm; NaN where an element is an
+ * infinity or a NaN.
+ * max_norm [host] >= 0, may be infinite
+ * norm_out, factor_out f32 [1], one of them may be NULL
+ * Squares and sums are binary64, in an order fixed by the sizes.
+ * workspace: pace_grad_norm_workspace_bytes() bytes for at most n_tensors of
+ *   n_elements together. */
+int pace_grad_norm_workspace_bytes(int64_t n_tensors, int64_t n_elements, size_t *bytes_out);
+int pace_grad_norm(int64_t n_tensors, const void *const *grads, const int32_t *grad_dtypes, const int64_t *sizes, double max_norm,
+                   float *norm_out, float *factor_out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* pace_adamw -- one AdamW step over many tensors, in place. With g = gradient x
+ * grad_scale and t = step, for every element:
+ *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2
+ *   p <- p (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps)
+ * computed in binary32 and rounded to the parameter's type once.
+ * params, grads: of param_dtypes and grad_dtypes, which may differ
+ * state_bits 32: exp_avg (m) and exp_avg_sq (v) are f32, scales is not read
+ * state_bits 8: every PACE_ADAMW_BLOCK consecutive elements of a tensor (its last may
+ *   be fewer) share two scales, M = max |m| and V = max v of the block, binary32:
+ *     exp_avg int8: code c in -127 .. 127 stands for c |c| M / 127^2
+ *     exp_avg_sq uint8: code c in 0 .. 255 stands for (c / 255)^4 V
+ *     scales f32 [blocks, 2]: M, V
+ *   The step uses the new moments before they are rounded (held in binary64); then
+ *   |m| and v go to the code nearest in the root that the codes are evenly spaced in,
+ *   against the block's largest before its own rounding (halfway to the larger code), a
+ *   positive v to 1 at least.
+ *   Blocks whose largest is below 2^-126 are zeros. Zeros are fresh states.
+ *   A code moves when a moment changes by half a step between codes: small moments
+ *   that shrink towards zero are held while their block's largest keeps its size.
+ *   An infinity or a NaN (or a g^2 beyond binary32) spoils its block's moments.
+ * copies: copy_dtypes (PACE_BF16 or PACE_F16) copies of the new parameters, an entry
+ *   or all NULL: none
+ * weight_decay: [host] f32 [n_tensors], finite and >= 0, or NULL (0)
+ * hyper [host]: lr finite; betas in [0, 1); eps 1e-30 .. 1e30; step >= 1, the number of this update
+ * grad_scale: f32 [1] (device) or NULL (1). Where it is an infinity or a NaN nothing
+ *   is written: the step is left out, without the host having to look.
+ * schedule: f64 [2] (device) or NULL: lr and step, in place of hyper's, for calls
+ *   that are captured once and replayed. */
+#define PACE_ADAMW_BLOCK 256
+typedef struct pace_adamw_params {
+    double lr;
+    double beta1;
+    double beta2;
+    double eps;
+    int64_t step;
+} pace_adamw_params;
+int pace_adamw(int64_t n_tensors, const int64_t *sizes, void *const *params, const int32_t *param_dtypes, const void *const *grads,
+               const int32_t *grad_dtypes, int state_bits, void *const *exp_avg, void *const *exp_avg_sq, float *const *scales,
+               void *const *copies, const int32_t *copy_dtypes, const float *weight_decay, const pace_adamw_params *hyper,
+               const float *grad_scale, const double *schedule, void *stream);
+
+/* pace_adamw_unpack -- the values that moments in 8 bits stand for, rounded to
+ * binary32. exp_avg_out or exp_avg_sq_out may be NULL: not wanted. */
+int pace_adamw_unpack(int64_t n_tensors, const int64_t *sizes, const int8_t *const *exp_avg, const uint8_t *const *exp_avg_sq,
+                      const float *const *scales, float *const *exp_avg_out, float *const *exp_avg_sq_out, void *stream);
+
 /* pace_time_next_kernel -- measurement hook, not part of the method.
  * Arms a one-shot timer for one phase of the device work of the NEXT call
  * made from the calling host thread to an entry point that enqueues device

@@ -24,6 +24,13 @@ the packed batch to a weight update:
     grad_logp, loss, *_      = pace_policy_loss(logp, lp_behavior, offsets, advantage, tags)
     grad_logits              = pace_token_logprob_backward(logits, token_ids, stats, grad_logp)
     update                   = pace_orthogonalize(momentum)
+
+The norm before the head, and the element-wise update of any weights:
+
+    hidden, stats            = pace_layer_norm(states, weight, bias)
+    grad_states, grad_w, grad_b = pace_layer_norm_backward(states, stats, grad_hidden, weight)
+    norm, factor             = pace_grad_norm(grads, max_norm=1.0)
+    pace_adamw(params, grads, state, lr, step, grad_scale=factor)     # state = adamw_state(params, bits=8)
 """
 from __future__ import annotations
 
@@ -32,7 +39,7 @@ from typing import Optional, Sequence
 
 import torch
 
-from ._lib import PaceParams, lib, library_path
+from ._lib import AdamwParams, PaceParams, lib, library_path
 
 __all__ = [
     "PaceError", "PaceParams", "default_params", "pace_workspace_bytes", "pace_score",
@@ -40,6 +47,8 @@ __all__ = [
     "pace_filter_step_noalloc", "FilterStep",
     "pace_token_logprob", "pace_token_logprob_backward", "token_logprob_buffers", "pace_policy_loss", "policy_loss_buffers",
     "pace_quantize_rows", "pace_matmul_i8", "matmul_i8_buffers", "pace_orthogonalize", "orthogonalize_buffers",
+    "pace_layer_norm", "pace_layer_norm_backward", "layer_norm_buffers", "pace_grad_norm", "grad_norm_buffers",
+    "pace_adamw", "adamw_state", "pace_adamw_unpack",
     "library_path", "WS_SCORE", "WS_SELECT", "WS_COMPACT", "WS_FILTER_STEP",
     "BAD_OFFSETS", "BAD_COMPLETION", "BAD_TAG", "BAD_WINDOW",
 ]
@@ -797,6 +806,222 @@ def pace_orthogonalize(update, steps: int = 5, coefs=(3.4445, -4.7750, 2.0315), 
                                     (ctypes.c_double * 3)(*map(float, coefs)), float(eps), out.data_ptr(), ws,
                                     ws_bytes, _stream(dev, stream)), "pace_orthogonalize")
     return out
+
+
+# ---- the norm before the head, gradient norm and AdamW ---------------------------
+ADAMW_BLOCK = 256        # elements of a tensor that share the scales of moments in 8 bits
+
+
+def pace_layer_norm_backward_workspace_bytes(n_rows: int, n_cols: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().pace_layer_norm_backward_workspace_bytes(int(n_rows), int(n_cols), ctypes.byref(out)),
+           "pace_layer_norm_backward_workspace_bytes")
+    return int(out.value)
+
+
+def layer_norm_buffers(n_rows: int, n_cols: int, dtype, device, backward: bool = False, stream=None):
+    """Outputs for repeated pace_layer_norm calls on rows of one shape (pass as ``buffers``); with ``backward`` those of
+    pace_layer_norm_backward and its workspace too."""
+    e = _allocator(device, stream)
+    b = dict(out=e((n_rows, n_cols), dtype), stats=e((n_rows, 2), torch.float32))
+    if backward:
+        b.update(grad_x=e((n_rows, n_cols), dtype), grad_weight=e(n_cols, torch.float32), grad_bias=e(n_cols, torch.float32),
+                 workspace=e(pace_layer_norm_backward_workspace_bytes(n_rows, n_cols), torch.uint8))
+    return b
+
+
+def _norm_weight(w, x, n_cols: int, name: str):
+    if w.dtype is not x.dtype and w.dtype is not torch.float32:
+        raise ValueError("%s must be float32 or of x's type, got %s" % (name, w.dtype))
+    return _vector(w, w.dtype, n_cols, x.device, name)
+
+
+def pace_layer_norm(x, weight=None, bias=None, eps: float = 1e-5, buffers=None, stream=None):
+    """Rows of x at mean 0 and variance 1, then weighted (weight and bias of one type: float32 or x's). Returns
+    (out of x's type and shape, stats f32[n, 2]: mean and 1 / sqrt(variance + eps))."""
+    dt, n, k, stride = _matrix(x, "x")
+    dev = x.device
+    wt = dt
+    if weight is not None:
+        wt = DTYPES[_norm_weight(weight, x, k, "weight").dtype]
+    if bias is not None:
+        bt = DTYPES[_norm_weight(bias, x, k, "bias").dtype]
+        if weight is not None and bt != wt:
+            raise ValueError("weight and bias must have one type")
+        wt = bt
+    b = layer_norm_buffers(n, k, x.dtype, dev, stream=stream) if buffers is None else buffers
+    out, stats = _sized(b["out"], x.dtype, (n, k), dev, "out"), _sized(b["stats"], torch.float32, (n, 2), dev, "stats")
+    _check(lib().pace_layer_norm(x.data_ptr(), dt, n, k, stride, _ptr(weight), _ptr(bias), wt, float(eps), out.data_ptr(), k,
+                                 stats.data_ptr(), _stream(dev, stream)), "pace_layer_norm")
+    return out, stats
+
+
+def pace_layer_norm_backward(x, stats, grad_out, weight=None, buffers=None, stream=None):
+    """Gradients of pace_layer_norm. Returns (grad_x of x's type, grad_weight f32[k], grad_bias f32[k]). buffers["grad_x"]
+    may be grad_out itself."""
+    dt, n, k, stride = _matrix(x, "x")
+    gt, gn, gk, gstride = _matrix(grad_out, "grad_out")
+    dev = x.device
+    if (gt, gn, gk) != (dt, n, k) or grad_out.device != dev:
+        raise ValueError("grad_out must have x's type and shape")
+    _vector(stats, torch.float32, 2 * n, dev, "stats")
+    wt = dt if weight is None else DTYPES[_norm_weight(weight, x, k, "weight").dtype]
+    if buffers is None:
+        e = _allocator(dev, stream)
+        buffers = dict(grad_x=e((n, k), x.dtype), grad_weight=e(k, torch.float32), grad_bias=e(k, torch.float32),
+                       workspace=e(pace_layer_norm_backward_workspace_bytes(n, k), torch.uint8))
+    grad_x = buffers["grad_x"]
+    xt, xn, xk, xstride = _matrix(grad_x, "grad_x")
+    if (xt, xn, xk) != (dt, n, k) or grad_x.device != dev:
+        raise ValueError("grad_x must have x's type and shape")
+    grad_weight = _sized(buffers["grad_weight"], torch.float32, (k,), dev, "grad_weight")
+    grad_bias = _sized(buffers["grad_bias"], torch.float32, (k,), dev, "grad_bias")
+    ws, ws_bytes = _scratch(buffers["workspace"], dev)
+    _check(lib().pace_layer_norm_backward(x.data_ptr(), dt, n, k, stride, _ptr(weight), wt, stats.data_ptr(), grad_out.data_ptr(),
+                                          gstride, grad_x.data_ptr(), xstride, grad_weight.data_ptr(), grad_bias.data_ptr(), ws,
+                                          ws_bytes, _stream(dev, stream)), "pace_layer_norm_backward")
+    return grad_x, grad_weight, grad_bias
+
+
+def _each(tensors, name: str, device=None, dtypes=None, sizes=None):
+    """A list of contiguous device tensors on one device; returns the list, its device, pointers and sizes as the C ABI takes them.
+    dtypes: the types allowed; sizes: the elements that each must have."""
+    ts = list(tensors)
+    for k, t in enumerate(ts):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous() or t.dtype not in dtypes:
+            raise ValueError("%s[%d] must be a contiguous device tensor of %s" % (name, k, " or ".join(map(str, dtypes))))
+        if device is None:
+            device = t.device
+        if t.device != device:
+            raise ValueError("%s[%d] must be on %s" % (name, k, device))
+    if device is None:
+        raise ValueError("%s must hold a tensor" % name)
+    counts = [t.numel() for t in ts]
+    if sizes is not None and counts != sizes:
+        raise ValueError("%s must have %s elements, got %s" % (name, sizes, counts))
+    n = max(len(ts), 1)
+    return ts, device, (ctypes.c_void_p * n)(*[t.data_ptr() for t in ts]), counts
+
+
+def _int32s(values):
+    return (ctypes.c_int32 * max(len(values), 1))(*values)
+
+
+def _sizes(counts):
+    return (ctypes.c_int64 * max(len(counts), 1))(*counts)
+
+
+def _codes(ts):
+    return _int32s([DTYPES[t.dtype] for t in ts])
+
+
+def pace_grad_norm_workspace_bytes(n_tensors: int, n_elements: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().pace_grad_norm_workspace_bytes(int(n_tensors), int(n_elements), ctypes.byref(out)), "pace_grad_norm_workspace_bytes")
+    return int(out.value)
+
+
+def grad_norm_buffers(n_tensors: int, n_elements: int, device, stream=None):
+    """Outputs and workspace for repeated pace_grad_norm calls on up to n_tensors tensors of n_elements together."""
+    e = _allocator(device, stream)
+    return dict(norm=e(1, torch.float32), factor=e(1, torch.float32),
+                workspace=e(pace_grad_norm_workspace_bytes(n_tensors, n_elements), torch.uint8))
+
+
+def pace_grad_norm(grads, max_norm: float = float("inf"), buffers=None, stream=None):
+    """The 2-norm of all gradients together. Returns (norm f32[1], factor f32[1]: min(1, max_norm / norm), NaN where the norm
+    is no number)."""
+    ts, dev, ptrs, counts = _each(grads, "grads", dtypes=DTYPES)
+    b = grad_norm_buffers(len(ts), sum(counts), dev, stream) if buffers is None else buffers
+    norm, factor = _sized(b["norm"], torch.float32, (1,), dev, "norm"), _sized(b["factor"], torch.float32, (1,), dev, "factor")
+    ws, ws_bytes = _scratch(b["workspace"], dev)
+    _check(lib().pace_grad_norm(len(ts), ptrs, _codes(ts), _sizes(counts), float(max_norm), norm.data_ptr(), factor.data_ptr(),
+                                ws, ws_bytes, _stream(dev, stream)), "pace_grad_norm")
+    return norm, factor
+
+
+def adamw_state(params, bits: int = 32, copy_dtype=None, stream=None):
+    """Fresh moments for pace_adamw of these tensors: zeros, in float32 or with ``bits`` 8 as codes with two scales for every
+    ADAMW_BLOCK elements. With copy_dtype (bfloat16 or float16) each step writes the new parameters in that type too."""
+    ts, dev, _, counts = _each(params, "params", dtypes=DTYPES)
+    if bits not in (32, 8):
+        raise ValueError("bits must be 32 or 8")
+    if copy_dtype not in (None, torch.bfloat16, torch.float16):
+        raise ValueError("copy_dtype must be bfloat16 or float16")
+    e = _allocator(dev, stream)
+
+    def zeros(shape, dtype):
+        t = e(shape, dtype)
+        if stream is None:
+            return t.zero_()
+        s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(dev, stream), device=dev)
+        with torch.cuda.stream(s):
+            return t.zero_()
+
+    moments = (torch.float32, torch.float32) if bits == 32 else (torch.int8, torch.uint8)
+    return dict(bits=bits, exp_avg=[zeros(t.shape, moments[0]) for t in ts], exp_avg_sq=[zeros(t.shape, moments[1]) for t in ts],
+                scale=[zeros((-(-n // ADAMW_BLOCK), 2), torch.float32) for n in counts] if bits == 8 else None,
+                copies=[zeros(t.shape, copy_dtype) for t in ts] if copy_dtype is not None else None)
+
+
+def _moments(state, dev, counts):
+    """The state's moments and scales as the C ABI takes them."""
+    if state["bits"] == 32:
+        kinds, scales = ((torch.float32,), (torch.float32,)), None
+    elif state["bits"] == 8:
+        kinds = ((torch.int8,), (torch.uint8,))
+        scales = _each(state["scale"], "scale", dev, (torch.float32,), [2 * -(-n // ADAMW_BLOCK) for n in counts])[2]
+    else:
+        raise ValueError("bits must be 32 or 8")
+    m = _each(state["exp_avg"], "exp_avg", dev, kinds[0], counts)[2]
+    return m, _each(state["exp_avg_sq"], "exp_avg_sq", dev, kinds[1], counts)[2], scales
+
+
+def pace_adamw(params, grads, state, lr: float = 1e-3, step: int = 1, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.0,
+               grad_scale=None, schedule=None, stream=None):
+    """One AdamW step over a list of tensors, in place: params, the moments in ``state`` (adamw_state) and its copies. step is
+    the number of this update, from 1. weight_decay: a number, or one for each tensor. grad_scale (f32[1], pace_grad_norm's
+    factor) multiplies the gradients; where it is no number nothing changes. schedule (f64[2] on the device: lr, step) stands
+    in for lr and step in calls that are captured and replayed."""
+    ps, dev, p, counts = _each(params, "params", dtypes=DTYPES)
+    gs, _, g, _ = _each(grads, "grads", dev, DTYPES, counts)
+    m, v, scales = _moments(state, dev, counts)
+    written = [t.data_ptr() for t in ps if t.numel()]
+    if len(set(written)) != len(written):
+        raise ValueError("params must not hold a tensor twice")
+    copies = codes = None
+    if state["copies"] is not None:
+        cs, _, copies, _ = _each(state["copies"], "copies", dev, (torch.bfloat16, torch.float16), counts)
+        codes = _codes(cs)
+    decay = [float(weight_decay)] * len(ps) if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
+    if len(decay) != len(ps):
+        raise ValueError("weight_decay must be a number or one for each tensor")
+    if len(betas) != 2:
+        raise ValueError("betas must be two numbers")
+    if grad_scale is not None:
+        _vector(grad_scale, torch.float32, 1, dev, "grad_scale")
+    if schedule is not None:
+        _vector(schedule, torch.float64, 2, dev, "schedule")
+    hyper = AdamwParams(float(lr), float(betas[0]), float(betas[1]), float(eps), int(step))
+    _check(lib().pace_adamw(len(ps), _sizes(counts), p, _codes(ps), g, _codes(gs), state["bits"], m, v, scales, copies, codes,
+                            (ctypes.c_float * max(len(decay), 1))(*decay), ctypes.byref(hyper), _ptr(grad_scale), _ptr(schedule),
+                            _stream(dev, stream)), "pace_adamw")
+    return params
+
+
+def pace_adamw_unpack(state, out=None, stream=None):
+    """The values that moments in 8 bits stand for. Returns (exp_avg, exp_avg_sq), two lists of float32 tensors (``out``, where
+    it is given)."""
+    if state["bits"] != 8:
+        raise ValueError("the moments must be held in 8 bits")
+    ts, dev, _, counts = _each(state["exp_avg"], "exp_avg", dtypes=(torch.int8,))
+    m, v, scales = _moments(state, dev, counts)
+    if out is None:
+        e = _allocator(dev, stream)
+        out = [[e(t.shape, torch.float32) for t in ts] for _ in range(2)]
+    m_out, v_out = (_each(o, "out", dev, (torch.float32,), counts)[2] for o in out)
+    _check(lib().pace_adamw_unpack(len(ts), _sizes(counts), m, v, scales, m_out, v_out, _stream(dev, stream)), "pace_adamw_unpack")
+    return out[0], out[1]
 
 
 def pace_time_next_kernel(phase: int, start=None, stop=None):

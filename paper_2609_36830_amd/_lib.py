@@ -16,6 +16,12 @@ class PaceParams(ctypes.Structure):
                 ("r_max", ctypes.c_double)]
 
 
+class AdamwParams(ctypes.Structure):
+    """Mirror of ``pace_adamw_params``."""
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("step", ctypes.c_int64)]
+
+
 # (name, restype, argtypes) of every exported entry point.
 P, i64, i32, d, sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_double, ctypes.c_size_t
 SIGNATURES = [
@@ -51,6 +57,13 @@ SIGNATURES = [
     ("pace_matmul_i8", ctypes.c_int, [P, i64, P, P, i64, P, i64, i64, i64, P, ctypes.c_int, i64, P, sz, P]),
     ("pace_orthogonalize_workspace_bytes", ctypes.c_int, [i64, i64, i64, P]),
     ("pace_orthogonalize", ctypes.c_int, [P, ctypes.c_int, i64, i64, i64, i64, i64, ctypes.c_int, P, d, P, P, sz, P]),
+    ("pace_layer_norm", ctypes.c_int, [P, ctypes.c_int, i64, i64, i64, P, P, ctypes.c_int, d, P, i64, P, P]),
+    ("pace_layer_norm_backward_workspace_bytes", ctypes.c_int, [i64, i64, P]),
+    ("pace_layer_norm_backward", ctypes.c_int, [P, ctypes.c_int, i64, i64, i64, P, ctypes.c_int, P, P, i64, P, i64, P, P, P, sz, P]),
+    ("pace_grad_norm_workspace_bytes", ctypes.c_int, [i64, i64, P]),
+    ("pace_grad_norm", ctypes.c_int, [i64, P, P, P, d, P, P, P, sz, P]),
+    ("pace_adamw", ctypes.c_int, [i64, P, P, P, P, P, ctypes.c_int, P, P, P, P, P, P, P, P, P, P]),
+    ("pace_adamw_unpack", ctypes.c_int, [i64, P, P, P, P, P, P, P]),
     ("pace_time_next_kernel", ctypes.c_int, [ctypes.c_int, P, P]),
     ("pace_strerror", ctypes.c_char_p, [ctypes.c_int]),
 ]

@@ -8,6 +8,7 @@
 #include <stdint.h>
 
 #include <tuple>
+#include <type_traits>
 
 #include "rules.hpp"
 
@@ -365,6 +366,42 @@ size_t ortho_ws_most(int64_t batch, int64_t rows, int64_t cols);
 hipError_t launch_orthogonalize(const void *g, int dtype, int64_t batch, int64_t rows, int64_t cols, int64_t stride,
                                 int64_t batch_stride, int steps, const double *coefs, double eps, void *out, void *ws,
                                 hipStream_t stream);
+
+// ---- layer norm ---------------------------------------------------------------------
+hipError_t launch_layer_norm(const void *x, int dtype, int64_t rows, int64_t cols, int64_t stride, const void *weight,
+                             const void *bias, int weight_dtype, double eps, void *out, int64_t out_stride, float *stats,
+                             hipStream_t stream);
+size_t layer_norm_backward_ws_bytes(int64_t rows, int64_t cols);
+size_t layer_norm_backward_ws_most(int64_t rows, int64_t cols);
+hipError_t launch_layer_norm_backward(const void *x, int dtype, int64_t rows, int64_t cols, int64_t stride, const void *weight,
+                                      int weight_dtype, const float *stats, const void *dy, int64_t dy_stride, void *dx,
+                                      int64_t dx_stride, float *dw, float *db, void *ws, hipStream_t stream);
+
+// ---- gradient norm and AdamW -----------------------------------------------------------
+// Arrays of a call, on the host: one entry a tensor. Null where a call has none of a kind.
+struct Tensors {
+    int64_t n;
+    const int64_t *sizes;
+    void *const *params;
+    const int32_t *param_dtypes;
+    const void *const *grads;
+    const int32_t *grad_dtypes;
+    void *const *m, *const *v;
+    float *const *scales;
+    void *const *copies;
+    const int32_t *copy_dtypes;
+    const float *decay;
+};
+struct AdamHyper {
+    double lr, beta1, beta2, eps, keep1, keep2;      // keep: 1 - beta^step, where there is no schedule
+    const float *factor;                             // of the gradients; null: 1
+    const double *schedule;                          // {lr, step} on the device, or null
+};
+size_t grad_norm_ws_bytes(const Tensors &t);
+size_t grad_norm_ws_most(int64_t n_tensors, int64_t n_elements);
+hipError_t launch_grad_norm(const Tensors &t, double max_norm, float *norm, float *factor, void *ws, hipStream_t stream);
+hipError_t launch_adamw(const Tensors &t, int bits, const AdamHyper &h, hipStream_t stream);
+hipError_t launch_adamw_unpack(const Tensors &t, float *const *m_out, float *const *v_out, hipStream_t stream);
 
 // ---- validate --------------------------------------------------------------
 hipError_t launch_validate(const int32_t *tags, const int64_t *offsets, int64_t n, int64_t n_tokens,

@@ -716,6 +716,137 @@ int pace_orthogonalize(const void *update, int dtype, int64_t batch, int64_t row
                                            workspace, (hipStream_t)stream));
 }
 
+// Whole numbers up to this are binary32 numbers, and a grid's workgroups of 64 columns fit.
+static bool layer_norm_ok(const void *x, int dtype, int64_t rows, int64_t cols, int64_t stride, int weight_dtype) {
+    return rows_ok(x, dtype, rows, cols, stride) && cols <= kLnColsMax && (weight_dtype == dtype || weight_dtype == kF32);
+}
+
+int pace_layer_norm(const void *x, int dtype, int64_t n_rows, int64_t n_cols, int64_t row_stride, const void *weight,
+                    const void *bias, int weight_dtype, double eps, void *out, int64_t out_stride, float *stats_out,
+                    void *stream) {
+    const TimerScope timers;
+    if (!layer_norm_ok(x, dtype, n_rows, n_cols, row_stride, weight_dtype) || !rows_ok(out, dtype, n_rows, n_cols, out_stride))
+        return PACE_ERR_INVALID_ARG;
+    if (!aligned(weight, elem_bytes_of(weight_dtype)) || !aligned(bias, elem_bytes_of(weight_dtype)) || !aligned(stats_out, 4))
+        return PACE_ERR_INVALID_ARG;
+    if (!(eps >= 1e-30 && eps <= 1e30)) return PACE_ERR_INVALID_ARG;
+    return hip_status(launch_layer_norm(x, dtype, n_rows, n_cols, row_stride, weight, bias, weight_dtype, eps, out, out_stride,
+                                        stats_out, (hipStream_t)stream));
+}
+
+int pace_layer_norm_backward_workspace_bytes(int64_t n_rows, int64_t n_cols, size_t *bytes_out) {
+    if (!bytes_out || n_rows < 0 || n_rows >= INT32_MAX || n_cols < 1 || n_cols > kLnColsMax) return PACE_ERR_INVALID_ARG;
+    *bytes_out = layer_norm_backward_ws_most(n_rows, n_cols);
+    return PACE_OK;
+}
+
+int pace_layer_norm_backward(const void *x, int dtype, int64_t n_rows, int64_t n_cols, int64_t row_stride, const void *weight,
+                             int weight_dtype, const float *stats, const void *grad_out, int64_t grad_out_stride,
+                             void *grad_x_out, int64_t grad_x_stride, float *grad_weight_out, float *grad_bias_out,
+                             void *workspace, size_t workspace_bytes, void *stream) {
+    const TimerScope timers;
+    if (!layer_norm_ok(x, dtype, n_rows, n_cols, row_stride, weight_dtype) ||
+        !rows_ok(grad_out, dtype, n_rows, n_cols, grad_out_stride) || !rows_ok(grad_x_out, dtype, n_rows, n_cols, grad_x_stride))
+        return PACE_ERR_INVALID_ARG;
+    if (n_rows > 0 && !stats) return PACE_ERR_INVALID_ARG;
+    // In place only element for element.
+    if (n_rows > 0 && (grad_x_out == x || (grad_x_out == grad_out && grad_x_stride != grad_out_stride))) return PACE_ERR_INVALID_ARG;
+    if (!aligned(weight, elem_bytes_of(weight_dtype)) || !aligned(stats, 4) || !aligned(grad_weight_out, 4) || !aligned(grad_bias_out, 4))
+        return PACE_ERR_INVALID_ARG;
+    if ((grad_weight_out || grad_bias_out) &&
+        (!workspace || !aligned(workspace, 256) || workspace_bytes < layer_norm_backward_ws_bytes(n_rows, n_cols)))
+        return PACE_ERR_WORKSPACE;
+    return hip_status(launch_layer_norm_backward(x, dtype, n_rows, n_cols, row_stride, weight, weight_dtype, stats, grad_out,
+                                                 grad_out_stride, grad_x_out, grad_x_stride, grad_weight_out, grad_bias_out,
+                                                 workspace, (hipStream_t)stream));
+}
+
+// Sizes within the limit, together too, and a pointer aligned to its element for each tensor that is not empty.
+static bool sizes_ok(int64_t n, const int64_t *sizes) {
+    if (n < 0 || n >= INT32_MAX || (n > 0 && !sizes)) return false;
+    int64_t total = 0;
+    for (int64_t i = 0; i < n; ++i) {
+        if (sizes[i] < 0 || sizes[i] > kAdamElementsMax || total > INT64_MAX / 4) return false;
+        total += sizes[i];
+    }
+    return true;
+}
+static bool each_ok(int64_t n, const int64_t *sizes, const void *const *p, const int32_t *dtypes, uintptr_t bytes) {
+    if (n > 0 && !p) return false;
+    for (int64_t i = 0; i < n; ++i) {
+        if (dtypes && (dtypes[i] < 0 || dtypes[i] >= kElemTypes)) return false;
+        if (sizes[i] > 0 && (!p[i] || !aligned(p[i], dtypes ? (uintptr_t)elem_bytes_of(dtypes[i]) : bytes))) return false;
+    }
+    return true;
+}
+
+int pace_grad_norm_workspace_bytes(int64_t n_tensors, int64_t n_elements, size_t *bytes_out) {
+    if (!bytes_out || n_tensors < 0 || n_tensors >= INT32_MAX || n_elements < 0 || n_elements > INT64_MAX / 4)
+        return PACE_ERR_INVALID_ARG;
+    *bytes_out = grad_norm_ws_most(n_tensors, n_elements);
+    return PACE_OK;
+}
+
+int pace_grad_norm(int64_t n_tensors, const void *const *grads, const int32_t *grad_dtypes, const int64_t *sizes, double max_norm,
+                   float *norm_out, float *factor_out, void *workspace, size_t workspace_bytes, void *stream) {
+    const TimerScope timers;
+    if (!sizes_ok(n_tensors, sizes) || (n_tensors > 0 && !grad_dtypes) || !each_ok(n_tensors, sizes, grads, grad_dtypes, 0))
+        return PACE_ERR_INVALID_ARG;
+    if (!(max_norm >= 0.0) || (!norm_out && !factor_out) || !aligned(norm_out, 4) || !aligned(factor_out, 4)) return PACE_ERR_INVALID_ARG;
+    Tensors t = {};
+    t.n = n_tensors, t.sizes = sizes, t.grads = grads, t.grad_dtypes = grad_dtypes;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < grad_norm_ws_bytes(t)) return PACE_ERR_WORKSPACE;
+    return hip_status(launch_grad_norm(t, max_norm, norm_out, factor_out, workspace, (hipStream_t)stream));
+}
+
+int pace_adamw(int64_t n_tensors, const int64_t *sizes, void *const *params, const int32_t *param_dtypes, const void *const *grads,
+               const int32_t *grad_dtypes, int state_bits, void *const *exp_avg, void *const *exp_avg_sq, float *const *scales,
+               void *const *copies, const int32_t *copy_dtypes, const float *weight_decay, const pace_adamw_params *hyper,
+               const float *grad_scale, const double *schedule, void *stream) {
+    const TimerScope timers;
+    if (!hyper || (state_bits != 32 && state_bits != 8) || !sizes_ok(n_tensors, sizes)) return PACE_ERR_INVALID_ARG;
+    if (n_tensors > 0 && (!param_dtypes || !grad_dtypes)) return PACE_ERR_INVALID_ARG;
+    const uintptr_t moment = state_bits == 32 ? 4 : 1;
+    if (!each_ok(n_tensors, sizes, params, param_dtypes, 0) || !each_ok(n_tensors, sizes, grads, grad_dtypes, 0) ||
+        !each_ok(n_tensors, sizes, exp_avg, nullptr, moment) || !each_ok(n_tensors, sizes, exp_avg_sq, nullptr, moment))
+        return PACE_ERR_INVALID_ARG;
+    if (state_bits == 8 && !each_ok(n_tensors, sizes, (const void *const *)scales, nullptr, 4)) return PACE_ERR_INVALID_ARG;
+    for (int64_t i = 0; i < n_tensors; ++i) {
+        if (copies && copies[i] && (!copy_dtypes || (copy_dtypes[i] != kBf16 && copy_dtypes[i] != kF16) || !aligned(copies[i], 2)))
+            return PACE_ERR_INVALID_ARG;
+        if (weight_decay && !(weight_decay[i] >= 0.0f && weight_decay[i] <= 1e30f)) return PACE_ERR_INVALID_ARG;
+    }
+    const double b1 = hyper->beta1, b2 = hyper->beta2;
+    if (!(b1 >= 0.0 && b1 < 1.0) || !(b2 >= 0.0 && b2 < 1.0) || !(hyper->eps >= 1e-30 && hyper->eps <= 1e30)) return PACE_ERR_INVALID_ARG;
+    if (!aligned(grad_scale, 4) || !aligned(schedule, 8)) return PACE_ERR_INVALID_ARG;
+    AdamHyper h = {0.0, b1, b2, hyper->eps, 1.0, 1.0, grad_scale, schedule};
+    if (!schedule) {
+        if (!isfinite(hyper->lr) || hyper->step < 1) return PACE_ERR_INVALID_ARG;
+        h.lr = hyper->lr;
+        h.keep1 = 1.0 - pow(b1, (double)hyper->step);
+        h.keep2 = 1.0 - pow(b2, (double)hyper->step);
+    }
+    const Tensors t = {n_tensors, sizes, params, param_dtypes, grads, grad_dtypes, exp_avg, exp_avg_sq, scales, copies, copy_dtypes, weight_decay};
+    return hip_status(launch_adamw(t, state_bits, h, (hipStream_t)stream));
+}
+
+int pace_adamw_unpack(int64_t n_tensors, const int64_t *sizes, const int8_t *const *exp_avg, const uint8_t *const *exp_avg_sq,
+                      const float *const *scales, float *const *exp_avg_out, float *const *exp_avg_sq_out, void *stream) {
+    const TimerScope timers;
+    if (!sizes_ok(n_tensors, sizes) || (!exp_avg_out && !exp_avg_sq_out && n_tensors > 0)) return PACE_ERR_INVALID_ARG;
+    if (!each_ok(n_tensors, sizes, (const void *const *)exp_avg, nullptr, 1) || !each_ok(n_tensors, sizes, (const void *const *)exp_avg_sq, nullptr, 1) ||
+        !each_ok(n_tensors, sizes, (const void *const *)scales, nullptr, 4))
+        return PACE_ERR_INVALID_ARG;
+    if ((exp_avg_out && !each_ok(n_tensors, sizes, (const void *const *)exp_avg_out, nullptr, 4)) ||
+        (exp_avg_sq_out && !each_ok(n_tensors, sizes, (const void *const *)exp_avg_sq_out, nullptr, 4)))
+        return PACE_ERR_INVALID_ARG;
+    Tensors t = {};
+    t.n = n_tensors, t.sizes = sizes;
+    t.m = (void *const *)exp_avg, t.v = (void *const *)exp_avg_sq, t.scales = (float *const *)scales;
+    return hip_status(launch_adamw_unpack(t, exp_avg_out, exp_avg_sq_out, (hipStream_t)stream));
+}
+
+static_assert(PACE_ADAMW_BLOCK == kAdamBlock, "elements of a scale");
 static_assert(PACE_PHASE_COUNT == kPhaseCount, "phase count");
 
 int pace_time_next_kernel(int phase, void *start_event, void *stop_event) {

@@ -249,4 +249,65 @@ inline int64_t logprob_backward_parts(int64_t rows, int64_t vocab) {
     return most < 1 ? 1 : (parts < most ? parts : most);
 }
 
+// ---- layer norm (layer_norm.hip) --------------------------------------------------
+// Lanes that hold a row, kLnPer elements each; wider rows than the largest
+// workgroup holds are read once for each step.
+constexpr int kLnPer = 16;
+constexpr int64_t kLnRegister = 16384, kLnColsMax = (int64_t)1 << 24;
+constexpr int layer_norm_lanes(int64_t cols) {
+    int lanes = 16;
+    while ((int64_t)lanes * kLnPer < cols && lanes < 1024) lanes *= 2;
+    return lanes;
+}
+// Rows that a workgroup of the backward pass has at once.
+constexpr int layer_norm_backward_rows(int lanes) { return lanes >= 512 ? 1 : 512 / lanes; }
+// Column sums that the backward pass writes and adds up afterwards: one a workgroup, as many
+// workgroups as the chip holds, but no chain of more than kLnChain rows.
+constexpr int64_t kLnChain = 1024, kLnWideParts = 64, kLnWidePartsMax = 65535;
+inline int64_t layer_norm_register_parts(int64_t rows, int lanes) {
+    const int64_t at_once = layer_norm_backward_rows(lanes), need = (rows + at_once - 1) / at_once;
+    const int64_t fill = lanes > 512 ? 256 : 512, chain = (rows + at_once * kLnChain - 1) / (at_once * kLnChain);
+    const int64_t parts = need < fill ? need : fill;
+    return parts > chain ? parts : chain;
+}
+inline int64_t layer_norm_wide_parts(int64_t rows) {
+    const int64_t parts = rows < kLnWideParts ? rows : kLnWideParts, chain = (rows + kLnChain - 1) / kLnChain;
+    return parts > chain ? parts : (chain < kLnWidePartsMax ? chain : kLnWidePartsMax);
+}
+inline int64_t layer_norm_backward_parts(int64_t rows, int64_t cols) {
+    return cols > kLnRegister ? layer_norm_wide_parts(rows) : layer_norm_register_parts(rows, layer_norm_lanes(cols));
+}
+// No fewer floats than the parts of any rows and columns up to these take.
+inline int64_t layer_norm_part_floats_most(int64_t rows, int64_t cols) {
+    int64_t most = 0;
+    for (int lanes = 16;; lanes *= 2) {
+        const bool wide = lanes > 1024;
+        const int64_t widest = wide || cols < (int64_t)lanes * kLnPer ? cols : (int64_t)lanes * kLnPer;
+        const int64_t parts = wide ? layer_norm_wide_parts(rows) : layer_norm_register_parts(rows, lanes);
+        const int64_t floats = parts * 2 * ((widest + 3) / 4 * 4);
+        most = floats > most ? floats : most;
+        if (wide || cols <= (int64_t)lanes * kLnPer) return most;
+    }
+}
+
+// ---- gradient norm and AdamW (adamw.hip) -----------------------------------------------
+// Elements of a tensor that a workgroup squares and adds: at most 4096 sums to
+// join, or as many as of the longest there are.
+constexpr int64_t kNormChunkMin = 8192, kNormChunkMax = 65536, kNormSlots = 4096;
+inline int64_t grad_norm_chunk(int64_t n_elements) {
+    int64_t chunk = kNormChunkMin;
+    while (chunk < kNormChunkMax && n_elements / chunk > kNormSlots) chunk *= 2;
+    return chunk;
+}
+// No fewer sums than any tensors of at most this number and these elements together have.
+inline int64_t grad_norm_slots_most(int64_t n_tensors, int64_t n_elements) {
+    const int64_t most = kNormSlots > n_elements / kNormChunkMax ? kNormSlots : n_elements / kNormChunkMax;
+    const int64_t whole = n_elements / kNormChunkMin;
+    return n_tensors + (whole < most ? whole : most);
+}
+// Elements that a workgroup updates, and those that share the scales of moments in 8 bits.
+constexpr int64_t kAdamChunk = 4096, kAdamBlock = 256;
+// Tensors of a call together, so that their workgroups are numbered in 32 bits; longer tensors are refused.
+constexpr int64_t kAdamElementsMax = (int64_t)1 << 35;
+
 }  // namespace pace

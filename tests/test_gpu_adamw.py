@@ -1,0 +1,409 @@
+"""GPU tests of the gradients' norm and of AdamW over many tensors, against the formulas in 64 bits.
+
+Tolerances count roundings, u = 2^-24; codes of moments in 8 bits have to be equal."""
+import math
+import sys
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+INF, NAN = float("inf"), float("nan")
+BLOCK = 256
+
+
+def say(msg):
+    sys.stdout.write("[gpu] %s\n" % msg)
+    sys.stdout.flush()
+
+
+@pytest.fixture(scope="module")
+def pace():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import os
+    from paper_2609_36830_amd import _lib
+    if not os.path.exists(_lib.library_path):
+        from paper_2609_36830_amd import build
+        build.build()
+    import paper_2609_36830_amd as pace
+    return pace
+
+
+def tensors(sizes, dtypes, seed, scale=1.0, odd=False):
+    """Random tensors; with `odd` each starts one element behind an aligned address."""
+    g = torch.Generator(DEV).manual_seed(seed)
+    got = []
+    for k, n in enumerate(sizes):
+        dt = dtypes[k % len(dtypes)]
+        size = torch.exp(1.5 * torch.randn(n, generator=g, device=DEV))
+        t = torch.empty(n + 1, dtype=dt, device=DEV)[1:] if odd else torch.empty(n, dtype=dt, device=DEV)
+        got.append(t.copy_(scale * size * torch.randn(n, generator=g, device=DEV)))
+    return got
+
+
+# ---- the norm -----------------------------------------------------------------------
+def norm_of(ts):
+    return math.sqrt(sum(float(t.double().square().sum()) for t in ts))
+
+
+@pytest.mark.parametrize("sizes", [[1], [0, 5, 0], [7, 8192, 8193, 1, 0, 65537], list(range(300)), [3000000, 17], [40000001]])
+@pytest.mark.parametrize("dtypes", [(F32,), (BF16,), (F16, F32, BF16)])
+@pytest.mark.parametrize("odd", [False, True])
+def test_norm(pace, sizes, dtypes, odd):
+    say("gradient norm of %d tensors %s" % (len(sizes), dtypes))
+    g = tensors(sizes, dtypes, 1, 0.01, odd)
+    ref = norm_of(g)
+    for most in (INF, 0.0, ref / 3, ref * 3):
+        norm, factor = pace.pace_grad_norm(g, most)
+        # sums in 64 bits: the roundings to binary32 are all that shows
+        assert abs(float(norm) - ref) <= 1.01 * U * ref
+        want = 1.0 if ref <= most else most / ref
+        assert abs(float(factor) - want) <= 1.01 * U * want
+
+
+def test_norm_of_large_small_and_no_numbers(pace):
+    say("gradient norm at the ends of the range")
+    for value, n in ((1e30, 1000), (1e-30, 1000), (3e38, 2), (1e-40, 100)):
+        g = [torch.full((n,), value, device=DEV)]
+        norm, factor = pace.pace_grad_norm(g, 1.0)
+        ref = float(g[0][0].double()) * math.sqrt(n)
+        assert (float(norm) == INF if ref > 3.5e38 else abs(float(norm) - ref) <= 1.01 * U * ref + 1e-45)
+        assert abs(float(factor) - min(1.0, 1.0 / ref)) <= 1.01 * U * min(1.0, 1.0 / ref) + 1e-45
+    g = tensors([5000, 9000, 3], (BF16,), 2)
+    for value in (INF, -INF, NAN):
+        g[1][8999] = value
+        norm, factor = pace.pace_grad_norm(g, 1.0)
+        assert not math.isfinite(float(norm)) and math.isnan(float(factor))
+    norm, factor = pace.pace_grad_norm([torch.empty(0, device=DEV)], 1.0)
+    assert float(norm) == 0.0 and float(factor) == 1.0
+
+
+def test_norm_in_a_workspace_of_more(pace):
+    say("gradient norms in one workspace")
+    k = pace.grad_norm_buffers(50, 5000000, DEV)
+    for sizes in ([5000000], [100000] * 50, [1] * 50, [33], [4999951] + [1] * 49):
+        g = tensors(sizes, (F32,), 3)
+        k["workspace"].fill_(255)
+        got = [float(v) for v in pace.pace_grad_norm(g, 1.0, buffers=k)]
+        assert got == [float(v) for v in pace.pace_grad_norm(g, 1.0)]
+    with pytest.raises(pace.PaceError):
+        pace.pace_grad_norm(tensors([5000000], (F32,), 3), buffers=dict(k, workspace=k["workspace"][:256]))
+
+
+# ---- AdamW ----------------------------------------------------------------------------
+HYPER = dict(lr=3e-3, betas=(0.9, 0.99), eps=1e-8)
+
+
+def decoded(mc, vc, scale):
+    s = scale.double().repeat_interleave(BLOCK, 0)[: mc.numel()]
+    c, d = mc.double().flatten(), vc.double().flatten()
+    return c * c.abs() / 127.0 ** 2 * s[:, 0], (d / 255.0) ** 4 * s[:, 1]
+
+
+def encoded(m, v):
+    """Codes of moments in 64 bits and the largest that they go by, a tensor's last block filled up with zeros."""
+    n = m.numel()
+    m, v = (torch.nn.functional.pad(t, (0, -n % BLOCK)).view(-1, BLOCK) for t in (m, v))
+    to = torch.stack([m.abs().amax(1), v.amax(1)], 1)
+    to = torch.where(to < 2.0 ** -126, 0.0, to)
+    cm = torch.where(to[:, :1] > 0, (127 * (m.abs() / to[:, :1]).sqrt()).round(), 0.0) * m.sign()
+    cv = torch.where(to[:, 1:] > 0, (255 * (v / to[:, 1:]).sqrt().sqrt()).round(), 0.0)
+    cv = torch.where((v > 0) & (to[:, 1:] > 0), cv.clamp(min=1), cv)
+    return cm.to(torch.int8).flatten()[:n], cv.to(torch.uint8).flatten()[:n], to
+
+
+def near_scales(got, scale):
+    """One rounding: the largest moments in 64 bits are within a few 2^-53 of each other."""
+    return bool(((got.double() - scale).abs() <= 1.01 * U * scale).all())
+
+
+class Reference:
+    """A step in 64 bits of each tensor, from the same binary values."""
+
+    def __init__(self, params, grads, state, step, decay, factor=1.0, lr=HYPER["lr"], betas=HYPER["betas"], eps=HYPER["eps"]):
+        self.p, self.off, self.m, self.v, self.m_off = [], [], [], [], []
+        for k, (p, g) in enumerate(zip(params, grads)):
+            g = g.double() * factor
+            if state["bits"] == 8:
+                m, v = decoded(state["exp_avg"][k], state["exp_avg_sq"][k], state["scale"][k])
+                m, v = m.view(p.shape), v.view(p.shape)
+            else:
+                m, v = state["exp_avg"][k].double(), state["exp_avg_sq"][k].double()
+            sizes = betas[0] * m.abs() + (1 - betas[0]) * g.abs()
+            m, v = betas[0] * m + (1 - betas[0]) * g, betas[1] * v + (1 - betas[1]) * g * g
+            keep, size = 1 - lr * decay[k], lr / (1 - betas[0] ** step)
+            div = (v / (1 - betas[1] ** step)).sqrt() + eps
+            to = p.double() * keep - size * m / div
+            # m is within 4 u of its terms' sizes; the quotient adds 12 u: v 5 (halved), root, its factor twice, sum, division, size twice
+            off = abs(size) / div * (4 * U * sizes + 12 * U * m.abs()) + 3 * U * (p.double() * keep).abs() + U * to.abs() + 1e-44
+            self.p.append(to)
+            self.off.append(off)
+            self.m.append(m)
+            self.v.append(v)
+            self.m_off.append(4 * U * sizes + 1e-44)
+
+
+def half_step(v, dtype):
+    info = torch.finfo(dtype)
+    return info.eps / 2 * v.abs() + info.smallest_normal * info.eps / 2
+
+
+def random_state(pace, params, bits, copy_dtype=None, seed=5):
+    """Moments as a running model has them: v near the gradients' squares."""
+    state = pace.adamw_state(params, bits, copy_dtype)
+    g = torch.Generator(DEV).manual_seed(seed)
+    for k, p in enumerate(params):
+        size = torch.exp(torch.randn(p.numel(), generator=g, device=DEV))
+        m = 0.3 * size * torch.randn(p.numel(), generator=g, device=DEV)
+        v = size.square() * torch.exp(torch.randn(p.numel(), generator=g, device=DEV))
+        if bits == 8:
+            mc, vc, scale = encoded(m.double(), v.double())
+            state["exp_avg"][k].copy_(mc), state["exp_avg_sq"][k].copy_(vc), state["scale"][k].copy_(scale)
+        else:
+            state["exp_avg"][k].copy_(m), state["exp_avg_sq"][k].copy_(v)
+    return state
+
+
+def check(params, state, ref, copies=None):
+    for k, p in enumerate(params):
+        assert ((p.double() - ref.p[k]).abs() <= ref.off[k] + half_step(ref.p[k], p.dtype)).all(), k
+        if copies is not None:
+            c = copies[k]
+            assert ((c.double() - ref.p[k]).abs() <= ref.off[k] * 1.01 + half_step(ref.p[k], c.dtype) * 1.01 + half_step(ref.p[k], p.dtype)).all()
+        if state["bits"] == 8:
+            mc, vc, scale = encoded(ref.m[k].flatten(), ref.v[k].flatten())
+            assert near_scales(state["scale"][k], scale), k
+            assert torch.equal(state["exp_avg"][k].flatten(), mc), (k, (state["exp_avg"][k].flatten() != mc).nonzero()[:5])
+            assert torch.equal(state["exp_avg_sq"][k].flatten(), vc), (k, (state["exp_avg_sq"][k].flatten() != vc).nonzero()[:5])
+        else:
+            assert ((state["exp_avg"][k].double() - ref.m[k]).abs() <= ref.m_off[k]).all()
+            assert ((state["exp_avg_sq"][k].double() - ref.v[k]).abs() <= 5 * U * ref.v[k] + 1e-44).all()
+
+
+SIZES = [[1], [255], [256], [257], [4095], [4096], [4097], [0, 3, 0], [10000, 1, 300, 70001], list(range(1, 131)), [1000003]]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("param, grad, copy", [(F32, F32, None), (F32, BF16, BF16), (F32, F16, F16), (BF16, BF16, None), (BF16, F32, None), (F16, F16, None)])
+@pytest.mark.parametrize("sizes", SIZES, ids=lambda s: "%dx%d" % (len(s), max(s)))
+def test_steps(pace, sizes, param, grad, copy, bits):
+    """Two steps from a running state."""
+    say("adamw %d bits, %d tensors of up to %d, %s %s %s" % (bits, len(sizes), max(sizes), param, grad, copy))
+    params = tensors(sizes, (param,), 6, 0.05, odd=len(sizes) == 4)
+    grads = tensors(sizes, (grad,), 7, 1.0, odd=len(sizes) == 4)
+    state = random_state(pace, params, bits, copy)
+    decay = [0.1 * (k % 3) for k in range(len(sizes))]
+    decay = [float(torch.tensor(w, dtype=F32)) for w in decay]           # given in binary32
+    for step in (4, 5):
+        ref = Reference(params, grads, state, step, decay)
+        pace.pace_adamw(params, grads, state, step=step, weight_decay=decay, **HYPER)
+        check(params, state, ref, state["copies"])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_types_together(pace, bits):
+    """Tensors of every pair of types in one call, more than one table of them."""
+    say("adamw %d bits, mixed types" % bits)
+    sizes = [1 + 37 * k % 900 for k in range(180)]
+    params, grads = tensors(sizes, (F32, BF16, F16), 8, 0.05), tensors(sizes, (F32,) * 3 + (BF16,) * 3 + (F16,) * 3, 9)
+    state = random_state(pace, params, bits)
+    ref = Reference(params, grads, state, 3, [0.0] * 180)
+    pace.pace_adamw(params, grads, state, step=3, **HYPER)
+    check(params, state, ref)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_first_steps_of_a_fresh_state(pace, bits):
+    say("adamw %d bits from zeros" % bits)
+    params = [torch.randn(3, 100, 7, device=DEV), torch.randn(1, device=DEV)]
+    grads = [torch.randn(3, 100, 7, device=DEV), torch.zeros(1, device=DEV)]
+    state = pace.adamw_state(params, bits)
+    before = params[1].clone()
+    for step in (1, 2, 3):
+        ref = Reference(params, grads, state, step, [0.0, 0.0])
+        pace.pace_adamw(params, grads, state, step=step, **HYPER)
+        check(params, state, ref)
+        assert torch.equal(params[1], before)        # nothing over nothing: eps
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_clipped_by_the_norm(pace, bits):
+    """The factor that pace_grad_norm leaves on the device."""
+    say("adamw %d bits, clipped" % bits)
+    sizes = [5000, 70, 300]
+    params, grads = tensors(sizes, (F32,), 10), tensors(sizes, (BF16,), 11)
+    state = random_state(pace, params, bits)
+    _, factor = pace.pace_grad_norm(grads, 0.7)
+    ref = Reference(params, grads, state, 9, [0.0] * 3, factor=float(factor))
+    pace.pace_adamw(params, grads, state, step=9, grad_scale=factor, **HYPER)
+    assert 0 < float(factor) < 0.1
+    check(params, state, ref)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_factor_that_is_no_number_leaves_everything(pace, bits):
+    say("adamw %d bits, skipped" % bits)
+    sizes = [5000, 70]
+    params, grads = tensors(sizes, (F32,), 12), tensors(sizes, (BF16,), 13)
+    state = random_state(pace, params, bits, BF16)
+    for c in state["copies"]:
+        c.fill_(5.0)
+    everything = lambda: params + state["exp_avg"] + state["exp_avg_sq"] + (state["scale"] or []) + state["copies"]
+    before = [t.clone() for t in everything()]
+    grads[1][3] = INF
+    _, factor = pace.pace_grad_norm(grads, 1.0)
+    pace.pace_adamw(params, grads, state, step=2, grad_scale=factor, **HYPER)
+    for bad in (INF, -INF):
+        pace.pace_adamw(params, grads, state, step=2, grad_scale=torch.tensor([bad], device=DEV), **HYPER)
+    assert all(torch.equal(a, b) for a, b in zip(everything(), before))
+
+
+def test_nan_spoils_its_block_only(pace):
+    say("adamw 8 bits, NaN")
+    params, grads = tensors([1500], (F32,), 14), tensors([1500], (F32,), 15)
+    state = random_state(pace, params, 8)
+    ref = Reference(params, grads, state, 2, [0.0])
+    grads[0][600] = NAN
+    pace.pace_adamw(params, grads, state, step=2, **HYPER)
+    mc, vc, scale = encoded(ref.m[0], ref.v[0])
+    keep = torch.ones(1500, dtype=torch.bool, device=DEV)
+    keep[600] = False
+    assert ((params[0].double() - ref.p[0]).abs() <= ref.off[0] + U * ref.p[0].abs())[keep].all() and params[0][600].isnan()
+    keep[512:768] = False
+    assert torch.equal(state["exp_avg"][0][keep], mc[keep]) and torch.equal(state["exp_avg_sq"][0][keep], vc[keep])
+    assert state["scale"][0][2].isnan().all() and near_scales(state["scale"][0][[0, 1, 3, 4, 5]], scale[[0, 1, 3, 4, 5]])
+    m, v = pace.pace_adamw_unpack(state)
+    assert m[0][512:768].isnan().all() and not m[0][keep].isnan().any() and not v[0][keep].isnan().any()
+
+
+@pytest.mark.parametrize("size", [1e-25, 1e-18, 1e-12, 1e15])
+def test_moments_in_8_bits_over_the_range(pace, size):
+    """Gradients whose squares leave binary32, or whose scales are its smallest numbers."""
+    say("adamw 8 bits at %g" % size)
+    params, grads = [torch.randn(2000, device=DEV)], [(size * torch.randn(2000, device=DEV))]
+    state = pace.adamw_state(params, 8)
+    for step in (1, 2):
+        ref = Reference(params, grads, state, step, [0.0])
+        pace.pace_adamw(params, grads, state, step=step, **HYPER)
+        mc, vc, scale = encoded(ref.m[0], ref.v[0])
+        assert near_scales(state["scale"][0], scale) and torch.equal(state["exp_avg"][0], mc) and torch.equal(state["exp_avg_sq"][0], vc)
+        assert params[0].isfinite().all()
+
+
+@pytest.mark.parametrize("sizes", [[1], [300, 0, 5000], [70001]])
+def test_unpack(pace, sizes):
+    say("adamw unpack")
+    params = tensors(sizes, (F32,), 16)
+    state = random_state(pace, params, 8)
+    m, v = pace.pace_adamw_unpack(state)
+    for k in range(len(sizes)):
+        rm, rv = decoded(state["exp_avg"][k], state["exp_avg_sq"][k], state["scale"][k])
+        assert ((m[k].double() - rm).abs() <= 1.01 * U * rm.abs() + 1e-45).all() and ((v[k].double() - rv).abs() <= 1.01 * U * rv + 1e-45).all()
+    out = ([torch.zeros(n + 1, device=DEV)[1:] for n in sizes], [torch.zeros(n + 3, device=DEV)[3:] for n in sizes])
+    pace.pace_adamw_unpack(state, out=out)
+    assert all(torch.equal(a, b) for a, b in zip(out[0] + out[1], m + v))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_captured_with_a_schedule(pace, bits):
+    """Captured once: replays go on with the rate and the step that stand in the schedule."""
+    say("adamw %d bits, captured" % bits)
+    sizes = [9000, 300, 1]
+    params, grads = tensors(sizes, (F32,), 18), tensors(sizes, (BF16,), 19)
+    twin = [p.clone() for p in params]
+    state, other = random_state(pace, params, bits), random_state(pace, params, bits)
+    schedule = torch.tensor([1e-3, 0.0], dtype=torch.float64, device=DEV)
+    k = pace.grad_norm_buffers(3, sum(sizes), DEV)
+
+    def one():
+        schedule[1:].add_(1.0)
+        _, factor = pace.pace_grad_norm(grads, 1.0, buffers=k)
+        pace.pace_adamw(params, grads, state, betas=HYPER["betas"], schedule=schedule, grad_scale=factor)
+
+    one()                                            # the first step, before the capture
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        one()
+    rates = [1e-3, 2e-3, 5e-4, 0.0]
+    for step, lr in enumerate(rates, 1):
+        if step > 1:
+            for g in grads:
+                g.mul_(0.9)
+            schedule[:1].fill_(lr)
+            graph.replay()
+        torch.cuda.synchronize()
+        _, factor = pace.pace_grad_norm(grads, 1.0)
+        pace.pace_adamw(twin, grads, other, lr=lr, step=step, betas=HYPER["betas"], grad_scale=factor)
+        # 1 - beta^t of the device is within a few 2^-53 of the host's: each of the step's two factors may differ by one place, 2 u,
+        # and the step's size be 100 lr at most (the first moments stand for 10 of their roots, divided by 0.1)
+        for a, b in zip(params, twin):
+            assert ((a - b).abs() <= step * (2 * U * b.abs() + 4 * U * 100 * max(rates))).all()
+        for key in ("exp_avg", "exp_avg_sq"):
+            assert all(torch.equal(a, b) for a, b in zip(state[key], other[key]))
+
+
+def test_same_bits_again_and_on_a_stream(pace):
+    say("adamw on a stream")
+    sizes = [100000, 7, 513]
+    got = []
+    for stream in (None, torch.cuda.Stream()):
+        params, grads = tensors(sizes, (F32,), 20), tensors(sizes, (F16,), 21)
+        torch.cuda.synchronize()
+        state = pace.adamw_state(params, 8, F16, stream=stream)
+        for step in (1, 2):
+            _, factor = pace.pace_grad_norm(grads, 1.0, stream=stream)
+            pace.pace_adamw(params, grads, state, step=step, grad_scale=factor, stream=stream)
+        m, v = pace.pace_adamw_unpack(state, stream=stream)
+        torch.cuda.synchronize()
+        got.append(params + state["exp_avg"] + state["exp_avg_sq"] + state["scale"] + state["copies"] + m + v + [factor])
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_tensor_beyond_32_bits(pace):
+    say("adamw of more than 2^31 elements")
+    n = (1 << 31) + 777
+    params, grads = [torch.zeros(n, dtype=BF16, device=DEV)], [torch.zeros(n, dtype=BF16, device=DEV)]
+    state = pace.adamw_state(params, 8)
+    near = tensors([777], (BF16,), 22)
+    grads[0][-777:] = near[0]
+    norm, factor = pace.pace_grad_norm(grads, 1.0)
+    assert float(factor) == float(pace.pace_grad_norm(near, 1.0)[1])
+    pace.pace_adamw(params, grads, state, step=1, grad_scale=factor)
+    small = [torch.zeros(777, dtype=BF16, device=DEV)]
+    other = pace.adamw_state(small, 8)
+    pace.pace_adamw(small, near, other, step=1, grad_scale=factor)
+    assert torch.equal(params[0][-777:], small[0]) and not params[0][:-777].any()
+    assert torch.equal(state["exp_avg"][0][-777:], other["exp_avg"][0]) and torch.equal(state["scale"][0][-4:], other["scale"][0])
+
+
+def test_refusals(pace):
+    say("adamw refusals")
+    p, g = [torch.zeros(10, device=DEV), torch.zeros(300, device=DEV)], [torch.zeros(10, device=DEV), torch.zeros(300, device=DEV)]
+    state = pace.adamw_state(p, 8)
+    for bad in (dict(params=[]), dict(grads=g[:1]), dict(params=[p[0], p[0].clone()]), dict(params=[p[0], p[0]], grads=[g[0], g[0]]),
+                dict(params=[p[0], p[1].cpu()]), dict(params=[p[0], p[1].double()]), dict(grads=[g[0], torch.zeros(600, device=DEV)[::2]]),
+                dict(weight_decay=[0.1]), dict(betas=(0.9,)), dict(grad_scale=torch.ones(2, device=DEV)), dict(schedule=torch.ones(2, device=DEV)),
+                dict(state=dict(state, bits=4)), dict(state=dict(state, bits=32)), dict(state=dict(state, scale=state["scale"][:1])),
+                dict(state=dict(state, exp_avg=state["exp_avg_sq"])), dict(state=dict(state, copies=[t.clone() for t in p]))):
+        with pytest.raises(ValueError):
+            pace.pace_adamw(**{**dict(params=p, grads=g, state=state), **bad})
+    for bad in (dict(step=0), dict(lr=NAN), dict(betas=(1.0, 0.9)), dict(betas=(0.9, -0.1)), dict(eps=0.0), dict(eps=INF), dict(weight_decay=-0.1),
+                dict(weight_decay=NAN)):
+        with pytest.raises(pace.PaceError):
+            pace.pace_adamw(p, g, state, **bad)
+    for bad in (dict(max_norm=-1.0), dict(max_norm=NAN)):
+        with pytest.raises(pace.PaceError):
+            pace.pace_grad_norm(g, **bad)
+    with pytest.raises(ValueError):
+        pace.pace_grad_norm([torch.zeros(3)])
+    with pytest.raises(ValueError):
+        pace.adamw_state(p, 16)
+    with pytest.raises(ValueError):
+        pace.adamw_state(p, 8, F32)
+    with pytest.raises(ValueError):
+        pace.pace_adamw_unpack(pace.adamw_state(p, 32))

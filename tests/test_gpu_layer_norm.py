@@ -1,0 +1,300 @@
+"""GPU tests of the layer norm and its backward pass against the formulas in 64 bits.
+
+Tolerances count roundings, u = 2^-24. A sum of a row's n elements goes through at most 16 additions in a lane (rows
+wider than 16384: 8, then n / 8192 more), 6 across a wave and 16 across waves, say K = 40 + n / 8192 in all, so it is
+within K u of the sum of the sizes. A result of type t adds half a step, eps(t) / 2."""
+import sys
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+def say(msg):
+    sys.stdout.write("[gpu] %s\n" % msg)
+    sys.stdout.flush()
+
+
+@pytest.fixture(scope="module")
+def pace():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import os
+    from paper_2609_36830_amd import _lib
+    if not os.path.exists(_lib.library_path):
+        from paper_2609_36830_amd import build
+        build.build()
+    import paper_2609_36830_amd as pace
+    return pace
+
+
+def matrix(rows, cols, dtype, pad=0, seed=0, scale=1.0, offset=0.0):
+    g = torch.Generator(DEV).manual_seed(seed)
+    x = scale * torch.randn(rows, cols, generator=g, device=DEV) + offset
+    if cols > 8:
+        x[:, cols // 3] *= 30.0
+    t = torch.full((rows * (cols + pad) + 8,), 7.0, dtype=dtype, device=DEV)[: rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+    return t.copy_(x)
+
+
+def half_step(v, dtype):
+    """Half a step of the type at |v|, its smallest steps included."""
+    info = torch.finfo(dtype)
+    return info.eps / 2 * v.abs() + info.smallest_normal * info.eps / 2
+
+
+def k_of(cols):
+    return 40 + cols / 8192
+
+
+def check_forward(x, w, b, eps, out, stats):
+    n = x.shape[1]
+    xd = x.double()
+    mean = xd.mean(1, keepdim=True)
+    var = (xd - mean).square().mean(1, keepdim=True)
+    rstd = (var + eps).rsqrt()
+    k, sigma = k_of(n), var.sqrt()
+    # the mean: its correction is a sum of differences, which are about sigma
+    mean_off = U * (2 * mean.abs() + (k + 4) * sigma) + 2e-45
+    assert ((stats[:, :1].double() - mean).abs() <= mean_off).all()
+    # the variance: K u of itself for the sum, 4 u for what the terms and the mean add, halved by the root; root and inverse
+    rstd_off = (k / 2 + 6) * U
+    assert ((stats[:, 1:].double() / rstd - 1).abs() <= rstd_off).all()
+    h = (xd - mean) * rstd
+    wd = torch.ones(n, device=DEV, dtype=torch.float64) if w is None else w.double()
+    bd = torch.zeros(n, device=DEV, dtype=torch.float64) if b is None else b.double()
+    y = h * wd + bd
+    # the difference: two roundings, and the mean's error without the part that its own size adds
+    off = wd.abs() * (h.abs() * (rstd_off + 4 * U) + (k + 4) * U * sigma * rstd) + 2 * U * y.abs()
+    assert ((out.double() - y).abs() <= off + half_step(y, out.dtype)).all()
+
+
+def check_backward(x, w, stats, dy, dx, dw, db):
+    rows, n = x.shape
+    mean, rstd = stats.double()[:, :1], stats.double()[:, 1:]
+    h, g = (x.double() - mean) * rstd, dy.double()
+    a = g if w is None else g * w.double()
+    c1, c2 = a.mean(1, keepdim=True), (a * h).mean(1, keepdim=True)
+    ref = rstd * (a - c1 - h * c2)
+    k = k_of(n) + 4
+    s1, s2 = a.abs().mean(1, keepdim=True), (a * h).abs().mean(1, keepdim=True)
+    off = rstd * U * (6 * a.abs() + (k + 2) * s1 + h.abs() * ((k + 8) * s2))
+    assert ((dx.double() - ref).abs() <= off + half_step(ref, dx.dtype)).all()
+    # columns: at most 1024 rows in a chain, the rows of a workgroup (32), the parts (n / 16, then 16)
+    chain = min(rows, 1024) + 32 + 64 + 16
+    assert ((dw.double() - (g * h).sum(0)).abs() <= U * (chain + 4) * (g * h).abs().sum(0) + 1e-44).all()
+    assert ((db.double() - g.sum(0)).abs() <= U * chain * g.abs().sum(0) + 1e-44).all()
+
+
+SHAPES = [(1, 1), (3, 1), (1, 7), (2, 8), (5, 15), (33, 64), (7, 127), (64, 128), (9, 255), (17, 256), (6, 257), (5, 511), (4, 513), (31, 1000),
+          (3, 1025), (2, 2047), (7, 2049), (3, 4095), (5, 4096), (2, 4097), (3, 8191), (2, 8200), (2, 16383), (3, 16384), (2, 16385), (2, 20001),
+          (1, 50000), (600, 16), (1100, 100), (5000, 130), (2100, 2049), (700, 4097), (530, 9001)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("rows, cols", SHAPES)
+def test_shapes(pace, rows, cols, dtype):
+    say("layer norm %d x %d %s" % (rows, cols, dtype))
+    same = (rows + cols) % 2 == 0
+    pad = (0, 3, 8)[rows % 3]
+    wt = dtype if same else F32
+    g = torch.Generator(DEV).manual_seed(rows)
+    w = (1 + 0.3 * torch.randn(cols, generator=g, device=DEV)).to(wt)
+    b = (0.3 * torch.randn(cols, generator=g, device=DEV)).to(wt)
+    x, dy = matrix(rows, cols, dtype, pad, seed=1, offset=0.4), matrix(rows, cols, dtype, (pad * 2) % 7, seed=2, scale=0.1)
+    out, stats = pace.pace_layer_norm(x, w, b, eps=1e-5)
+    assert out.dtype == dtype and out.shape == x.shape
+    check_forward(x, w, b, 1e-5, out, stats)
+    dx, dw, db = pace.pace_layer_norm_backward(x, stats, dy, w)
+    check_backward(x, w, stats, dy, dx, dw, db)
+
+
+@pytest.mark.parametrize("cols", [100, 4096, 17000])
+@pytest.mark.parametrize("weight, bias", [(False, False), (True, False), (False, True)])
+def test_without_weights(pace, cols, weight, bias):
+    say("layer norm without weights, %d columns" % cols)
+    x, dy = matrix(9, cols, BF16, seed=3), matrix(9, cols, BF16, seed=4)
+    w = torch.rand(cols, device=DEV) if weight else None
+    b = torch.rand(cols, device=DEV).to(BF16) if bias else None
+    out, stats = pace.pace_layer_norm(x, w, b)
+    check_forward(x, w, b, 1e-5, out, stats)
+    check_backward(x, w, stats, dy, *pace.pace_layer_norm_backward(x, stats, dy, w))
+
+
+@pytest.mark.parametrize("cols", [64, 1000, 4096, 16385])
+def test_rows_far_from_zero(pace, cols):
+    """A mean a thousand times the deviation keeps the variance: differences are taken before squares."""
+    say("layer norm far from zero, %d columns" % cols)
+    x = matrix(5, cols, F32, seed=5, scale=0.01, offset=1000.0)
+    x[:, cols // 3] = 1000.0
+    x[3] = 0.0
+    x[4] = -3.25                                     # a constant row: its variance is 0, all but the bias goes
+    out, stats = pace.pace_layer_norm(x, None, None, eps=1e-6)
+    check_forward(x, None, None, 1e-6, out, stats)
+    assert (out[3:] == 0).all() and (stats[3:, 0].cpu() == torch.tensor([0.0, -3.25])).all()
+
+
+@pytest.mark.parametrize("cols", [48, 300, 4096, 17000])
+def test_infinities_and_nan_stay_in_their_rows(pace, cols):
+    say("layer norm with infinities, %d columns" % cols)
+    x, dy = matrix(40, cols, BF16, seed=6), matrix(40, cols, BF16, seed=7)
+    clean = pace.pace_layer_norm(x)
+    y, stats = clean
+    grad = pace.pace_layer_norm_backward(x, stats, dy)[0]
+    bad = x.clone()
+    bad[7, cols // 2] = float("inf")
+    bad[20, 0] = float("nan")
+    bad[39, cols - 1] = -float("inf")
+    out, st = pace.pace_layer_norm(bad)
+    dx = pace.pace_layer_norm_backward(bad, st, dy)[0]
+    keep = torch.ones(40, dtype=torch.bool, device=DEV)
+    keep[[7, 20, 39]] = False
+    assert torch.equal(out[keep], y[keep]) and torch.equal(st[keep], stats[keep]) and torch.equal(dx[keep], grad[keep])
+    assert out[~keep].isnan().all() and dx[~keep].isnan().all()
+
+
+@pytest.mark.parametrize("cols", [100, 2049, 17000])
+def test_in_place_gradient(pace, cols):
+    say("layer norm gradient in place, %d columns" % cols)
+    x, dy = matrix(1500, cols, BF16, seed=8), matrix(1500, cols, BF16, seed=9)
+    _, stats = pace.pace_layer_norm(x)
+    ref = pace.pace_layer_norm_backward(x, stats, dy)
+    b = pace.layer_norm_buffers(1500, cols, BF16, DEV, backward=True)
+    b["grad_x"] = dy
+    got = pace.pace_layer_norm_backward(x, stats, dy, buffers=b)
+    assert all(torch.equal(p, q) for p, q in zip(got, ref))
+    with pytest.raises(pace.PaceError):              # the rows themselves are still read
+        pace.pace_layer_norm_backward(x, stats, dy, buffers=dict(b, grad_x=x))
+
+
+def test_no_rows(pace):
+    say("layer norm of no rows")
+    x = torch.empty(0, 100, device=DEV)
+    out, stats = pace.pace_layer_norm(x)
+    assert out.shape == (0, 100) and stats.shape == (0, 2)
+    dx, dw, db = pace.pace_layer_norm_backward(x, stats, x.clone())
+    assert dx.shape == (0, 100) and (dw == 0).all() and (db == 0).all()
+
+
+@pytest.mark.parametrize("rows, cols, dtype", [(3, 33, F32), (2, 1025, F32), (2, 16390, F32)])
+def test_against_differences(pace, rows, cols, dtype):
+    """The gradient against central differences of the forward pass: within what the outputs are rounded by, and what the
+    same differences in 64 bits are off the derivative."""
+    say("layer norm against differences %d x %d" % (rows, cols))
+    g = torch.Generator(DEV).manual_seed(11)
+    draw = lambda *s: torch.randn(*s, generator=g, device=DEV)
+    x, dy, w, b, eps, step = draw(rows, cols), draw(rows, cols), 1 + 0.2 * draw(cols), 0.1 * draw(cols), 1e-5, 2.0 ** -7
+    dx, dw, db = pace.pace_layer_norm_backward(x, pace.pace_layer_norm(x, w, b, eps)[1], dy, w)
+
+    def plain(x, w, b):
+        m = x.mean(1, keepdim=True)
+        return (x - m) * ((x - m).square().mean(1, keepdim=True) + eps).rsqrt() * w + b
+
+    for which, grad in enumerate((dx, dw, db)):
+        at = [x, w, b]
+        u = torch.randint(0, 2, at[which].shape, generator=g, device=DEV) * 2.0 - 1.0
+        ends = []
+        for sign in (1, -1):
+            moved = list(at)
+            moved[which] = at[which] + sign * step * u           # rounded: the direction is what was really moved
+            ends.append(moved)
+        way = (ends[0][which].double() - ends[1][which].double()) / (2 * step)
+        value = lambda y: float((dy.double() * y.double()).sum())
+        got = (value(pace.pace_layer_norm(*ends[0], eps)[0]) - value(pace.pace_layer_norm(*ends[1], eps)[0])) / (2 * step)
+        wide = (value(plain(*(t.double() for t in ends[0]))) - value(plain(*(t.double() for t in ends[1])))) / (2 * step)
+        slope = float((grad.double() * way).sum())
+        leaf = [t.double().requires_grad_(k == which) for k, t in enumerate(at)]
+        true = float((torch.autograd.grad(plain(*leaf), leaf[which], dy.double())[0] * way).sum())
+        y = plain(*(t.double() for t in at))
+        # each output of each end is off by at most 30 u (|y| + 2), as in check_forward with its K of 40; so is the gradient, relatively
+        noise = 2 * float((dy.abs() * (y.abs() + 2)).sum()) * 30 * U / (2 * step)
+        size = float((grad.double().abs() * way.abs()).sum()) + float(dy.double().abs().sum())
+        assert abs(got - slope) <= abs(wide - true) + noise + 60 * U * size, (which, got, slope, wide, true, noise)
+
+
+@pytest.mark.parametrize("rows, cols", [(1, 64), (4099, 300), (513, 4096), (70, 17000)])
+def test_same_bits_again_and_on_a_stream(pace, rows, cols):
+    say("layer norm twice %d x %d" % (rows, cols))
+    x, dy = matrix(rows, cols, F16, seed=12), matrix(rows, cols, F16, seed=13)
+    w = torch.rand(cols, device=DEV)
+    first = pace.pace_layer_norm(x, w)
+    first += pace.pace_layer_norm_backward(x, first[1], dy, w)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    second = pace.pace_layer_norm(x, w, stream=side)
+    second += pace.pace_layer_norm_backward(x, second[1], dy, w, stream=side)
+    side.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(first, second))
+
+
+def test_captured(pace):
+    """Captured once and replayed on new contents, with eager calls on the same buffers between."""
+    say("layer norm captured")
+    rows, cols = 700, 1000
+    x, dy, w = matrix(rows, cols, BF16, seed=14), matrix(rows, cols, BF16, seed=15), torch.rand(cols, device=DEV)
+    k = pace.layer_norm_buffers(rows, cols, BF16, DEV, backward=True)
+
+    def call(b):
+        y, stats = pace.pace_layer_norm(x, w, buffers=b)
+        return (y, stats) + pace.pace_layer_norm_backward(x, stats, dy, w, buffers=b)
+
+    call(k)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = call(k)
+    for turn in range(3):
+        x.copy_(matrix(rows, cols, BF16, seed=20 + turn))
+        ref = call(pace.layer_norm_buffers(rows, cols, BF16, DEV, backward=True))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, ref))
+
+
+def test_workspace_of_a_larger_problem(pace):
+    say("layer norm gradients in one workspace")
+    ws = torch.full((pace.pace_layer_norm_backward_workspace_bytes(3000, 9000),), 255, dtype=torch.uint8, device=DEV)
+    for rows, cols in ((3000, 9000), (3000, 100), (2900, 1025), (1, 8193), (40, 4096)):
+        x, dy = matrix(rows, cols, BF16, seed=16), matrix(rows, cols, BF16, seed=17)
+        stats = pace.pace_layer_norm(x)[1]
+        b = dict(pace.layer_norm_buffers(rows, cols, BF16, DEV, backward=True), workspace=ws)
+        assert all(torch.equal(p, q) for p, q in zip(pace.pace_layer_norm_backward(x, stats, dy, buffers=b),
+                                                     pace.pace_layer_norm_backward(x, stats, dy)))
+    with pytest.raises(pace.PaceError):
+        pace.pace_layer_norm_backward(x, stats, dy, buffers=dict(b, workspace=ws[:512]))
+
+
+def test_rows_beyond_32_bits(pace):
+    say("layer norm of rows beyond 2^31 elements")
+    rows, stride, cols = 2100, 1 << 20, 100
+    x = torch.zeros(rows * stride, dtype=BF16, device=DEV).view(rows, stride)[:, :cols]
+    x.copy_(matrix(rows, cols, BF16, seed=18))
+    dy, w = matrix(rows, cols, BF16, seed=19), torch.rand(cols, device=DEV)
+    y, stats = pace.pace_layer_norm(x, w)
+    near = x.contiguous()
+    ref, ref_stats = pace.pace_layer_norm(near, w)
+    assert torch.equal(y, ref) and torch.equal(stats, ref_stats)
+    assert all(torch.equal(p, q) for p, q in zip(pace.pace_layer_norm_backward(x, stats, dy, w), pace.pace_layer_norm_backward(near, stats, dy, w)))
+
+
+def test_nothing_beyond_the_rows(pace):
+    """Outputs with padding between their rows, through the C entry: what stands between stays."""
+    say("layer norm into padded rows")
+    from paper_2609_36830_amd import _lib
+    L = _lib.lib()
+    s = torch.cuda.current_stream().cuda_stream
+    for rows, cols in ((37, 61), (5, 4099), (3, 16400)):
+        x, dy = matrix(rows, cols, F16, seed=21), matrix(rows, cols, F16, seed=22)
+        out, dx = (torch.full((rows, cols + 5), 3.0, dtype=F16, device=DEV) for _ in range(2))
+        ref, stats = pace.pace_layer_norm(x)
+        grad = pace.pace_layer_norm_backward(x, stats, dy)[0]
+        assert L.pace_layer_norm(x.data_ptr(), 2, rows, cols, cols, None, None, 2, 1e-5, out.data_ptr(), cols + 5, None, s) == 0
+        # without the weights' sums no workspace is taken
+        assert L.pace_layer_norm_backward(x.data_ptr(), 2, rows, cols, cols, None, 2, stats.data_ptr(), dy.data_ptr(), cols, dx.data_ptr(),
+                                          cols + 5, None, None, None, 0, s) == 0
+        for got, want in ((out, ref), (dx, grad)):
+            assert torch.equal(got[:, :cols], want) and (got[:, cols:] == 3.0).all()
