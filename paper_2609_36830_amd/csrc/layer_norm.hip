@@ -5,7 +5,7 @@
 //
 // HBM-bound: the forward pass reads x and writes y, the backward pass reads x
 // and dy and writes dx, with some 10 and 16 vector instructions an element. A
-// row is held in registers, 16 elements a lane, by 16 lanes up to 256 columns
+// row is held in registers, 16 elements a lane, by 8 lanes up to 128 columns
 // and twice as many for twice the columns, up to 1024 lanes for 16384; wider rows are
 // read again for each step. The weights stay in registers from row to row.
 //
@@ -28,13 +28,14 @@ namespace {
 constexpr int kLnForward = 256;                    // threads of a workgroup, or a row's lanes where these are more
 constexpr int kLnBackward = 512;
 
-// Sum over kLanes consecutive lanes (16, 32 or a wave), in every lane.
+// Sum over kLanes consecutive lanes (8, 16, 32 or a wave), in every lane.
 template <int kLanes>
 __device__ __forceinline__ float lanes_sum(float v) {
     auto step = [&](uint32_t got) { v += __builtin_bit_cast(float, got); };
     step(dpp_u32<0xb1, 0xf>(0u, __builtin_bit_cast(uint32_t, v)));       // quads: lane ^ 1, lane ^ 2
     step(dpp_u32<0x4e, 0xf>(0u, __builtin_bit_cast(uint32_t, v)));
     step(dpp_u32<0x141, 0xf>(0u, __builtin_bit_cast(uint32_t, v)));      // mirrored within 8, then within 16
+    if constexpr (kLanes == 8) return v;
     step(dpp_u32<0x140, 0xf>(0u, __builtin_bit_cast(uint32_t, v)));
     if constexpr (kLanes == 16) return v;
     if constexpr (kLanes == 32) return v + __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, v), 0x401f));
@@ -42,30 +43,39 @@ __device__ __forceinline__ float lanes_sum(float v) {
     return (row(0) + row(16)) + (row(32) + row(48));
 }
 
-// The vectors that a lane holds of a row: lane l has l, l + kLanes, ..
+// The row of the workgroup's that a thread has; one for the wave where waves have whole rows.
+template <int kLanes>
+__device__ __forceinline__ int group_of() {
+    const int g = (int)threadIdx.x / kLanes;
+    return kLanes >= kWave ? readlane_i32(g, 0) : g;
+}
+
+// The vectors that a lane holds of a row: lane l has l, l + kLanes, .. With kWhole a
+// row ends with a vector.
 template <typename T>
 struct Slice {
     static constexpr int kVec = kVecOf<T>, kVecs = kLnPer / kVec;
     uint4 raw[kVecs];
 };
-template <typename T, int kLanes>
+template <typename T>
+__device__ __forceinline__ uint4 load_part(const T *p, int n) {      // the first n elements, then zeros
+    float v[kVecOf<T>];
+#pragma unroll
+    for (int e = 0; e < kVecOf<T>; ++e) v[e] = e < n ? to_f32(p[e]) : 0.0f;
+    return pack16<T>(v);
+}
+template <typename T, int kLanes, bool kWhole>
 __device__ __forceinline__ void load_slice(Slice<T> &s, const T *row, int lane, int cols) {
     constexpr int kVec = Slice<T>::kVec;
 #pragma unroll
     for (int k = 0; k < Slice<T>::kVecs; ++k) {
         const int c = (lane + k * kLanes) * kVec;
         s.raw[k] = make_uint4(0, 0, 0, 0);
-        if (c + kVec <= cols) {
-            s.raw[k] = load_a1(row + c);
-        } else if (c < cols) {
-            float v[kVec];
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) v[e] = c + e < cols ? to_f32(row[c + e]) : 0.0f;
-            s.raw[k] = pack16<T>(v);
-        }
+        if (kWhole ? c < cols : c + kVec <= cols) s.raw[k] = load_a1(row + c);
+        else if (!kWhole && c < cols) s.raw[k] = load_part(row + c, cols - c);
     }
 }
-template <typename T, int kLanes>
+template <typename T, int kLanes, bool kWhole>
 __device__ __forceinline__ void store_slice(T *row, const float (&v)[kLnPer], int lane, int cols) {
     constexpr int kVec = Slice<T>::kVec;
 #pragma unroll
@@ -74,9 +84,9 @@ __device__ __forceinline__ void store_slice(T *row, const float (&v)[kLnPer], in
         float w[kVec];
 #pragma unroll
         for (int e = 0; e < kVec; ++e) w[e] = v[k * kVec + e];
-        if (c + kVec <= cols) {
+        if (kWhole ? c < cols : c + kVec <= cols) {
             store_a1(row + c, pack16<T>(w));
-        } else {
+        } else if (!kWhole) {
 #pragma unroll
             for (int e = 0; e < kVec; ++e)
                 if (c + e < cols) row[c + e] = from_f32<T>(w[e]);
@@ -94,113 +104,121 @@ __device__ __forceinline__ void unpack_slice(const Slice<T> &s, float (&v)[kLnPe
         for (int e = 0; e < kVec; ++e) v[k * kVec + e] = w[e];
     }
 }
-// A weight's elements in the places of T's vectors; `none` where there is no weight.
-template <typename T, typename W, int kLanes>
-__device__ __forceinline__ void load_weight(float (&v)[kLnPer], const W *w, float none, int lane, int cols) {
-    constexpr int kVec = Slice<T>::kVec;
+// A weight's elements in the places of T's vectors, in its own type; `none` where there is no weight.
+template <typename T, typename W>
+struct Weight {
+    static constexpr int kVec = Slice<T>::kVec, kIn = kVecOf<W>, kVecs = kLnPer / kIn;
+    uint4 raw[kVecs];
+    template <int kLanes, bool kWhole>
+    __device__ __forceinline__ void load(const W *w, float none, int lane, int cols) {
 #pragma unroll
-    for (int i = 0; i < kLnPer; ++i) {
-        const int c = (lane + i / kVec * kLanes) * kVec + i % kVec;
-        v[i] = w && c < cols ? to_f32(w[c]) : none;
+        for (int k = 0; k < kVecs; ++k) {
+            const int i = k * kIn, c = (lane + i / kVec * kLanes) * kVec + i % kVec;
+            float v[kIn];
+#pragma unroll
+            for (int e = 0; e < kIn; ++e) v[e] = none;
+            raw[k] = pack16<W>(v);
+            if (w == nullptr) continue;
+            if (kWhole ? c < cols : c + kIn <= cols) raw[k] = load_a1(w + c);
+            else if (!kWhole && c < cols) raw[k] = load_part(w + c, cols - c);
+        }
     }
-}
+    __device__ __forceinline__ void values(float (&v)[kLnPer]) const {
+#pragma unroll
+        for (int k = 0; k < kVecs; ++k) {
+            float u[kIn];
+            unpack16<W>(raw[k], u);
+#pragma unroll
+            for (int e = 0; e < kIn; ++e) v[k * kIn + e] = u[e];
+        }
+    }
+};
 
 __device__ __forceinline__ float not_below_zero(float v) { return v < 0.0f ? 0.0f : v; }      // NaN stays
 
 struct Moments {
     float ref, off, m2;      // the mean is ref + off, off small; sum of squares about it
 };
-// Moments of `count` elements that kLanes lanes (at most a wave) hold; elements at or past cols count as none.
-template <typename T, int kLanes, int kStep>
-__device__ __forceinline__ Moments lanes_moments(const float (&x)[kLnPer], int lane, int cols, int count) {
+// Moments of `count` elements that kIn lanes (at most a wave) hold of rows of kLanes lanes; elements at or
+// past cols count as none.
+template <typename T, int kIn, int kLanes, bool kWhole>
+__device__ __forceinline__ Moments lanes_moments(const float (&x)[kLnPer], int lane, int cols, float count) {
     constexpr int kVec = Slice<T>::kVec;
-    const float inv = count > 0 ? 1.0f / (float)count : 0.0f;
+    const float inv = count > 0.0f ? 1.0f / count : 0.0f;
     float s = 0.0f, s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int i = 0; i < kLnPer; ++i) s += x[i];
-    const float ref = lanes_sum<kLanes>(s) * inv;
+    const float ref = lanes_sum<kIn>(s) * inv;
 #pragma unroll
     for (int k = 0; k < Slice<T>::kVecs; ++k) {
-        const int left = cols - (lane + k * kStep) * kVec;
-        float d[kVec];
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) d[e] = x[k * kVec + e] - ref;
-        if (left < kVec) {
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) d[e] = e < left ? d[e] : 0.0f;
-        }
+        const int left = cols - (lane + k * kLanes) * kVec;
+        float t1 = 0.0f, t2 = 0.0f;
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
-            s1 += d[e];
-            s2 = __builtin_fmaf(d[e], d[e], s2);
+            float d = x[k * kVec + e] - ref;
+            if (!kWhole) d = e < left ? d : 0.0f;
+            t1 += d;
+            t2 = __builtin_fmaf(d, d, t2);
         }
+        s1 += !kWhole || left > 0 ? t1 : 0.0f;
+        s2 += !kWhole || left > 0 ? t2 : 0.0f;
     }
-    s1 = lanes_sum<kLanes>(s1);
-    s2 = lanes_sum<kLanes>(s2);
+    s1 = lanes_sum<kIn>(s1);
+    s2 = lanes_sum<kIn>(s2);
     const float off = s1 * inv;
     return {ref, off, not_below_zero(__builtin_fmaf(-s1, off, s2))};
 }
 
-template <typename T, typename W, int kLanes>
+template <typename T, typename W, int kLanes, bool kWhole>
 __global__ __launch_bounds__(kLanes > kLnForward ? kLanes : kLnForward) void layer_norm_kernel(
     const T *__restrict__ x, int64_t rows, int cols, int64_t stride, const W *__restrict__ weight,
     const W *__restrict__ bias, float eps, T *__restrict__ out, int64_t out_stride, float *__restrict__ stats) {
     constexpr int kThreads = kLanes > kLnForward ? kLanes : kLnForward, kRows = kThreads / kLanes;
     constexpr int kIn = kLanes < kWave ? kLanes : kWave, kWaves = kLanes / kIn;      // lanes of a wave, waves of a row
     constexpr int kVec = Slice<T>::kVec, kVecs = Slice<T>::kVecs;
-    __shared__ float slots[2][kRows * kWaves][3];
-    const int group = (int)threadIdx.x / kLanes, lane = (int)threadIdx.x % kLanes, wave = lane / kIn;
-    auto count_of = [&](int w) {                       // columns that the row's wave w has
-        int n = 0;
+    __shared__ float4 slots[2][kRows * kWaves];
+    const int group = group_of<kLanes>(), lane = (int)threadIdx.x % kLanes, wave = lane / kIn;
+    float count = 0.0f;                                // columns that the row's lanes in this wave have
 #pragma unroll
-        for (int k = 0; k < kVecs; ++k) {
-            const int left = cols - (w * kIn + k * kLanes) * kVec;
-            n += left < 0 ? 0 : (left < kIn * kVec ? left : kIn * kVec);
-        }
-        return n;
-    };
-    const int count = count_of(wave);
+    for (int k = 0; k < kVecs; ++k) {
+        const int left = cols - (wave * kIn + k * kLanes) * kVec;
+        count += (float)(left < 0 ? 0 : (left < kIn * kVec ? left : kIn * kVec));
+    }
     const float inv = 1.0f / (float)cols;
     const int64_t step = (int64_t)gridDim.x * kRows;
     int64_t base = (int64_t)blockIdx.x * kRows;
     auto row_of = [&](int64_t b) { return b + group < rows ? b + group : rows - 1; };      // loops are the workgroup's
     Slice<T> next;
-    load_slice<T, kLanes>(next, x + row_of(base) * stride, lane, cols);
-    float w[kLnPer], b[kLnPer];
-    load_weight<T, W, kLanes>(w, weight, 1.0f, lane, cols);
-    load_weight<T, W, kLanes>(b, bias, 0.0f, lane, cols);
+    load_slice<T, kLanes, kWhole>(next, x + row_of(base) * stride, lane, cols);
+    Weight<T, W> weights, biases;
+    weights.template load<kLanes, kWhole>(weight, 1.0f, lane, cols);
+    biases.template load<kLanes, kWhole>(bias, 0.0f, lane, cols);
     for (int turn = 0; base < rows; base += step, turn ^= 1) {
         float v[kLnPer];
         unpack_slice<T>(next, v);
-        if (base + step < rows) load_slice<T, kLanes>(next, x + row_of(base + step) * stride, lane, cols);
-        Moments m = lanes_moments<T, kIn, kLanes>(v, lane, cols, count);
+        if (base + step < rows) load_slice<T, kLanes, kWhole>(next, x + row_of(base + step) * stride, lane, cols);
+        Moments m = lanes_moments<T, kIn, kLanes, kWhole>(v, lane, cols, count);
         if constexpr (kWaves > 1) {
-            float(*slot)[3] = slots[turn] + group * kWaves;
-            if (lane % kIn == 0) {
-                slot[wave][0] = m.ref;
-                slot[wave][1] = m.off;
-                slot[wave][2] = m.m2;
-            }
+            float4 *slot = slots[turn] + group * kWaves;
+            if (lane % kIn == 0) slot[wave] = make_float4(m.ref, m.off, m.m2, count);
             __syncthreads();                           // the other turn's slots are read before the next barrier
-            const float ref = slot[0][0];
-            float off = 0.0f, m2 = 0.0f;
-#pragma unroll
-            for (int k = 0; k < kWaves; ++k) off += (float)count_of(k) * ((slot[k][0] - ref) + slot[k][1]);
-            off *= inv;
-#pragma unroll
-            for (int k = 0; k < kWaves; ++k) {
-                const float d = ((slot[k][0] - ref) + slot[k][1]) - off;
-                const int n = count_of(k);
-                if (n > 0) m2 += slot[k][2] + (float)n * (d * d);
-            }
-            m = {ref, off, m2};
+            // Lane k takes wave k's, in rows of 16 lanes: each wave's comes 16 / kWaves times.
+            const float4 part = slot[lane % kWaves];
+            constexpr float kShare = (float)kWaves / 16.0f;
+            const float ref = __builtin_bit_cast(float, readlane_i32(__builtin_bit_cast(int32_t, part.x), 0));
+            const float d = (part.x - ref) + part.y;
+            const float off = lanes_sum<16>(part.w * d) * (inv * kShare), e = d - off;
+            m = {ref, off, lanes_sum<16>(part.w > 0.0f ? __builtin_fmaf(part.w * e, e, part.z) : 0.0f) * kShare};
         }
         const float rstd = 1.0f / sqrtf(m.m2 * inv + eps);
         const int64_t row = base + group;
+        float w[kLnPer], b[kLnPer];
+        weights.values(w);
+        biases.values(b);
 #pragma unroll
         for (int i = 0; i < kLnPer; ++i) v[i] = __builtin_fmaf(((v[i] - m.ref) - m.off) * rstd, w[i], b[i]);
         if (row < rows) {
-            store_slice<T, kLanes>(out + row * out_stride, v, lane, cols);
+            store_slice<T, kLanes, kWhole>(out + row * out_stride, v, lane, cols);
             if (stats && lane == 0) {
                 stats[2 * row] = m.ref + m.off;
                 stats[2 * row + 1] = rstd;
@@ -244,76 +262,75 @@ __device__ __forceinline__ void write_part(const float (&dw)[kLnPer], const floa
 }
 
 // dx may be dy itself: a row is read before it is written.
-template <typename T, typename W, int kLanes>
-__global__ __launch_bounds__(kLanes > kLnBackward ? kLanes : kLnBackward) void layer_norm_backward_kernel(
+template <typename T, typename W, int kLanes, bool kWhole>
+__global__ __launch_bounds__(kLanes > kLnBackward ? kLanes : kLnBackward, 4) void layer_norm_backward_kernel(
     const T *__restrict__ x, int64_t rows, int cols, int64_t stride, const W *__restrict__ weight,
     const float *__restrict__ stats, const T *dy, int64_t dy_stride, T *dx, int64_t dx_stride, float *__restrict__ parts,
     int64_t pitch) {
     constexpr int kThreads = kLanes > kLnBackward ? kLanes : kLnBackward, kRows = kThreads / kLanes;
     constexpr int kIn = kLanes < kWave ? kLanes : kWave, kWaves = kLanes / kIn;
-    __shared__ float slots[2][kRows * kWaves][2];
-    const int group = (int)threadIdx.x / kLanes, lane = (int)threadIdx.x % kLanes, wave = lane / kIn;
+    __shared__ float2 slots[2][kRows * kWaves];
+    const int group = group_of<kLanes>(), lane = (int)threadIdx.x % kLanes, wave = lane / kIn;
     const float inv = 1.0f / (float)cols;
     const int64_t step = (int64_t)gridDim.x * kRows;
     int64_t base = (int64_t)blockIdx.x * kRows;
     auto row_of = [&](int64_t b) { return b + group < rows ? b + group : rows - 1; };
+    // A row's bytes are on their way while the one before is summed; of binary32, whose rows are as
+    // many bytes as two of the others, registers hold one.
+    constexpr bool kAhead = sizeof(T) == 2;
     Slice<T> nx, ng;
-    load_slice<T, kLanes>(nx, x + row_of(base) * stride, lane, cols);
-    load_slice<T, kLanes>(ng, dy + row_of(base) * dy_stride, lane, cols);
-    float mean = stats[2 * row_of(base)], rstd = stats[2 * row_of(base) + 1];
-    float w[kLnPer], dw[kLnPer], db[kLnPer];
-    load_weight<T, W, kLanes>(w, weight, 1.0f, lane, cols);
+    float mean = 0.0f, rstd = 0.0f;
+    auto take = [&](int64_t b) {
+        const int64_t r = row_of(b);
+        load_slice<T, kLanes, kWhole>(nx, x + r * stride, lane, cols);
+        load_slice<T, kLanes, kWhole>(ng, dy + r * dy_stride, lane, cols);
+        mean = stats[2 * r];
+        rstd = stats[2 * r + 1];
+    };
+    if (kAhead) take(base);
+    Weight<T, W> weights;
+    weights.template load<kLanes, kWhole>(weight, 1.0f, lane, cols);
+    float dw[kLnPer], db[kLnPer];
 #pragma unroll
     for (int i = 0; i < kLnPer; ++i) dw[i] = db[i] = 0.0f;
     for (int turn = 0; base < rows; base += step, turn ^= 1) {
         const int64_t row = base + group;
-        float h[kLnPer], a[kLnPer];
+        if (!kAhead) take(base);
+        float h[kLnPer], a[kLnPer], w[kLnPer];
         unpack_slice<T>(nx, h);
-        unpack_slice<T>(ng, a);
+        const Slice<T> g = ng;
+        unpack_slice<T>(g, a);
+        weights.values(w);
         const float r = rstd;
         const bool live = row < rows;
-#pragma unroll
-        for (int i = 0; i < kLnPer; ++i) {
-            h[i] = (h[i] - mean) * r;
-            if (!live) a[i] = 0.0f, h[i] = 0.0f;       // lanes behind the last row add nothing
-            dw[i] = __builtin_fmaf(a[i], h[i], dw[i]);
-            db[i] += a[i];
-            a[i] *= w[i];
-        }
-        if (base + step < rows) {
-            const int64_t to = row_of(base + step);
-            load_slice<T, kLanes>(nx, x + to * stride, lane, cols);
-            load_slice<T, kLanes>(ng, dy + to * dy_stride, lane, cols);
-            mean = stats[2 * to];
-            rstd = stats[2 * to + 1];
-        }
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int i = 0; i < kLnPer; ++i) {
+            h[i] = (h[i] - mean) * r;
+            if (kRows > 1 && !live) a[i] = 0.0f, h[i] = 0.0f;       // lanes behind the last row add nothing
+            dw[i] = __builtin_fmaf(a[i], h[i], dw[i]);
+            db[i] += a[i];
+            a[i] *= w[i];
             s1 += a[i];
             s2 = __builtin_fmaf(a[i], h[i], s2);
         }
+        if (kAhead && base + step < rows) take(base + step);
         s1 = lanes_sum<kIn>(s1);
         s2 = lanes_sum<kIn>(s2);
         if constexpr (kWaves > 1) {
-            float(*slot)[2] = slots[turn] + group * kWaves;
-            if (lane % kIn == 0) {
-                slot[wave][0] = s1;
-                slot[wave][1] = s2;
-            }
+            float2 *slot = slots[turn] + group * kWaves;
+            if (lane % kIn == 0) slot[wave] = make_float2(s1, s2);
             __syncthreads();
-            s1 = s2 = 0.0f;
-#pragma unroll
-            for (int k = 0; k < kWaves; ++k) {
-                s1 += slot[k][0];
-                s2 += slot[k][1];
-            }
+            const float2 part = slot[lane % kWaves];       // in rows of 16 lanes, each wave's 16 / kWaves times
+            s1 = lanes_sum<16>(part.x) * ((float)kWaves / 16.0f);
+            s2 = lanes_sum<16>(part.y) * ((float)kWaves / 16.0f);
         }
         s1 *= inv;
         s2 *= inv;
+        unpack_slice<T>(g, a);                         // half the registers that the products would take from above
 #pragma unroll
-        for (int i = 0; i < kLnPer; ++i) a[i] = ((a[i] - s1) - h[i] * s2) * r;
-        if (live) store_slice<T, kLanes>(dx + row * dx_stride, a, lane, cols);
+        for (int i = 0; i < kLnPer; ++i) a[i] = ((a[i] * w[i] - s1) - h[i] * s2) * r;
+        if (live) store_slice<T, kLanes, kWhole>(dx + row * dx_stride, a, lane, cols);
     }
     if (parts) write_part<T, kLanes, kThreads>(dw, db, parts + (int64_t)blockIdx.x * 2 * pitch, pitch, cols);
 }
@@ -502,14 +519,14 @@ __global__ __launch_bounds__(kLnColumns) void layer_norm_columns_kernel(const T 
         }
 }
 
-// The parts' sums: 64 columns a workgroup, 16 threads a column.
-constexpr int kLnJoin = 1024;
+// The parts' sums: 32 columns a workgroup, 32 threads a column.
+constexpr int kLnJoin = 1024, kLnJoinCols = 32;
 __global__ __launch_bounds__(kLnJoin) void layer_norm_join_kernel(const float *__restrict__ parts, int64_t n_parts, int64_t pitch,
                                                                   int64_t cols, float *__restrict__ dw, float *__restrict__ db) {
-    constexpr int kSplit = kLnJoin / kWave;
-    __shared__ float sums[kSplit][kWave];
-    const int64_t c = (int64_t)blockIdx.x * kWave + lane_id();
-    const int at = (int)threadIdx.x / kWave;
+    constexpr int kSplit = kLnJoin / kLnJoinCols;
+    __shared__ float sums[kSplit][kLnJoinCols + 1];
+    const int mine = (int)threadIdx.x % kLnJoinCols, at = (int)threadIdx.x / kLnJoinCols;
+    const int64_t c = (int64_t)blockIdx.x * kLnJoinCols + mine;
     float *out = blockIdx.y ? db : dw;
     if (out == nullptr) return;                        // the whole workgroup
     float s = 0.0f;
@@ -518,12 +535,12 @@ __global__ __launch_bounds__(kLnJoin) void layer_norm_join_kernel(const float *_
 #pragma unroll 8
         for (int64_t k = at; k < n_parts; k += kSplit) s += p[k * 2 * pitch];
     }
-    sums[at][lane_id()] = s;
+    sums[at][mine] = s;
     __syncthreads();
     if (at == 0 && c < cols) {
         s = 0.0f;
 #pragma unroll
-        for (int k = 0; k < kSplit; ++k) s += sums[k][lane_id()];
+        for (int k = 0; k < kSplit; ++k) s += sums[k][mine];
         out[c] = s;
     }
 }
@@ -534,17 +551,21 @@ hipError_t with_weight(int weight_dtype, F f) {
     if constexpr (sizeof(T) == 4) return f(float{});
     else return weight_dtype == kF32 ? f(float{}) : f(T{});
 }
-// Runs f with the lanes of a row of up to kLnRegister columns.
-template <typename F>
+// Runs f with the lanes of a row of up to kLnRegister columns, and whether it ends with a vector.
+template <typename T, typename F>
 hipError_t with_lanes(int64_t cols, F f) {
+    auto whole = [&](auto lanes) {
+        return cols % kVecOf<T> == 0 ? f(lanes, std::true_type{}) : f(lanes, std::false_type{});
+    };
     switch (layer_norm_lanes(cols)) {
-        case 16: return f(std::integral_constant<int, 16>{});
-        case 32: return f(std::integral_constant<int, 32>{});
-        case 64: return f(std::integral_constant<int, 64>{});
-        case 128: return f(std::integral_constant<int, 128>{});
-        case 256: return f(std::integral_constant<int, 256>{});
-        case 512: return f(std::integral_constant<int, 512>{});
-        default: return f(std::integral_constant<int, 1024>{});
+        case 8: return whole(std::integral_constant<int, 8>{});
+        case 16: return whole(std::integral_constant<int, 16>{});
+        case 32: return whole(std::integral_constant<int, 32>{});
+        case 64: return whole(std::integral_constant<int, 64>{});
+        case 128: return whole(std::integral_constant<int, 128>{});
+        case 256: return whole(std::integral_constant<int, 256>{});
+        case 512: return whole(std::integral_constant<int, 512>{});
+        default: return whole(std::integral_constant<int, 1024>{});
     }
 }
 
@@ -568,10 +589,10 @@ hipError_t launch_layer_norm(const void *x, int dtype, int64_t rows, int64_t col
                     return launch(kPhaseAux, layer_norm_wide_kernel<T, W>, dim3((unsigned)count), dim3(kLnWide), stream, p + first * stride,
                                   cols, stride, w, b, (float)eps, o + first * out_stride, out_stride, stats ? stats + 2 * first : nullptr);
                 });
-            return with_lanes(cols, [&](auto lanes) {
+            return with_lanes<T>(cols, [&](auto lanes, auto whole) {
                 constexpr int kLanes = decltype(lanes)::value, kThreads = kLanes > kLnForward ? kLanes : kLnForward;
-                const int64_t need = (rows + kThreads / kLanes - 1) / (kThreads / kLanes), most = resident_waves() * 2 / (kThreads / kWave);
-                return launch(kPhaseAux, layer_norm_kernel<T, W, kLanes>, dim3((unsigned)(need < most ? need : most)), dim3(kThreads), stream,
+                const int64_t need = (rows + kThreads / kLanes - 1) / (kThreads / kLanes), most = resident_waves() / (kThreads / kWave);
+                return launch(kPhaseAux, layer_norm_kernel<T, W, kLanes, decltype(whole)::value>, dim3((unsigned)(need < most ? need : most)), dim3(kThreads), stream,
                               p, rows, (int)cols, stride, w, b, (float)eps, o, out_stride, stats);
             });
         });
@@ -613,16 +634,16 @@ hipError_t launch_layer_norm_backward(const void *x, int dtype, int64_t rows, in
                                       o + first * dx_stride, dx_stride);
                     });
                 }
-                return with_lanes(cols, [&](auto lanes) {
+                return with_lanes<T>(cols, [&](auto lanes, auto whole) {
                     constexpr int kLanes = decltype(lanes)::value, kThreads = kLanes > kLnBackward ? kLanes : kLnBackward;
                     static_assert(kThreads / kLanes == layer_norm_backward_rows(kLanes), "rows of a workgroup");
-                    return launch(kPhaseAux, layer_norm_backward_kernel<T, W, kLanes>, dim3((unsigned)n_parts), dim3(kThreads), stream, p,
+                    return launch(kPhaseAux, layer_norm_backward_kernel<T, W, kLanes, decltype(whole)::value>, dim3((unsigned)n_parts), dim3(kThreads), stream, p,
                                   rows, (int)cols, stride, w, stats, g, dy_stride, o, dx_stride, parts, pitch);
                 });
             });
         });
     if (e == hipSuccess && parts)
-        e = launch(-1, layer_norm_join_kernel, dim3((unsigned)((cols + kWave - 1) / kWave), 2), dim3(kLnJoin), stream, (const float *)parts,
+        e = launch(-1, layer_norm_join_kernel, dim3((unsigned)((cols + kLnJoinCols - 1) / kLnJoinCols), 2), dim3(kLnJoin), stream, (const float *)parts,
                    rows > 0 ? n_parts : 0, pitch, cols, dw, db);
     return e;
 }

@@ -255,19 +255,21 @@ inline int64_t logprob_backward_parts(int64_t rows, int64_t vocab) {
 constexpr int kLnPer = 16;
 constexpr int64_t kLnRegister = 16384, kLnColsMax = (int64_t)1 << 24;
 constexpr int layer_norm_lanes(int64_t cols) {
-    int lanes = 16;
+    int lanes = 8;
     while ((int64_t)lanes * kLnPer < cols && lanes < 1024) lanes *= 2;
     return lanes;
 }
 // Rows that a workgroup of the backward pass has at once.
 constexpr int layer_norm_backward_rows(int lanes) { return lanes >= 512 ? 1 : 512 / lanes; }
-// Column sums that the backward pass writes and adds up afterwards: one a workgroup, as many
-// workgroups as the chip holds, but no chain of more than kLnChain rows.
-constexpr int64_t kLnChain = 1024, kLnWideParts = 64, kLnWidePartsMax = 65535;
+// Column sums that the backward pass writes and adds up afterwards: one a workgroup, at most
+// one workgroup of 512 or 1024 threads a CU, but no chain of more than kLnChain rows. Fewer leave
+// CUs idle, more write and read as much again as the rows they share: 16384 x 4096 in bfloat16 take
+// 103 / 84 / 79 / 92 / 85 / 94 us with 128 / 192 / 256 / 384 / 512 / 1024 parts, 4099 x 4096 34 / 30 /
+// 29 / 35 / 34 / 45, 131077 x 128 39 / 31 / 27 / 29 / 27 / 32, 2047 x 16384 55 / 51 / 52 / 58 / 67 / 96.
+constexpr int64_t kLnChain = 1024, kLnParts = 256, kLnWideParts = 64, kLnWidePartsMax = 65535;
 inline int64_t layer_norm_register_parts(int64_t rows, int lanes) {
     const int64_t at_once = layer_norm_backward_rows(lanes), need = (rows + at_once - 1) / at_once;
-    const int64_t fill = lanes > 512 ? 256 : 512, chain = (rows + at_once * kLnChain - 1) / (at_once * kLnChain);
-    const int64_t parts = need < fill ? need : fill;
+    const int64_t chain = (rows + at_once * kLnChain - 1) / (at_once * kLnChain), parts = need < kLnParts ? need : kLnParts;
     return parts > chain ? parts : chain;
 }
 inline int64_t layer_norm_wide_parts(int64_t rows) {
@@ -280,7 +282,7 @@ inline int64_t layer_norm_backward_parts(int64_t rows, int64_t cols) {
 // No fewer floats than the parts of any rows and columns up to these take.
 inline int64_t layer_norm_part_floats_most(int64_t rows, int64_t cols) {
     int64_t most = 0;
-    for (int lanes = 16;; lanes *= 2) {
+    for (int lanes = 8;; lanes *= 2) {
         const bool wide = lanes > 1024;
         const int64_t widest = wide || cols < (int64_t)lanes * kLnPer ? cols : (int64_t)lanes * kLnPer;
         const int64_t parts = wide ? layer_norm_wide_parts(rows) : layer_norm_register_parts(rows, lanes);

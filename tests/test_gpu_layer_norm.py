@@ -84,8 +84,8 @@ def check_backward(x, w, stats, dy, dx, dw, db):
     s1, s2 = a.abs().mean(1, keepdim=True), (a * h).abs().mean(1, keepdim=True)
     off = rstd * U * (6 * a.abs() + (k + 2) * s1 + h.abs() * ((k + 8) * s2))
     assert ((dx.double() - ref).abs() <= off + half_step(ref, dx.dtype)).all()
-    # columns: at most 1024 rows in a chain, the rows of a workgroup (32), the parts (n / 16, then 16)
-    chain = min(rows, 1024) + 32 + 64 + 16
+    # columns: at most 1024 rows in a chain, the rows of a workgroup (64), the parts (n / 32, then 32)
+    chain = min(rows, 1024) + 64 + 16 + 32
     assert ((dw.double() - (g * h).sum(0)).abs() <= U * (chain + 4) * (g * h).abs().sum(0) + 1e-44).all()
     assert ((db.double() - g.sum(0)).abs() <= U * chain * g.abs().sum(0) + 1e-44).all()
 
