@@ -16,7 +16,8 @@
 // HBM-bound: with a binary32 parameter, a bfloat16 gradient and copy 28 bytes an
 // element, 16 with moments in 8 bits. A launch takes up to kTable tensors by a
 // table in its arguments: workgroups of 4096 elements find their tensor in one
-// load and vote of a wave. A wave takes a block of 256 elements, four a lane.
+// load and vote of a wave. A wave takes 512 elements at a time, eight a lane in two
+// runs of four: two blocks of 256, each by half a wave.
 #include "elem.hpp"
 #include "kernels.hpp"
 
@@ -27,15 +28,20 @@ namespace pace {
 namespace {
 
 constexpr int kAdamThreads = 256;
-constexpr int kWaveTurns = (int)(kAdamChunk / (kAdamThreads / kWave) / kAdamBlock);      // blocks that a wave takes
-constexpr int kPerLane = (int)kAdamBlock / kWave;
+constexpr int64_t kWaveRun = 2 * kAdamBlock;                     // elements that a wave takes at a time
+constexpr int kWaveTurns = (int)(kAdamChunk / (kAdamThreads / kWave) / kWaveRun);
+constexpr int kLaneRuns = 2, kPerRun = 4;                       // of a lane: elements 4 l .. and 128 + 4 l .. of its half's block
+// The first element of a lane's run j, in the elements from `at` on.
+__device__ __forceinline__ int64_t run_of(int64_t at, int j) {
+    return at + (lane_id() / 32) * kAdamBlock + j * (kAdamBlock / kLaneRuns) + lane_id() % 32 * kPerRun;
+}
 
 // Four elements at any element's alignment, those at or past n as zeros.
 template <typename T> struct Four { T e[4]; };
 template <typename T, bool kFull>
 __device__ __forceinline__ Four<T> load_four_of(const T *p, int64_t i, int64_t n) {
     typedef uint8_t bytes_a1 __attribute__((ext_vector_type(sizeof(T) * 4), aligned(1)));
-    if constexpr (kFull) return __builtin_bit_cast(Four<T>, *reinterpret_cast<const bytes_a1 *>(p + i));
+    if (kFull || i + 4 <= n) return __builtin_bit_cast(Four<T>, *reinterpret_cast<const bytes_a1 *>(p + i));
     Four<T> v = {};
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -45,7 +51,7 @@ __device__ __forceinline__ Four<T> load_four_of(const T *p, int64_t i, int64_t n
 template <typename T, bool kFull>
 __device__ __forceinline__ void store_four_of(T *p, int64_t i, int64_t n, const Four<T> &v) {
     typedef uint8_t bytes_a1 __attribute__((ext_vector_type(sizeof(T) * 4), aligned(1)));
-    if constexpr (kFull) {
+    if (kFull || i + 4 <= n) {
         *reinterpret_cast<bytes_a1 *>(p + i) = __builtin_bit_cast(bytes_a1, v);
     } else {
 #pragma unroll
@@ -125,23 +131,37 @@ __device__ __forceinline__ double wave_sum_f64(double v) {
     return __builtin_bit_cast(double, readlane_i64(__builtin_bit_cast(int64_t, v), kWave - 1));
 }
 
+template <int kVec>
+__device__ __forceinline__ void add_squares(const float (&v)[kVec], double (&s)[2]) {
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) s[e % 2] = __builtin_fma((double)v[e], (double)v[e], s[e % 2]);
+}
 template <typename T>
 __device__ __forceinline__ double squares(const T *g, int64_t from, int64_t to) {
-    constexpr int kVec = kVecOf<T>;
-    double s = 0.0;
-#pragma unroll 4
-    for (int64_t i = from + (int64_t)threadIdx.x * kVec; i < to; i += kNormThreads * kVec) {
-        float v[kVec];
+    constexpr int kVec = kVecOf<T>, kRound = kNormThreads * kVec, kAtOnce = 4;
+    double s[2] = {0.0, 0.0};
+    float v[kVec];
+    int64_t i = from + (int64_t)threadIdx.x * kVec;
+    for (; i + (kAtOnce - 1) * kRound + kVec <= to; i += kAtOnce * kRound) {
+        uint4 r[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) r[k] = load_a1(g + i + k * kRound);
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            unpack16<T>(r[k], v);
+            add_squares(v, s);
+        }
+    }
+    for (; i < to; i += kRound) {
         if (i + kVec <= to) {
             unpack16<T>(load_a1(g + i), v);
         } else {
 #pragma unroll
             for (int e = 0; e < kVec; ++e) v[e] = i + e < to ? to_f32(g[i + e]) : 0.0f;
         }
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) s = __builtin_fma((double)v[e], (double)v[e], s);
+        add_squares(v, s);
     }
-    return s;
+    return s[0] + s[1];
 }
 
 __global__ __launch_bounds__(kNormThreads) void grad_norm_kernel(Table<NormEntry, kNormTable> t, int64_t chunk, double *__restrict__ sums) {
@@ -166,7 +186,7 @@ constexpr int kNormJoin = 1024;
 __global__ __launch_bounds__(kNormJoin) void grad_norm_join_kernel(const double *__restrict__ sums, int64_t n, double max_norm,
                                                                    float *__restrict__ norm_out, float *__restrict__ factor_out) {
     double s = 0.0;
-#pragma unroll 4
+#pragma unroll 8
     for (int64_t i = threadIdx.x; i < n; i += kNormJoin) s += sums[i];
     s = wave_sum_f64(s);
     __shared__ double wave[kNormJoin / kWave];
@@ -221,13 +241,31 @@ struct AdamStep {
         unbias = (float)(1.0 / sqrt(keep2));
         eps = (float)h.eps;
     }
-    __device__ __forceinline__ float operator()(float p, float m, float v) const {
-        return p * keep - size * (m / (sqrtf(v) * unbias + eps));
+    // root = sqrt(v') and the quotient by the chip's own square root and reciprocal, a unit of 2^-23 each.
+    __device__ __forceinline__ float operator()(float p, float m, float root) const {
+        const float q = m * __builtin_amdgcn_rcpf(__builtin_fmaf(root, unbias, eps));
+        return __builtin_fmaf(-size, q, p * keep);
     }
 };
 
+// Square roots of a lane's v, which the chip takes of normal numbers only.
+template <int kN>
+__device__ __forceinline__ void roots(const float (&v)[kN], float (&root)[kN]) {
+    uint32_t least = UINT32_MAX;
+#pragma unroll
+    for (int e = 0; e < kN; ++e) {
+        root[e] = __builtin_amdgcn_sqrtf(v[e]);
+        const uint32_t bits = __builtin_bit_cast(uint32_t, v[e]) - 1u;      // 0 comes last
+        least = bits < least ? bits : least;
+    }
+    if (least < 0x7fffffu) {
+#pragma unroll
+        for (int e = 0; e < kN; ++e) root[e] = sqrtf(v[e]);
+    }
+}
+
 template <typename P, bool kFull>
-__device__ __forceinline__ void store_params(const AdamEntry &t, int copy_dtype, int64_t i, const float (&p)[4]) {
+__device__ __forceinline__ void store_params(const AdamEntry &t, int copy_dtype, int64_t i, const float *p) {
     Four<P> to;
 #pragma unroll
     for (int e = 0; e < 4; ++e) to.e[e] = from_f32<P>(p[e]);
@@ -247,115 +285,186 @@ __device__ __forceinline__ void store_params(const AdamEntry &t, int copy_dtype,
 
 template <typename P, typename G>
 struct Adam32 {
-    Four<P> p;
-    Four<G> g;
-    Four<float> m, v;
+    Four<P> p[kLaneRuns];
+    Four<G> g[kLaneRuns];
+    Four<float> m[kLaneRuns], v[kLaneRuns];
     template <bool kFull>
-    __device__ __forceinline__ void load(const AdamEntry &t, int64_t i, int64_t) {
-        p = load_four_of<P, kFull>((const P *)t.p, i, t.n);
-        g = load_four_of<G, kFull>((const G *)t.g, i, t.n);
-        m = load_four_of<float, kFull>((const float *)t.m, i, t.n);
-        v = load_four_of<float, kFull>((const float *)t.v, i, t.n);
+    __device__ __forceinline__ void load(const AdamEntry &t, int64_t at) {
+#pragma unroll
+        for (int j = 0; j < kLaneRuns; ++j) {
+            const int64_t i = run_of(at, j);
+            p[j] = load_four_of<P, kFull>((const P *)t.p, i, t.n);
+            g[j] = load_four_of<G, kFull>((const G *)t.g, i, t.n);
+            m[j] = load_four_of<float, kFull>((const float *)t.m, i, t.n);
+            v[j] = load_four_of<float, kFull>((const float *)t.v, i, t.n);
+        }
     }
     template <bool kFull>
-    __device__ __forceinline__ void step(const AdamEntry &t, const AdamHyper &h, const AdamStep &s, float factor, int copy_dtype,
-                                         int64_t i, int64_t) {
+    __device__ __forceinline__ void step(const AdamEntry &t, const AdamHyper &h, const AdamStep &s, float factor, int copy_dtype, int64_t at) {
         const float b1 = (float)h.beta1, c1 = (float)(1.0 - h.beta1), b2 = (float)h.beta2, c2 = (float)(1.0 - h.beta2);
-        float to[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float d = to_f32(g.e[e]) * factor;
-            m.e[e] = __builtin_fmaf(b1, m.e[e], c1 * d);
-            v.e[e] = __builtin_fmaf(b2, v.e[e], c2 * d * d);
-            to[e] = s(to_f32(p.e[e]), m.e[e], v.e[e]);
+        for (int j = 0; j < kLaneRuns; ++j) {
+            const int64_t i = run_of(at, j);
+            float to[kPerRun], root[kPerRun];
+#pragma unroll
+            for (int e = 0; e < kPerRun; ++e) {
+                const float d = to_f32(g[j].e[e]) * factor;
+                m[j].e[e] = __builtin_fmaf(b1, m[j].e[e], c1 * d);
+                v[j].e[e] = __builtin_fmaf(b2, v[j].e[e], c2 * d * d);
+            }
+            roots(v[j].e, root);
+#pragma unroll
+            for (int e = 0; e < kPerRun; ++e) to[e] = s(to_f32(p[j].e[e]), m[j].e[e], root[e]);
+            store_params<P, kFull>(t, copy_dtype, i, to);
+            store_four_of<float, kFull>((float *)t.m, i, t.n, m[j]);
+            store_four_of<float, kFull>((float *)t.v, i, t.n, v[j]);
         }
-        store_params<P, kFull>(t, copy_dtype, i, to);
-        store_four_of<float, kFull>((float *)t.m, i, t.n, m);
-        store_four_of<float, kFull>((float *)t.v, i, t.n, v);
     }
 };
 
-// The code of x >= 0 against a scale, from its root t in binary32: the nearest whole
-// number. `reaches(b)`: whether x is at or above what b stands for, in binary64. t is
-// within 2^-13 of the root: a rounding of x over the scale, a unit of 2^-23 of each
-// square root and a rounding of the product, (1/4 + 2/2 + 2 + 1) 2^-24 x 255 = 6.5e-5 where
-// the root is the fourth.
-template <typename F>
-__device__ __forceinline__ int code_of(float t, F reaches) {
-    const float low = __builtin_floorf(t), rest = t - low;
-    int c = (int)low + (rest >= 0.5f ? 1 : 0);
-    if (__builtin_fabsf(rest - 0.5f) < 0x1p-13f) c = (int)low + (reaches((double)low + 0.5) ? 1 : 0);
-    return c;
+// The largest of 32 lanes' numbers (no NaN), in each of them.
+__device__ __forceinline__ double half_max_f64(double v) {
+    auto step = [&](uint64_t got) {
+        const double x = __builtin_bit_cast(double, got);
+        v = x > v ? x : v;
+    };
+    step(dpp_u64<0xb1, 0xf>(0ull, __builtin_bit_cast(uint64_t, v)));
+    step(dpp_u64<0x4e, 0xf>(0ull, __builtin_bit_cast(uint64_t, v)));
+    step(dpp_u64<0x141, 0xf>(0ull, __builtin_bit_cast(uint64_t, v)));
+    step(dpp_u64<0x140, 0xf>(0ull, __builtin_bit_cast(uint64_t, v)));
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_swizzle((int)(uint32_t)b, 0x401f), hi = (uint32_t)__builtin_amdgcn_ds_swizzle((int)(b >> 32), 0x401f);
+    step(((uint64_t)hi << 32) | lo);
+    return v;
+}
+// The four bytes of a word as numbers, and four numbers 0 .. 255 as bytes, to the nearest.
+__device__ __forceinline__ float byte_of(uint32_t w, int e) { return (float)((w >> (8 * e)) & 0xffu); }
+__device__ __forceinline__ uint32_t bytes_from(const float *v) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w = __builtin_amdgcn_cvt_pk_u8_f32(v[e], e, w);
+    return w;
+}
+// Whether x (of a block whose largest is `most`) is at or above what lies halfway between the codes c and c + 1.
+__device__ __forceinline__ bool above_m(double x, double c, double most) { return x * kRoots2 >= (c + 0.5) * (c + 0.5) * most; }
+__device__ __forceinline__ bool above_v(double x, double c, double most) {
+    const double b = (c + 0.5) * (c + 0.5);
+    return x * kRoots4 >= b * b * most;
 }
 
 template <typename P, typename G>
 struct Adam8 {
-    Four<P> p;
-    Four<G> g;
-    Four<int8_t> mc;
-    Four<uint8_t> vc;
-    float m_scale, v_scale;
+    Four<P> p[kLaneRuns];
+    Four<G> g[kLaneRuns];
+    Four<uint8_t> mc[kLaneRuns], vc[kLaneRuns];
+    float2 scale;
+    static __device__ __forceinline__ int64_t block_of(int64_t at) { return at / kAdamBlock + lane_id() / 32; }
     template <bool kFull>
-    __device__ __forceinline__ void load(const AdamEntry &t, int64_t i, int64_t block) {
-        p = load_four_of<P, kFull>((const P *)t.p, i, t.n);
-        g = load_four_of<G, kFull>((const G *)t.g, i, t.n);
-        mc = load_four_of<int8_t, kFull>((const int8_t *)t.m, i, t.n);
-        vc = load_four_of<uint8_t, kFull>((const uint8_t *)t.v, i, t.n);
-        m_scale = t.scale[2 * block];
-        v_scale = t.scale[2 * block + 1];
+    __device__ __forceinline__ void load(const AdamEntry &t, int64_t at) {
+#pragma unroll
+        for (int j = 0; j < kLaneRuns; ++j) {
+            const int64_t i = run_of(at, j);
+            p[j] = load_four_of<P, kFull>((const P *)t.p, i, t.n);
+            g[j] = load_four_of<G, kFull>((const G *)t.g, i, t.n);
+            mc[j] = load_four_of<uint8_t, kFull>((const uint8_t *)t.m, i, t.n);
+            vc[j] = load_four_of<uint8_t, kFull>((const uint8_t *)t.v, i, t.n);
+        }
+        const int64_t block = block_of(at);
+        scale = make_float2(0.0f, 0.0f);
+        if (kFull || block * kAdamBlock < t.n) scale = make_float2(t.scale[2 * block], t.scale[2 * block + 1]);
     }
     template <bool kFull>
-    __device__ __forceinline__ void step(const AdamEntry &t, const AdamHyper &h, const AdamStep &s, float factor, int copy_dtype,
-                                         int64_t i, int64_t block) {
-        const double m_unit = h.beta1 * ((double)m_scale * (1.0 / kRoots2)), v_unit = h.beta2 * ((double)v_scale * (1.0 / kRoots4));
-        const double c1 = 1.0 - h.beta1, c2 = 1.0 - h.beta2, f = (double)factor;
-        double m[4], v[4];
-        float to[4];
-        uint64_t m_most = 0, v_most = 0;      // numbers as bits: in order, NaN above infinity
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const double d = (double)to_f32(g.e[e]) * f;
-            const int c = mc.e[e], a = c < 0 ? -c : c;
-            const uint32_t q = (uint32_t)vc.e[e] * (uint32_t)vc.e[e];
-            m[e] = __builtin_fma((double)(c * a), m_unit, c1 * d);
-            v[e] = __builtin_fma((double)(q * q), v_unit, c2 * d * d);
-            const float m32 = (float)m[e], v32 = (float)v[e];
-            to[e] = s(to_f32(p.e[e]), m32, v32);
-            const uint64_t mb = __builtin_bit_cast(uint64_t, __builtin_fabs(m[e])), vb = __builtin_bit_cast(uint64_t, __builtin_fabs(v[e]));
-            m_most = mb > m_most ? mb : m_most;
-            v_most = vb > v_most ? vb : v_most;
-        }
-        store_params<P, kFull>(t, copy_dtype, i, to);
+    __device__ __forceinline__ void step(const AdamEntry &t, const AdamHyper &h, const AdamStep &s, float factor, int copy_dtype, int64_t at) {
+        const double m_unit = h.beta1 * ((double)scale.x * (1.0 / kRoots2)), v_unit = h.beta2 * ((double)scale.y * (1.0 / kRoots4));
+        const double f = (double)factor, c1 = (1.0 - h.beta1) * f, c2 = (1.0 - h.beta2) * f * f;
+        constexpr int kN = kLaneRuns * kPerRun;
+        double m[kN], v[kN], m_most = 0.0, v_most = 0.0;
+        float m32[kN], v32[kN], root[kN];
+        uint32_t largest = 0;                          // of v's bits: infinities and NaN are above numbers
         // Elements behind the tensor's last are zeros, codes, gradient and all.
-        const double m_in = __builtin_bit_cast(double, wave_max_u64(m_most)), v_in = __builtin_bit_cast(double, wave_max_u64(v_most));
-        const float m_new = new_scale(m_in), v_new = new_scale(v_in);
-        const double m_inv = 1.0 / m_in, v_inv = 1.0 / v_in;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const double x = __builtin_fabs(m[e]);
-            int c = 0;
-            if (m_new > 0.0f)
-                c = code_of(127.0f * __builtin_amdgcn_sqrtf((float)(x * m_inv)), [&](double b) { return x * kRoots2 >= b * b * m_in; });
-            mc.e[e] = (int8_t)(m[e] < 0.0 ? -c : c);
-            c = 0;
-            if (v_new > 0.0f) {
-                const double y = v[e];
-                c = code_of(255.0f * __builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf((float)(y * v_inv))),
-                            [&](double b) { return y * kRoots4 >= (b * b) * (b * b) * v_in; });
-                c = y > 0.0 && c == 0 ? 1 : c;
-            }
-            vc.e[e] = (uint8_t)c;
+        for (int k = 0; k < kN; ++k) {
+            const int j = k / kPerRun, e = k % kPerRun;
+            const double d = (double)to_f32(g[j].e[e]);
+            const float c = byte_of(__builtin_bit_cast(uint32_t, mc[j]) ^ 0x80808080u, e) - 128.0f, q = byte_of(__builtin_bit_cast(uint32_t, vc[j]), e);
+            const double qq = (double)(q * q);
+            m[k] = __builtin_fma((double)(c * __builtin_fabsf(c)), m_unit, c1 * d);
+            v[k] = __builtin_fma(qq * v_unit, qq, c2 * d * d);
+            m32[k] = (float)m[k];
+            v32[k] = (float)v[k];
+            const uint32_t bits = __builtin_bit_cast(uint32_t, v32[k]);
+            largest = bits > largest ? bits : largest;
+            const double x = __builtin_fabs(m[k]);
+            m_most = x > m_most ? x : m_most;
+            v_most = v[k] > v_most ? v[k] : v_most;
         }
-        store_four_of<int8_t, kFull>((int8_t *)t.m, i, t.n, mc);
-        store_four_of<uint8_t, kFull>((uint8_t *)t.v, i, t.n, vc);
-        if (lane_id() == 0) {
+        roots(v32, root);
+#pragma unroll
+        for (int j = 0; j < kLaneRuns; ++j) {
+            float to[kPerRun];
+#pragma unroll
+            for (int e = 0; e < kPerRun; ++e) to[e] = s(to_f32(p[j].e[e]), m32[j * kPerRun + e], root[j * kPerRun + e]);
+            store_params<P, kFull>(t, copy_dtype, run_of(at, j), to);
+        }
+        m_most = half_max_f64(m_most);
+        v_most = half_max_f64(v_most);
+        const uint64_t spoilt = ballot(largest >= 0x7f800000u || !(__builtin_fabsf(scale.x) < __builtin_inff()));
+        const bool bad = (uint32_t)(spoilt >> (lane_id() & 32)) != 0;
+        const float m_new = new_scale(m_most, bad), v_new = new_scale(v_most, bad);
+
+        // Codes from roots in binary32. 127 sqrt(|m| / M): roundings of m, of 1 / M and of their product, halved, a unit of 2^-23 of
+        // the root and a rounding of the product with 127, 4.5 x 2^-24 x 127 = 2^-14.8 in all; 255 sqrt(sqrt(v) / sqrt(V)): a unit
+        // of each root and two roundings, halved, a unit and a rounding, 5.5 x 2^-24 x 255 = 2^-13.5.
+        constexpr float kNearM = 0.5f - 0x1p-14f, kNearV = 0.5f - 0x1p-13f;
+        const float m_inv = 1.0f / m_new, v_inv = 1.0f / sqrtf(v_new);
+        float cm[kN], cv[kN], far_m = 0.0f, far_v = 0.0f, least = 1.0f;
+#pragma unroll
+        for (int k = 0; k < kN; ++k) {
+            const float tm = 127.0f * __builtin_amdgcn_sqrtf(__builtin_fabsf(m32[k]) * m_inv), tv = 255.0f * __builtin_amdgcn_sqrtf(root[k] * v_inv);
+            cm[k] = __builtin_rintf(tm);
+            cv[k] = __builtin_rintf(tv);
+            far_m = __builtin_fmaxf(far_m, __builtin_fabsf(tm - cm[k]));
+            far_v = __builtin_fmaxf(far_v, __builtin_fabsf(tv - cv[k]));
+            least = __builtin_fminf(least, cv[k]);
+        }
+        auto far_out = [](float scale) { return scale > 0.0f && (scale < 0x1p-80f || scale > 0x1p100f); };
+        const bool tiny = far_out(m_new) || far_out(v_new);
+        if (far_m >= kNearM || far_v >= kNearV || least < 1.0f || tiny) {
+#pragma unroll
+            for (int k = 0; k < kN; ++k) {
+                const double x = __builtin_fabs(m[k]), y = v[k];
+                if (tiny) {      // shares that leave binary32's normal numbers
+                    cm[k] = (float)__builtin_floor(127.0 * sqrt(x / m_most));
+                    cv[k] = (float)__builtin_floor(255.0 * sqrt(sqrt(y / v_most)));
+                    cm[k] += above_m(x, cm[k], m_most) ? 1.0f : 0.0f;
+                    cv[k] += above_v(y, cv[k], v_most) ? 1.0f : 0.0f;
+                } else {
+                    const float tm = 127.0f * __builtin_amdgcn_sqrtf(__builtin_fabsf(m32[k]) * m_inv);
+                    const float tv = 255.0f * __builtin_amdgcn_sqrtf(root[k] * v_inv);
+                    if (__builtin_fabsf(tm - cm[k]) >= kNearM) cm[k] = __builtin_floorf(tm) + (above_m(x, __builtin_floorf(tm), m_most) ? 1.0f : 0.0f);
+                    if (__builtin_fabsf(tv - cv[k]) >= kNearV) cv[k] = __builtin_floorf(tv) + (above_v(y, __builtin_floorf(tv), v_most) ? 1.0f : 0.0f);
+                }
+                cv[k] = y > 0.0 && cv[k] < 1.0f ? 1.0f : cv[k];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kN; ++k) cm[k] = __builtin_copysignf(cm[k], m32[k]) + 128.0f;
+#pragma unroll
+        for (int j = 0; j < kLaneRuns; ++j) {
+            const int64_t i = run_of(at, j);
+            const uint32_t mw = m_new > 0.0f ? bytes_from(cm + j * kPerRun) ^ 0x80808080u : 0u, vw = v_new > 0.0f ? bytes_from(cv + j * kPerRun) : 0u;
+            store_four_of<uint8_t, kFull>((uint8_t *)t.m, i, t.n, __builtin_bit_cast(Four<uint8_t>, mw));
+            store_four_of<uint8_t, kFull>((uint8_t *)t.v, i, t.n, __builtin_bit_cast(Four<uint8_t>, vw));
+        }
+        const int64_t block = block_of(at);
+        if (lane_id() % 32 == 0 && (kFull || block * kAdamBlock < t.n)) {
             t.scale[2 * block] = m_new;
             t.scale[2 * block + 1] = v_new;
         }
     }
-    static __device__ __forceinline__ float new_scale(double most) {
+    static __device__ __forceinline__ float new_scale(double most, bool bad) {
         const float v = (float)most;
-        return v < __builtin_inff() ? (most < (double)kScaleMin ? 0.0f : v) : __builtin_nanf("");
+        return bad || !(v < __builtin_inff()) ? __builtin_nanf("") : (most < (double)kScaleMin ? 0.0f : v);
     }
 };
 
@@ -371,22 +480,25 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(AdamTable table, Ad
     const AdamStep s(h, t.decay);
     const int wave = readlane_i32((int)threadIdx.x / kWave, 0);
     const int64_t from = (int64_t)(blockIdx.x - table.first[k]) * kAdamChunk;
-    auto first_of = [&](int turn) { return from + (int64_t)(turn * (kAdamThreads / kWave) + wave) * kAdamBlock; };
-    const int lane = lane_id() * kPerLane;
+    auto first_of = [&](int turn) { return from + (int64_t)(turn * (kAdamThreads / kWave) + wave) * kWaveRun; };
     if (from + kAdamChunk <= t.n) {
         State<P, G> state[kWaveTurns];
 #pragma unroll
-        for (int turn = 0; turn < kWaveTurns; ++turn) state[turn].template load<true>(t, first_of(turn) + lane, first_of(turn) / kAdamBlock);
+        for (int turn = 0; turn < kWaveTurns; ++turn) state[turn].template load<true>(t, first_of(turn));
 #pragma unroll
-        for (int turn = 0; turn < kWaveTurns; ++turn)
-            state[turn].template step<true>(t, h, s, factor, copy_dtype, first_of(turn) + lane, first_of(turn) / kAdamBlock);
+        for (int turn = 0; turn < kWaveTurns; ++turn) state[turn].template step<true>(t, h, s, factor, copy_dtype, first_of(turn));
     } else {
         for (int turn = 0; turn < kWaveTurns; ++turn) {
             const int64_t at = first_of(turn);
             if (at >= t.n) break;                      // the whole wave
             State<P, G> state;
-            state.template load<false>(t, at + lane, at / kAdamBlock);
-            state.template step<false>(t, h, s, factor, copy_dtype, at + lane, at / kAdamBlock);
+            if (at + kWaveRun <= t.n) {
+                state.template load<true>(t, at);
+                state.template step<true>(t, h, s, factor, copy_dtype, at);
+            } else {
+                state.template load<false>(t, at);
+                state.template step<false>(t, h, s, factor, copy_dtype, at);
+            }
         }
     }
 }
@@ -401,32 +513,52 @@ struct UnpackEntry {
 };
 constexpr int kUnpackTable = 64;
 
+struct Codes {
+    Four<uint8_t> m, v;
+    float2 scale;
+    template <bool kFull>
+    __device__ __forceinline__ void load(const UnpackEntry &t, int64_t at) {
+        const int64_t i = at + lane_id() * kPerRun, block = at / kAdamBlock;
+        m = load_four_of<uint8_t, kFull>((const uint8_t *)t.m, i, t.n);
+        v = load_four_of<uint8_t, kFull>(t.v, i, t.n);
+        scale = make_float2(t.scale[2 * block], t.scale[2 * block + 1]);
+    }
+    template <bool kFull>
+    __device__ __forceinline__ void store(const UnpackEntry &t, int64_t at) const {
+        const int64_t i = at + lane_id() * kPerRun;
+        const double m_unit = (double)scale.x * (1.0 / kRoots2), v_unit = (double)scale.y * (1.0 / kRoots4);
+        Four<float> x, y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float c = byte_of(__builtin_bit_cast(uint32_t, m) ^ 0x80808080u, e) - 128.0f, q = byte_of(__builtin_bit_cast(uint32_t, v), e);
+            const double qq = (double)(q * q);
+            x.e[e] = (float)((double)(c * __builtin_fabsf(c)) * m_unit);
+            y.e[e] = (float)(qq * v_unit * qq);
+        }
+        if (t.m_out) store_four_of<float, kFull>(t.m_out, i, t.n, x);
+        if (t.v_out) store_four_of<float, kFull>(t.v_out, i, t.n, y);
+    }
+};
+
 __global__ __launch_bounds__(kAdamThreads) void adamw_unpack_kernel(Table<UnpackEntry, kUnpackTable> table) {
+    constexpr int kTurns = (int)(kAdamChunk / (kAdamThreads / kWave) / kAdamBlock);      // a block a wave
     const int k = tensor_of(table, blockIdx.x);
     const UnpackEntry t = table.entry[k];
     const int wave = readlane_i32((int)threadIdx.x / kWave, 0);
     const int64_t from = (int64_t)(blockIdx.x - table.first[k]) * kAdamChunk;
-    auto one = [&](auto full, int64_t at) {
-        constexpr bool kFull = decltype(full)::value;
-        const int64_t i = at + lane_id() * kPerLane, block = at / kAdamBlock;
-        const Four<int8_t> mc = load_four_of<int8_t, kFull>(t.m, i, t.n);
-        const Four<uint8_t> vc = load_four_of<uint8_t, kFull>(t.v, i, t.n);
-        const double m_unit = (double)t.scale[2 * block] * (1.0 / kRoots2), v_unit = (double)t.scale[2 * block + 1] * (1.0 / kRoots4);
-        Four<float> m, v;
+    auto first_of = [&](int turn) { return from + (int64_t)(turn * (kAdamThreads / kWave) + wave) * kAdamBlock; };
+    if (from + kAdamChunk <= t.n) {
+        Codes c[kTurns];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int c = mc.e[e], a = c < 0 ? -c : c;
-            const uint32_t q = (uint32_t)vc.e[e] * (uint32_t)vc.e[e];
-            m.e[e] = (float)((double)(c * a) * m_unit);
-            v.e[e] = (float)((double)(q * q) * v_unit);
+        for (int turn = 0; turn < kTurns; ++turn) c[turn].load<true>(t, first_of(turn));
+#pragma unroll
+        for (int turn = 0; turn < kTurns; ++turn) c[turn].store<true>(t, first_of(turn));
+    } else {
+        for (int turn = 0; turn < kTurns && first_of(turn) < t.n; ++turn) {
+            Codes c;
+            c.load<false>(t, first_of(turn));
+            c.store<false>(t, first_of(turn));
         }
-        if (t.m_out) store_four_of<float, kFull>(t.m_out, i, t.n, m);
-        if (t.v_out) store_four_of<float, kFull>(t.v_out, i, t.n, v);
-    };
-    for (int turn = 0; turn < kWaveTurns; ++turn) {
-        const int64_t at = from + (int64_t)(turn * (kAdamThreads / kWave) + wave) * kAdamBlock;
-        if (at + kAdamBlock <= t.n) one(std::true_type{}, at);
-        else if (at < t.n) one(std::false_type{}, at);
     }
 }
 

@@ -293,9 +293,9 @@ inline int64_t layer_norm_part_floats_most(int64_t rows, int64_t cols) {
 }
 
 // ---- gradient norm and AdamW (adamw.hip) -----------------------------------------------
-// Elements of a tensor that a workgroup squares and adds: at most 4096 sums to
+// Elements of a tensor that a workgroup squares and adds: at most 16384 sums to
 // join, or as many as of the longest there are.
-constexpr int64_t kNormChunkMin = 8192, kNormChunkMax = 65536, kNormSlots = 4096;
+constexpr int64_t kNormChunkMin = 8192, kNormChunkMax = 65536, kNormSlots = 16384;
 inline int64_t grad_norm_chunk(int64_t n_elements) {
     int64_t chunk = kNormChunkMin;
     while (chunk < kNormChunkMax && n_elements / chunk > kNormSlots) chunk *= 2;
