@@ -35,10 +35,12 @@ The norm before the head, and the element-wise update of any weights:
 from __future__ import annotations
 
 import ctypes
+from array import array
 from typing import Optional, Sequence
 
 import torch
 
+from . import _lib
 from ._lib import AdamwParams, PaceParams, lib, library_path
 
 __all__ = [
@@ -883,36 +885,14 @@ def pace_layer_norm_backward(x, stats, grad_out, weight=None, buffers=None, stre
     return grad_x, grad_weight, grad_bias
 
 
-def _each(tensors, name: str, device=None, dtypes=None, sizes=None):
-    """A list of contiguous device tensors on one device; returns the list, its device, pointers and sizes as the C ABI takes them.
-    dtypes: the types allowed; sizes: the elements that each must have."""
-    ts = list(tensors)
-    for k, t in enumerate(ts):
-        if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous() or t.dtype not in dtypes:
-            raise ValueError("%s[%d] must be a contiguous device tensor of %s" % (name, k, " or ".join(map(str, dtypes))))
-        if device is None:
-            device = t.device
-        if t.device != device:
-            raise ValueError("%s[%d] must be on %s" % (name, k, device))
-    if device is None:
-        raise ValueError("%s must hold a tensor" % name)
-    counts = [t.numel() for t in ts]
-    if sizes is not None and counts != sizes:
-        raise ValueError("%s must have %s elements, got %s" % (name, sizes, counts))
-    n = max(len(ts), 1)
-    return ts, device, (ctypes.c_void_p * n)(*[t.data_ptr() for t in ts]), counts
+_FLOATS, _F32, _HALVES, _INT8, _UINT8 = 7, 1, 6, 8, 16      # sets of types, a bit for each
 
 
-def _int32s(values):
-    return (ctypes.c_int32 * max(len(values), 1))(*values)
-
-
-def _sizes(counts):
-    return (ctypes.c_int64 * max(len(counts), 1))(*counts)
-
-
-def _codes(ts):
-    return _int32s([DTYPES[t.dtype] for t in ts])
+def _each(tensors, name: str, types: int, device: int = -1, written: bool = False, sizes=None, block: int = 0):
+    """A list of contiguous device tensors on one device, as the C ABI takes them: (count, device index, pointers, dtypes, sizes,
+    elements), the three arrays as bytes. written: they must not overlap; sizes (bytes): the elements that each must have, or
+    with `block` two for every so many."""
+    return _lib.lists().read(tensors, name, types, device, written, sizes, block)
 
 
 def pace_grad_norm_workspace_bytes(n_tensors: int, n_elements: int) -> int:
@@ -931,11 +911,12 @@ def grad_norm_buffers(n_tensors: int, n_elements: int, device, stream=None):
 def pace_grad_norm(grads, max_norm: float = float("inf"), buffers=None, stream=None):
     """The 2-norm of all gradients together. Returns (norm f32[1], factor f32[1]: min(1, max_norm / norm), NaN where the norm
     is no number)."""
-    ts, dev, ptrs, counts = _each(grads, "grads", dtypes=DTYPES)
-    b = grad_norm_buffers(len(ts), sum(counts), dev, stream) if buffers is None else buffers
+    n, at, ptrs, codes, sizes, total = _each(grads, "grads", _FLOATS)
+    dev = torch.device("cuda", at)
+    b = grad_norm_buffers(n, total, dev, stream) if buffers is None else buffers
     norm, factor = _sized(b["norm"], torch.float32, (1,), dev, "norm"), _sized(b["factor"], torch.float32, (1,), dev, "factor")
     ws, ws_bytes = _scratch(b["workspace"], dev)
-    _check(lib().pace_grad_norm(len(ts), ptrs, _codes(ts), _sizes(counts), float(max_norm), norm.data_ptr(), factor.data_ptr(),
+    _check(lib().pace_grad_norm(n, ptrs, codes, sizes, float(max_norm), norm.data_ptr(), factor.data_ptr(),
                                 ws, ws_bytes, _stream(dev, stream)), "pace_grad_norm")
     return norm, factor
 
@@ -943,7 +924,8 @@ def pace_grad_norm(grads, max_norm: float = float("inf"), buffers=None, stream=N
 def adamw_state(params, bits: int = 32, copy_dtype=None, stream=None):
     """Fresh moments for pace_adamw of these tensors: zeros, in float32 or with ``bits`` 8 as codes with two scales for every
     ADAMW_BLOCK elements. With copy_dtype (bfloat16 or float16) each step writes the new parameters in that type too."""
-    ts, dev, _, counts = _each(params, "params", dtypes=DTYPES)
+    ts = list(params)
+    dev = torch.device("cuda", _each(ts, "params", _FLOATS)[1])
     if bits not in (32, 8):
         raise ValueError("bits must be 32 or 8")
     if copy_dtype not in (None, torch.bfloat16, torch.float16):
@@ -960,21 +942,18 @@ def adamw_state(params, bits: int = 32, copy_dtype=None, stream=None):
 
     moments = (torch.float32, torch.float32) if bits == 32 else (torch.int8, torch.uint8)
     return dict(bits=bits, exp_avg=[zeros(t.shape, moments[0]) for t in ts], exp_avg_sq=[zeros(t.shape, moments[1]) for t in ts],
-                scale=[zeros((-(-n // ADAMW_BLOCK), 2), torch.float32) for n in counts] if bits == 8 else None,
+                scale=[zeros((-(-t.numel() // ADAMW_BLOCK), 2), torch.float32) for t in ts] if bits == 8 else None,
                 copies=[zeros(t.shape, copy_dtype) for t in ts] if copy_dtype is not None else None)
 
 
-def _moments(state, dev, counts):
+def _moments(state, device: int, sizes):
     """The state's moments and scales as the C ABI takes them."""
-    if state["bits"] == 32:
-        kinds, scales = ((torch.float32,), (torch.float32,)), None
-    elif state["bits"] == 8:
-        kinds = ((torch.int8,), (torch.uint8,))
-        scales = _each(state["scale"], "scale", dev, (torch.float32,), [2 * -(-n // ADAMW_BLOCK) for n in counts])[2]
-    else:
+    bits = state["bits"]
+    if bits not in (32, 8):
         raise ValueError("bits must be 32 or 8")
-    m = _each(state["exp_avg"], "exp_avg", dev, kinds[0], counts)[2]
-    return m, _each(state["exp_avg_sq"], "exp_avg_sq", dev, kinds[1], counts)[2], scales
+    m = _each(state["exp_avg"], "exp_avg", _F32 if bits == 32 else _INT8, device, True, sizes)[2]
+    v = _each(state["exp_avg_sq"], "exp_avg_sq", _F32 if bits == 32 else _UINT8, device, True, sizes)[2]
+    return bits, m, v, _each(state["scale"], "scale", _F32, device, True, sizes, ADAMW_BLOCK)[2] if bits == 8 else None
 
 
 def pace_adamw(params, grads, state, lr: float = 1e-3, step: int = 1, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.0,
@@ -982,30 +961,26 @@ def pace_adamw(params, grads, state, lr: float = 1e-3, step: int = 1, betas=(0.9
     """One AdamW step over a list of tensors, in place: params, the moments in ``state`` (adamw_state) and its copies. step is
     the number of this update, from 1. weight_decay: a number, or one for each tensor. grad_scale (f32[1], pace_grad_norm's
     factor) multiplies the gradients; where it is no number nothing changes. schedule (f64[2] on the device: lr, step) stands
-    in for lr and step in calls that are captured and replayed."""
-    ps, dev, p, counts = _each(params, "params", dtypes=DTYPES)
-    gs, _, g, _ = _each(grads, "grads", dev, DTYPES, counts)
-    m, v, scales = _moments(state, dev, counts)
-    written = [t.data_ptr() for t in ps if t.numel()]
-    if len(set(written)) != len(written):
-        raise ValueError("params must not hold a tensor twice")
-    copies = codes = None
+    in for lr and step in calls that are captured and replayed. Returns params."""
+    n, at, p, types, sizes, _ = _each(params, "params", _FLOATS, written=True)
+    _, _, g, grad_types, _, _ = _each(grads, "grads", _FLOATS, at, sizes=sizes)
+    bits, m, v, scales = _moments(state, at, sizes)
+    copies = copy_types = None
     if state["copies"] is not None:
-        cs, _, copies, _ = _each(state["copies"], "copies", dev, (torch.bfloat16, torch.float16), counts)
-        codes = _codes(cs)
-    decay = [float(weight_decay)] * len(ps) if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
-    if len(decay) != len(ps):
+        _, _, copies, copy_types, _, _ = _each(state["copies"], "copies", _HALVES, at, True, sizes)
+    decay = array("f", [weight_decay]) * n if isinstance(weight_decay, (int, float)) else array("f", weight_decay)
+    if len(decay) != n:
         raise ValueError("weight_decay must be a number or one for each tensor")
     if len(betas) != 2:
         raise ValueError("betas must be two numbers")
+    dev = torch.device("cuda", at)
     if grad_scale is not None:
         _vector(grad_scale, torch.float32, 1, dev, "grad_scale")
     if schedule is not None:
         _vector(schedule, torch.float64, 2, dev, "schedule")
     hyper = AdamwParams(float(lr), float(betas[0]), float(betas[1]), float(eps), int(step))
-    _check(lib().pace_adamw(len(ps), _sizes(counts), p, _codes(ps), g, _codes(gs), state["bits"], m, v, scales, copies, codes,
-                            (ctypes.c_float * max(len(decay), 1))(*decay), ctypes.byref(hyper), _ptr(grad_scale), _ptr(schedule),
-                            _stream(dev, stream)), "pace_adamw")
+    _check(lib().pace_adamw(n, sizes, p, types, g, grad_types, bits, m, v, scales, copies, copy_types, decay.tobytes(),
+                            ctypes.byref(hyper), _ptr(grad_scale), _ptr(schedule), _stream(dev, stream)), "pace_adamw")
     return params
 
 
@@ -1014,13 +989,14 @@ def pace_adamw_unpack(state, out=None, stream=None):
     it is given)."""
     if state["bits"] != 8:
         raise ValueError("the moments must be held in 8 bits")
-    ts, dev, _, counts = _each(state["exp_avg"], "exp_avg", dtypes=(torch.int8,))
-    m, v, scales = _moments(state, dev, counts)
+    n, at, _, _, sizes, _ = _each(state["exp_avg"], "exp_avg", _INT8)
+    _, m, v, scales = _moments(state, at, sizes)
+    dev = torch.device("cuda", at)
     if out is None:
         e = _allocator(dev, stream)
-        out = [[e(t.shape, torch.float32) for t in ts] for _ in range(2)]
-    m_out, v_out = (_each(o, "out", dev, (torch.float32,), counts)[2] for o in out)
-    _check(lib().pace_adamw_unpack(len(ts), _sizes(counts), m, v, scales, m_out, v_out, _stream(dev, stream)), "pace_adamw_unpack")
+        out = [[e(t.shape, torch.float32) for t in state["exp_avg"]] for _ in range(2)]
+    m_out, v_out = (_each(o, "out", _F32, at, True, sizes)[2] for o in out)
+    _check(lib().pace_adamw_unpack(n, sizes, m, v, scales, m_out, v_out, _stream(dev, stream)), "pace_adamw_unpack")
     return out[0], out[1]
 
 

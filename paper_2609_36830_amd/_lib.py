@@ -6,7 +6,9 @@ import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 library_path = os.path.join(_HERE, "libpace.so")
+lists_path = os.path.join(_HERE, "_lists.so")
 _lib = None
+_lists = None
 
 
 class PaceParams(ctypes.Structure):
@@ -80,6 +82,21 @@ def load(path: str = library_path):
         fn.restype = res
         fn.argtypes = args
     return h
+
+
+def lists():
+    """The extension that reads lists of tensors; raises if it has not been built (no fallback exists)."""
+    global _lists
+    if _lists is None:
+        import importlib.util
+        import torch  # noqa: F401  (its libraries)
+        if not os.path.exists(lists_path):
+            raise ImportError("_lists.so is not built at %s; run __graft_entry__.build() "
+                              "or python -m paper_2609_36830_amd.build" % lists_path)
+        spec = importlib.util.spec_from_file_location(__package__ + "._lists", lists_path)
+        _lists = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(_lists)
+    return _lists
 
 
 def lib():

@@ -1,0 +1,122 @@
+// Python extension _lists: what the C ABI's calls on many tensors take, read from a
+// list of torch tensors. From Python each tensor costs some 0.4 us for its pointer,
+// type, size, device and layout, five times a step and tensor; here 10 ns.
+#define PY_SSIZE_T_CLEAN
+#include <torch/csrc/autograd/python_variable.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <cstring>
+#include <string>
+#include <utility>
+#include <vector>
+
+namespace {
+
+// Codes of the C ABI's element types, and two more for moments in 8 bits.
+int code_of(const at::Tensor &t) {
+    switch (t.scalar_type()) {
+        case at::kFloat: return 0;
+        case at::kBFloat16: return 1;
+        case at::kHalf: return 2;
+        case at::kChar: return 3;
+        case at::kByte: return 4;
+        default: return -1;
+    }
+}
+std::string names_of(int types) {
+    static const char *const name[] = {"float32", "bfloat16", "float16", "int8", "uint8"};
+    std::string s;
+    for (int k = 0; k < 5; ++k)
+        if (types >> k & 1) s += (s.empty() ? "" : " or ") + std::string(name[k]);
+    return s;
+}
+
+template <typename T>
+PyObject *bytes_of(const std::vector<T> &v) {
+    return PyBytes_FromStringAndSize(reinterpret_cast<const char *>(v.data()), (Py_ssize_t)(v.size() * sizeof(T)));
+}
+
+bool overlap(std::vector<std::pair<uintptr_t, uintptr_t>> &spans) {
+    auto meet = [&]() {
+        for (size_t k = 1; k < spans.size(); ++k)
+            if (spans[k].first < spans[k - 1].second) return true;
+        return false;
+    };
+    if (!std::is_sorted(spans.begin(), spans.end())) std::sort(spans.begin(), spans.end());
+    return meet();
+}
+
+struct Held {      // a reference that ends with its scope
+    PyObject *p;
+    ~Held() { Py_XDECREF(p); }
+};
+
+PyObject *fail(const std::string &text) {
+    PyErr_SetString(PyExc_ValueError, text.c_str());
+    return nullptr;
+}
+
+// read(tensors, name, types, device, written, sizes, block) -> (count, device, pointers, codes, sizes, elements)
+//   types: bit k allows code k; device: index, or -1: the first tensor's; written: whether the
+//   tensors must not overlap; sizes: bytes of int64 that the elements have to be, or None;
+//   with block > 0 two for each block of so many.
+PyObject *read(PyObject *, PyObject *args) {
+    PyObject *tensors, *expected;
+    const char *name;
+    int types, device, written;
+    long long block;
+    if (!PyArg_ParseTuple(args, "OsiipOL", &tensors, &name, &types, &device, &written, &expected, &block)) return nullptr;
+    try {
+        const Held list{PySequence_Fast(tensors, "a list of tensors is wanted")};
+        if (!list.p) return nullptr;
+        const size_t n = (size_t)PySequence_Fast_GET_SIZE(list.p);
+        if (n == 0 && device < 0) return fail(std::string(name) + " must hold a tensor");
+        const int64_t *want = nullptr;
+        if (expected != Py_None) {
+            if (!PyBytes_Check(expected)) return fail("sizes must be bytes");
+            if ((size_t)PyBytes_GET_SIZE(expected) != n * sizeof(int64_t))
+                return fail(std::string(name) + " must hold " + std::to_string(PyBytes_GET_SIZE(expected) / sizeof(int64_t)) + " tensors");
+            want = reinterpret_cast<const int64_t *>(PyBytes_AS_STRING(expected));
+        }
+        std::vector<uintptr_t> pointers(n);
+        std::vector<int32_t> codes(n);
+        std::vector<int64_t> sizes(n);
+        std::vector<std::pair<uintptr_t, uintptr_t>> spans;
+        if (written) spans.reserve(n);
+        int64_t total = 0;
+        for (size_t k = 0; k < n; ++k) {
+            PyObject *item = PySequence_Fast_GET_ITEM(list.p, (Py_ssize_t)k);
+            auto at = [&]() { return std::string(name) + "[" + std::to_string(k) + "]"; };
+            if (!THPVariable_Check(item)) return fail(at() + " must be a tensor");
+            const at::Tensor &t = THPVariable_Unpack(item);
+            codes[k] = code_of(t);
+            if (!t.is_cuda() || t.layout() != at::kStrided || codes[k] < 0 || !(types >> codes[k] & 1) || !t.is_contiguous())
+                return fail(at() + " must be a contiguous device tensor of " + names_of(types));
+            if (device < 0) device = (int)t.get_device();
+            if (t.get_device() != device) return fail(at() + " must be on cuda:" + std::to_string(device));
+            sizes[k] = t.numel();
+            if (want) {
+                int64_t w;
+                std::memcpy(&w, want + k, sizeof w);
+                if (block > 0) w = 2 * ((w + block - 1) / block);
+                if (sizes[k] != w) return fail(at() + " must have " + std::to_string(w) + " elements, got " + std::to_string(sizes[k]));
+            }
+            total += sizes[k];
+            pointers[k] = sizes[k] > 0 ? reinterpret_cast<uintptr_t>(t.data_ptr()) : 0;
+            if (written && sizes[k] > 0) spans.emplace_back(pointers[k], pointers[k] + (uintptr_t)sizes[k] * t.element_size());
+        }
+        if (written && overlap(spans)) return fail(std::string(name) + " must not overlap each other");
+        return Py_BuildValue("niNNNL", (Py_ssize_t)n, device, bytes_of(pointers), bytes_of(codes), bytes_of(sizes), (long long)total);
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_ValueError, (std::string(name) + ": " + e.what()).c_str());
+        return nullptr;
+    }
+}
+
+PyMethodDef methods[] = {{"read", read, METH_VARARGS, "Pointers, types and sizes of a list of tensors."}, {nullptr, nullptr, 0, nullptr}};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lists", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__lists() { return PyModule_Create(&module); }

@@ -385,12 +385,14 @@ def test_refusals(pace):
     say("adamw refusals")
     p, g = [torch.zeros(10, device=DEV), torch.zeros(300, device=DEV)], [torch.zeros(10, device=DEV), torch.zeros(300, device=DEV)]
     state = pace.adamw_state(p, 8)
-    for bad in (dict(params=[]), dict(grads=g[:1]), dict(params=[p[0], p[0].clone()]), dict(params=[p[0], p[0]], grads=[g[0], g[0]]),
+    twice = torch.zeros(600, device=DEV)
+    for bad in (dict(params=[twice[:10], twice[9:309]]), dict(state=dict(state, exp_avg=[state["exp_avg"][1][:10], state["exp_avg"][1]])),
+                dict(params=[]), dict(grads=g[:1]), dict(params=[p[0], p[0].clone()]), dict(params=[p[1][:10], p[1]]), dict(grads=3),
                 dict(params=[p[0], p[1].cpu()]), dict(params=[p[0], p[1].double()]), dict(grads=[g[0], torch.zeros(600, device=DEV)[::2]]),
                 dict(weight_decay=[0.1]), dict(betas=(0.9,)), dict(grad_scale=torch.ones(2, device=DEV)), dict(schedule=torch.ones(2, device=DEV)),
                 dict(state=dict(state, bits=4)), dict(state=dict(state, bits=32)), dict(state=dict(state, scale=state["scale"][:1])),
                 dict(state=dict(state, exp_avg=state["exp_avg_sq"])), dict(state=dict(state, copies=[t.clone() for t in p]))):
-        with pytest.raises(ValueError):
+        with pytest.raises((ValueError, TypeError)):
             pace.pace_adamw(**{**dict(params=p, grads=g, state=state), **bad})
     for bad in (dict(step=0), dict(lr=NAN), dict(betas=(1.0, 0.9)), dict(betas=(0.9, -0.1)), dict(eps=0.0), dict(eps=INF), dict(weight_decay=-0.1),
                 dict(weight_decay=NAN)):

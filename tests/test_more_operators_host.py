@@ -175,3 +175,27 @@ def test_grad_norm_sums_of_every_smaller_call(R):
         chunk = R.chunk(n)
         assert sum(-(-s // chunk) for s in sizes) <= R.slots_most(most, total)
         assert R.slots_most(k, n) <= R.slots_most(most, total)
+
+
+def test_lists_are_refused_before_any_call(L):
+    """What is no contiguous device tensor of the right type never reaches the library."""
+    import torch
+    import paper_2609_36830_amd as pace
+    x = torch.zeros(6)
+    for bad in ([x], [3], [None], (x.numpy(),), [x.to_sparse()], [torch.zeros(6, device="meta")], [], 7):
+        with pytest.raises((ValueError, TypeError)):
+            pace.pace_grad_norm(bad)
+        with pytest.raises((ValueError, TypeError)):
+            pace.adamw_state(bad)
+    read = pace._lib.lists().read
+    with pytest.raises(ValueError, match=r"grads must hold 2 tensors"):
+        read([x], "grads", 7, 0, False, b"\0" * 16, 0)
+    with pytest.raises(ValueError, match=r"grads\[0\] must be a contiguous device tensor of float32 or float16"):
+        read([x], "grads", 5, 0, False, b"\0" * 8, 0)
+    with pytest.raises(ValueError, match="sizes must be bytes"):
+        read([], "grads", 7, 0, False, 3, 0)
+    assert read([], "grads", 7, 0, True, b"", 0) == (0, 0, b"", b"", b"", 0)
+    with pytest.raises(ValueError):
+        pace.adamw_state([x], bits=8)
+    with pytest.raises(ValueError, match="8 bits"):
+        pace.pace_adamw_unpack(dict(bits=32))
