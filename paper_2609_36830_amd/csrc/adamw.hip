@@ -15,7 +15,7 @@
 //
 // HBM-bound: with a binary32 parameter, a bfloat16 gradient and copy 28 bytes an
 // element, 16 with moments in 8 bits. A launch takes up to kTable tensors by a
-// table in its arguments: workgroups of 4096 elements find their tensor in one
+// table in its arguments: workgroups find their tensor in one
 // load and vote of a wave. A wave takes 512 elements at a time, eight a lane in two
 // runs of four: two blocks of 256, each by half a wave.
 #include "elem.hpp"
@@ -29,7 +29,7 @@ namespace {
 
 constexpr int kAdamThreads = 256;
 constexpr int64_t kWaveRun = 2 * kAdamBlock;                     // elements that a wave takes at a time
-constexpr int kWaveTurns = (int)(kAdamChunk / (kAdamThreads / kWave) / kWaveRun);
+static_assert(kAdamRound == kAdamThreads / kWave * kWaveRun, "elements of a workgroup at a time");
 constexpr int kLaneRuns = 2, kPerRun = 4;                       // of a lane: elements 4 l .. and 128 + 4 l .. of its half's block
 // The first element of a lane's run j, in the elements from `at` on.
 __device__ __forceinline__ int64_t run_of(int64_t at, int j) {
@@ -41,11 +41,13 @@ template <typename T> struct Four { T e[4]; };
 template <typename T, bool kFull>
 __device__ __forceinline__ Four<T> load_four_of(const T *p, int64_t i, int64_t n) {
     typedef uint8_t bytes_a1 __attribute__((ext_vector_type(sizeof(T) * 4), aligned(1)));
-    if (kFull || i + 4 <= n) return __builtin_bit_cast(Four<T>, *reinterpret_cast<const bytes_a1 *>(p + i));
-    Four<T> v = {};
+    if constexpr (kFull) return __builtin_bit_cast(Four<T>, *reinterpret_cast<const bytes_a1 *>(p + i));
+    // From the last element where there is none: no branch that would have each load waited for.
+    Four<T> v;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (i + e < n) v.e[e] = p[i + e];
+    for (int e = 0; e < 4; ++e) v.e[e] = p[i + e < n ? i + e : n - 1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v.e[e] = i + e < n ? v.e[e] : T{};
     return v;
 }
 template <typename T, bool kFull>
@@ -370,8 +372,8 @@ struct Adam8 {
             vc[j] = load_four_of<uint8_t, kFull>((const uint8_t *)t.v, i, t.n);
         }
         const int64_t block = block_of(at);
-        scale = make_float2(0.0f, 0.0f);
-        if (kFull || block * kAdamBlock < t.n) scale = make_float2(t.scale[2 * block], t.scale[2 * block + 1]);
+        const int64_t from = kFull || block * kAdamBlock < t.n ? 2 * block : 0;      // behind the last block all are zeros
+        scale = make_float2(t.scale[from], t.scale[from + 1]);
     }
     template <bool kFull>
     __device__ __forceinline__ void step(const AdamEntry &t, const AdamHyper &h, const AdamStep &s, float factor, int copy_dtype, int64_t at) {
@@ -469,36 +471,35 @@ struct Adam8 {
 };
 
 template <typename P, typename G, template <typename, typename> class State>
-__global__ __launch_bounds__(kAdamThreads) void adamw_kernel(AdamTable table, AdamHyper h, int copy_dtype) {
-    float factor = 1.0f;
-    if (h.factor) {
-        factor = *h.factor;
-        if (!(__builtin_fabsf(factor) < __builtin_inff())) return;      // no number: the step is left out
-    }
+__global__ __launch_bounds__(kAdamThreads) void adamw_kernel(AdamTable table, AdamHyper h, int copy_dtype, int turns) {
+    const float factor = h.factor ? *h.factor : 1.0f;
+    const bool skip = !(__builtin_fabsf(factor) < __builtin_inff());      // no number: the step is left out
     const int k = tensor_of(table, blockIdx.x);
     const AdamEntry t = table.entry[k];
-    const AdamStep s(h, t.decay);
     const int wave = readlane_i32((int)threadIdx.x / kWave, 0);
-    const int64_t from = (int64_t)(blockIdx.x - table.first[k]) * kAdamChunk;
-    auto first_of = [&](int turn) { return from + (int64_t)(turn * (kAdamThreads / kWave) + wave) * kWaveRun; };
-    if (from + kAdamChunk <= t.n) {
-        State<P, G> state[kWaveTurns];
-#pragma unroll
-        for (int turn = 0; turn < kWaveTurns; ++turn) state[turn].template load<true>(t, first_of(turn));
-#pragma unroll
-        for (int turn = 0; turn < kWaveTurns; ++turn) state[turn].template step<true>(t, h, s, factor, copy_dtype, first_of(turn));
+    const int64_t from = (int64_t)(blockIdx.x - table.first[k]) * turns * kAdamRound;
+    auto first_of = [&](int turn) { return from + (int64_t)turn * kAdamRound + wave * kWaveRun; };
+    // The next run's bytes are on their way while this one is computed. One copy of the code a path: a launch begins with
+    // none of it in the caches.
+    State<P, G> state;
+    if (from + turns * kAdamRound <= t.n) {
+        state.template load<true>(t, first_of(0));
+        const AdamStep s(h, t.decay);
+        if (skip) return;
+#pragma unroll 1
+        for (int turn = 0; turn < turns; ++turn) {
+            State<P, G> next = state;
+            if (turn + 1 < turns) next.template load<true>(t, first_of(turn + 1));
+            state.template step<true>(t, h, s, factor, copy_dtype, first_of(turn));
+            state = next;
+        }
     } else {
-        for (int turn = 0; turn < kWaveTurns; ++turn) {
-            const int64_t at = first_of(turn);
-            if (at >= t.n) break;                      // the whole wave
-            State<P, G> state;
-            if (at + kWaveRun <= t.n) {
-                state.template load<true>(t, at);
-                state.template step<true>(t, h, s, factor, copy_dtype, at);
-            } else {
-                state.template load<false>(t, at);
-                state.template step<false>(t, h, s, factor, copy_dtype, at);
-            }
+        const AdamStep s(h, t.decay);
+        if (skip) return;
+#pragma unroll 1
+        for (int turn = 0; turn < turns && first_of(turn) < t.n; ++turn) {
+            state.template load<false>(t, first_of(turn));
+            state.template step<false>(t, h, s, factor, copy_dtype, first_of(turn));
         }
     }
 }
@@ -512,6 +513,7 @@ struct UnpackEntry {
     int64_t n;
 };
 constexpr int kUnpackTable = 64;
+constexpr int64_t kUnpackChunk = 4096;           // elements of a workgroup
 
 struct Codes {
     Four<uint8_t> m, v;
@@ -541,13 +543,13 @@ struct Codes {
 };
 
 __global__ __launch_bounds__(kAdamThreads) void adamw_unpack_kernel(Table<UnpackEntry, kUnpackTable> table) {
-    constexpr int kTurns = (int)(kAdamChunk / (kAdamThreads / kWave) / kAdamBlock);      // a block a wave
+    constexpr int kTurns = (int)(kUnpackChunk / (kAdamThreads / kWave) / kAdamBlock);      // a block a wave
     const int k = tensor_of(table, blockIdx.x);
     const UnpackEntry t = table.entry[k];
     const int wave = readlane_i32((int)threadIdx.x / kWave, 0);
-    const int64_t from = (int64_t)(blockIdx.x - table.first[k]) * kAdamChunk;
+    const int64_t from = (int64_t)(blockIdx.x - table.first[k]) * kUnpackChunk;
     auto first_of = [&](int turn) { return from + (int64_t)(turn * (kAdamThreads / kWave) + wave) * kAdamBlock; };
-    if (from + kAdamChunk <= t.n) {
+    if (from + kUnpackChunk <= t.n) {
         Codes c[kTurns];
 #pragma unroll
         for (int turn = 0; turn < kTurns; ++turn) c[turn].load<true>(t, first_of(turn));
@@ -604,11 +606,14 @@ hipError_t launch_adamw(const Tensors &t, int bits, const AdamHyper &h, hipStrea
     auto kind_of = [&](int64_t i) { return (t.param_dtypes[i] * kElemTypes + t.grad_dtypes[i]) * kElemTypes + copy_of(i); };
     for (int64_t i = 0; i < t.n; ++i)
         if (t.sizes[i] > 0) kinds |= (uint64_t)1 << kind_of(i);
+    int64_t total = 0;
+    for (int64_t i = 0; i < t.n; ++i) total += t.sizes[i];
+    const int turns = adamw_turns(total);
     for (int kind = 0; kinds >> kind; ++kind) {
         if (!(kinds >> kind & 1)) continue;
         const int copy = kind % kElemTypes;
         const hipError_t e = by_tables<AdamEntry, kTable>(
-            t, kAdamChunk, kAdamBlocksMost,
+            t, turns * kAdamRound, kAdamBlocksMost,
             [&](int64_t i, AdamEntry &to) {
                 if (kind_of(i) != kind) return false;
                 to = {t.params[i], t.grads[i], t.m[i], t.v[i], bits == 8 ? t.scales[i] : nullptr, copy ? t.copies[i] : nullptr, t.sizes[i],
@@ -621,8 +626,8 @@ hipError_t launch_adamw(const Tensors &t, int bits, const AdamHyper &h, hipStrea
                         using P = decltype(p);
                         using G = decltype(g);
                         const dim3 grid((unsigned)blocks), block(kAdamThreads);
-                        return bits == 8 ? launch(kPhaseAux, adamw_kernel<P, G, Adam8>, grid, block, stream, table, h, copy)
-                                         : launch(kPhaseAux, adamw_kernel<P, G, Adam32>, grid, block, stream, table, h, copy);
+                        return bits == 8 ? launch(kPhaseAux, adamw_kernel<P, G, Adam8>, grid, block, stream, table, h, copy, turns)
+                                         : launch(kPhaseAux, adamw_kernel<P, G, Adam32>, grid, block, stream, table, h, copy, turns);
                     });
                 });
             });
@@ -633,7 +638,7 @@ hipError_t launch_adamw(const Tensors &t, int bits, const AdamHyper &h, hipStrea
 
 hipError_t launch_adamw_unpack(const Tensors &t, float *const *m_out, float *const *v_out, hipStream_t stream) {
     return by_tables<UnpackEntry, kUnpackTable>(
-        t, kAdamChunk, kAdamBlocksMost,
+        t, kUnpackChunk, kAdamBlocksMost,
         [&](int64_t i, UnpackEntry &to) {
             to = {(const int8_t *)t.m[i], (const uint8_t *)t.v[i], t.scales[i], m_out ? m_out[i] : nullptr, v_out ? v_out[i] : nullptr, t.sizes[i]};
             return true;

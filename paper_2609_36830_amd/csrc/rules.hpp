@@ -307,8 +307,10 @@ inline int64_t grad_norm_slots_most(int64_t n_tensors, int64_t n_elements) {
     const int64_t whole = n_elements / kNormChunkMin;
     return n_tensors + (whole < most ? whole : most);
 }
-// Elements that a workgroup updates, and those that share the scales of moments in 8 bits.
-constexpr int64_t kAdamChunk = 4096, kAdamBlock = 256;
+// Elements that a workgroup updates at a time, and those that share the scales of moments in 8 bits.
+constexpr int64_t kAdamRound = 2048, kAdamBlock = 256;
+// Rounds of a workgroup: one while the call is few workgroups, which then end sooner.
+inline int adamw_turns(int64_t n_elements) { return n_elements < 1024 * 2 * kAdamRound ? 1 : 2; }
 // Tensors of a call together, so that their workgroups are numbered in 32 bits; longer tensors are refused.
 constexpr int64_t kAdamElementsMax = (int64_t)1 << 35;
 
