@@ -12,6 +12,11 @@ weights [vocab, hidden], answers prompts of random tokens:
    gradient to the head, a momentum, and the orthogonalised update.
 
     python examples/trainer_step.py --steps 8
+    python examples/trainer_step.py --steps 8 --norm --bits 8
+
+With --norm a learned layer norm stands before the head, in rollouts, rescoring
+and training; its weight and bias, which are no matrices, are updated by AdamW with
+their gradients clipped, its moments in 32 bits or in 8.
 
 The reward is the share of a trajectory's tokens below the vocabulary's middle,
 so the policy learns to answer with those; each step prints one line.
@@ -29,7 +34,8 @@ import paper_2609_36830_amd as pace  # noqa: E402
 class Trainer:
     """The policy and the buffers of pools of one shape: trajectories of the given lengths."""
 
-    def __init__(self, lengths, hidden=256, vocab=4096, capacity=None, lag=2, lr=0.5, momentum=0.9, seed=0, device="cuda:0"):
+    def __init__(self, lengths, hidden=256, vocab=4096, capacity=None, lag=2, lr=0.5, momentum=0.9, seed=0, device="cuda:0",
+                 norm=False, bits=32, norm_lr=0.01, max_norm=1.0):
         self.dev = torch.device(device)
         self.gen = torch.Generator(self.dev).manual_seed(seed)
         self.lengths = torch.as_tensor(lengths, dtype=torch.int64).to(self.dev)
@@ -38,7 +44,11 @@ class Trainer:
         self.capacity = self.n * 3 // 4 if capacity is None else capacity
         self.head = torch.randn(vocab, hidden, generator=self.gen, device=self.dev) * hidden ** -0.5
         self.velocity = torch.zeros_like(self.head)
-        self.version, self.served = 0, {}
+        self.version, self.served, self.served_norm = 0, {}, {}
+        self.norm, self.norm_lr, self.max_norm = None, norm_lr, max_norm
+        if norm:
+            self.norm = [torch.ones(hidden, device=self.dev), torch.zeros(hidden, device=self.dev)]      # weight, bias
+            self.norm_state = pace.adamw_state(self.norm, bits)
         self.offsets = torch.cat([self.lengths.new_zeros(1), self.lengths.cumsum(0)])
         self.owner = torch.repeat_interleave(torch.arange(self.n, device=self.dev), self.lengths)
         self.at = torch.arange(self.n_tokens, device=self.dev) - self.offsets[self.owner]
@@ -48,14 +58,20 @@ class Trainer:
         self.step = pace.FilterStep(self.n, self.n_tokens, [torch.int32, torch.int32, torch.float32, torch.int32], self.dev)
         self.update = pace.orthogonalize_buffers(1, vocab, hidden, self.dev)
         self.update["out"] = self.update["out"][0]
+        self.clip = pace.grad_norm_buffers(2, 2 * hidden, self.dev)
 
     def publish(self):
-        """The head as rollouts and rescoring serve it: 8 bits and a scale for each token's row. Old versions go."""
+        """The head as rollouts and rescoring serve it: 8 bits and a scale for each token's row, with the norm before it. Old
+        versions go."""
         self.served[self.version] = pace.pace_quantize_rows(self.head)
+        self.served_norm[self.version] = None if self.norm is None else [w.clone() for w in self.norm]
+        self.served_norm.pop(self.version - self.lag - 1, None)
         self.served.pop(self.version - self.lag - 1, None)
 
     def logits(self, states, version):
         """Logits after the hidden states, by a served head; a whole pool's go to the kept buffers."""
+        if self.norm is not None:
+            states, _ = pace.pace_layer_norm(states, *self.served_norm[version])
         if states.shape[0] < self.n_tokens:
             return pace.pace_matmul_i8(*pace.pace_quantize_rows(states), *self.served[version])
         p = self.product
@@ -100,18 +116,27 @@ class Trainer:
         states = pool["states"][place.long()]
         scored = torch.where(tags >= 0, tokens, -1)
         response = max(int((tags >= 0).sum()), 1)
-        logits = states @ self.head.to(torch.bfloat16).t()
+        head, hidden = self.head.to(torch.bfloat16), states
+        if self.norm is not None:
+            hidden, norm_stats = pace.pace_layer_norm(states, *self.norm)
+        logits = hidden @ head.t()
         lp, entropy, stats, *_ = pace.pace_token_logprob(logits, scored)
         grad_lp, loss, kl, clipped = pace.pace_policy_loss(lp, lp_behavior, offsets, advantage, tags, scale=1.0 / response)
         grad_logits = pace.pace_token_logprob_backward(logits, scored, stats, grad_lp, grad_logits_out=logits)
-        grad_head = (grad_logits.t() @ states).float()
+        grad_head = (grad_logits.t() @ hidden).float()
+        more = {}
+        if self.norm is not None:
+            _, *grads = pace.pace_layer_norm_backward(states, norm_stats, grad_logits @ head, self.norm[0])
+            clipped_norm, factor = pace.pace_grad_norm(grads, self.max_norm, buffers=self.clip)
+            pace.pace_adamw(self.norm, grads, self.norm_state, lr=self.norm_lr, step=self.version + 1, grad_scale=factor)
+            more = dict(grad_norm=grads, grad_size=float(clipped_norm))
         self.velocity.mul_(self.momentum).add_(grad_head)
         update = pace.pace_orthogonalize(self.velocity, **self.update)
         self.head.add_(update, alpha=-self.lr)
         self.version += 1
         return dict(kept=kept, tokens=n_tokens, reward=float(pool["reward"].mean()), loss=float(loss.sum()),
                     kl=float(kl.sum()) / response, entropy=float(entropy.sum()) / response, clipped=int(clipped.sum()),
-                    grad_head=grad_head, update=update)
+                    grad_head=grad_head, update=update, **more)
 
 
 def main():
@@ -121,9 +146,11 @@ def main():
     ap.add_argument("--max-tokens", type=int, default=200)
     ap.add_argument("--lag", type=int, default=2, help="versions that a trajectory may be behind")
     ap.add_argument("--seed", type=int, default=0)
+    ap.add_argument("--norm", action="store_true", help="a learned layer norm before the head")
+    ap.add_argument("--bits", type=int, default=32, choices=(32, 8), help="of the moments of its weight and bias")
     args = ap.parse_args()
     lengths = torch.randint(1, args.max_tokens + 1, (args.trajectories,), generator=torch.Generator().manual_seed(args.seed))
-    trainer = Trainer(lengths.tolist(), lag=args.lag, seed=args.seed)
+    trainer = Trainer(lengths.tolist(), lag=args.lag, seed=args.seed, norm=args.norm, bits=args.bits)
     for k in range(args.steps):
         trainer.publish()
         r = trainer.train(trainer.rollout())

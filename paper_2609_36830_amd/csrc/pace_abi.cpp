@@ -716,7 +716,7 @@ int pace_orthogonalize(const void *update, int dtype, int64_t batch, int64_t row
                                            workspace, (hipStream_t)stream));
 }
 
-// Whole numbers up to this are binary32 numbers, and a grid's workgroups of 64 columns fit.
+// Whole numbers up to kLnColsMax are binary32 numbers, and a grid's workgroups of columns fit.
 static bool layer_norm_ok(const void *x, int dtype, int64_t rows, int64_t cols, int64_t stride, int weight_dtype) {
     return rows_ok(x, dtype, rows, cols, stride) && cols <= kLnColsMax && (weight_dtype == dtype || weight_dtype == kF32);
 }
@@ -729,7 +729,7 @@ int pace_layer_norm(const void *x, int dtype, int64_t n_rows, int64_t n_cols, in
         return PACE_ERR_INVALID_ARG;
     if (!aligned(weight, elem_bytes_of(weight_dtype)) || !aligned(bias, elem_bytes_of(weight_dtype)) || !aligned(stats_out, 4))
         return PACE_ERR_INVALID_ARG;
-    if (!(eps >= 1e-30 && eps <= 1e30)) return PACE_ERR_INVALID_ARG;
+    if (!(eps >= 1e-30 && eps <= 1e30) || (n_rows > 0 && out == x)) return PACE_ERR_INVALID_ARG;
     return hip_status(launch_layer_norm(x, dtype, n_rows, n_cols, row_stride, weight, bias, weight_dtype, eps, out, out_stride,
                                         stats_out, (hipStream_t)stream));
 }

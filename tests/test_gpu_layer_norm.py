@@ -92,7 +92,7 @@ def check_backward(x, w, stats, dy, dx, dw, db):
 
 SHAPES = [(1, 1), (3, 1), (1, 7), (2, 8), (5, 15), (33, 64), (7, 127), (64, 128), (9, 255), (17, 256), (6, 257), (5, 511), (4, 513), (31, 1000),
           (3, 1025), (2, 2047), (7, 2049), (3, 4095), (5, 4096), (2, 4097), (3, 8191), (2, 8200), (2, 16383), (3, 16384), (2, 16385), (2, 20001),
-          (1, 50000), (600, 16), (1100, 100), (5000, 130), (2100, 2049), (700, 4097), (530, 9001)]
+          (1, 50000), (600, 16), (1100, 100), (5000, 130), (2100, 2049), (700, 4097), (530, 9001), (2000, 400), (9, 512), (700, 1032), (5, 2048), (6, 8192), (600, 4104)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
@@ -169,6 +169,13 @@ def test_in_place_gradient(pace, cols):
     assert all(torch.equal(p, q) for p, q in zip(got, ref))
     with pytest.raises(pace.PaceError):              # the rows themselves are still read
         pace.pace_layer_norm_backward(x, stats, dy, buffers=dict(b, grad_x=x))
+
+
+def test_rows_are_not_written_over(pace):
+    say("layer norm into its rows: refused")
+    x = matrix(3, 100, F32)
+    with pytest.raises(pace.PaceError):
+        pace.pace_layer_norm(x, buffers=dict(out=x, stats=torch.empty(3, 2, device=DEV)))
 
 
 def test_no_rows(pace):

@@ -20,6 +20,7 @@ int64_t floats(int64_t rows, int64_t cols) { return parts(rows, cols) * 2 * ((co
 int64_t floats_most(int64_t rows, int64_t cols) { return layer_norm_part_floats_most(rows, cols); }
 int64_t chunk(int64_t n) { return grad_norm_chunk(n); }
 int64_t slots_most(int64_t k, int64_t n) { return grad_norm_slots_most(k, n); }
+int64_t turns(int64_t n) { return adamw_turns(n); }
 }
 """ % os.path.join(ROOT, "paper_2609_36830_amd", "csrc", "rules.hpp")
 
@@ -30,7 +31,7 @@ def R(tmp_path_factory):
     (d / "r.cpp").write_text(SOURCE)
     subprocess.check_call(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", str(d / "r.cpp"), "-o", str(d / "r.so")])
     lib = ctypes.CDLL(str(d / "r.so"))
-    for name, n in (("lanes", 1), ("rows_of", 1), ("parts", 2), ("floats", 2), ("floats_most", 2), ("chunk", 1), ("slots_most", 2)):
+    for name, n in (("lanes", 1), ("rows_of", 1), ("parts", 2), ("floats", 2), ("floats_most", 2), ("chunk", 1), ("slots_most", 2), ("turns", 1)):
         getattr(lib, name).restype, getattr(lib, name).argtypes = ctypes.c_int64, [ctypes.c_int64] * n
     return lib
 
@@ -55,7 +56,7 @@ def test_layer_norm_host_argument_errors(L):
     for kw in (dict(x=None), dict(out=None), dict(x=FAKE + 1), dict(out=FAKE + 1), dict(dt=3), dict(dt=-1), dict(wt=2), dict(wt=-1), dict(wt=3),
                dict(dt=0, wt=1), dict(n=-1), dict(n=2 ** 31), dict(k=0), dict(k=2 ** 24 + 1, st=2 ** 25, ost=2 ** 25), dict(st=99), dict(ost=99),
                dict(n=2 ** 31 - 2, st=2 ** 40), dict(w=FAKE + 2), dict(b=FAKE + 2), dict(stats=FAKE + 2), dict(eps=0.0), dict(eps=-1.0),
-               dict(eps=1e-31), dict(eps=float("inf")), dict(eps=float("nan"))):
+               dict(eps=1e-31), dict(out=FAKE), dict(eps=float("inf")), dict(eps=float("nan"))):
         assert call(**kw) == -1, kw
 
 
@@ -175,6 +176,19 @@ def test_grad_norm_sums_of_every_smaller_call(R):
         chunk = R.chunk(n)
         assert sum(-(-s // chunk) for s in sizes) <= R.slots_most(most, total)
         assert R.slots_most(k, n) <= R.slots_most(most, total)
+
+
+def test_gpu_tests_reach_every_form(R):
+    """Rows of every number of lanes, whole and ragged, and wider ones; steps of one round a workgroup and of two."""
+    from tests.test_gpu_adamw import SIZES
+    from tests.test_gpu_layer_norm import SHAPES
+    for vec in (4, 8):
+        forms = {(R.lanes(c) if c <= 16384 else 0, c % vec == 0) for _, c in SHAPES}
+        assert {f for f, _ in forms} == {0, 8, 16, 32, 64, 128, 256, 512, 1024}
+        assert forms >= {(n, whole) for n in (8, 16, 32, 64, 128, 256, 512, 1024) for whole in (True, False)}, forms
+        # rows beyond one turn of the forward pass's workgroups, and of the backward pass's
+        assert any(r > R.parts(r, c) * R.rows_of(R.lanes(c)) for r, c in SHAPES if c <= 16384)
+    assert {R.turns(sum(s)) for s in SIZES} == {1, 2}
 
 
 def test_lists_are_refused_before_any_call(L):
