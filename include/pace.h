@@ -14,7 +14,9 @@
  * Around the step: log-probabilities of tokens from logits (pace_token_logprob),
  * logits from states in 8 bits (pace_quantize_rows, pace_matmul_i8), the packed
  * batch's loss and gradient (pace_policy_loss, pace_token_logprob_backward), and
- * orthogonalised weight updates (pace_orthogonalize).
+ * orthogonalised weight updates (pace_orthogonalize); the norm before the output
+ * head (pace_layer_norm and its backward pass), the gradients' norm (pace_grad_norm)
+ * and the element-wise update of any weights (pace_adamw).
  *
  * Conventions shared by every call
  * --------------------------------
@@ -560,8 +562,9 @@ int pace_orthogonalize(const void *update, int dtype, int64_t batch, int64_t row
  * eps         [host] 1e-30 .. 1e30
  * stats_out   f32 [n_rows, 2] or NULL: mu and rstd, which the backward pass takes
  * Statistics are binary32, the variance from differences to the mean, with the
- * mean's own rounding made good. An infinity or a NaN spoils its own row; so may
- * elements beyond 2^60, whose squares' sum leaves binary32. */
+ * mean's own rounding made good. An infinity or a NaN spoils its own row (and the
+ * sums down the columns that pace_layer_norm_backward takes); so may elements beyond
+ * 2^60, whose squares' sum leaves binary32. out must not be x. */
 int pace_layer_norm(const void *x, int dtype, int64_t n_rows, int64_t n_cols, int64_t row_stride, const void *weight,
                     const void *bias, int weight_dtype, double eps, void *out, int64_t out_stride, float *stats_out,
                     void *stream);
@@ -675,7 +678,8 @@ int pace_adamw_unpack(int64_t n_tensors, const int64_t *sizes, const int8_t *con
  *   the kernel that reads the logits, the tokens or the operands in
  *   pace_token_logprob, its backward pass, pace_policy_loss, pace_quantize_rows
  *   and pace_matmul_i8 (its first launch, where rows or channels are more than
- *   one launch holds); the first product C X of pace_orthogonalize, or its only
+ *   one launch holds), the rows in pace_layer_norm and its backward pass, the
+ *   first tensors in pace_grad_norm, pace_adamw and pace_adamw_unpack; the first product C X of pace_orthogonalize, or its only
  *   kernel;
  *   the window-cutoff kernel of the streaming rule, or in
  *   pace_group_filter_step the kernel that expands the group flags),

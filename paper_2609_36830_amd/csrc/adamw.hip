@@ -17,7 +17,13 @@
 // element, 16 with moments in 8 bits. A launch takes up to kTable tensors by a
 // table in its arguments: workgroups find their tensor in one
 // load and vote of a wave. A wave takes 512 elements at a time, eight a lane in two
-// runs of four: two blocks of 256, each by half a wave.
+// runs of four: two blocks of 256, each by half a wave, so that a block's largest is five
+// steps for eight elements of a lane (with a wave a block, six for four, and the library's
+// square roots and divisions, the step in 8 bits was bound by its instructions: 787 us for 550).
+// 201M elements of that kind take 937 us (6.0 TB/s; a device copy 4.6, an addition in
+// place 5.9) and 548 (5.9 TB/s) with moments in 8 bits, their unpacking 350, the
+// norm 66 (bfloat16, 6.1 TB/s). Small calls are launches: 96 vectors of 4096 are 2.7 + 4.6
+// us for the norm and 3.8 + 3.4 for the step, in two tables.
 #include "elem.hpp"
 #include "kernels.hpp"
 
@@ -361,7 +367,7 @@ struct Adam8 {
     Four<P> p[kLaneRuns];
     Four<G> g[kLaneRuns];
     Four<uint8_t> mc[kLaneRuns], vc[kLaneRuns];
-    float2 scale;
+    float2 scale;      // M, V
     static __device__ __forceinline__ int64_t block_of(int64_t at) { return at / kAdamBlock + lane_id() / 32; }
     template <bool kFull>
     __device__ __forceinline__ void load(const AdamEntry &t, int64_t at) {

@@ -294,7 +294,8 @@ inline int64_t layer_norm_part_floats_most(int64_t rows, int64_t cols) {
 
 // ---- gradient norm and AdamW (adamw.hip) -----------------------------------------------
 // Elements of a tensor that a workgroup squares and adds: at most 16384 sums to
-// join, or as many as of the longest there are.
+// join, or as many as of the longest there are. 201M elements of bfloat16 take 69.4 / 69.2 / 70.9 /
+// 71.7 us in chunks of 8192 / 16384 / 32768 / 65536, 20M 10.3 / 10.3 / 10.1 / 10.2.
 constexpr int64_t kNormChunkMin = 8192, kNormChunkMax = 65536, kNormSlots = 16384;
 inline int64_t grad_norm_chunk(int64_t n_elements) {
     int64_t chunk = kNormChunkMin;
@@ -309,7 +310,8 @@ inline int64_t grad_norm_slots_most(int64_t n_tensors, int64_t n_elements) {
 }
 // Elements that a workgroup updates at a time, and those that share the scales of moments in 8 bits.
 constexpr int64_t kAdamRound = 2048, kAdamBlock = 256;
-// Rounds of a workgroup: one while the call is few workgroups, which then end sooner.
+// Rounds of a workgroup: one while the call is few workgroups, which then end sooner. One / two, us: 96 vectors
+// of 4096 3.8 + 3.6 / 5.2 + 4.1, 30 tensors of 2.3M with moments in 8 bits 13.8 / 14.6; but 201M elements 635 / 555.
 inline int adamw_turns(int64_t n_elements) { return n_elements < 1024 * 2 * kAdamRound ? 1 : 2; }
 // Tensors of a call together, so that their workgroups are numbered in 32 bits; longer tensors are refused.
 constexpr int64_t kAdamElementsMax = (int64_t)1 << 35;

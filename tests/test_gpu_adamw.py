@@ -207,6 +207,40 @@ def test_steps(pace, sizes, param, grad, copy, bits):
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+def test_views_of_flat_buffers(pace, bits):
+    """Tensors packed one behind the other, at any address; what stands between and behind them stays."""
+    say("adamw %d bits, views" % bits)
+    sizes = [1001, 257, 1, 4099, 300]
+    params, grads = tensors(sizes, (F32,), 25, 0.05), tensors(sizes, (BF16,), 26)
+    state, other = random_state(pace, params, bits, BF16), random_state(pace, params, bits, BF16)
+    flats = []
+
+    def packed(ts, fill):
+        """Copies with one element between them and behind the last."""
+        flat = torch.full((sum(t.numel() + 1 for t in ts) + 1,), fill, dtype=ts[0].dtype, device=DEV)
+        views, gaps, at = [], torch.ones(flat.numel(), dtype=torch.bool, device=DEV), 1
+        for t in ts:
+            views.append(flat[at: at + t.numel()].view(t.shape).copy_(t))
+            gaps[at: at + t.numel()] = False
+            at += t.numel() + 1
+        flats.append((flat, gaps, fill))
+        return views
+
+    p, g = packed(params, 3.0), packed(grads, 3.0)
+    packs = dict(bits=bits, scale=packed(state["scale"], 3.0) if bits == 8 else None,
+                 **{k: packed(state[k], 77) for k in ("exp_avg", "exp_avg_sq", "copies")})
+    pace.pace_adamw(params, grads, other, step=3, weight_decay=0.1, **HYPER)
+    pace.pace_adamw(p, g, packs, step=3, weight_decay=0.1, **HYPER)
+    assert all(torch.equal(a, b) for a, b in zip(p, params))
+    for key in ("exp_avg", "exp_avg_sq", "copies") + (("scale",) if bits == 8 else ()):
+        assert all(torch.equal(a, b) for a, b in zip(packs[key], other[key])), key
+    assert all((flat[gaps] == fill).all() for flat, gaps, fill in flats)
+    if bits == 8:
+        assert all(torch.equal(a, b) for x, y in zip(pace.pace_adamw_unpack(packs), pace.pace_adamw_unpack(other)) for a, b in zip(x, y))
+    assert [float(v) for v in pace.pace_grad_norm(g, 1.0)] == [float(v) for v in pace.pace_grad_norm(grads, 1.0)]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 def test_types_together(pace, bits):
     """Tensors of every pair of types in one call, more than one table of them."""
     say("adamw %d bits, mixed types" % bits)
