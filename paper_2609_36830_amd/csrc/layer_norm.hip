@@ -17,10 +17,13 @@
 // the rows that its workgroup takes, in binary32, at most kLnChain of them one
 // after the other; the workgroups' sums are added by a second kernel, in their order.
 //
-// 16384 rows of 4096 in bfloat16 take 54 us forward (5.0 TB/s; a device copy 4.6 to 5.4)
-// and 79 backward (5.1, with 5 us of the second kernel), 4099 of them 14.6 and 29,
-// 2047 of 16384 in binary16 27 and 52 (the column sums of 256 workgroups are 34 MB there,
+// 16384 rows of 4096 in bfloat16 take 53 us forward (5.1 TB/s; a device copy 4.6 to 5.4)
+// and 79 to 82 backward (4.9 to 5.1, with 5 us of the second kernel), 4099 of them 13.2 and 29,
+// 2047 of 16384 in binary16 26 and 52 (the column sums of 256 workgroups are 34 MB there,
 // written and read), 131077 of 128 12 and 24. One row of 4096 is 2.6 us on the card.
+// Forward, a lane's reductions and its row's root cost as much as its 16 elements: with the
+// library's square root and division, and each sum gathered by four lanes' reads, 20
+// instructions an element kept the vector units 77% busy (4099 x 4096 14.8 us for 13.2).
 // Rows that end inside a vector are a kernel of their own: with both in one, tests and their
 // masks took 24 to 67 scalar registers out of the loop (16384 x 4096 forward 71 us for 54).
 #include "elem.hpp"
@@ -46,8 +49,9 @@ __device__ __forceinline__ float lanes_sum(float v) {
     step(dpp_u32<0x140, 0xf>(0u, __builtin_bit_cast(uint32_t, v)));
     if constexpr (kLanes == 16) return v;
     if constexpr (kLanes == 32) return v + __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, v), 0x401f));
-    auto row = [&](int k) { return __builtin_bit_cast(float, readlane_i32(__builtin_bit_cast(int32_t, v), k)); };
-    return (row(0) + row(16)) + (row(32) + row(48));
+    step(dpp_u32<0x142, 0xa>(0u, __builtin_bit_cast(uint32_t, v)));      // rows of 16 into the next, the first two into the last
+    step(dpp_u32<0x143, 0xc>(0u, __builtin_bit_cast(uint32_t, v)));
+    return __builtin_bit_cast(float, readlane_i32(__builtin_bit_cast(int32_t, v), kWave - 1));
 }
 
 // The row of the workgroup's that a thread has; one for the wave where waves have whole rows.
@@ -147,9 +151,9 @@ struct Moments {
     float ref, off, m2;      // the mean is ref + off, off small; sum of squares about it
 };
 // Moments of `count` elements that kIn lanes (at most a wave) hold of rows of kLanes lanes; elements at or
-// past cols count as none.
+// past cols count as none. x becomes x - ref.
 template <typename T, int kIn, int kLanes, bool kWhole>
-__device__ __forceinline__ Moments lanes_moments(const float (&x)[kLnPer], int lane, int cols, float count) {
+__device__ __forceinline__ Moments lanes_moments(float (&x)[kLnPer], int lane, int cols, float count) {
     constexpr int kVec = Slice<T>::kVec;
     const float inv = count > 0.0f ? 1.0f / count : 0.0f;
     float s = 0.0f, s1 = 0.0f, s2 = 0.0f;
@@ -164,6 +168,7 @@ __device__ __forceinline__ Moments lanes_moments(const float (&x)[kLnPer], int l
         for (int e = 0; e < kVec; ++e) {
             float d = x[k * kVec + e] - ref;
             if (!kWhole) d = e < left ? d : 0.0f;
+            x[k * kVec + e] = d;
             t1 += d;
             t2 = __builtin_fmaf(d, d, t2);
         }
@@ -215,15 +220,17 @@ __global__ __launch_bounds__(kLanes > kLnForward ? kLanes : kLnForward) void lay
             const float ref = __builtin_bit_cast(float, readlane_i32(__builtin_bit_cast(int32_t, part.x), 0));
             const float d = (part.x - ref) + part.y;
             const float off = lanes_sum<16>(part.w * d) * (inv * kShare), e = d - off;
-            m = {ref, off, lanes_sum<16>(part.w > 0.0f ? __builtin_fmaf(part.w * e, e, part.z) : 0.0f) * kShare};
+            m.off = (ref - m.ref) + off;               // of the wave's own ref, which v has left behind
+            m.m2 = lanes_sum<16>(part.w > 0.0f ? __builtin_fmaf(part.w * e, e, part.z) : 0.0f) * kShare;
         }
-        const float rstd = 1.0f / sqrtf(m.m2 * inv + eps);
+        // The chip's inverse root, a unit of 2^-23: its argument is eps at least, a normal number.
+        const float rstd = __builtin_amdgcn_rsqf(m.m2 * inv + eps), shift = -m.off * rstd;
         const int64_t row = base + group;
         float w[kLnPer], b[kLnPer];
         weights.values(w);
         biases.values(b);
 #pragma unroll
-        for (int i = 0; i < kLnPer; ++i) v[i] = __builtin_fmaf(((v[i] - m.ref) - m.off) * rstd, w[i], b[i]);
+        for (int i = 0; i < kLnPer; ++i) v[i] = __builtin_fmaf(__builtin_fmaf(v[i], rstd, shift), w[i], b[i]);
         if (row < rows) {
             store_slice<T, kLanes, kWhole>(out + row * out_stride, v, lane, cols);
             if (stats && lane == 0) {

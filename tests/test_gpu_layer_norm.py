@@ -61,7 +61,7 @@ def check_forward(x, w, b, eps, out, stats):
     # the mean: its correction is a sum of differences, which are about sigma
     mean_off = U * (2 * mean.abs() + (k + 4) * sigma) + 2e-45
     assert ((stats[:, :1].double() - mean).abs() <= mean_off).all()
-    # the variance: K u of itself for the sum, 4 u for what the terms and the mean add, halved by the root; root and inverse
+    # the variance: K u of itself for the sum, 4 u for what the terms and the mean add, halved by the root; the inverse root, 2 u
     rstd_off = (k / 2 + 6) * U
     assert ((stats[:, 1:].double() / rstd - 1).abs() <= rstd_off).all()
     h = (xd - mean) * rstd
