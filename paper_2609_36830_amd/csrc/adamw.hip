@@ -528,7 +528,7 @@ struct Codes {
     float2 scale;
     template <bool kFull>
     __device__ __forceinline__ void load(const UnpackEntry &t, int64_t at) {
-        const int64_t i = at + lane_id() * kPerRun, block = at / kAdamBlock;
+        const int64_t i = at + lane_id() * kPerRun, block = (kFull || at < t.n ? at : t.n - 1) / kAdamBlock;
         m = load_four_of<uint8_t, kFull>((const uint8_t *)t.m, i, t.n);
         v = load_four_of<uint8_t, kFull>(t.v, i, t.n);
         scale = make_float2(t.scale[2 * block], t.scale[2 * block + 1]);
@@ -557,19 +557,16 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_unpack_kernel(Table<Unpack
     const int wave = readlane_i32((int)threadIdx.x / kWave, 0);
     const int64_t from = (int64_t)(blockIdx.x - table.first[k]) * kUnpackChunk;
     auto first_of = [&](int turn) { return from + (int64_t)(turn * (kAdamThreads / kWave) + wave) * kAdamBlock; };
-    if (from + kUnpackChunk <= t.n) {
+    auto all = [&](auto full) {      // every load before the first store, also where runs are behind the last element
+        constexpr bool kFull = decltype(full)::value;
         Codes c[kTurns];
 #pragma unroll
-        for (int turn = 0; turn < kTurns; ++turn) c[turn].load<true>(t, first_of(turn));
+        for (int turn = 0; turn < kTurns; ++turn) c[turn].template load<kFull>(t, first_of(turn));
 #pragma unroll
-        for (int turn = 0; turn < kTurns; ++turn) c[turn].store<true>(t, first_of(turn));
-    } else {
-        for (int turn = 0; turn < kTurns && first_of(turn) < t.n; ++turn) {
-            Codes c;
-            c.load<false>(t, first_of(turn));
-            c.store<false>(t, first_of(turn));
-        }
-    }
+        for (int turn = 0; turn < kTurns; ++turn) c[turn].template store<kFull>(t, first_of(turn));
+    };
+    if (from + kUnpackChunk <= t.n) all(std::true_type{});
+    else all(std::false_type{});
 }
 
 constexpr int64_t kAdamBlocksMost = kGridThreads / kAdamThreads;
