@@ -573,7 +573,9 @@ int pace_layer_norm(const void *x, int dtype, int64_t n_rows, int64_t n_cols, in
  * and a = grad_out weight,
  *   grad_x = rstd (a - mean a - h mean(a h))
  *   grad_weight = sum over rows of grad_out h,  grad_bias = sum over rows of grad_out
- * x .. weight_dtype, stats: as given to and written by pace_layer_norm.
+ * x .. weight_dtype, stats: as given to and written by pace_layer_norm. mu is
+ *   rounded to binary32 there: in rows whose mean is k deviations from zero h is
+ *   within k 2^-24.
  * grad_out, grad_x_out: [n_rows, n_cols] of dtype, with strides of their own.
  *   grad_x_out may be grad_out itself (with the same stride), which it then
  *   replaces; otherwise the two must not overlap.
@@ -623,8 +625,9 @@ int pace_grad_norm(int64_t n_tensors, const void *const *grads, const int32_t *g
  *   against the block's largest before its own rounding (halfway to the larger code), a
  *   positive v to 1 at least.
  *   Blocks whose largest is below 2^-126 are zeros. Zeros are fresh states.
- *   A code moves when a moment changes by half a step between codes: small moments
- *   that shrink towards zero are held while their block's largest keeps its size.
+ *   A code moves when a moment changes by half a step between codes: while a block's
+ *   largest keeps its size, a smaller |m| that shrinks by beta1 = 0.9 is held from 0.5%
+ *   of it on, a v that shrinks by beta2 = 0.999 wherever it is.
  *   An infinity or a NaN (or a g^2 beyond binary32) spoils its block's moments.
  * copies: copy_dtypes (PACE_BF16 or PACE_F16) copies of the new parameters, an entry
  *   or all NULL: none

@@ -833,8 +833,8 @@ def layer_norm_buffers(n_rows: int, n_cols: int, dtype, device, backward: bool =
 
 
 def _norm_weight(w, x, n_cols: int, name: str):
-    if w.dtype is not x.dtype and w.dtype is not torch.float32:
-        raise ValueError("%s must be float32 or of x's type, got %s" % (name, w.dtype))
+    if not isinstance(w, torch.Tensor) or (w.dtype is not x.dtype and w.dtype is not torch.float32):
+        raise ValueError("%s must be a tensor of float32 or of x's type" % name)
     return _vector(w, w.dtype, n_cols, x.device, name)
 
 

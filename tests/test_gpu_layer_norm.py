@@ -138,6 +138,24 @@ def test_rows_far_from_zero(pace, cols):
     assert (out[3:] == 0).all() and (stats[3:, 0].cpu() == torch.tensor([0.0, -3.25])).all()
 
 
+def test_refusals(pace):
+    say("layer norm refusals")
+    x = torch.zeros(3, 8, dtype=BF16, device=DEV)
+    stats = torch.zeros(3, 2, device=DEV)
+    w = torch.ones(8, device=DEV)
+    for bad in (dict(weight=w[:7]), dict(weight=w.half()), dict(weight=w.cpu()), dict(weight=3), dict(bias=w.double()), dict(weight=w, bias=w.to(BF16)),
+                dict(x=x.double()), dict(x=x.cpu()), dict(x=x[0]), dict(x=x.t()), dict(buffers=dict(out=x.float(), stats=stats)),
+                dict(buffers=dict(out=x.clone(), stats=stats[:2]))):
+        with pytest.raises(ValueError):
+            pace.pace_layer_norm(**{**dict(x=x), **bad})
+    for bad in (dict(grad_out=x.float()), dict(grad_out=x[:2]), dict(grad_out=x.cpu()), dict(stats=stats[:2]), dict(stats=stats.double()), dict(weight=w[:7]),
+                dict(buffers=dict(pace.layer_norm_buffers(3, 8, BF16, DEV, backward=True), grad_weight=w.half()))):
+        with pytest.raises(ValueError):
+            pace.pace_layer_norm_backward(**{**dict(x=x, stats=stats, grad_out=x.clone()), **bad})
+    with pytest.raises(pace.PaceError):
+        pace.pace_layer_norm(x, eps=0.0)
+
+
 @pytest.mark.parametrize("cols", [48, 300, 4096, 17000])
 def test_infinities_and_nan_stay_in_their_rows(pace, cols):
     say("layer norm with infinities, %d columns" % cols)
