@@ -832,60 +832,50 @@ def layer_norm_buffers(n_rows: int, n_cols: int, dtype, device, backward: bool =
     return b
 
 
-def _norm_weight(w, x, n_cols: int, name: str):
-    if not isinstance(w, torch.Tensor) or (w.dtype is not x.dtype and w.dtype is not torch.float32):
-        raise ValueError("%s must be a tensor of float32 or of x's type" % name)
-    return _vector(w, w.dtype, n_cols, x.device, name)
+_FLOATS, _F32, _F64, _HALVES, _INT8, _UINT8 = 7, 1, 32, 6, 8, 16      # sets of types, a bit for each
 
 
 def pace_layer_norm(x, weight=None, bias=None, eps: float = 1e-5, buffers=None, stream=None):
     """Rows of x at mean 0 and variance 1, then weighted (weight and bias of one type: float32 or x's). Returns
     (out of x's type and shape, stats f32[n, 2]: mean and 1 / sqrt(variance + eps))."""
-    dt, n, k, stride = _matrix(x, "x")
-    dev = x.device
-    wt = dt
+    of = _lib.lists()
+    p, dt, n, k, stride, at = of.matrix(x, "x", _FLOATS, -1, -1, -1)
+    w, b, wt = None, None, dt
     if weight is not None:
-        wt = DTYPES[_norm_weight(weight, x, k, "weight").dtype]
+        w, wt, _ = of.vector(weight, "weight", _F32 | 1 << dt, at, k)
     if bias is not None:
-        bt = DTYPES[_norm_weight(bias, x, k, "bias").dtype]
-        if weight is not None and bt != wt:
-            raise ValueError("weight and bias must have one type")
-        wt = bt
-    b = layer_norm_buffers(n, k, x.dtype, dev, stream=stream) if buffers is None else buffers
-    out, stats = _sized(b["out"], x.dtype, (n, k), dev, "out"), _sized(b["stats"], torch.float32, (n, 2), dev, "stats")
-    _check(lib().pace_layer_norm(x.data_ptr(), dt, n, k, stride, _ptr(weight), _ptr(bias), wt, float(eps), out.data_ptr(), k,
-                                 stats.data_ptr(), _stream(dev, stream)), "pace_layer_norm")
+        b, wt, _ = of.vector(bias, "bias", _F32 | 1 << dt if weight is None else 1 << wt, at, k)
+    if buffers is None:
+        buffers = layer_norm_buffers(n, k, x.dtype, x.device, stream=stream)
+    out, stats = buffers["out"], buffers["stats"]
+    o, _, _, _, out_stride, _ = of.matrix(out, "out", 1 << dt, at, n, k)
+    s, _, _ = of.vector(stats, "stats", _F32, at, 2 * n)
+    _check(lib().pace_layer_norm(p, dt, n, k, stride, w, b, wt, eps, o, out_stride, s, _stream(x.device, stream)), "pace_layer_norm")
     return out, stats
 
 
 def pace_layer_norm_backward(x, stats, grad_out, weight=None, buffers=None, stream=None):
     """Gradients of pace_layer_norm. Returns (grad_x of x's type, grad_weight f32[k], grad_bias f32[k]). buffers["grad_x"]
     may be grad_out itself."""
-    dt, n, k, stride = _matrix(x, "x")
-    gt, gn, gk, gstride = _matrix(grad_out, "grad_out")
-    dev = x.device
-    if (gt, gn, gk) != (dt, n, k) or grad_out.device != dev:
-        raise ValueError("grad_out must have x's type and shape")
-    _vector(stats, torch.float32, 2 * n, dev, "stats")
-    wt = dt if weight is None else DTYPES[_norm_weight(weight, x, k, "weight").dtype]
+    of = _lib.lists()
+    p, dt, n, k, stride, at = of.matrix(x, "x", _FLOATS, -1, -1, -1)
+    g, _, _, _, grad_stride, _ = of.matrix(grad_out, "grad_out", 1 << dt, at, n, k)
+    s, _, _ = of.vector(stats, "stats", _F32, at, 2 * n)
+    w, wt = None, dt
+    if weight is not None:
+        w, wt, _ = of.vector(weight, "weight", _F32 | 1 << dt, at, k)
     if buffers is None:
-        e = _allocator(dev, stream)
+        e = _allocator(x.device, stream)
         buffers = dict(grad_x=e((n, k), x.dtype), grad_weight=e(k, torch.float32), grad_bias=e(k, torch.float32),
                        workspace=e(pace_layer_norm_backward_workspace_bytes(n, k), torch.uint8))
-    grad_x = buffers["grad_x"]
-    xt, xn, xk, xstride = _matrix(grad_x, "grad_x")
-    if (xt, xn, xk) != (dt, n, k) or grad_x.device != dev:
-        raise ValueError("grad_x must have x's type and shape")
-    grad_weight = _sized(buffers["grad_weight"], torch.float32, (k,), dev, "grad_weight")
-    grad_bias = _sized(buffers["grad_bias"], torch.float32, (k,), dev, "grad_bias")
-    ws, ws_bytes = _scratch(buffers["workspace"], dev)
-    _check(lib().pace_layer_norm_backward(x.data_ptr(), dt, n, k, stride, _ptr(weight), wt, stats.data_ptr(), grad_out.data_ptr(),
-                                          gstride, grad_x.data_ptr(), xstride, grad_weight.data_ptr(), grad_bias.data_ptr(), ws,
-                                          ws_bytes, _stream(dev, stream)), "pace_layer_norm_backward")
+    grad_x, grad_weight, grad_bias = buffers["grad_x"], buffers["grad_weight"], buffers["grad_bias"]
+    o, _, _, _, out_stride, _ = of.matrix(grad_x, "grad_x", 1 << dt, at, n, k)
+    gw, _, _ = of.vector(grad_weight, "grad_weight", _F32, at, k)
+    gb, _, _ = of.vector(grad_bias, "grad_bias", _F32, at, k)
+    ws, _, ws_bytes = of.vector(buffers["workspace"], "workspace", _UINT8, at, -1)
+    _check(lib().pace_layer_norm_backward(p, dt, n, k, stride, w, wt, s, g, grad_stride, o, out_stride, gw, gb, ws, ws_bytes,
+                                          _stream(x.device, stream)), "pace_layer_norm_backward")
     return grad_x, grad_weight, grad_bias
-
-
-_FLOATS, _F32, _HALVES, _INT8, _UINT8 = 7, 1, 6, 8, 16      # sets of types, a bit for each
 
 
 def _each(tensors, name: str, types: int, device: int = -1, written: bool = False, sizes=None, block: int = 0):
@@ -911,13 +901,14 @@ def grad_norm_buffers(n_tensors: int, n_elements: int, device, stream=None):
 def pace_grad_norm(grads, max_norm: float = float("inf"), buffers=None, stream=None):
     """The 2-norm of all gradients together. Returns (norm f32[1], factor f32[1]: min(1, max_norm / norm), NaN where the norm
     is no number)."""
+    of = _lib.lists()
     n, at, ptrs, codes, sizes, total = _each(grads, "grads", _FLOATS)
-    dev = torch.device("cuda", at)
-    b = grad_norm_buffers(n, total, dev, stream) if buffers is None else buffers
-    norm, factor = _sized(b["norm"], torch.float32, (1,), dev, "norm"), _sized(b["factor"], torch.float32, (1,), dev, "factor")
-    ws, ws_bytes = _scratch(b["workspace"], dev)
-    _check(lib().pace_grad_norm(n, ptrs, codes, sizes, float(max_norm), norm.data_ptr(), factor.data_ptr(),
-                                ws, ws_bytes, _stream(dev, stream)), "pace_grad_norm")
+    b = grad_norm_buffers(n, total, torch.device("cuda", at), stream) if buffers is None else buffers
+    norm, factor = b["norm"], b["factor"]
+    out, _, _ = of.vector(norm, "norm", _F32, at, 1)
+    clip, _, _ = of.vector(factor, "factor", _F32, at, 1)
+    ws, _, ws_bytes = of.vector(b["workspace"], "workspace", _UINT8, at, -1)
+    _check(lib().pace_grad_norm(n, ptrs, codes, sizes, max_norm, out, clip, ws, ws_bytes, _stream(norm.device, stream)), "pace_grad_norm")
     return norm, factor
 
 
@@ -973,14 +964,11 @@ def pace_adamw(params, grads, state, lr: float = 1e-3, step: int = 1, betas=(0.9
         raise ValueError("weight_decay must be a number or one for each tensor")
     if len(betas) != 2:
         raise ValueError("betas must be two numbers")
-    dev = torch.device("cuda", at)
-    if grad_scale is not None:
-        _vector(grad_scale, torch.float32, 1, dev, "grad_scale")
-    if schedule is not None:
-        _vector(schedule, torch.float64, 2, dev, "schedule")
+    factor = None if grad_scale is None else _lib.lists().vector(grad_scale, "grad_scale", _F32, at, 1)[0]
+    rates = None if schedule is None else _lib.lists().vector(schedule, "schedule", _F64, at, 2)[0]
     hyper = AdamwParams(float(lr), float(betas[0]), float(betas[1]), float(eps), int(step))
     _check(lib().pace_adamw(n, sizes, p, types, g, grad_types, bits, m, v, scales, copies, copy_types, decay.tobytes(),
-                            ctypes.byref(hyper), _ptr(grad_scale), _ptr(schedule), _stream(dev, stream)), "pace_adamw")
+                            ctypes.byref(hyper), factor, rates, _stream(torch.device("cuda", at), stream)), "pace_adamw")
     return params
 
 

@@ -241,9 +241,20 @@ __global__ __launch_bounds__(kLanes > kLnForward ? kLanes : kLnForward) void lay
     }
 }
 
-// Adds this workgroup's column sums of all its rows' lanes and writes them as its part: [2][pitch].
+// Four consecutive columns' sums from c on, those at or past cols left out.
+__device__ __forceinline__ void store_sums(float *p, int64_t c, int64_t cols, float a, float b, float d, float e) {
+    if (c + 4 <= cols) {
+        store_a1(p + c, make_uint4(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, d), __builtin_bit_cast(uint32_t, e)));
+    } else {
+        if (c < cols) p[c] = a;
+        if (c + 1 < cols) p[c + 1] = b;
+        if (c + 2 < cols) p[c + 2] = d;
+    }
+}
+
+// Adds this workgroup's column sums of all its rows' lanes and writes them; dw or db may be null.
 template <typename T, int kLanes, int kThreads>
-__device__ __forceinline__ void write_part(const float (&dw)[kLnPer], const float (&db)[kLnPer], float *part, int64_t pitch, int cols) {
+__device__ __forceinline__ void write_sums(const float (&dw)[kLnPer], const float (&db)[kLnPer], float *dw_out, float *db_out, int cols) {
     constexpr int kVec = Slice<T>::kVec, kRows = kThreads / kLanes;
     const int lane = (int)threadIdx.x % kLanes;
     auto column = [&](int l, int i) { return (l + i / kVec * kLanes) * kVec + i % kVec; };
@@ -251,15 +262,14 @@ __device__ __forceinline__ void write_part(const float (&dw)[kLnPer], const floa
 #pragma unroll
         for (int i = 0; i < kLnPer; i += 4) {
             const int c = column(lane, i);
-            if (c < cols) {                            // the pitch is a multiple of 4
-                *reinterpret_cast<float4 *>(part + c) = make_float4(dw[i], dw[i + 1], dw[i + 2], dw[i + 3]);
-                *reinterpret_cast<float4 *>(part + pitch + c) = make_float4(db[i], db[i + 1], db[i + 2], db[i + 3]);
-            }
+            if (dw_out) store_sums(dw_out, c, cols, dw[i], dw[i + 1], dw[i + 2], dw[i + 3]);
+            if (db_out) store_sums(db_out, c, cols, db[i], db[i + 1], db[i + 2], db[i + 3]);
         }
     } else {
         __shared__ float sums[kLnPer][kThreads];
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
+            float *out = which ? db_out : dw_out;
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < kLnPer; ++i) sums[i][threadIdx.x] = which ? db[i] : dw[i];
@@ -269,7 +279,7 @@ __device__ __forceinline__ void write_part(const float (&dw)[kLnPer], const floa
                 float s = 0.0f;
 #pragma unroll
                 for (int r = 0; r < kRows; ++r) s += sums[i][r * kLanes + l];
-                if (c < cols) part[which * pitch + c] = s;
+                if (out && c < cols) out[c] = s;
             }
         }
     }
@@ -281,8 +291,8 @@ __device__ __forceinline__ void write_part(const float (&dw)[kLnPer], const floa
 template <typename T, typename W, int kLanes, bool kWhole>
 __global__ __launch_bounds__(kLanes > kLnBackward ? kLanes : kLnBackward, kLanes > kWave ? 4 : 2) void layer_norm_backward_kernel(
     const T *__restrict__ x, int64_t rows, int cols, int64_t stride, const W *__restrict__ weight,
-    const float *__restrict__ stats, const T *dy, int64_t dy_stride, T *dx, int64_t dx_stride, float *__restrict__ parts,
-    int64_t pitch) {
+    const float *__restrict__ stats, const T *dy, int64_t dy_stride, T *dx, int64_t dx_stride, float *__restrict__ dw_out,
+    float *__restrict__ db_out, int64_t part_stride) {
     constexpr int kThreads = kLanes > kLnBackward ? kLanes : kLnBackward, kRows = kThreads / kLanes;
     constexpr int kIn = kLanes < kWave ? kLanes : kWave, kWaves = kLanes / kIn;
     __shared__ float2 slots[2][kRows * kWaves];
@@ -348,7 +358,10 @@ __global__ __launch_bounds__(kLanes > kLnBackward ? kLanes : kLnBackward, kLanes
         for (int i = 0; i < kLnPer; ++i) a[i] = ((a[i] * w[i] - s1) - h[i] * s2) * r;
         if (live) store_slice<T, kLanes, kWhole>(dx + row * dx_stride, a, lane, cols);
     }
-    if (parts) write_part<T, kLanes, kThreads>(dw, db, parts + (int64_t)blockIdx.x * 2 * pitch, pitch, cols);
+    if (dw_out || db_out) {
+        const int64_t at = (int64_t)blockIdx.x * part_stride;
+        write_sums<T, kLanes, kThreads>(dw, db, dw_out ? dw_out + at : nullptr, db_out ? db_out + at : nullptr, cols);
+    }
 }
 
 // ---- rows wider than registers hold -------------------------------------------------
@@ -498,7 +511,8 @@ template <typename T>
 __global__ __launch_bounds__(kLnColumns) void layer_norm_columns_kernel(const T *__restrict__ x, int64_t rows, int64_t cols,
                                                                         int64_t stride, const float *__restrict__ stats,
                                                                         const T *__restrict__ dy, int64_t dy_stride,
-                                                                        float *__restrict__ parts, int64_t pitch) {
+                                                                        float *__restrict__ dw_out, float *__restrict__ db_out,
+                                                                        int64_t part_stride) {
     constexpr int kVec = kVecOf<T>;
     const int64_t c = ((int64_t)blockIdx.x * kLnColumns + threadIdx.x) * kVec;
     if (c >= cols) return;
@@ -526,13 +540,12 @@ __global__ __launch_bounds__(kLnColumns) void layer_norm_columns_kernel(const T 
             db[e] += g[e];
         }
     }
-    float *part = parts + (int64_t)blockIdx.y * 2 * pitch + c;
+    const int64_t at = (int64_t)blockIdx.y * part_stride + c;
 #pragma unroll
-    for (int e = 0; e < kVec; ++e)
-        if (e < n) {
-            part[e] = dw[e];
-            part[pitch + e] = db[e];
-        }
+    for (int e = 0; e < kVec; ++e) {
+        if (dw_out && e < n) dw_out[at + e] = dw[e];
+        if (db_out && e < n) db_out[at + e] = db[e];
+    }
 }
 
 // The parts' sums: 32 columns a workgroup, 32 threads a column.
@@ -626,7 +639,10 @@ hipError_t launch_layer_norm_backward(const void *x, int dtype, int64_t rows, in
                                       int weight_dtype, const float *stats, const void *dy, int64_t dy_stride, void *dx,
                                       int64_t dx_stride, float *dw, float *db, void *ws, hipStream_t stream) {
     const int64_t n_parts = layer_norm_backward_parts(rows, cols), pitch = pitch_of(cols);
-    float *parts = dw || db ? (float *)ws : nullptr;
+    // Each workgroup's sums go to its part, or, where there is one workgroup, where they are wanted.
+    const bool sums = dw || db, parts = sums && n_parts != 1;
+    float *part = (float *)ws, *dw_to = parts ? part : dw, *db_to = parts ? part + pitch : db;
+    const int64_t part_stride = parts ? 2 * pitch : 0;
     hipError_t e = hipSuccess;
     if (rows > 0)
         e = with_elem(dtype, [&](auto t) {
@@ -638,10 +654,10 @@ hipError_t launch_layer_norm_backward(const void *x, int dtype, int64_t rows, in
                 T *o = (T *)dx;
                 if (cols > kLnRegister) {
                     hipError_t err = hipSuccess;
-                    if (parts) {
+                    if (sums) {
                         const int64_t per = kLnColumns * kVecOf<T>;
                         err = launch(-1, layer_norm_columns_kernel<T>, dim3((unsigned)((cols + per - 1) / per), (unsigned)n_parts),
-                                     dim3(kLnColumns), stream, p, rows, cols, stride, stats, g, dy_stride, parts, pitch);
+                                     dim3(kLnColumns), stream, p, rows, cols, stride, stats, g, dy_stride, dw_to, db_to, part_stride);
                     }
                     if (err != hipSuccess) return err;
                     return in_launches(rows, kLnWide, [&](int64_t first, int64_t count) {
@@ -653,14 +669,15 @@ hipError_t launch_layer_norm_backward(const void *x, int dtype, int64_t rows, in
                 return with_lanes<T>(cols, [&](auto lanes, auto whole) {
                     constexpr int kLanes = decltype(lanes)::value, kThreads = kLanes > kLnBackward ? kLanes : kLnBackward;
                     static_assert(kThreads / kLanes == layer_norm_backward_rows(kLanes), "rows of a workgroup");
-                    return launch(kPhaseAux, layer_norm_backward_kernel<T, W, kLanes, decltype(whole)::value>, dim3((unsigned)n_parts), dim3(kThreads), stream, p,
-                                  rows, (int)cols, stride, w, stats, g, dy_stride, o, dx_stride, parts, pitch);
+                    const int64_t need = (rows + kThreads / kLanes - 1) / (kThreads / kLanes), blocks = sums || need > kLnAlone ? n_parts : need;
+                    return launch(kPhaseAux, layer_norm_backward_kernel<T, W, kLanes, decltype(whole)::value>, dim3((unsigned)blocks), dim3(kThreads), stream, p,
+                                  rows, (int)cols, stride, w, stats, g, dy_stride, o, dx_stride, dw_to, db_to, part_stride);
                 });
             });
         });
     if (e == hipSuccess && parts)
-        e = launch(-1, layer_norm_join_kernel, dim3((unsigned)((cols + kLnJoinCols - 1) / kLnJoinCols), 2), dim3(kLnJoin), stream, (const float *)parts,
-                   rows > 0 ? n_parts : 0, pitch, cols, dw, db);
+        e = launch(-1, layer_norm_join_kernel, dim3((unsigned)((cols + kLnJoinCols - 1) / kLnJoinCols), 2), dim3(kLnJoin), stream, (const float *)part,
+                   n_parts, pitch, cols, dw, db);
     return e;
 }
 

@@ -266,13 +266,16 @@ constexpr int layer_norm_backward_rows(int lanes) { return lanes >= 512 ? 1 : 51
 // CUs idle, more write and read as much again as the rows they share: 16384 x 4096 in bfloat16 take
 // 103 / 84 / 79 / 92 / 85 / 94 us with 128 / 192 / 256 / 384 / 512 / 1024 parts, 4099 x 4096 34 / 30 /
 // 29 / 35 / 34 / 45, 131077 x 128 39 / 31 / 27 / 29 / 27 / 32, 2047 x 16384 55 / 51 / 52 / 58 / 67 / 96.
-constexpr int64_t kLnChain = 1024, kLnParts = 256, kLnWideParts = 64, kLnWidePartsMax = 65535;
+// Up to kLnAlone turns of rows are one workgroup's, whose sums need no second launch.
+constexpr int64_t kLnChain = 1024, kLnParts = 256, kLnAlone = 4, kLnWideParts = 64, kLnWidePartsMax = 65535;
 inline int64_t layer_norm_register_parts(int64_t rows, int lanes) {
     const int64_t at_once = layer_norm_backward_rows(lanes), need = (rows + at_once - 1) / at_once;
+    if (need > 0 && need <= kLnAlone) return 1;
     const int64_t chain = (rows + at_once * kLnChain - 1) / (at_once * kLnChain), parts = need < kLnParts ? need : kLnParts;
     return parts > chain ? parts : chain;
 }
 inline int64_t layer_norm_wide_parts(int64_t rows) {
+    if (rows > 0 && rows <= kLnAlone) return 1;
     const int64_t parts = rows < kLnWideParts ? rows : kLnWideParts, chain = (rows + kLnChain - 1) / kLnChain;
     return parts > chain ? parts : (chain < kLnWidePartsMax ? chain : kLnWidePartsMax);
 }

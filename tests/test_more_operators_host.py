@@ -209,6 +209,14 @@ def test_lists_are_refused_before_any_call(L):
     with pytest.raises(ValueError, match="sizes must be bytes"):
         read([], "grads", 7, 0, False, 3, 0)
     assert read([], "grads", 7, 0, True, b"", 0) == (0, 0, b"", b"", b"", 0)
+    m = pace._lib.lists()
+    for bad in (x, 3, None, torch.zeros(2, 3), torch.zeros(2, 3, device="meta"), torch.zeros(2, 3).to_sparse()):
+        with pytest.raises(ValueError):
+            m.matrix(bad, "x", 7, -1, -1, -1)
+        with pytest.raises(ValueError, match="x must be a"):
+            m.vector(bad, "x", 7, -1, -1)
+    with pytest.raises(ValueError, match="x must be a device tensor of float32 or bfloat16 or float16"):
+        pace.pace_layer_norm(torch.zeros(2, 3))
     with pytest.raises(ValueError):
         pace.adamw_state([x], bits=8)
     with pytest.raises(ValueError, match="8 bits"):

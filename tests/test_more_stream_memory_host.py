@@ -37,13 +37,22 @@ def test_a_call_allocates_in_its_streams_memory(monkeypatch, name):
         made.append(inside[-1] if inside else None)
         return empty(shape, dtype=dtype).as_subclass(type(T(1)))
 
-    def each(tensors, name, types, device=-1, written=False, sizes=None, block=0):
-        return len(tensors), 0, b"", b"", b"", sum(t.numel() for t in tensors)
+    class Lists:
+        """The extension's answers for host tensors."""
+        @staticmethod
+        def read(tensors, name, types, device, written, sizes, block):
+            return len(tensors), 0, b"", b"", b"", sum(t.numel() for t in tensors)
+
+        @staticmethod
+        def matrix(t, name, types, device, rows, cols):
+            return 0, 0, t.shape[0], t.shape[1], t.shape[1], 0
+
+        @staticmethod
+        def vector(t, name, types, device, n):
+            return 0, 0, t.numel()
 
     monkeypatch.setattr(pace, "lib", Library)
-    monkeypatch.setattr(pace, "_each", each)
-    monkeypatch.setattr(pace, "_sized", lambda t, *a, **k: t)
-    monkeypatch.setattr(pace, "_scratch", lambda ws, device: (0, 0))
+    monkeypatch.setattr(pace._lib, "lists", lambda: Lists)
     monkeypatch.setattr(pace, "_stream", lambda device, stream=None: 0)
     monkeypatch.setattr(torch.cuda, "stream", under)
     monkeypatch.setattr(torch.cuda, "Stream", SideStream)
