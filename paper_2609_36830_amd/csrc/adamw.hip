@@ -70,13 +70,6 @@ __device__ __forceinline__ void store_four_of(T *p, int64_t i, int64_t n, const 
     }
 }
 
-// ---- the table of a launch ---------------------------------------------------------
-// first: the tensor's first workgroup; entries behind the last hold 2^32 - 1.
-template <typename E, int kMost>
-struct Table {
-    E entry[kMost];
-    uint32_t first[kMost];
-};
 // The tensor that workgroup `b` belongs to: the last whose first is at most b.
 template <typename E, int kMost>
 __device__ __forceinline__ int tensor_of(const Table<E, kMost> &t, uint32_t b) {
@@ -88,40 +81,6 @@ __device__ __forceinline__ int tensor_of(const Table<E, kMost> &t, uint32_t b) {
     }
     return readlane_i32(k, 0);
 }
-// Fills tables with the tensors that `take` makes an entry of, `per` elements a workgroup, and hands each
-// to `flush` with its number of workgroups: when it is full, or its workgroups are as many as a grid holds.
-template <typename E, int kMost, typename Take, typename Flush>
-hipError_t by_tables(const Tensors &t, int64_t per, int64_t blocks_most, Take take, Flush flush) {
-    Table<E, kMost> table;
-    int n = 0;
-    int64_t blocks = 0;
-    auto out = [&]() {
-        for (int k = n; k < kMost; ++k) table.first[k] = UINT32_MAX;
-        const hipError_t e = flush(table, blocks);
-        n = 0;
-        blocks = 0;
-        return e;
-    };
-    for (int64_t i = 0; i < t.n; ++i) {
-        if (t.sizes[i] == 0) continue;
-        const int64_t need = (t.sizes[i] + per - 1) / per;
-        if (!take(i, table.entry[n])) continue;
-        if (n > 0 && blocks + need > blocks_most) {
-            const E held = table.entry[n];
-            const hipError_t e = out();
-            if (e != hipSuccess) return e;
-            table.entry[0] = held;
-        }
-        table.first[n++] = (uint32_t)blocks;
-        blocks += need;
-        if (n == kMost) {
-            const hipError_t e = out();
-            if (e != hipSuccess) return e;
-        }
-    }
-    return n > 0 ? out() : hipSuccess;
-}
-
 // ---- gradient norm ----------------------------------------------------------------------
 struct NormEntry {
     const void *g;
@@ -589,8 +548,8 @@ hipError_t launch_grad_norm(const Tensors &t, double max_norm, float *norm, floa
     for (int64_t i = 0; i < t.n; ++i) total += t.sizes[i];
     const int64_t chunk = grad_norm_chunk(total);
     double *sums = (double *)ws;
-    const hipError_t e = by_tables<NormEntry, kNormTable>(
-        t, chunk, kGridThreads / kNormThreads,
+    const hipError_t e = by_tables<hipError_t, NormEntry, kNormTable>(
+        t.n, t.sizes, chunk, kGridThreads / kNormThreads,
         [&](int64_t i, NormEntry &to) {
             to = {t.grads[i], t.sizes[i], t.grad_dtypes[i]};
             return true;
@@ -617,8 +576,8 @@ hipError_t launch_adamw(const Tensors &t, int bits, const AdamHyper &h, hipStrea
     for (int kind = 0; kinds >> kind; ++kind) {
         if (!(kinds >> kind & 1)) continue;
         const int copy = kind % kElemTypes;
-        const hipError_t e = by_tables<AdamEntry, kTable>(
-            t, turns * kAdamRound, kAdamBlocksMost,
+        const hipError_t e = by_tables<hipError_t, AdamEntry, kTable>(
+            t.n, t.sizes, turns * kAdamRound, kAdamBlocksMost,
             [&](int64_t i, AdamEntry &to) {
                 if (kind_of(i) != kind) return false;
                 to = {t.params[i], t.grads[i], t.m[i], t.v[i], bits == 8 ? t.scales[i] : nullptr, copy ? t.copies[i] : nullptr, t.sizes[i],
@@ -642,8 +601,8 @@ hipError_t launch_adamw(const Tensors &t, int bits, const AdamHyper &h, hipStrea
 }
 
 hipError_t launch_adamw_unpack(const Tensors &t, float *const *m_out, float *const *v_out, hipStream_t stream) {
-    return by_tables<UnpackEntry, kUnpackTable>(
-        t, kUnpackChunk, kAdamBlocksMost,
+    return by_tables<hipError_t, UnpackEntry, kUnpackTable>(
+        t.n, t.sizes, kUnpackChunk, kAdamBlocksMost,
         [&](int64_t i, UnpackEntry &to) {
             to = {(const int8_t *)t.m[i], (const uint8_t *)t.v[i], t.scales[i], m_out ? m_out[i] : nullptr, v_out ? v_out[i] : nullptr, t.sizes[i]};
             return true;

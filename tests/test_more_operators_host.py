@@ -21,6 +21,30 @@ int64_t floats_most(int64_t rows, int64_t cols) { return layer_norm_part_floats_
 int64_t chunk(int64_t n) { return grad_norm_chunk(n); }
 int64_t slots_most(int64_t k, int64_t n) { return grad_norm_slots_most(k, n); }
 int64_t turns(int64_t n) { return adamw_turns(n); }
+// Tables of at most 5 tensors and `most` workgroups: how many, or a negative number where a tensor that is taken (every
+// number but 3 k + 1) is not in one of them in order, with the workgroups that its elements need.
+int64_t tables(int64_t n, const int64_t *sizes, int64_t per, int64_t most, int64_t fail_at) {
+    int64_t next = 0, count = 0, wrong = 0;
+    const int e = by_tables<int, int64_t, 5>(n, sizes, per, most, [&](int64_t i, int64_t &to) { to = i; return i %% 3 != 1; },
+        [&](const Table<int64_t, 5> &t, int64_t blocks) {
+            int64_t at = 0;
+            if (blocks < 1 || blocks > most) wrong = 1;
+            for (int k = 0; k < 5; ++k) {
+                if (t.first[k] == UINT32_MAX) {
+                    if (k == 0) wrong = 2;
+                    continue;
+                }
+                while (next < n && (sizes[next] == 0 || next %% 3 == 1)) ++next;
+                if (t.entry[k] != next || t.first[k] != at || (k > 0 && t.first[k - 1] == UINT32_MAX)) wrong = 3;
+                at += (sizes[next++] + per - 1) / per;
+            }
+            if (at != blocks) wrong = 4;
+            return count++ == fail_at ? 7 : 0;
+        });
+    while (next < n && (sizes[next] == 0 || next %% 3 == 1)) ++next;
+    if (e != (fail_at >= 0 && count > fail_at ? 7 : 0) || (e == 0 && next != n)) wrong = 5;
+    return wrong ? -wrong : count;
+}
 }
 """ % os.path.join(ROOT, "paper_2609_36830_amd", "csrc", "rules.hpp")
 
@@ -33,6 +57,7 @@ def R(tmp_path_factory):
     lib = ctypes.CDLL(str(d / "r.so"))
     for name, n in (("lanes", 1), ("rows_of", 1), ("parts", 2), ("floats", 2), ("floats_most", 2), ("chunk", 1), ("slots_most", 2), ("turns", 1)):
         getattr(lib, name).restype, getattr(lib, name).argtypes = ctypes.c_int64, [ctypes.c_int64] * n
+    lib.tables.restype, lib.tables.argtypes = ctypes.c_int64, [ctypes.c_int64, ctypes.c_void_p] + [ctypes.c_int64] * 3
     return lib
 
 
@@ -176,6 +201,19 @@ def test_grad_norm_sums_of_every_smaller_call(R):
         chunk = R.chunk(n)
         assert sum(-(-s // chunk) for s in sizes) <= R.slots_most(most, total)
         assert R.slots_most(k, n) <= R.slots_most(most, total)
+
+
+def test_tables_hold_every_tensor_once(R):
+    rng = random.Random(4)
+    for _ in range(3000):
+        most, per, n = rng.choice([4, 9, 1000]), rng.choice([1, 7, 4096]), rng.randint(0, 40)
+        sizes = [rng.choice([0, 1, per, per + 1, rng.randint(0, most * per), most * per]) for _ in range(n)]
+        a = (ctypes.c_int64 * max(n, 1))(*sizes)
+        count = R.tables(n, a, per, most, -1)
+        taken = [s for k, s in enumerate(sizes) if s and k % 3 != 1]
+        assert -(-len(taken) // 5) <= count <= len(taken)
+        if count > 1:                                # an error ends it
+            assert R.tables(n, a, per, most, count - 2) == count - 1
 
 
 def test_gpu_tests_reach_every_form(R):
