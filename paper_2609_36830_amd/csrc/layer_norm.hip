@@ -256,7 +256,9 @@ __device__ __forceinline__ void store_sums(float *p, int64_t c, int64_t cols, fl
 template <typename T, int kLanes, int kThreads>
 __device__ __forceinline__ void write_sums(const float (&dw)[kLnPer], const float (&db)[kLnPer], float *dw_out, float *db_out, int cols) {
     constexpr int kVec = Slice<T>::kVec, kRows = kThreads / kLanes;
-    const int lane = (int)threadIdx.x % kLanes;
+    int thread = (int)threadIdx.x;
+    asm volatile("" : "+v"(thread));                   // places are worked out here, not kept in registers over the rows
+    const int lane = thread % kLanes;
     auto column = [&](int l, int i) { return (l + i / kVec * kLanes) * kVec + i % kVec; };
     if constexpr (kRows == 1) {
 #pragma unroll
@@ -289,7 +291,7 @@ __device__ __forceinline__ void write_sums(const float (&dw)[kLnPer], const floa
 // waves a SIMD would do; with 128 the rows of several waves are faster all the same (16384 x 4096 79 us, 82), those of
 // less than a wave spill (131077 x 128 27, 24).
 template <typename T, typename W, int kLanes, bool kWhole>
-__global__ __launch_bounds__(kLanes > kLnBackward ? kLanes : kLnBackward, kLanes > kWave ? 4 : 2) void layer_norm_backward_kernel(
+__global__ __launch_bounds__(kLanes > kLnBackward ? kLanes : kLnBackward, kLanes > kLnBackward || (kLanes > kWave && kWhole) ? 4 : 2) void layer_norm_backward_kernel(
     const T *__restrict__ x, int64_t rows, int cols, int64_t stride, const W *__restrict__ weight,
     const float *__restrict__ stats, const T *dy, int64_t dy_stride, T *dx, int64_t dx_stride, float *__restrict__ dw_out,
     float *__restrict__ db_out, int64_t part_stride) {
