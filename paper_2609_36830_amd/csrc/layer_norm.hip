@@ -61,47 +61,79 @@ __device__ __forceinline__ int group_of() {
     return kLanes >= kWave ? readlane_i32(g, 0) : g;
 }
 
-// The vectors that a lane holds of a row: lane l has l, l + kLanes, .. With kWhole a
-// row ends with a vector.
+// The vectors that a lane holds of a row: lane l has l, l + kLanes, .. Where a row does not end
+// with a vector (kWhole false) its last one is the row's last kVec elements: those that the one
+// before has too, below low_of, count as none. So all loads are vectors, with no branch that has
+// each waited for (backward, with a tail by elements: 4099 x 2049 in binary32 35.3 us for 26.5, in
+// bfloat16 29.2 for 24.1, 30000 x 130 17.1 for 14.3). Only in rows shorter than a vector do the
+// elements below low_of lie before the row; they are not read.
 template <typename T>
 struct Slice {
     static constexpr int kVec = kVecOf<T>, kVecs = kLnPer / kVec;
     uint4 raw[kVecs];
 };
+template <typename T, int kLanes, bool kWhole>
+__device__ __forceinline__ int place_of(int lane, int k, int cols) {      // the column of vector k's first element
+    constexpr int kVec = Slice<T>::kVec;
+    const int c = (lane + k * kLanes) * kVec;
+    return kWhole || c + kVec <= cols ? c : cols - kVec;
+}
+template <typename T, int kLanes, bool kWhole>
+__device__ __forceinline__ int low_of(int lane, int k, int cols) {
+    return kWhole ? 0 : (lane + k * kLanes) * Slice<T>::kVec - place_of<T, kLanes, kWhole>(lane, k, cols);
+}
+// The row's vector that may be short; the same for all lanes.
+template <typename T, int kLanes>
+__device__ __forceinline__ int last_of(int cols) { return cols / Slice<T>::kVec / kLanes; }
 template <typename T>
-__device__ __forceinline__ uint4 load_part(const T *p, int n) {      // the first n elements, then zeros
+__device__ __forceinline__ uint4 load_from(const T *p, int from) {      // the elements from `from` on, behind zeros
     float v[kVecOf<T>];
 #pragma unroll
-    for (int e = 0; e < kVecOf<T>; ++e) v[e] = e < n ? to_f32(p[e]) : 0.0f;
+    for (int e = 0; e < kVecOf<T>; ++e) v[e] = e >= from ? to_f32(p[e]) : 0.0f;
     return pack16<T>(v);
 }
 template <typename T, int kLanes, bool kWhole>
 __device__ __forceinline__ void load_slice(Slice<T> &s, const T *row, int lane, int cols) {
     constexpr int kVec = Slice<T>::kVec;
 #pragma unroll
-    for (int k = 0; k < Slice<T>::kVecs; ++k) {
-        const int c = (lane + k * kLanes) * kVec;
-        s.raw[k] = make_uint4(0, 0, 0, 0);
-        if (kWhole ? c < cols : c + kVec <= cols) s.raw[k] = load_a1(row + c);
-        else if (!kWhole && c < cols) s.raw[k] = load_part(row + c, cols - c);
+    for (int k = 0; k < Slice<T>::kVecs; ++k) s.raw[k] = make_uint4(0, 0, 0, 0);
+    if (!kWhole && kLanes == layer_norm_lanes(1) && cols < kVec) {
+        if (lane == 0) s.raw[0] = load_from(row + (cols - kVec), kVec - cols);
+        return;
     }
+#pragma unroll
+    for (int k = 0; k < Slice<T>::kVecs; ++k)
+        if ((lane + k * kLanes) * kVec < cols) s.raw[k] = load_a1(row + place_of<T, kLanes, kWhole>(lane, k, cols));
 }
 template <typename T, int kLanes, bool kWhole>
 __device__ __forceinline__ void store_slice(T *row, const float (&v)[kLnPer], int lane, int cols) {
     constexpr int kVec = Slice<T>::kVec;
 #pragma unroll
     for (int k = 0; k < Slice<T>::kVecs; ++k) {
-        const int c = (lane + k * kLanes) * kVec;
+        const int at = place_of<T, kLanes, kWhole>(lane, k, cols), low = low_of<T, kLanes, kWhole>(lane, k, cols);
+        if ((lane + k * kLanes) * kVec >= cols) continue;
         float w[kVec];
 #pragma unroll
         for (int e = 0; e < kVec; ++e) w[e] = v[k * kVec + e];
-        if (kWhole ? c < cols : c + kVec <= cols) {
-            store_a1(row + c, pack16<T>(w));
-        } else if (!kWhole) {
+        if (low == 0) {
+            store_a1(row + at, pack16<T>(w));
+        } else {
 #pragma unroll
             for (int e = 0; e < kVec; ++e)
-                if (c + e < cols) row[c + e] = from_f32<T>(w[e]);
+                if (e >= low) row[at + e] = from_f32<T>(w[e]);
         }
+    }
+}
+// Zeros in the places of elements that count as none.
+template <typename T, int kLanes, bool kWhole>
+__device__ __forceinline__ void clear_low(float (&v)[kLnPer], int lane, int cols) {
+    constexpr int kVec = Slice<T>::kVec;
+#pragma unroll
+    for (int k = 0; k < Slice<T>::kVecs; ++k) {
+        if (kWhole || k != last_of<T, kLanes>(cols)) continue;
+        const int low = low_of<T, kLanes, kWhole>(lane, k, cols);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[k * kVec + e] = e >= low ? v[k * kVec + e] : 0.0f;
     }
 }
 template <typename T>
@@ -124,14 +156,14 @@ struct Weight {
     __device__ __forceinline__ void load(const W *w, float none, int lane, int cols) {
 #pragma unroll
         for (int k = 0; k < kVecs; ++k) {
-            const int i = k * kIn, c = (lane + i / kVec * kLanes) * kVec + i % kVec;
+            const int i = k * kIn, at = place_of<T, kLanes, kWhole>(lane, i / kVec, cols) + i % kVec;
             float v[kIn];
 #pragma unroll
             for (int e = 0; e < kIn; ++e) v[e] = none;
             raw[k] = pack16<W>(v);
-            if (w == nullptr) continue;
-            if (kWhole ? c < cols : c + kIn <= cols) raw[k] = load_a1(w + c);
-            else if (!kWhole && c < cols) raw[k] = load_part(w + c, cols - c);
+            if (w == nullptr || (lane + i / kVec * kLanes) * kVec >= cols) continue;
+            if (!kWhole && kLanes == layer_norm_lanes(1) && at < 0) raw[k] = load_from(w + at, -at);
+            else raw[k] = load_a1(w + at);
         }
     }
     __device__ __forceinline__ void values(float (&v)[kLnPer]) const {
@@ -161,19 +193,20 @@ __device__ __forceinline__ Moments lanes_moments(float (&x)[kLnPer], int lane, i
     for (int i = 0; i < kLnPer; ++i) s += x[i];
     const float ref = lanes_sum<kIn>(s) * inv;
 #pragma unroll
+    for (int i = 0; i < kLnPer; ++i) x[i] -= ref;
+    clear_low<T, kLanes, kWhole>(x, lane, cols);
+#pragma unroll
     for (int k = 0; k < Slice<T>::kVecs; ++k) {
-        const int left = cols - (lane + k * kLanes) * kVec;
+        const bool any = (lane + k * kLanes) * kVec < cols;
         float t1 = 0.0f, t2 = 0.0f;
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
-            float d = x[k * kVec + e] - ref;
-            if (!kWhole) d = e < left ? d : 0.0f;
-            x[k * kVec + e] = d;
+            const float d = x[k * kVec + e];
             t1 += d;
             t2 = __builtin_fmaf(d, d, t2);
         }
-        s1 += !kWhole || left > 0 ? t1 : 0.0f;
-        s2 += !kWhole || left > 0 ? t2 : 0.0f;
+        s1 += any ? t1 : 0.0f;
+        s2 += any ? t2 : 0.0f;
     }
     s1 = lanes_sum<kIn>(s1);
     s2 = lanes_sum<kIn>(s2);
@@ -208,6 +241,7 @@ __global__ __launch_bounds__(kLanes > kLnForward ? kLanes : kLnForward) void lay
     for (int turn = 0; base < rows; base += step, turn ^= 1) {
         float v[kLnPer];
         unpack_slice<T>(next, v);
+        clear_low<T, kLanes, kWhole>(v, lane, cols);
         if (base + step < rows) load_slice<T, kLanes, kWhole>(next, x + row_of(base + step) * stride, lane, cols);
         Moments m = lanes_moments<T, kIn, kLanes, kWhole>(v, lane, cols, count);
         if constexpr (kWaves > 1) {
@@ -241,31 +275,31 @@ __global__ __launch_bounds__(kLanes > kLnForward ? kLanes : kLnForward) void lay
     }
 }
 
-// Four consecutive columns' sums from c on, those at or past cols left out.
-__device__ __forceinline__ void store_sums(float *p, int64_t c, int64_t cols, float a, float b, float d, float e) {
-    if (c + 4 <= cols) {
-        store_a1(p + c, make_uint4(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, d), __builtin_bit_cast(uint32_t, e)));
+// Four consecutive columns' sums, those below `low` left out.
+__device__ __forceinline__ void store_sums(float *p, int low, float a, float b, float d, float e) {
+    if (low <= 0) {
+        store_a1(p, make_uint4(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, d), __builtin_bit_cast(uint32_t, e)));
     } else {
-        if (c < cols) p[c] = a;
-        if (c + 1 < cols) p[c + 1] = b;
-        if (c + 2 < cols) p[c + 2] = d;
+        if (low <= 1) p[1] = b;
+        if (low <= 2) p[2] = d;
+        if (low <= 3) p[3] = e;
     }
 }
 
 // Adds this workgroup's column sums of all its rows' lanes and writes them; dw or db may be null.
-template <typename T, int kLanes, int kThreads>
+template <typename T, int kLanes, bool kWhole, int kThreads>
 __device__ __forceinline__ void write_sums(const float (&dw)[kLnPer], const float (&db)[kLnPer], float *dw_out, float *db_out, int cols) {
     constexpr int kVec = Slice<T>::kVec, kRows = kThreads / kLanes;
     int thread = (int)threadIdx.x;
     asm volatile("" : "+v"(thread));                   // places are worked out here, not kept in registers over the rows
     const int lane = thread % kLanes;
-    auto column = [&](int l, int i) { return (l + i / kVec * kLanes) * kVec + i % kVec; };
     if constexpr (kRows == 1) {
 #pragma unroll
         for (int i = 0; i < kLnPer; i += 4) {
-            const int c = column(lane, i);
-            if (dw_out) store_sums(dw_out, c, cols, dw[i], dw[i + 1], dw[i + 2], dw[i + 3]);
-            if (db_out) store_sums(db_out, c, cols, db[i], db[i + 1], db[i + 2], db[i + 3]);
+            if ((lane + i / kVec * kLanes) * kVec >= cols) continue;
+            const int c = place_of<T, kLanes, kWhole>(lane, i / kVec, cols) + i % kVec, low = low_of<T, kLanes, kWhole>(lane, i / kVec, cols) - i % kVec;
+            if (dw_out) store_sums(dw_out + c, low, dw[i], dw[i + 1], dw[i + 2], dw[i + 3]);
+            if (db_out) store_sums(db_out + c, low, db[i], db[i + 1], db[i + 2], db[i + 3]);
         }
     } else {
         __shared__ float sums[kLnPer][kThreads];
@@ -277,21 +311,23 @@ __device__ __forceinline__ void write_sums(const float (&dw)[kLnPer], const floa
             for (int i = 0; i < kLnPer; ++i) sums[i][threadIdx.x] = which ? db[i] : dw[i];
             __syncthreads();
             for (int o = (int)threadIdx.x; o < kLnPer * kLanes; o += kThreads) {
-                const int i = o / kLanes, l = o % kLanes, c = column(l, i);
+                const int i = o / kLanes, l = o % kLanes, k = i / kVec;
+                const int c = place_of<T, kLanes, kWhole>(l, k, cols) + i % kVec;
+                const bool mine = (l + k * kLanes) * kVec < cols && i % kVec >= low_of<T, kLanes, kWhole>(l, k, cols);
                 float s = 0.0f;
 #pragma unroll
                 for (int r = 0; r < kRows; ++r) s += sums[i][r * kLanes + l];
-                if (out && c < cols) out[c] = s;
+                if (out && mine) out[c] = s;
             }
         }
     }
 }
 
 // dx may be dy itself: a row is read before it is written. There is one workgroup a CU (kLnParts), so registers for two
-// waves a SIMD would do; with 128 the rows of several waves are faster all the same (16384 x 4096 79 us, 82), those of
-// less than a wave spill (131077 x 128 27, 24).
+// waves a SIMD would do; with 128 the rows of several waves are faster all the same (16384 x 4096 79 us, 82), but those of
+// less than a wave spill (131077 x 128 27, 24), and so do ragged ones and binary32 with a row ahead.
 template <typename T, typename W, int kLanes, bool kWhole>
-__global__ __launch_bounds__(kLanes > kLnBackward ? kLanes : kLnBackward, kLanes > kLnBackward || (kLanes > kWave && kWhole) ? 4 : 2) void layer_norm_backward_kernel(
+__global__ __launch_bounds__(kLanes > kLnBackward ? kLanes : kLnBackward, kLanes > kLnBackward || (kLanes > kWave && kWhole && sizeof(T) == 2) ? 4 : 2) void layer_norm_backward_kernel(
     const T *__restrict__ x, int64_t rows, int cols, int64_t stride, const W *__restrict__ weight,
     const float *__restrict__ stats, const T *dy, int64_t dy_stride, T *dx, int64_t dx_stride, float *__restrict__ dw_out,
     float *__restrict__ db_out, int64_t part_stride) {
@@ -303,9 +339,9 @@ __global__ __launch_bounds__(kLanes > kLnBackward ? kLanes : kLnBackward, kLanes
     const int64_t step = (int64_t)gridDim.x * kRows;
     int64_t base = (int64_t)blockIdx.x * kRows;
     auto row_of = [&](int64_t b) { return b + group < rows ? b + group : rows - 1; };
-    // A row's bytes are on their way while the one before is summed; of binary32, whose rows are as
-    // many bytes as two of the others, registers hold one.
-    constexpr bool kAhead = sizeof(T) == 2;
+    // A row's bytes are on their way while the one before is summed. Of binary32 a row takes twice the registers, which
+    // workgroups of 1024 lanes do not have (1000 x 8192 26.7 us, 28.8 without the row ahead, 4096 x 4096 44.0, 45.7).
+    constexpr bool kAhead = sizeof(T) == 2 || kLanes <= kLnBackward;
     Slice<T> nx, ng;
     float mean = 0.0f, rstd = 0.0f;
     auto take = [&](int64_t b) {
@@ -328,6 +364,7 @@ __global__ __launch_bounds__(kLanes > kLnBackward ? kLanes : kLnBackward, kLanes
         unpack_slice<T>(nx, h);
         const Slice<T> g = ng;
         unpack_slice<T>(g, a);
+        clear_low<T, kLanes, kWhole>(a, lane, cols);
         weights.values(w);
         const float r = rstd;
         const bool live = row < rows;
@@ -362,7 +399,7 @@ __global__ __launch_bounds__(kLanes > kLnBackward ? kLanes : kLnBackward, kLanes
     }
     if (dw_out || db_out) {
         const int64_t at = (int64_t)blockIdx.x * part_stride;
-        write_sums<T, kLanes, kThreads>(dw, db, dw_out ? dw_out + at : nullptr, db_out ? db_out + at : nullptr, cols);
+        write_sums<T, kLanes, kWhole, kThreads>(dw, db, dw_out ? dw_out + at : nullptr, db_out ? db_out + at : nullptr, cols);
     }
 }
 

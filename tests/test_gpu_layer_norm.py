@@ -323,3 +323,39 @@ def test_nothing_beyond_the_rows(pace):
                                           cols + 5, None, None, None, 0, s) == 0
         for got, want in ((out, ref), (dx, grad)):
             assert torch.equal(got[:, :cols], want) and (got[:, cols:] == 3.0).all()
+
+
+@pytest.mark.parametrize("dtype, weight", [(F32, F32), (BF16, BF16), (BF16, F32), (F16, F32)])
+@pytest.mark.parametrize("cols", list(range(1, 18)) + [127, 129, 131, 250, 501, 1003, 2042, 2049, 4093, 4103, 8190, 9007, 16383, 16389])
+def test_ends_of_rows(pace, cols, dtype, weight):
+    """A row's last vector shares elements with the one before it: nothing counts twice, what stands around rows, weights and
+    sums is neither used (NaN) nor written over, and a gradient may replace the one that it comes from."""
+    say("layer norm, ends of rows of %d %s, weights %s" % (cols, dtype, weight))
+    nan = float("nan")
+    for rows in (1, 6, 130):
+        def around(values):
+            t = torch.full((values.shape[0] + 2, cols + 5), nan, dtype=values.dtype, device=DEV)
+            t[1:-1, 3:-2] = values
+            return t[1:-1, 3:-2]
+
+        def alone(values):
+            t = torch.full((cols + 9,), nan, dtype=values.dtype, device=DEV)
+            t[3:cols + 3] = values
+            return t[3:cols + 3]
+
+        x, dy = around(matrix(rows, cols, dtype, seed=23, offset=0.2)), around(matrix(rows, cols, dtype, seed=24))
+        w, b = (alone((1 + 0.1 * torch.randn(cols, device=DEV)).to(weight)) for _ in range(2))
+        kept = pace.layer_norm_buffers(rows, cols, dtype, DEV, backward=True)
+        kept.update(out=around(x), grad_weight=alone(torch.zeros(cols, device=DEV)), grad_bias=alone(torch.zeros(cols, device=DEV)))
+        out, stats = pace.pace_layer_norm(x, w, b, buffers=kept)
+        check_forward(x, w, b, 1e-5, out, stats)
+        dx, dw, db = pace.pace_layer_norm_backward(x, stats, dy, w, buffers=kept)
+        check_backward(x, w, stats, dy, dx, dw, db)
+        sums = dw.clone(), db.clone()
+        into = around(dy)
+        same, dw, db = pace.pace_layer_norm_backward(x, stats, into, w, buffers=dict(kept, grad_x=into))
+        assert torch.equal(same, dx) and torch.equal(dw, sums[0]) and torch.equal(db, sums[1])
+        for t in (out, into):
+            whole = t._base
+            assert whole.isnan().sum() == whole.numel() - rows * cols
+        assert all(t._base.isnan().sum() == 9 for t in (dw, db))
