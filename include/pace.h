@@ -28,7 +28,8 @@
  *   multi-turn rollout). Masked tokens are not response tokens of Eq. (1): they
  *   count neither in T nor in the staleness sums, but compaction copies them.
  * - Pointers are DEVICE pointers unless marked [host]. Every device call is
- *   enqueued on `stream` (a hipStream_t passed as void*, NULL = null stream)
+ *   enqueued on `stream` (a hipStream_t passed as void*, NULL = null stream of
+ *   the device current on the calling thread, which has to be the pointers')
  *   and returns without synchronising. Nothing is allocated or freed inside a
  *   call; the caller owns every buffer, including the workspace, and no
  *   pointer is retained after a call returns. Inputs and outputs must not

@@ -968,6 +968,7 @@ def pace_adamw(params, grads, state, lr: float = 1e-3, step: int = 1, betas=(0.9
     copies = copy_types = None
     if state["copies"] is not None:
         _, _, copies, copy_types, _, _ = _each(state["copies"], "copies", _HALVES, at, True, sizes)
+    _lib.lists().apart(("params", "grads", "exp_avg", "exp_avg_sq", "scale", "copies"), (p, g, m, v, scales, copies))
     decay = array("f", [weight_decay]) * n if isinstance(weight_decay, (int, float)) else array("f", weight_decay)
     if len(decay) != n:
         raise ValueError("weight_decay must be a number or one for each tensor")
@@ -993,6 +994,7 @@ def pace_adamw_unpack(state, out=None, stream=None):
         e = _allocator(dev, stream)
         out = [[e(t.shape, torch.float32) for t in state["exp_avg"]] for _ in range(2)]
     m_out, v_out = (_each(o, "out", _F32, at, True, sizes)[2] for o in out)
+    _lib.lists().apart(("exp_avg", "exp_avg_sq", "scale", "out[0]", "out[1]"), (m, v, scales, m_out, v_out))
     _check(_on(at, lib().pace_adamw_unpack, n, sizes, m, v, scales, m_out, v_out, _stream(dev, stream)), "pace_adamw_unpack")
     return out[0], out[1]
 

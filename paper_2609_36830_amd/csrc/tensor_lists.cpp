@@ -115,6 +115,37 @@ PyObject *read(PyObject *, PyObject *args) {
     }
 }
 
+// apart(names, pointers): that no two of the lists have the same tensor at a place; pointers as read() gives them, or None.
+PyObject *apart(PyObject *, PyObject *args) {
+    PyObject *names, *lists;
+    if (!PyArg_ParseTuple(args, "O!O!", &PyTuple_Type, &names, &PyTuple_Type, &lists)) return nullptr;
+    const Py_ssize_t n = PyTuple_GET_SIZE(lists);
+    if (PyTuple_GET_SIZE(names) != n) return fail("as many names as lists are wanted");
+    Py_ssize_t size = -1;
+    for (Py_ssize_t a = 0; a < n; ++a) {
+        PyObject *list = PyTuple_GET_ITEM(lists, a);
+        if (!PyUnicode_Check(PyTuple_GET_ITEM(names, a)) || (list != Py_None && !PyBytes_Check(list))) return fail("names and bytes are wanted");
+        if (list == Py_None) continue;
+        if (size >= 0 && PyBytes_GET_SIZE(list) != size) return fail("lists must be as long as each other");
+        size = PyBytes_GET_SIZE(list);
+    }
+    for (Py_ssize_t a = 0; a < n; ++a)
+        for (Py_ssize_t b = a + 1; b < n; ++b) {
+            PyObject *x = PyTuple_GET_ITEM(lists, a), *y = PyTuple_GET_ITEM(lists, b);
+            if (x == Py_None || y == Py_None) continue;
+            for (Py_ssize_t k = 0; k + (Py_ssize_t)sizeof(uintptr_t) <= size; k += sizeof(uintptr_t)) {
+                uintptr_t p, q;
+                std::memcpy(&p, PyBytes_AS_STRING(x) + k, sizeof p);
+                std::memcpy(&q, PyBytes_AS_STRING(y) + k, sizeof q);
+                if (p != 0 && p == q) {
+                    PyErr_Format(PyExc_ValueError, "%U and %U must not overlap each other", PyTuple_GET_ITEM(names, a), PyTuple_GET_ITEM(names, b));
+                    return nullptr;
+                }
+            }
+        }
+    Py_RETURN_NONE;
+}
+
 std::string shape_of(long long rows, long long cols) {
     auto side = [](long long n) { return n < 0 ? std::string("any") : std::to_string(n); };
     return "(" + side(rows) + ", " + side(cols) + ")";
@@ -184,6 +215,7 @@ PyObject *vector(PyObject *, PyObject *args) {
 
 PyMethodDef methods[] = {{"matrix", matrix, METH_VARARGS, "Pointer, type, sizes and row stride of a matrix."},
                          {"vector", vector, METH_VARARGS, "Pointer, type and size of a contiguous tensor."},
+                         {"apart", apart, METH_VARARGS, "Refuses lists with the same tensor at a place."},
                          {"read", read, METH_VARARGS, "Pointers, types and sizes of a list of tensors."}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lists", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

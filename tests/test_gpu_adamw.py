@@ -470,3 +470,25 @@ def test_refusals(pace):
         pace.adamw_state(p, 8, F32)
     with pytest.raises(ValueError):
         pace.pace_adamw_unpack(pace.adamw_state(p, 32))
+
+
+def test_the_same_tensors_twice(pace):
+    """A list given in another's place: nothing is written."""
+    say("adamw of the same tensors twice")
+    sizes = [10, 0, 300]
+    p, g = ([torch.full((n,), 1.5, device=DEV) for n in sizes] for _ in range(2))
+    wide, small = pace.adamw_state(p), pace.adamw_state(p, 8)
+    half = [t.to(BF16) for t in p]
+    signed = [t.view(torch.int8) for t in small["exp_avg_sq"]]
+    for args in ((p, p, wide), (p, g, dict(wide, exp_avg_sq=wide["exp_avg"])), (p, g, dict(wide, exp_avg=p)), (p, g, dict(wide, exp_avg_sq=g)),
+                 (p, g, dict(wide, exp_avg=wide["exp_avg"][:2] + p[2:])), (p, g, dict(small, exp_avg=signed)), (half, g, dict(wide, copies=half)),
+                 (p, half, dict(wide, copies=half))):
+        with pytest.raises(ValueError, match="must not overlap each other"):
+            pace.pace_adamw(*args)
+    out = [torch.zeros(n, device=DEV) for n in sizes]
+    with pytest.raises(ValueError, match="must not overlap each other"):
+        pace.pace_adamw_unpack(small, out=(out, out))
+    assert all((t == 1.5).all() for t in p + g + half)
+    assert all((t == 0).all() for t in wide["exp_avg"] + wide["exp_avg_sq"] + out)
+    assert pace.pace_adamw(p, g, wide) is p
+    assert all((t != 1.5).all() for t in p)

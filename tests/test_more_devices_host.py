@@ -37,6 +37,10 @@ def test_a_call_runs_on_its_tensors_device(monkeypatch, name, current, fails):
             return len(tensors), 1, b"", b"", b"", sum(t.numel() for t in tensors)
 
         @staticmethod
+        def apart(names, pointers):
+            return None
+
+        @staticmethod
         def matrix(t, name, types, device, rows, cols):
             return 0, 0, t.shape[0], t.shape[1], t.shape[1], 1
 

@@ -259,3 +259,17 @@ def test_lists_are_refused_before_any_call(L):
         pace.adamw_state([x], bits=8)
     with pytest.raises(ValueError, match="8 bits"):
         pace.pace_adamw_unpack(dict(bits=32))
+
+
+def test_the_same_tensor_in_two_lists(L):
+    import array
+    import paper_2609_36830_amd as pace
+    apart = pace._lib.lists().apart
+    of = lambda *p: array.array("Q", p).tobytes()
+    assert apart(("a", "b", "c"), (of(1, 2, 0), None, of(2, 1, 0))) is None       # empty tensors have no place
+    assert apart((), ()) is None and apart(("a", "b"), (b"", b"")) is None
+    with pytest.raises(ValueError, match="a and c must not overlap each other"):
+        apart(("a", "b", "c"), (of(1, 2, 5), of(3, 4, 6), of(7, 8, 5)))
+    for bad in ((("a",), ()), (("a", "b"), (of(1), of(1, 2))), ((1, "b"), (of(1), of(2))), (("a", "b"), (3, of(2))), (["a"], (of(1),)), (3, 4)):
+        with pytest.raises((ValueError, TypeError)):
+            apart(*bad)

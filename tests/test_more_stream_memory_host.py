@@ -44,6 +44,10 @@ def test_a_call_allocates_in_its_streams_memory(monkeypatch, name):
             return len(tensors), 0, b"", b"", b"", sum(t.numel() for t in tensors)
 
         @staticmethod
+        def apart(names, pointers):
+            return None
+
+        @staticmethod
         def matrix(t, name, types, device, rows, cols):
             return 0, 0, t.shape[0], t.shape[1], t.shape[1], 0
 
