@@ -4,7 +4,7 @@
 //   dx = rstd (a - mean a - h mean(a h)),  dw = sum over rows of dy h,  db = sum over rows of dy.
 //
 // HBM-bound: the forward pass reads x and writes y, the backward pass reads x
-// and dy and writes dx, with some 10 and 16 vector instructions an element. A
+// and dy and writes dx, with 16 and 25 vector instructions an element. A
 // row is held in registers, 16 elements a lane, by 8 lanes up to 128 columns
 // and twice as many for twice the columns, up to 1024 lanes for 16384; wider rows are
 // read again for each step. The weights stay in registers from row to row.
