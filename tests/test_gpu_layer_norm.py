@@ -344,7 +344,7 @@ def test_ends_of_rows(pace, cols, dtype, weight):
             return t[3:cols + 3]
 
         x, dy = around(matrix(rows, cols, dtype, seed=23, offset=0.2)), around(matrix(rows, cols, dtype, seed=24))
-        w, b = (alone((1 + 0.1 * torch.randn(cols, device=DEV)).to(weight)) for _ in range(2))
+        w, b = (alone(1 + matrix(1, cols, weight, seed=k, scale=0.1)[0]) for k in (25, 26))
         kept = pace.layer_norm_buffers(rows, cols, dtype, DEV, backward=True)
         kept.update(out=around(x), grad_weight=alone(torch.zeros(cols, device=DEV)), grad_bias=alone(torch.zeros(cols, device=DEV)))
         out, stats = pace.pace_layer_norm(x, w, b, buffers=kept)
