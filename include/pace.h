@@ -635,7 +635,8 @@ int pace_grad_norm(int64_t n_tensors, const void *const *grads, const int32_t *g
  * weight_decay: [host] f32 [n_tensors], finite and >= 0, or NULL (0)
  * hyper [host]: lr finite; betas in [0, 1); eps 1e-30 .. 1e30; step >= 1, the number of this update
  * grad_scale: f32 [1] (device) or NULL (1). Where it is an infinity or a NaN nothing
- *   is written: the step is left out, without the host having to look.
+ *   is written: the step is left out, without the host having to look. copies are no
+ *   exception: before the first step they are the caller's to fill.
  * schedule: f64 [2] (device) or NULL: lr and step, in place of hyper's, for calls
  *   that are captured once and replayed. */
 #define PACE_ADAMW_BLOCK 256

@@ -923,7 +923,8 @@ def pace_grad_norm(grads, max_norm: float = float("inf"), buffers=None, stream=N
 
 def adamw_state(params, bits: int = 32, copy_dtype=None, stream=None):
     """Fresh moments for pace_adamw of these tensors: zeros, in float32 or with ``bits`` 8 as codes with two scales for every
-    ADAMW_BLOCK elements. With copy_dtype (bfloat16 or float16) each step writes the new parameters in that type too."""
+    ADAMW_BLOCK elements. With copy_dtype (bfloat16 or float16) each step writes the new parameters in that type too; before
+    the first, and where it is left out, the copies are the parameters as they are now."""
     ts = list(params)
     dev = torch.device("cuda", _each(ts, "params", _FLOATS)[1])
     if bits not in (32, 8):
@@ -932,18 +933,19 @@ def adamw_state(params, bits: int = 32, copy_dtype=None, stream=None):
         raise ValueError("copy_dtype must be bfloat16 or float16")
     e = _allocator(dev, stream)
 
-    def zeros(shape, dtype):
+    def made(shape, dtype, of=None):
         t = e(shape, dtype)
+        fill = t.zero_ if of is None else lambda: t.copy_(of.detach())
         if stream is None:
-            return t.zero_()
+            return fill()
         s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(dev, stream), device=dev)
         with torch.cuda.stream(s):
-            return t.zero_()
+            return fill()
 
     moments = (torch.float32, torch.float32) if bits == 32 else (torch.int8, torch.uint8)
-    return dict(bits=bits, exp_avg=[zeros(t.shape, moments[0]) for t in ts], exp_avg_sq=[zeros(t.shape, moments[1]) for t in ts],
-                scale=[zeros((-(-t.numel() // ADAMW_BLOCK), 2), torch.float32) for t in ts] if bits == 8 else None,
-                copies=[zeros(t.shape, copy_dtype) for t in ts] if copy_dtype is not None else None)
+    return dict(bits=bits, exp_avg=[made(t.shape, moments[0]) for t in ts], exp_avg_sq=[made(t.shape, moments[1]) for t in ts],
+                scale=[made((-(-t.numel() // ADAMW_BLOCK), 2), torch.float32) for t in ts] if bits == 8 else None,
+                copies=[made(t.shape, copy_dtype, t) for t in ts] if copy_dtype is not None else None)
 
 
 def _moments(state, device: int, sizes):
