@@ -625,7 +625,9 @@ int pace_grad_norm(int64_t n_tensors, const void *const *grads, const int32_t *g
  *   |m| and v go to the code nearest in the root that the codes are evenly spaced in,
  *   against the block's largest before its own rounding (halfway to the larger code), a
  *   positive v to 1 at least.
- *   Blocks whose largest is below 2^-126 are zeros. Zeros are fresh states.
+ *   A block's moments whose largest is below 2^-126 are zeros, those of either kind by
+ *   themselves: where only v is lost, steps go by eps, within 1/256 of what they were by both,
+ *   as eps is no less than 2^-55 / sqrt(1 - beta2) here. Zeros are fresh states.
  *   A code moves when a moment changes by half a step between codes: while a block's
  *   largest keeps its size, a smaller |m| that shrinks by beta1 = 0.9 is held from 0.5%
  *   of it on, a v that shrinks by beta2 = 0.999 wherever it is.
@@ -633,7 +635,10 @@ int pace_grad_norm(int64_t n_tensors, const void *const *grads, const int32_t *g
  * copies: copy_dtypes (PACE_BF16 or PACE_F16) copies of the new parameters, an entry
  *   or all NULL: none
  * weight_decay: [host] f32 [n_tensors], finite and >= 0, or NULL (0)
- * hyper [host]: lr finite; betas in [0, 1); eps 1e-30 .. 1e30; step >= 1, the number of this update
+ * hyper [host]: lr finite; betas in [0, 1); eps 1e-30 .. 1e30, with state_bits 8 no less than
+ *   2^-55 / sqrt(1 - beta2) (8.8e-16 at 0.999); step >= 1, the number of this update. With
+ *   state_bits 32 v is zero below 2^-150, as binary32 has it: the steps of gradients below
+ *   2^-75 / sqrt(1 - beta2) (8.4e-22 at 0.999) are divided by eps alone.
  * grad_scale: f32 [1] (device) or NULL (1). Where it is an infinity or a NaN nothing
  *   is written: the step is left out, without the host having to look. copies are no
  *   exception: before the first step they are the caller's to fill.

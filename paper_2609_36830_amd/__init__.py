@@ -963,7 +963,8 @@ def pace_adamw(params, grads, state, lr: float = 1e-3, step: int = 1, betas=(0.9
     """One AdamW step over a list of tensors, in place: params, the moments in ``state`` (adamw_state) and its copies. step is
     the number of this update, from 1. weight_decay: a number, or one for each tensor. grad_scale (f32[1], pace_grad_norm's
     factor) multiplies the gradients; where it is no number nothing changes. schedule (f64[2] on the device: lr, step) stands
-    in for lr and step in calls that are captured and replayed. Returns params."""
+    in for lr and step in calls that are captured and replayed. With moments in 8 bits eps is 2^-55 / sqrt(1 - betas[1]) at
+    least. Returns params."""
     n, at, p, types, sizes, _ = _each(params, "params", _FLOATS, written=True)
     _, _, g, grad_types, _, _ = _each(grads, "grads", _FLOATS, at, sizes=sizes)
     bits, m, v, scales = _moments(state, at, sizes)

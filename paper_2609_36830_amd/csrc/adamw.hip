@@ -7,8 +7,12 @@
 // 256 consecutive elements of a tensor, M = max |m'| and V = max v':
 //   code c in -127 .. 127 stands for c |c| M / 127^2,  c in 0 .. 255 for (c / 255)^4 V,
 // so that the square root that the step takes of v is held like m. A moment
-// goes to the code that is nearest in that root, a positive v' to 1 at least: no
-// step is divided by a zero that rounding made. Codes change at borders, where a
+// goes to the code that is nearest in that root, a positive v' to 1 at least: a
+// small v beside large ones is never a zero that rounding made. A block's whole v
+// is, where V would be below 2^-126. As long as that goes on (1 - b2) g^2 < 2^-126, so
+// the formula's sqrt(v / (1 - b2^t)) stays below 2^-63 / sqrt(1 - b2); an eps of no
+// less than 256 times that is demanded, and what is lost changes a step by less than
+// half of the way between two codes of v does. Codes change at borders, where a
 // last place decides, so they go by the largest moment itself, of which the scale is
 // the rounding: m', v' and the largest are binary64, and a root of binary32 that
 // comes within its own error of a border is decided by comparing in binary64.

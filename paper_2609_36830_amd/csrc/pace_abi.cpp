@@ -818,6 +818,8 @@ int pace_adamw(int64_t n_tensors, const int64_t *sizes, void *const *params, con
     }
     const double b1 = hyper->beta1, b2 = hyper->beta2;
     if (!(b1 >= 0.0 && b1 < 1.0) || !(b2 >= 0.0 && b2 < 1.0) || !(hyper->eps >= 1e-30 && hyper->eps <= 1e30)) return PACE_ERR_INVALID_ARG;
+    // What a block loses where its V counts as zero is below eps / 256 then (adamw.hip).
+    if (state_bits == 8 && !(hyper->eps * sqrt(1.0 - b2) >= 0x1p-55)) return PACE_ERR_INVALID_ARG;
     if (!aligned(grad_scale, 4) || !aligned(schedule, 8)) return PACE_ERR_INVALID_ARG;
     AdamHyper h = {0.0, b1, b2, hyper->eps, 1.0, 1.0, grad_scale, schedule};
     if (!schedule) {
