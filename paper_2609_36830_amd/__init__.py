@@ -949,13 +949,18 @@ def adamw_state(params, bits: int = 32, copy_dtype=None, stream=None):
 
 
 def _moments(state, device: int, sizes):
-    """The state's moments and scales as the C ABI takes them."""
+    """The state's bits, and its moments and scales as they are read."""
     bits = state["bits"]
     if bits not in (32, 8):
         raise ValueError("bits must be 32 or 8")
-    m = _each(state["exp_avg"], "exp_avg", _F32 if bits == 32 else _INT8, device, True, sizes)[2]
-    v = _each(state["exp_avg_sq"], "exp_avg_sq", _F32 if bits == 32 else _UINT8, device, True, sizes)[2]
-    return bits, m, v, _each(state["scale"], "scale", _F32, device, True, sizes, ADAMW_BLOCK)[2] if bits == 8 else None
+    m = _each(state["exp_avg"], "exp_avg", _F32 if bits == 32 else _INT8, device, True, sizes)
+    v = _each(state["exp_avg_sq"], "exp_avg_sq", _F32 if bits == 32 else _UINT8, device, True, sizes)
+    return bits, m, v, _each(state["scale"], "scale", _F32, device, True, sizes, ADAMW_BLOCK) if bits == 8 else None
+
+
+def _pointers(read):
+    """A read list's pointers; of none, none."""
+    return None if read is None else read[2]
 
 
 def pace_adamw(params, grads, state, lr: float = 1e-3, step: int = 1, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.0,
@@ -965,12 +970,11 @@ def pace_adamw(params, grads, state, lr: float = 1e-3, step: int = 1, betas=(0.9
     factor) multiplies the gradients; where it is no number nothing changes. schedule (f64[2] on the device: lr, step) stands
     in for lr and step in calls that are captured and replayed. With moments in 8 bits eps is 2^-55 / sqrt(1 - betas[1]) at
     least. Returns params."""
-    n, at, p, types, sizes, _ = _each(params, "params", _FLOATS, written=True)
-    _, _, g, grad_types, _, _ = _each(grads, "grads", _FLOATS, at, sizes=sizes)
+    p = _each(params, "params", _FLOATS, written=True)
+    n, at, _, types, sizes, _ = p
+    g = _each(grads, "grads", _FLOATS, at, sizes=sizes)
     bits, m, v, scales = _moments(state, at, sizes)
-    copies = copy_types = None
-    if state["copies"] is not None:
-        _, _, copies, copy_types, _, _ = _each(state["copies"], "copies", _HALVES, at, True, sizes)
+    copies = None if state["copies"] is None else _each(state["copies"], "copies", _HALVES, at, True, sizes)
     _lib.lists().apart(("params", "grads", "exp_avg", "exp_avg_sq", "scale", "copies"), (p, g, m, v, scales, copies))
     decay = array("f", [weight_decay]) * n if isinstance(weight_decay, (int, float)) else array("f", weight_decay)
     if len(decay) != n:
@@ -980,8 +984,9 @@ def pace_adamw(params, grads, state, lr: float = 1e-3, step: int = 1, betas=(0.9
     factor = None if grad_scale is None else _lib.lists().vector(grad_scale, "grad_scale", _F32, at, 1)[0]
     rates = None if schedule is None else _lib.lists().vector(schedule, "schedule", _F64, at, 2)[0]
     hyper = AdamwParams(float(lr), float(betas[0]), float(betas[1]), float(eps), int(step))
-    _check(_on(at, lib().pace_adamw, n, sizes, p, types, g, grad_types, bits, m, v, scales, copies, copy_types, decay.tobytes(),
-                            ctypes.byref(hyper), factor, rates, _stream(torch.device("cuda", at), stream)), "pace_adamw")
+    _check(_on(at, lib().pace_adamw, n, sizes, p[2], types, g[2], g[3], bits, m[2], v[2], _pointers(scales), _pointers(copies),
+               None if copies is None else copies[3], decay.tobytes(), ctypes.byref(hyper), factor, rates,
+               _stream(torch.device("cuda", at), stream)), "pace_adamw")
     return params
 
 
@@ -996,9 +1001,9 @@ def pace_adamw_unpack(state, out=None, stream=None):
     if out is None:
         e = _allocator(dev, stream)
         out = [[e(t.shape, torch.float32) for t in state["exp_avg"]] for _ in range(2)]
-    m_out, v_out = (_each(o, "out", _F32, at, True, sizes)[2] for o in out)
+    m_out, v_out = (_each(o, "out", _F32, at, True, sizes) for o in out)
     _lib.lists().apart(("exp_avg", "exp_avg_sq", "scale", "out[0]", "out[1]"), (m, v, scales, m_out, v_out))
-    _check(_on(at, lib().pace_adamw_unpack, n, sizes, m, v, scales, m_out, v_out, _stream(dev, stream)), "pace_adamw_unpack")
+    _check(_on(at, lib().pace_adamw_unpack, n, sizes, *map(_pointers, (m, v, scales, m_out, v_out)), _stream(dev, stream)), "pace_adamw_unpack")
     return out[0], out[1]
 
 

@@ -115,24 +115,99 @@ PyObject *read(PyObject *, PyObject *args) {
     }
 }
 
-// apart(names, pointers): that no two of the lists have the same tensor at a place; pointers as read() gives them, or None.
-PyObject *apart(PyObject *, PyObject *args) {
+struct Span {      // of bytes that a list's tensors have
+    uintptr_t first, end;
+    Py_ssize_t list;
+    bool operator<(const Span &other) const { return first < other.first; }
+};
+
+// Adds what the tensors of a list, as read() gives it, have: in order, and as one where they touch or overlap each other.
+bool add_spans(PyObject *read, Py_ssize_t list, std::vector<Span> &spans) {
+    if (PyTuple_GET_SIZE(read) != 6) return false;
+    for (int k = 2; k < 5; ++k)
+        if (!PyBytes_Check(PyTuple_GET_ITEM(read, k))) return false;
+    const auto size = [&](int k) { return (size_t)PyBytes_GET_SIZE(PyTuple_GET_ITEM(read, k)); };
+    const size_t n = size(2) / sizeof(uintptr_t), from = spans.size();
+    if (size(3) != n * sizeof(int32_t) || size(4) != n * sizeof(int64_t)) return false;
+    const char *pointers = PyBytes_AS_STRING(PyTuple_GET_ITEM(read, 2)), *codes = PyBytes_AS_STRING(PyTuple_GET_ITEM(read, 3)),
+               *sizes = PyBytes_AS_STRING(PyTuple_GET_ITEM(read, 4));
+    static const uintptr_t width[] = {4, 2, 2, 1, 1, 8};
+    bool in_order = true;
+    for (size_t k = 0; k < n; ++k) {
+        uintptr_t p;
+        int32_t code;
+        int64_t elements;
+        std::memcpy(&p, pointers + k * sizeof p, sizeof p);
+        std::memcpy(&code, codes + k * sizeof code, sizeof code);
+        std::memcpy(&elements, sizes + k * sizeof elements, sizeof elements);
+        if (code < 0 || code > 5 || elements < 0) return false;
+        if (elements == 0) continue;
+        const uintptr_t end = p + (uintptr_t)elements * width[code];
+        if (spans.size() > from && p == spans.back().end) {
+            spans.back().end = end;
+            continue;
+        }
+        in_order = in_order && (spans.size() == from || p > spans.back().end);
+        spans.push_back({p, end, list});
+    }
+    if (in_order) return true;
+    std::sort(spans.begin() + (std::ptrdiff_t)from, spans.end());
+    size_t to = from;
+    for (size_t k = from; k < spans.size(); ++k) {
+        if (to > from && spans[k].first <= spans[to - 1].end) spans[to - 1].end = std::max(spans[to - 1].end, spans[k].end);
+        else spans[to++] = spans[k];
+    }
+    spans.resize(to);
+    return true;
+}
+
+// Sorts spans whose runs, from each of `starts` to the next, are in order.
+void merge_runs(std::vector<Span> &spans, std::vector<size_t> starts) {
+    if (std::is_sorted(spans.begin(), spans.end())) return;
+    std::vector<Span> other(spans.size());
+    for (; starts.size() > 1; spans.swap(other)) {
+        std::vector<size_t> next;
+        const auto at = [&](size_t k) { return spans.begin() + (std::ptrdiff_t)(k < starts.size() ? starts[k] : spans.size()); };
+        for (size_t k = 0; k < starts.size(); k += 2) {
+            next.push_back(starts[k]);
+            std::merge(at(k), at(k + 1), at(k + 1), at(k + 2), other.begin() + (std::ptrdiff_t)starts[k]);
+        }
+        starts.swap(next);
+    }
+}
+
+// apart(names, lists): that no tensor of a list overlaps one of another; lists as read() gives them, or None. Of lists that
+// are their pointers alone (bytes) only that no two have the same at a place.
+PyObject *apart(PyObject *, PyObject *args) try {
     PyObject *names, *lists;
     if (!PyArg_ParseTuple(args, "O!O!", &PyTuple_Type, &names, &PyTuple_Type, &lists)) return nullptr;
     const Py_ssize_t n = PyTuple_GET_SIZE(lists);
     if (PyTuple_GET_SIZE(names) != n) return fail("as many names as lists are wanted");
     Py_ssize_t size = -1;
+    std::vector<Span> spans;
+    std::vector<size_t> starts;
     for (Py_ssize_t a = 0; a < n; ++a) {
         PyObject *list = PyTuple_GET_ITEM(lists, a);
-        if (!PyUnicode_Check(PyTuple_GET_ITEM(names, a)) || (list != Py_None && !PyBytes_Check(list))) return fail("names and bytes are wanted");
+        if (!PyUnicode_Check(PyTuple_GET_ITEM(names, a))) return fail("names are wanted");
         if (list == Py_None) continue;
+        if (PyTuple_Check(list)) {
+            starts.push_back(spans.size());
+            if (!add_spans(list, a, spans)) return fail("lists must be as they were read");
+            continue;
+        }
+        if (!PyBytes_Check(list)) return fail("bytes are wanted");
         if (size >= 0 && PyBytes_GET_SIZE(list) != size) return fail("lists must be as long as each other");
         size = PyBytes_GET_SIZE(list);
     }
+    merge_runs(spans, std::move(starts));
+    for (size_t k = 1; k < spans.size(); ++k)
+        if (spans[k].first < spans[k - 1].end)
+            return PyErr_Format(PyExc_ValueError, "%U and %U must not overlap each other", PyTuple_GET_ITEM(names, std::min(spans[k - 1].list, spans[k].list)),
+                                PyTuple_GET_ITEM(names, std::max(spans[k - 1].list, spans[k].list)));
     for (Py_ssize_t a = 0; a < n; ++a)
         for (Py_ssize_t b = a + 1; b < n; ++b) {
             PyObject *x = PyTuple_GET_ITEM(lists, a), *y = PyTuple_GET_ITEM(lists, b);
-            if (x == Py_None || y == Py_None) continue;
+            if (!PyBytes_Check(x) || !PyBytes_Check(y)) continue;
             for (Py_ssize_t k = 0; k + (Py_ssize_t)sizeof(uintptr_t) <= size; k += sizeof(uintptr_t)) {
                 uintptr_t p, q;
                 std::memcpy(&p, PyBytes_AS_STRING(x) + k, sizeof p);
@@ -144,6 +219,8 @@ PyObject *apart(PyObject *, PyObject *args) {
             }
         }
     Py_RETURN_NONE;
+} catch (const std::exception &e) {
+    return fail(e.what());
 }
 
 std::string shape_of(long long rows, long long cols) {
@@ -215,7 +292,7 @@ PyObject *vector(PyObject *, PyObject *args) {
 
 PyMethodDef methods[] = {{"matrix", matrix, METH_VARARGS, "Pointer, type, sizes and row stride of a matrix."},
                          {"vector", vector, METH_VARARGS, "Pointer, type and size of a contiguous tensor."},
-                         {"apart", apart, METH_VARARGS, "Refuses lists with the same tensor at a place."},
+                         {"apart", apart, METH_VARARGS, "Refuses lists whose tensors overlap."},
                          {"read", read, METH_VARARGS, "Pointers, types and sizes of a list of tensors."}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lists", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,4 +1,4 @@
-"""GPU tests of AdamW's states: what a fresh one holds before its first step, and what a step tells of the tensors that it writes."""
+"""GPU tests of AdamW's states: what a fresh one holds before its first step, and which tensors a step refuses."""
 import sys
 
 import pytest
@@ -52,3 +52,35 @@ def test_a_first_step_that_is_left_out(pace, bits, dtype, side):
     pace.pace_adamw(params, grads, state, step=1, stream=stream)
     torch.cuda.synchronize()
     assert all(torch.equal(c, p.to(dtype)) and not torch.equal(p, b) for c, p, b in zip(state["copies"], params, before) if p.numel())
+
+
+def test_lists_that_share_memory(pace):
+    """In another order, or in part: refused, nothing is written. Neighbours in one buffer are taken."""
+    say("adamw of lists that share memory")
+    p, g = ([torch.full((n,), 1.5, device=DEV) for n in (300, 300)] for _ in range(2))
+    wide, small = pace.adamw_state(p), pace.adamw_state(p, 8)
+    flat = torch.full((5000,), 1.5, device=DEV)
+    view = lambda *starts: [flat[a: a + 300] for a in starts]
+    bytes_of = flat.view(torch.int8)
+    for args in ((p, p[::-1], wide), (p, g, dict(wide, exp_avg_sq=wide["exp_avg"][::-1])), (view(0, 1000), view(2000, 1299), wide),
+                 (view(0, 1000), g, dict(wide, exp_avg=view(2000, 299))), (p, view(0, 1000), dict(wide, exp_avg_sq=view(1001, 2000))),
+                 (view(0, 1000), g, dict(small, exp_avg=[bytes_of[1199: 1499], small["exp_avg"][1]])),
+                 (p, g, dict(small, scale=[flat[0:4].view(2, 2), flat[6:10].view(2, 2)], exp_avg=[bytes_of[1000:1300], bytes_of[39:339]])),
+                 (view(0, 1000), g, dict(wide, copies=[flat[2000:2150].view(BF16), flat[1299:1449].view(BF16)]))):
+        with pytest.raises(ValueError, match="must not overlap each other"):
+            pace.pace_adamw(*args)
+    with pytest.raises(ValueError, match="must not overlap each other"):
+        pace.pace_adamw_unpack(small, out=(view(0, 300), view(1000, 599)))
+    torch.cuda.synchronize()
+    assert all((t == 1.5).all() for t in p + g + [flat]) and not any(t.any() for t in wide["exp_avg"] + wide["exp_avg_sq"])
+    # one behind the other, and one gradient for two parameters
+    state = dict(bits=32, scale=None, copies=None, exp_avg=view(600, 900), exp_avg_sq=view(1200, 1500))
+    shared = g[:1] * 2
+    alone = [t.clone() for t in view(0, 300)], dict(state, **{k: [t.clone() for t in state[k]] for k in ("exp_avg", "exp_avg_sq")})
+    pace.pace_adamw(view(0, 300), shared, state)
+    pace.pace_adamw(alone[0], [g[0], g[0].clone()], alone[1])
+    for a, b in zip(view(0, 300) + state["exp_avg"] + state["exp_avg_sq"], alone[0] + alone[1]["exp_avg"] + alone[1]["exp_avg_sq"]):
+        assert torch.equal(a, b)
+    # moments of 1.5 beside gradients of 1.5 stay (0.9 and 0.1 of the same), what else there is changes
+    assert all((t != 1.5).all() for t in view(0, 300) + state["exp_avg_sq"])
+    assert (flat[1800:] == 1.5).all()
