@@ -969,8 +969,9 @@ def pace_adamw(params, grads, state, lr: float = 1e-3, step: int = 1, betas=(0.9
     the number of this update, from 1. weight_decay: a number, or one for each tensor. grad_scale (f32[1], pace_grad_norm's
     factor) multiplies the gradients; where it is no number nothing changes. schedule (f64[2] on the device: lr, step) stands
     in for lr and step in calls that are captured and replayed. With moments in 8 bits eps is 2^-55 / sqrt(1 - betas[1]) at
-    least. Returns params."""
-    p = _each(params, "params", _FLOATS, written=True)
+    least. Params and copies count as changed in place: a pending backward pass that saved one raises. Returns params."""
+    ts = params if isinstance(params, (list, tuple)) else list(params)
+    p = _each(ts, "params", _FLOATS, written=True)
     n, at, _, types, sizes, _ = p
     g = _each(grads, "grads", _FLOATS, at, sizes=sizes)
     bits, m, v, scales = _moments(state, at, sizes)
@@ -987,6 +988,7 @@ def pace_adamw(params, grads, state, lr: float = 1e-3, step: int = 1, betas=(0.9
     _check(_on(at, lib().pace_adamw, n, sizes, p[2], types, g[2], g[3], bits, m[2], v[2], _pointers(scales), _pointers(copies),
                None if copies is None else copies[3], decay.tobytes(), ctypes.byref(hyper), factor, rates,
                _stream(torch.device("cuda", at), stream)), "pace_adamw")
+    _lib.wrote(ts, state["copies"])                    # not the moments, which no graph saves: 12 ns a tensor
     return params
 
 

@@ -84,8 +84,7 @@ def load(path: str = library_path):
     return h
 
 
-def lists():
-    """The extension that reads lists of tensors; raises if it has not been built (no fallback exists)."""
+def _extension():
     global _lists
     if _lists is None:
         import importlib.util
@@ -97,6 +96,16 @@ def lists():
         _lists = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(_lists)
     return _lists
+
+
+def lists():
+    """The extension that reads lists of tensors; raises if it has not been built (no fallback exists)."""
+    return _extension()
+
+
+def wrote(*tensors):
+    """Tells torch, as its own operations in place do, that lists of tensors (or None) have been written through their pointers."""
+    _extension().wrote(*tensors)
 
 
 def lib():

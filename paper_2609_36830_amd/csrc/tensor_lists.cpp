@@ -186,6 +186,7 @@ PyObject *apart(PyObject *, PyObject *args) try {
     Py_ssize_t size = -1;
     std::vector<Span> spans;
     std::vector<size_t> starts;
+    spans.reserve(512);
     for (Py_ssize_t a = 0; a < n; ++a) {
         PyObject *list = PyTuple_GET_ITEM(lists, a);
         if (!PyUnicode_Check(PyTuple_GET_ITEM(names, a))) return fail("names are wanted");
@@ -218,6 +219,25 @@ PyObject *apart(PyObject *, PyObject *args) try {
                 }
             }
         }
+    Py_RETURN_NONE;
+} catch (const std::exception &e) {
+    return fail(e.what());
+}
+
+// wrote(list, ..): raises the versions of lists of tensors (or None) that a call has written through their pointers, as torch
+// does for its own operations in place: a graph that has saved one then refuses to use it.
+PyObject *wrote(PyObject *, PyObject *lists) try {
+    for (Py_ssize_t a = 0; a < PyTuple_GET_SIZE(lists); ++a) {
+        if (PyTuple_GET_ITEM(lists, a) == Py_None) continue;
+        const Held list{PySequence_Fast(PyTuple_GET_ITEM(lists, a), "a list of tensors is wanted")};
+        if (!list.p) return nullptr;
+        for (Py_ssize_t k = 0; k < PySequence_Fast_GET_SIZE(list.p); ++k) {
+            PyObject *item = PySequence_Fast_GET_ITEM(list.p, k);
+            if (!THPVariable_Check(item)) return fail("a list of tensors is wanted");
+            const at::Tensor &t = THPVariable_Unpack(item);
+            if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+        }
+    }
     Py_RETURN_NONE;
 } catch (const std::exception &e) {
     return fail(e.what());
@@ -293,7 +313,8 @@ PyObject *vector(PyObject *, PyObject *args) {
 PyMethodDef methods[] = {{"matrix", matrix, METH_VARARGS, "Pointer, type, sizes and row stride of a matrix."},
                          {"vector", vector, METH_VARARGS, "Pointer, type and size of a contiguous tensor."},
                          {"apart", apart, METH_VARARGS, "Refuses lists whose tensors overlap."},
-                         {"read", read, METH_VARARGS, "Pointers, types and sizes of a list of tensors."}, {nullptr, nullptr, 0, nullptr}};
+                         {"read", read, METH_VARARGS, "Pointers, types and sizes of a list of tensors."},
+                         {"wrote", wrote, METH_VARARGS, "Raises the versions of lists of tensors."}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lists", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,4 +1,5 @@
-"""GPU tests of AdamW's states: what a fresh one holds before its first step, and which tensors a step refuses."""
+"""GPU tests of AdamW's states: what a fresh one holds before its first step, which tensors a step refuses, and what
+torch learns of those that it writes."""
 import sys
 
 import pytest
@@ -84,3 +85,26 @@ def test_lists_that_share_memory(pace):
     # moments of 1.5 beside gradients of 1.5 stay (0.9 and 0.1 of the same), what else there is changes
     assert all((t != 1.5).all() for t in view(0, 300) + state["exp_avg_sq"])
     assert (flat[1800:] == 1.5).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_saved_parameters_and_copies(pace, bits):
+    """A pass that saved a parameter or a copy before the step raises, and does not use the new values; one after it runs."""
+    say("adamw %d bits, saved parameters" % bits)
+    p = [torch.randn(300, device=DEV, requires_grad=True), torch.randn(70, device=DEV, requires_grad=True)]
+    x = torch.randn(300, device=DEV, requires_grad=True)
+    state = pace.adamw_state(p, bits, BF16)
+    step = lambda **kw: pace.pace_adamw(p, [torch.ones_like(t) for t in p], state, **kw)
+    for loss in (lambda: sum((t * t).sum() for t in p), lambda: (x * state["copies"][0]).sum()):
+        saved = loss()
+        step()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            saved.backward()
+        saved = loss()
+        with pytest.raises(pace.PaceError):
+            step(lr=NAN)                             # refused: nothing is written
+        for t in p + [x]:
+            t.grad = None
+        saved.backward()
+        assert x.grad is None or torch.equal(x.grad, state["copies"][0].float())
+        assert p[0].grad is None or torch.equal(p[0].grad, 2 * p[0])
