@@ -102,10 +102,36 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 def _stream(device: torch.device, stream=None) -> int:
     if stream is None:
-        if _raw_stream is not None and device.index is not None:
-            return _raw_stream(device.index)
+        index = device.index
+        if _raw_stream is not None and index is not None:
+            return _raw_stream(index)
         stream = torch.cuda.current_stream(device)
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+class _Elsewhere:
+    """The library with another device than the current one made current for the length of each call."""
+
+    def __init__(self, device: int):
+        self.device = device
+
+    def __getattr__(self, name):
+        entry = getattr(lib(), name)
+
+        def call(*args):
+            with torch.cuda.device(self.device):
+                return entry(*args)
+        return call
+
+
+def _at(device: Optional[int]):
+    """The library for tensors of a device (its index), which is the current one nearly always (0.14 us to see). The default
+    stream's handle is that of whichever device is current, which kernels then run on."""
+    try:
+        here = device is None or torch._C._cuda_getDevice() == device
+    except RuntimeError:                               # no device at all
+        here = True
+    return lib() if here else _Elsewhere(device)
 
 
 def _allocator(device, stream=None):
@@ -176,11 +202,11 @@ def pace_score(tags, offsets, completion, current_version, prefix_score=None, wi
         if gen_count_out is None:
             gen_count_out = e(n, torch.int64)
     ws = _workspace(WS_SCORE, n, nt, e, workspace)
-    _check(lib().pace_score(_ptr(tags), _ptr(offsets), n, nt, _ptr(completion), int(current_version),
-                            _ptr(prefix_score), _ptr(window_sorted), W,
-                            ctypes.byref(params) if params is not None else None,
-                            _ptr(score_out), _ptr(gen_sum_out), _ptr(gen_count_out),
-                            _ptr(ws), ws.numel(), _stream(dev, stream)), "pace_score")
+    _check(_at(dev.index).pace_score(_ptr(tags), _ptr(offsets), n, nt, _ptr(completion), int(current_version),
+                                     _ptr(prefix_score), _ptr(window_sorted), W,
+                                     ctypes.byref(params) if params is not None else None,
+                                     _ptr(score_out), _ptr(gen_sum_out), _ptr(gen_count_out),
+                                     _ptr(ws), ws.numel(), _stream(dev, stream)), "pace_score")
     return score_out, gen_sum_out, gen_count_out
 
 
@@ -207,8 +233,8 @@ def pace_select(score, budget: int, keep_out=None, reject_ids_out=None, workspac
     if reject_ids_out is None:
         reject_ids_out = e(max(int(budget), 1), torch.int32)
     ws = _workspace(WS_SELECT, n, 0, e, workspace)
-    _check(lib().pace_select(_ptr(score), n, int(budget), _ptr(keep_out), _ptr(reject_ids_out),
-                             _ptr(ws), ws.numel(), _stream(dev, stream)), "pace_select")
+    _check(_at(dev.index).pace_select(_ptr(score), n, int(budget), _ptr(keep_out), _ptr(reject_ids_out),
+                                      _ptr(ws), ws.numel(), _stream(dev, stream)), "pace_select")
     return keep_out, reject_ids_out[: int(budget)]
 
 
@@ -239,9 +265,9 @@ def pace_compact(offsets, keep, cols: Sequence[torch.Tensor], cols_out=None, off
         n_kept_tokens_out = e(1, torch.int64)
     ws = _workspace(WS_COMPACT, n, n_tokens, e, workspace)
     nc, cin, eb, cout = _col_args(cols, cols_out)
-    _check(lib().pace_compact(_ptr(offsets), n, int(n_tokens), _ptr(keep), nc, cin, eb, cout,
-                              _ptr(offsets_out), _ptr(kept_ids_out), _ptr(n_kept_tokens_out),
-                              _ptr(ws), ws.numel(), _stream(dev, stream)), "pace_compact")
+    _check(_at(dev.index).pace_compact(_ptr(offsets), n, int(n_tokens), _ptr(keep), nc, cin, eb, cout,
+                                       _ptr(offsets_out), _ptr(kept_ids_out), _ptr(n_kept_tokens_out),
+                                       _ptr(ws), ws.numel(), _stream(dev, stream)), "pace_compact")
     return offsets_out, kept_ids_out, n_kept_tokens_out, cols_out
 
 
@@ -258,9 +284,9 @@ def pace_validate(tags, offsets, completion, current_version, window_sorted=None
         W = window_sorted.numel()
     if err_out is None:
         err_out = _allocator(dev, stream)(1, torch.int32)
-    _check(lib().pace_validate(_ptr(tags), _ptr(offsets), offsets.numel() - 1, tags.numel(),
-                               _ptr(completion), int(current_version), _ptr(window_sorted), W,
-                               _ptr(err_out), _stream(dev, stream)), "pace_validate")
+    _check(_at(dev.index).pace_validate(_ptr(tags), _ptr(offsets), offsets.numel() - 1, tags.numel(),
+                                        _ptr(completion), int(current_version), _ptr(window_sorted), W,
+                                        _ptr(err_out), _stream(dev, stream)), "pace_validate")
     return err_out
 
 
@@ -325,10 +351,10 @@ def _filter_step_call(tags, offsets, completion, current_version, occupancy, cap
             reject_ids_out.data_ptr(), nc, cin, eb, cout, offsets_out.data_ptr(), kept_ids_out.data_ptr(),
             n_kept_tokens_out.data_ptr())
     if noalloc:
-        _check(lib().pace_filter_step_noalloc(*args, _stream(dev, stream)), "pace_filter_step_noalloc")
+        _check(_at(dev.index).pace_filter_step_noalloc(*args, _stream(dev, stream)), "pace_filter_step_noalloc")
     else:
         ws = workspace if workspace is not None else _workspace(WS_FILTER_STEP, n, nt, _allocator(dev, stream), None)
-        _check(lib().pace_filter_step(*args, ws.data_ptr(), ws.numel(), _stream(dev, stream)), "pace_filter_step")
+        _check(_at(dev.index).pace_filter_step(*args, ws.data_ptr(), ws.numel(), _stream(dev, stream)), "pace_filter_step")
     return b.value, rh.value
 
 
@@ -351,10 +377,11 @@ def pace_group_score(score, group_offsets, group_score_out=None, stream=None):
     _dev(score, torch.float64, "score")
     _dev(group_offsets, torch.int64, "group_offsets")
     ng = group_offsets.numel() - 1
+    dev = score.device
     if group_score_out is None:
-        group_score_out = _allocator(score.device, stream)(ng, torch.float64)
-    _check(lib().pace_group_score(_ptr(score), score.numel(), _ptr(group_offsets), ng, _ptr(group_score_out),
-                                  _stream(score.device, stream)), "pace_group_score")
+        group_score_out = _allocator(dev, stream)(ng, torch.float64)
+    _check(_at(dev.index).pace_group_score(_ptr(score), score.numel(), _ptr(group_offsets), ng, _ptr(group_score_out),
+                                           _stream(dev, stream)), "pace_group_score")
     return group_score_out
 
 
@@ -363,10 +390,11 @@ def pace_group_expand(group_offsets, group_keep, n_traj: int, keep_out=None, str
     _dev(group_offsets, torch.int64, "group_offsets")
     _dev(group_keep, torch.uint8, "group_keep")
     ng = group_offsets.numel() - 1
+    dev = group_keep.device
     if keep_out is None:
-        keep_out = _allocator(group_keep.device, stream)(int(n_traj), torch.uint8)
-    _check(lib().pace_group_expand(_ptr(group_offsets), ng, int(n_traj), _ptr(group_keep), _ptr(keep_out),
-                                   _stream(group_keep.device, stream)), "pace_group_expand")
+        keep_out = _allocator(dev, stream)(int(n_traj), torch.uint8)
+    _check(_at(dev.index).pace_group_expand(_ptr(group_offsets), ng, int(n_traj), _ptr(group_keep), _ptr(keep_out),
+                                            _stream(dev, stream)), "pace_group_expand")
     return keep_out
 
 
@@ -376,8 +404,8 @@ def pace_validate_groups(group_offsets, n_traj: int, err_out=None, stream=None):
     dev = group_offsets.device
     if err_out is None:
         err_out = _allocator(dev, stream)(1, torch.int32)
-    _check(lib().pace_validate_groups(_ptr(group_offsets), group_offsets.numel() - 1, int(n_traj),
-                                      _ptr(err_out), _stream(dev, stream)), "pace_validate_groups")
+    _check(_at(dev.index).pace_validate_groups(_ptr(group_offsets), group_offsets.numel() - 1, int(n_traj),
+                                               _ptr(err_out), _stream(dev, stream)), "pace_validate_groups")
     return err_out
 
 
@@ -436,7 +464,7 @@ def pace_group_filter_step(tags, offsets, completion, current_version, group_off
     nc, cin, eb, cout = _col_args(cols, cols_out)
     rh = ctypes.c_double(float(r_hat_prev))
     b = ctypes.c_int64(0)
-    _check(lib().pace_group_filter_step(
+    _check(_at(dev.index).pace_group_filter_step(
         _ptr(tags), _ptr(offsets), n, nt, _ptr(completion), int(current_version), _ptr(prefix_score),
         _ptr(window_sorted), W, _ptr(group_offsets), ng, int(occupancy), int(capacity),
         ctypes.byref(params) if params is not None else None, ctypes.byref(rh), ctypes.byref(b),
@@ -474,10 +502,10 @@ def pace_stream_admit(score, r_hat: float, window: StreamWindow, batch_size: int
     reject_ids_out = e(max(n, 1), torch.int32) if reject_ids_out is None else reject_ids_out
     kappa_out = e(1, torch.float64) if kappa_out is None else kappa_out
     counts_out = e(3, torch.int64) if counts_out is None else counts_out
-    _check(lib().pace_stream_admit(_ptr(score), n, float(r_hat), ctypes.byref(params) if params is not None else None,
-                                   int(batch_size), _ptr(window.ring), window.cap, _ptr(window.state),
-                                   _ptr(status_out), _ptr(keep_out), _ptr(reject_ids_out), _ptr(kappa_out),
-                                   _ptr(counts_out), _stream(dev, stream)), "pace_stream_admit")
+    _check(_at(dev.index).pace_stream_admit(_ptr(score), n, float(r_hat), ctypes.byref(params) if params is not None else None,
+                                            int(batch_size), _ptr(window.ring), window.cap, _ptr(window.state),
+                                            _ptr(status_out), _ptr(keep_out), _ptr(reject_ids_out), _ptr(kappa_out),
+                                            _ptr(counts_out), _stream(dev, stream)), "pace_stream_admit")
     return _first(status_out, n), _first(keep_out, n), reject_ids_out, kappa_out, counts_out
 
 
@@ -515,7 +543,7 @@ def pace_stream_step(tags, offsets, completion, current_version, occupancy, capa
     nc, cin, eb, cout = _col_args(cols, b["cols_out"])
     rh = ctypes.c_double(float(r_hat_prev))
     ws = b["workspace"]
-    _check(lib().pace_stream_step(
+    _check(_at(dev.index).pace_stream_step(
         _ptr(tags), _ptr(offsets), n, nt, _ptr(completion), int(current_version), _ptr(prefix_score),
         _ptr(window_sorted), W, int(occupancy), int(capacity), ctypes.byref(params) if params is not None else None,
         ctypes.byref(rh), int(batch_size), _ptr(window.ring), window.cap, _ptr(window.state), _ptr(b["score"]),
@@ -534,11 +562,12 @@ def pace_prefix_score(lp_new, lp_behavior, prefix_offsets, tags=None, cap: int =
     if tags is not None:
         _dev(tags, torch.int32, "tags")
     n = prefix_offsets.numel() - 1
+    dev = lp_new.device
     if s_pre_out is None:
-        s_pre_out = _allocator(lp_new.device, stream)(max(n, 1), torch.float64)
-    _check(lib().pace_prefix_score(_ptr(lp_new), _ptr(lp_behavior), _ptr(tags), _ptr(prefix_offsets), n,
-                                   lp_new.numel(), int(cap), int(min_tokens), _ptr(s_pre_out),
-                                   _stream(lp_new.device, stream)), "pace_prefix_score")
+        s_pre_out = _allocator(dev, stream)(max(n, 1), torch.float64)
+    _check(_at(dev.index).pace_prefix_score(_ptr(lp_new), _ptr(lp_behavior), _ptr(tags), _ptr(prefix_offsets), n,
+                                            lp_new.numel(), int(cap), int(min_tokens), _ptr(s_pre_out),
+                                            _stream(dev, stream)), "pace_prefix_score")
     return _first(s_pre_out, n)
 
 
@@ -554,8 +583,8 @@ def pace_stale_k(gen_sum, gen_count, completion, current_version, k: int, keep_o
     keep_out = e(max(n, 1), torch.uint8) if keep_out is None else keep_out
     if with_lag and lag_out is None:
         lag_out = e(max(n, 1), torch.float64)
-    _check(lib().pace_stale_k(_ptr(gen_sum), _ptr(gen_count), _ptr(completion), int(current_version), n, int(k),
-                              _ptr(keep_out), _ptr(lag_out), _stream(dev, stream)), "pace_stale_k")
+    _check(_at(dev.index).pace_stale_k(_ptr(gen_sum), _ptr(gen_count), _ptr(completion), int(current_version), n, int(k),
+                                       _ptr(keep_out), _ptr(lag_out), _stream(dev, stream)), "pace_stale_k")
     return _first(keep_out, n), (_first(lag_out, n) if lag_out is not None else None)
 
 
@@ -571,9 +600,9 @@ def pace_diagnostics(score, gen_sum, gen_count, completion, current_version, kee
     e = _allocator(dev, stream)
     hist_out = e((3, 2, nbins + 2), torch.int64) if hist_out is None else hist_out
     totals_out = e((2, 4), torch.int64) if totals_out is None else totals_out
-    _check(lib().pace_diagnostics(_ptr(score), _ptr(gen_sum), _ptr(gen_count), _ptr(completion),
-                                  int(current_version), _ptr(keep), n, _ptr(edges), int(nbins), _ptr(hist_out),
-                                  _ptr(totals_out), _stream(dev, stream)), "pace_diagnostics")
+    _check(_at(dev.index).pace_diagnostics(_ptr(score), _ptr(gen_sum), _ptr(gen_count), _ptr(completion),
+                                           int(current_version), _ptr(keep), n, _ptr(edges), int(nbins), _ptr(hist_out),
+                                           _ptr(totals_out), _stream(dev, stream)), "pace_diagnostics")
     return hist_out, totals_out
 
 
@@ -648,9 +677,9 @@ def pace_token_logprob(logits, token_ids, temperature: float = 1.0, top_k: int =
     stats = _sized(b["stats"], torch.float32, (n, 2), dev, "stats")
     ids, top = _sized(b["top_ids"], torch.int32, (n, top_k), dev, "top_ids"), _sized(b["top_logp"], torch.float32, (n, top_k), dev, "top_logp")
     ws, ws_bytes = _scratch(b["workspace"], dev)
-    _check(lib().pace_token_logprob(logits.data_ptr(), dt, n, vocab, stride, token_ids.data_ptr(), float(temperature),
-                                    int(top_k), logp.data_ptr(), entropy.data_ptr(), stats.data_ptr(), ids.data_ptr(),
-                                    top.data_ptr(), ws, ws_bytes, _stream(dev, stream)), "pace_token_logprob")
+    _check(_at(dev.index).pace_token_logprob(logits.data_ptr(), dt, n, vocab, stride, token_ids.data_ptr(), float(temperature),
+                                             int(top_k), logp.data_ptr(), entropy.data_ptr(), stats.data_ptr(), ids.data_ptr(),
+                                             top.data_ptr(), ws, ws_bytes, _stream(dev, stream)), "pace_token_logprob")
     return logp, entropy, stats, ids, top
 
 
@@ -672,9 +701,9 @@ def pace_token_logprob_backward(logits, token_ids, stats, grad_logp, entropy=Non
     gdt, gn, gvocab, gstride = _matrix(grad_logits_out, "grad_logits_out")
     if (gdt, gn, gvocab) != (dt, n, vocab) or grad_logits_out.device != dev:
         raise ValueError("grad_logits_out must have the logits' type and shape")
-    _check(lib().pace_token_logprob_backward(logits.data_ptr(), dt, n, vocab, stride, token_ids.data_ptr(),
-                                             float(temperature), stats.data_ptr(), _ptr(entropy), grad_logp.data_ptr(),
-                                             _ptr(grad_entropy), grad_logits_out.data_ptr(), gstride, _stream(dev, stream)),
+    _check(_at(dev.index).pace_token_logprob_backward(logits.data_ptr(), dt, n, vocab, stride, token_ids.data_ptr(),
+                                                      float(temperature), stats.data_ptr(), _ptr(entropy), grad_logp.data_ptr(),
+                                                      _ptr(grad_entropy), grad_logits_out.data_ptr(), gstride, _stream(dev, stream)),
            "pace_token_logprob_backward")
     return grad_logits_out
 
@@ -710,20 +739,21 @@ def pace_policy_loss(lp_new, lp_behavior, offsets, advantage, tags=None, weight=
     grad, loss = _sized(b["grad"], torch.float32, (nt,), dev, "grad"), _sized(b["loss"], torch.float32, (n,), dev, "loss")
     kl, clipped = _sized(b["kl"], torch.float32, (n,), dev, "kl"), _sized(b["clipped"], torch.int32, (n,), dev, "clipped")
     ws, ws_bytes = _scratch(b["workspace"], dev)
-    _check(lib().pace_policy_loss(lp_new.data_ptr(), lp_behavior.data_ptr(), _ptr(tags), offsets.data_ptr(), n, nt,
-                                  advantage.data_ptr(), _ptr(weight), float(scale), float(clip_low), float(clip_high),
-                                  float(dual_clip), grad.data_ptr(), loss.data_ptr(), kl.data_ptr(), clipped.data_ptr(),
-                                  ws, ws_bytes, _stream(dev, stream)), "pace_policy_loss")
+    _check(_at(dev.index).pace_policy_loss(lp_new.data_ptr(), lp_behavior.data_ptr(), _ptr(tags), offsets.data_ptr(), n, nt,
+                                           advantage.data_ptr(), _ptr(weight), float(scale), float(clip_low), float(clip_high),
+                                           float(dual_clip), grad.data_ptr(), loss.data_ptr(), kl.data_ptr(), clipped.data_ptr(),
+                                           ws, ws_bytes, _stream(dev, stream)), "pace_policy_loss")
     return grad, loss, kl, clipped
 
 
 def pace_quantize_rows(x, q_out=None, scale_out=None, stream=None):
     """Rows in 8 bits: scale = max |x| / 127, q = rint(x (127 (1 / max |x|))). Returns (q int8[n, k], scale f32[n])."""
     dt, n, k, stride = _matrix(x, "x")
-    q_out = _sized(q_out, torch.int8, (n, k), x.device, "q_out", stream)
-    scale_out = _sized(scale_out, torch.float32, (n,), x.device, "scale_out", stream)
-    _check(lib().pace_quantize_rows(x.data_ptr(), dt, n, k, stride, q_out.data_ptr(), scale_out.data_ptr(),
-                                    _stream(x.device, stream)), "pace_quantize_rows")
+    dev = x.device
+    q_out = _sized(q_out, torch.int8, (n, k), dev, "q_out", stream)
+    scale_out = _sized(scale_out, torch.float32, (n,), dev, "scale_out", stream)
+    _check(_at(dev.index).pace_quantize_rows(x.data_ptr(), dt, n, k, stride, q_out.data_ptr(), scale_out.data_ptr(),
+                                             _stream(dev, stream)), "pace_quantize_rows")
     return q_out, scale_out
 
 
@@ -767,8 +797,8 @@ def pace_matmul_i8(a, a_scale, b, b_scale, out=None, out_dtype=torch.bfloat16, w
     if workspace is None:
         workspace = _allocator(dev, stream)(pace_matmul_i8_workspace_bytes(m, n, k), torch.uint8)
     ws, ws_bytes = _scratch(workspace, dev)
-    _check(lib().pace_matmul_i8(a.data_ptr(), lda, a_scale.data_ptr(), b.data_ptr(), ldb, b_scale.data_ptr(), m, n, k,
-                                out.data_ptr(), dt, ldo, ws, ws_bytes, _stream(dev, stream)), "pace_matmul_i8")
+    _check(_at(dev.index).pace_matmul_i8(a.data_ptr(), lda, a_scale.data_ptr(), b.data_ptr(), ldb, b_scale.data_ptr(), m, n, k,
+                                         out.data_ptr(), dt, ldo, ws, ws_bytes, _stream(dev, stream)), "pace_matmul_i8")
     return out
 
 
@@ -803,24 +833,15 @@ def pace_orthogonalize(update, steps: int = 5, coefs=(3.4445, -4.7750, 2.0315), 
         workspace = _allocator(dev, stream)(pace_orthogonalize_workspace_bytes(batch, rows, cols), torch.uint8)
     ws, ws_bytes = _scratch(workspace, dev)
     stride = u.stride(1) if rows > 1 else max(cols, 1)
-    _check(lib().pace_orthogonalize(update.data_ptr(), DTYPES[update.dtype], batch, rows, cols, stride,
-                                    u.stride(0) if batch > 1 else rows * stride, int(steps),
-                                    (ctypes.c_double * 3)(*map(float, coefs)), float(eps), out.data_ptr(), ws,
-                                    ws_bytes, _stream(dev, stream)), "pace_orthogonalize")
+    _check(_at(dev.index).pace_orthogonalize(update.data_ptr(), DTYPES[update.dtype], batch, rows, cols, stride,
+                                             u.stride(0) if batch > 1 else rows * stride, int(steps),
+                                             (ctypes.c_double * 3)(*map(float, coefs)), float(eps), out.data_ptr(), ws,
+                                             ws_bytes, _stream(dev, stream)), "pace_orthogonalize")
     return out
 
 
 # ---- the norm before the head, gradient norm and AdamW ---------------------------
 ADAMW_BLOCK = 256        # elements of a tensor that share the scales of moments in 8 bits
-
-
-def _on(device: int, call, *args):
-    """call(*args) with the tensors' device current, as it is already nearly always (0.1 us). The default stream's handle is
-    that of whichever device is current, which kernels then run on."""
-    if not torch.cuda.is_initialized() or torch._C._cuda_getDevice() == device:
-        return call(*args)
-    with torch.cuda.device(device):
-        return call(*args)
 
 
 def pace_layer_norm_backward_workspace_bytes(n_rows: int, n_cols: int) -> int:
@@ -859,7 +880,7 @@ def pace_layer_norm(x, weight=None, bias=None, eps: float = 1e-5, buffers=None, 
     out, stats = buffers["out"], buffers["stats"]
     o, _, _, _, out_stride, _ = of.matrix(out, "out", 1 << dt, at, n, k)
     s, _, _ = of.vector(stats, "stats", _F32, at, 2 * n)
-    _check(_on(at, lib().pace_layer_norm, p, dt, n, k, stride, w, b, wt, eps, o, out_stride, s, _stream(x.device, stream)), "pace_layer_norm")
+    _check(_at(at).pace_layer_norm(p, dt, n, k, stride, w, b, wt, eps, o, out_stride, s, _stream(x.device, stream)), "pace_layer_norm")
     return out, stats
 
 
@@ -882,8 +903,8 @@ def pace_layer_norm_backward(x, stats, grad_out, weight=None, buffers=None, stre
     gw, _, _ = of.vector(grad_weight, "grad_weight", _F32, at, k)
     gb, _, _ = of.vector(grad_bias, "grad_bias", _F32, at, k)
     ws, _, ws_bytes = of.vector(buffers["workspace"], "workspace", _UINT8, at, -1)
-    _check(_on(at, lib().pace_layer_norm_backward, p, dt, n, k, stride, w, wt, s, g, grad_stride, o, out_stride, gw, gb, ws, ws_bytes,
-                                          _stream(x.device, stream)), "pace_layer_norm_backward")
+    _check(_at(at).pace_layer_norm_backward(p, dt, n, k, stride, w, wt, s, g, grad_stride, o, out_stride, gw, gb, ws, ws_bytes,
+                                            _stream(x.device, stream)), "pace_layer_norm_backward")
     return grad_x, grad_weight, grad_bias
 
 
@@ -917,7 +938,7 @@ def pace_grad_norm(grads, max_norm: float = float("inf"), buffers=None, stream=N
     out, _, _ = of.vector(norm, "norm", _F32, at, 1)
     clip, _, _ = of.vector(factor, "factor", _F32, at, 1)
     ws, _, ws_bytes = of.vector(b["workspace"], "workspace", _UINT8, at, -1)
-    _check(_on(at, lib().pace_grad_norm, n, ptrs, codes, sizes, max_norm, out, clip, ws, ws_bytes, _stream(norm.device, stream)), "pace_grad_norm")
+    _check(_at(at).pace_grad_norm(n, ptrs, codes, sizes, max_norm, out, clip, ws, ws_bytes, _stream(norm.device, stream)), "pace_grad_norm")
     return norm, factor
 
 
@@ -985,9 +1006,9 @@ def pace_adamw(params, grads, state, lr: float = 1e-3, step: int = 1, betas=(0.9
     factor = None if grad_scale is None else _lib.lists().vector(grad_scale, "grad_scale", _F32, at, 1)[0]
     rates = None if schedule is None else _lib.lists().vector(schedule, "schedule", _F64, at, 2)[0]
     hyper = AdamwParams(float(lr), float(betas[0]), float(betas[1]), float(eps), int(step))
-    _check(_on(at, lib().pace_adamw, n, sizes, p[2], types, g[2], g[3], bits, m[2], v[2], _pointers(scales), _pointers(copies),
-               None if copies is None else copies[3], decay.tobytes(), ctypes.byref(hyper), factor, rates,
-               _stream(torch.device("cuda", at), stream)), "pace_adamw")
+    _check(_at(at).pace_adamw(n, sizes, p[2], types, g[2], g[3], bits, m[2], v[2], _pointers(scales), _pointers(copies),
+                              None if copies is None else copies[3], decay.tobytes(), ctypes.byref(hyper), factor, rates,
+                              _stream(torch.device("cuda", at), stream)), "pace_adamw")
     _lib.wrote(ts, state["copies"])                    # not the moments, which no graph saves: 12 ns a tensor
     return params
 
@@ -1005,7 +1026,7 @@ def pace_adamw_unpack(state, out=None, stream=None):
         out = [[e(t.shape, torch.float32) for t in state["exp_avg"]] for _ in range(2)]
     m_out, v_out = (_each(o, "out", _F32, at, True, sizes) for o in out)
     _lib.lists().apart(("exp_avg", "exp_avg_sq", "scale", "out[0]", "out[1]"), (m, v, scales, m_out, v_out))
-    _check(_on(at, lib().pace_adamw_unpack, n, sizes, *map(_pointers, (m, v, scales, m_out, v_out)), _stream(dev, stream)), "pace_adamw_unpack")
+    _check(_at(at).pace_adamw_unpack(n, sizes, *map(_pointers, (m, v, scales, m_out, v_out)), _stream(dev, stream)), "pace_adamw_unpack")
     return out[0], out[1]
 
 
