@@ -945,7 +945,12 @@ def pace_grad_norm(grads, max_norm: float = float("inf"), buffers=None, stream=N
 def adamw_state(params, bits: int = 32, copy_dtype=None, stream=None):
     """Fresh moments for pace_adamw of these tensors: zeros, in float32 or with ``bits`` 8 as codes with two scales for every
     ADAMW_BLOCK elements. With copy_dtype (bfloat16 or float16) each step writes the new parameters in that type too; before
-    the first, and where it is left out, the copies are the parameters as they are now."""
+    the first, and where it is left out, the copies are the parameters as they are now.
+
+    With bits 8 give pace_adamw betas whose second is at most 0.95. Codes are rounded to the nearest, and at its default of
+    0.999 a second moment whose gradients have become smaller than others of its block never shrinks: its root was 9 times
+    what 32 bits hold 5000 steps after a fall to a tenth, and steps as much too small. At 0.95 that is so below 2.3% of the
+    block's largest root only (0.99: 61%, 0.98: 15%, 0.9: 0.6%)."""
     ts = list(params)
     dev = torch.device("cuda", _each(ts, "params", _FLOATS)[1])
     if bits not in (32, 8):
@@ -990,7 +995,7 @@ def pace_adamw(params, grads, state, lr: float = 1e-3, step: int = 1, betas=(0.9
     the number of this update, from 1. weight_decay: a number, or one for each tensor. grad_scale (f32[1], pace_grad_norm's
     factor) multiplies the gradients; where it is no number nothing changes. schedule (f64[2] on the device: lr, step) stands
     in for lr and step in calls that are captured and replayed. With moments in 8 bits eps is 2^-55 / sqrt(1 - betas[1]) at
-    least. Params and copies count as changed in place: a pending backward pass that saved one raises. Returns params."""
+    least, and betas[1] better no more than 0.95 (adamw_state). Params and copies count as changed in place: a pending backward pass that saved one raises. Returns params."""
     ts = params if isinstance(params, (list, tuple)) else list(params)
     p = _each(ts, "params", _FLOATS, written=True)
     n, at, _, types, sizes, _ = p

@@ -1,4 +1,5 @@
-"""CPU test of a fresh AdamW state: its moments are zeros, its copies the parameters in the copies' type."""
+"""CPU tests of a fresh AdamW state, its moments zeros and its copies the parameters in the copies' type, and of what moments
+in 8 bits hold over many steps."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -27,3 +28,28 @@ def test_copies_of_a_fresh_state_are_the_parameters(monkeypatch, bits, dtype):
         assert copy.dtype == dtype and torch.equal(copy, p.detach().to(dtype)) and not copy.requires_grad
     assert not any(t.any() for k in ("exp_avg", "exp_avg_sq") for t in state[k])
     assert bits == 32 or not any(t.any() for t in state["scale"])
+
+
+@pytest.mark.parametrize("beta2, code, share", [(0.9, 19, 0.006), (0.95, 39, 0.023), (0.98, 99, 0.151), (0.99, 199, 0.61), (0.9921, 252, 0.98),
+                                                (0.9922, 255, 1.0), (0.999, 255, 1.0)])
+def test_second_moments_that_stay(beta2, code, share):
+    """The largest code that a shrinking v keeps while its block's largest stays, and what its root is of the largest root."""
+    stays = [c for c in range(1, 256) if round(255 * (beta2 * (c / 255) ** 4) ** 0.25) == c]
+    assert stays == list(range(1, code + 1)) and abs((code / 255) ** 2 - share) < 0.006
+
+
+@pytest.mark.parametrize("beta2, low, high", [(0.9, 0.93, 1.07), (0.95, 0.93, 1.07), (0.98, 0.9, 1.1), (0.99, 0.9, 1.16), (0.999, 8.0, 10.0)])
+def test_second_moments_after_gradients_fell(beta2, low, high):
+    """Half of a block's random gradients fall to a tenth: their roots beside those held in 64 bits, 5000 steps later."""
+    import numpy as np
+    r = np.random.default_rng(0)
+    scale, codes, ref, half = 0.0, np.zeros(256), np.zeros(256), np.arange(256) < 128
+    for t in range(7000):
+        g = r.standard_normal(256)
+        g = np.where(half, g / 10, g) if t >= 2000 else g
+        v = beta2 * ((codes / 255) ** 4 * scale) + (1 - beta2) * g * g
+        codes = np.rint(255 * np.sqrt(np.sqrt(v / v.max())))
+        codes, scale = np.where((v > 0) & (codes < 1), 1, codes), float(np.float32(v.max()))
+        ref = beta2 * ref + (1 - beta2) * g * g
+    root = (codes / 255) ** 2 * scale ** 0.5 / np.sqrt(ref)
+    assert low < np.percentile(root[half], 5) and np.percentile(root[half], 95) < high
