@@ -995,7 +995,8 @@ def pace_adamw(params, grads, state, lr: float = 1e-3, step: int = 1, betas=(0.9
     the number of this update, from 1. weight_decay: a number, or one for each tensor. grad_scale (f32[1], pace_grad_norm's
     factor) multiplies the gradients; where it is no number nothing changes. schedule (f64[2] on the device: lr, step) stands
     in for lr and step in calls that are captured and replayed. With moments in 8 bits eps is 2^-55 / sqrt(1 - betas[1]) at
-    least, and betas[1] better no more than 0.95 (adamw_state). Params and copies count as changed in place: a pending backward pass that saved one raises. Returns params."""
+    least, and betas[1] better no more than 0.95 (adamw_state). Params and copies count as changed in place: a pending backward
+    pass that saved one raises. Returns params."""
     ts = params if isinstance(params, (list, tuple)) else list(params)
     p = _each(ts, "params", _FLOATS, written=True)
     n, at, _, types, sizes, _ = p

@@ -121,49 +121,63 @@ struct Span {      // of bytes that a list's tensors have
     bool operator<(const Span &other) const { return first < other.first; }
 };
 
-// Adds what the tensors of a list, as read() gives it, have: in order, and as one where they touch or overlap each other.
-bool add_spans(PyObject *read, Py_ssize_t list, std::vector<Span> &spans) {
-    if (PyTuple_GET_SIZE(read) != 6) return false;
-    for (int k = 2; k < 5; ++k)
-        if (!PyBytes_Check(PyTuple_GET_ITEM(read, k))) return false;
-    const auto size = [&](int k) { return (size_t)PyBytes_GET_SIZE(PyTuple_GET_ITEM(read, k)); };
-    const size_t n = size(2) / sizeof(uintptr_t), from = spans.size();
-    if (size(3) != n * sizeof(int32_t) || size(4) != n * sizeof(int64_t)) return false;
-    const char *pointers = PyBytes_AS_STRING(PyTuple_GET_ITEM(read, 2)), *codes = PyBytes_AS_STRING(PyTuple_GET_ITEM(read, 3)),
-               *sizes = PyBytes_AS_STRING(PyTuple_GET_ITEM(read, 4));
-    static const uintptr_t width[] = {4, 2, 2, 1, 1, 8};
-    bool in_order = true;
-    for (size_t k = 0; k < n; ++k) {
-        uintptr_t p;
-        int32_t code;
-        int64_t elements;
-        std::memcpy(&p, pointers + k * sizeof p, sizeof p);
-        std::memcpy(&code, codes + k * sizeof code, sizeof code);
-        std::memcpy(&elements, sizes + k * sizeof elements, sizeof elements);
-        if (code < 0 || code > 5 || elements < 0) return false;
-        if (elements == 0) continue;
-        const uintptr_t end = p + (uintptr_t)elements * width[code];
-        if (spans.size() > from && p == spans.back().end) {
-            spans.back().end = end;
-            continue;
-        }
-        in_order = in_order && (spans.size() == from || p > spans.back().end);
-        spans.push_back({p, end, list});
+// A list as read() gives it; `n` below 0 where it is none.
+struct ReadList {
+    Py_ssize_t n = -1, number;
+    const char *pointers, *codes, *sizes;
+    ReadList(PyObject *read, Py_ssize_t number) : number(number) {
+        if (PyTuple_GET_SIZE(read) != 6) return;
+        for (int k = 2; k < 5; ++k)
+            if (!PyBytes_Check(PyTuple_GET_ITEM(read, k))) return;
+        const auto size = [&](int k) { return (size_t)PyBytes_GET_SIZE(PyTuple_GET_ITEM(read, k)); };
+        const size_t count = size(2) / sizeof(uintptr_t);
+        if (size(3) != count * sizeof(int32_t) || size(4) != count * sizeof(int64_t)) return;
+        pointers = PyBytes_AS_STRING(PyTuple_GET_ITEM(read, 2));
+        codes = PyBytes_AS_STRING(PyTuple_GET_ITEM(read, 3));
+        sizes = PyBytes_AS_STRING(PyTuple_GET_ITEM(read, 4));
+        n = (Py_ssize_t)count;
     }
-    if (in_order) return true;
-    std::sort(spans.begin() + (std::ptrdiff_t)from, spans.end());
+    // f(first byte, end) of each tensor that is not empty; false where there is no such type or size.
+    template <typename F>
+    bool each(F f) const {
+        static const uintptr_t width[] = {4, 2, 2, 1, 1, 8};
+        for (Py_ssize_t k = 0; k < n; ++k) {
+            uintptr_t p;
+            int32_t code;
+            int64_t elements;
+            std::memcpy(&p, pointers + k * sizeof p, sizeof p);
+            std::memcpy(&code, codes + k * sizeof code, sizeof code);
+            std::memcpy(&elements, sizes + k * sizeof elements, sizeof elements);
+            if (code < 0 || code > 5 || elements < 0) return false;
+            if (elements > 0) f(p, p + (uintptr_t)elements * width[code]);
+        }
+        return n >= 0;
+    }
+};
+
+// Whether spans in order are apart; `at` is the first of two that are not.
+bool in_order_apart(const std::vector<Span> &spans, size_t &at) {
+    for (at = 0; at + 1 < spans.size(); ++at)
+        if (spans[at + 1].first < spans[at].end) return false;
+    return true;
+}
+
+// Adds what a list's tensors have: in order, and as one where they touch or overlap each other.
+void add_spans(const ReadList &list, std::vector<Span> &spans) {
+    const size_t from = spans.size();
+    list.each([&](uintptr_t p, uintptr_t end) { spans.push_back({p, end, list.number}); });
+    const auto begin = spans.begin() + (std::ptrdiff_t)from;
+    if (!std::is_sorted(begin, spans.end())) std::sort(begin, spans.end());
     size_t to = from;
     for (size_t k = from; k < spans.size(); ++k) {
         if (to > from && spans[k].first <= spans[to - 1].end) spans[to - 1].end = std::max(spans[to - 1].end, spans[k].end);
         else spans[to++] = spans[k];
     }
     spans.resize(to);
-    return true;
 }
 
 // Sorts spans whose runs, from each of `starts` to the next, are in order.
 void merge_runs(std::vector<Span> &spans, std::vector<size_t> starts) {
-    if (std::is_sorted(spans.begin(), spans.end())) return;
     std::vector<Span> other(spans.size());
     for (; starts.size() > 1; spans.swap(other)) {
         std::vector<size_t> next;
@@ -184,27 +198,44 @@ PyObject *apart(PyObject *, PyObject *args) try {
     const Py_ssize_t n = PyTuple_GET_SIZE(lists);
     if (PyTuple_GET_SIZE(names) != n) return fail("as many names as lists are wanted");
     Py_ssize_t size = -1;
+    std::vector<ReadList> read;
     std::vector<Span> spans;
-    std::vector<size_t> starts;
-    spans.reserve(512);
     for (Py_ssize_t a = 0; a < n; ++a) {
         PyObject *list = PyTuple_GET_ITEM(lists, a);
         if (!PyUnicode_Check(PyTuple_GET_ITEM(names, a))) return fail("names are wanted");
         if (list == Py_None) continue;
         if (PyTuple_Check(list)) {
-            starts.push_back(spans.size());
-            if (!add_spans(list, a, spans)) return fail("lists must be as they were read");
+            // From the first byte of any to the last: lists of one buffer each are told apart by these.
+            Span all{UINTPTR_MAX, 0, a};
+            read.emplace_back(list, a);
+            if (!read.back().each([&](uintptr_t p, uintptr_t end) { all.first = std::min(all.first, p), all.end = std::max(all.end, end); }))
+                return fail("lists must be as they were read");
+            if (all.end > 0) spans.push_back(all);
             continue;
         }
         if (!PyBytes_Check(list)) return fail("bytes are wanted");
         if (size >= 0 && PyBytes_GET_SIZE(list) != size) return fail("lists must be as long as each other");
         size = PyBytes_GET_SIZE(list);
     }
-    merge_runs(spans, std::move(starts));
-    for (size_t k = 1; k < spans.size(); ++k)
-        if (spans[k].first < spans[k - 1].end)
-            return PyErr_Format(PyExc_ValueError, "%U and %U must not overlap each other", PyTuple_GET_ITEM(names, std::min(spans[k - 1].list, spans[k].list)),
-                                PyTuple_GET_ITEM(names, std::max(spans[k - 1].list, spans[k].list)));
+    std::sort(spans.begin(), spans.end());
+    size_t at = 0;
+    if (!in_order_apart(spans, at)) {
+        std::vector<size_t> starts;
+        size_t total = 0;
+        for (const ReadList &list : read) total += (size_t)list.n;
+        spans.clear();
+        spans.reserve(total);
+        for (const ReadList &list : read) {
+            starts.push_back(spans.size());
+            add_spans(list, spans);
+        }
+        merge_runs(spans, std::move(starts));
+        if (!in_order_apart(spans, at)) {
+            const Py_ssize_t x = spans[at].list, y = spans[at + 1].list;
+            return PyErr_Format(PyExc_ValueError, "%U and %U must not overlap each other", PyTuple_GET_ITEM(names, std::min(x, y)),
+                                PyTuple_GET_ITEM(names, std::max(x, y)));
+        }
+    }
     for (Py_ssize_t a = 0; a < n; ++a)
         for (Py_ssize_t b = a + 1; b < n; ++b) {
             PyObject *x = PyTuple_GET_ITEM(lists, a), *y = PyTuple_GET_ITEM(lists, b);
