@@ -563,7 +563,7 @@ int pace_orthogonalize(const void *update, int dtype, int64_t batch, int64_t row
  * eps         [host] 1e-30 .. 1e30
  * stats_out   f32 [n_rows, 2] or NULL: mu and rstd, which the backward pass takes
  * Statistics are binary32, the variance from differences to the mean, with the
- * mean's own rounding made good. An infinity or a NaN spoils its own row (and the
+ * mean's own rounding made good; the inverse root is within a unit of 2^-23. An infinity or a NaN spoils its own row (and the
  * sums down the columns that pace_layer_norm_backward takes); so may elements beyond
  * 2^60, whose squares' sum leaves binary32. out must not be x. */
 int pace_layer_norm(const void *x, int dtype, int64_t n_rows, int64_t n_cols, int64_t row_stride, const void *weight,
@@ -613,7 +613,8 @@ int pace_grad_norm(int64_t n_tensors, const void *const *grads, const int32_t *g
  * grad_scale and t = step, for every element:
  *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2
  *   p <- p (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps)
- * computed in binary32 and rounded to the parameter's type once.
+ * computed in binary32, root and quotient within a unit of 2^-23 each, and rounded to the
+ * parameter's type once.
  * params, grads: of param_dtypes and grad_dtypes, which may differ
  * state_bits 32: exp_avg (m) and exp_avg_sq (v) are f32, scales is not read
  * state_bits 8: every PACE_ADAMW_BLOCK consecutive elements of a tensor (its last may

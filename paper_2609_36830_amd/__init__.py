@@ -853,7 +853,8 @@ def pace_layer_norm_backward_workspace_bytes(n_rows: int, n_cols: int) -> int:
 
 def layer_norm_buffers(n_rows: int, n_cols: int, dtype, device, backward: bool = False, stream=None):
     """Outputs for repeated pace_layer_norm calls on rows of one shape (pass as ``buffers``); with ``backward`` those of
-    pace_layer_norm_backward and its workspace too."""
+    pace_layer_norm_backward and its workspace too. The next call writes them over, and torch is not told: what a pending
+    backward pass has saved of them has to be a copy."""
     e = _allocator(device, stream)
     b = dict(out=e((n_rows, n_cols), dtype), stats=e((n_rows, 2), torch.float32))
     if backward:

@@ -24,10 +24,10 @@
 // runs of four: two blocks of 256, each by half a wave, so that a block's largest is five
 // steps for eight elements of a lane (with a wave a block, six for four, and the library's
 // square roots and divisions, the step in 8 bits was bound by its instructions: 787 us for 550).
-// 201M elements of that kind take 937 us (6.0 TB/s; a device copy 4.6, an addition in
-// place 5.9) and 548 (5.9 TB/s) with moments in 8 bits, their unpacking 350, the
-// norm 66 (bfloat16, 6.1 TB/s). Small calls are launches: 96 vectors of 4096 are 2.7 + 4.6
-// us for the norm and 3.8 + 3.4 for the step, in two tables.
+// 201M elements of that kind take 945 us (6.0 TB/s; a device copy 4.6, an addition in
+// place 5.9) and 540 (6.0 TB/s) with moments in 8 bits, their unpacking 354, the
+// norm 66 (bfloat16, 6.1 TB/s). Small calls are launches: 96 vectors of 4096 are 2.8 + 1.9
+// us for the norm and 3.7 + 3.5 for the step, in two tables.
 #include "elem.hpp"
 #include "kernels.hpp"
 
@@ -385,9 +385,10 @@ struct Adam8 {
         const bool bad = (uint32_t)(spoilt >> (lane_id() & 32)) != 0;
         const float m_new = new_scale(m_most, bad), v_new = new_scale(v_most, bad);
 
-        // Codes from roots in binary32. 127 sqrt(|m| / M): roundings of m, of 1 / M and of their product, halved, a unit of 2^-23 of
-        // the root and a rounding of the product with 127, 4.5 x 2^-24 x 127 = 2^-14.8 in all; 255 sqrt(sqrt(v) / sqrt(V)): a unit
-        // of each root and two roundings, halved, a unit and a rounding, 5.5 x 2^-24 x 255 = 2^-13.5.
+        // Codes from roots in binary32. 127 sqrt(|m| / M): roundings of m, of M, of 1 / M and of their product, halved, a unit of 2^-23
+        // of the root and a rounding of the product with 127, 5 x 2^-24 x 127 = 2^-14.6 in all; 255 sqrt(sqrt(v) / sqrt(V)): the
+        // roundings of v and V, halved, a unit of one root and a rounding of the other, of its inverse and of the product, all of
+        // that halved, a unit and a rounding, 6 x 2^-24 x 255 = 2^-13.4.
         constexpr float kNearM = 0.5f - 0x1p-14f, kNearV = 0.5f - 0x1p-13f;
         const float m_inv = 1.0f / m_new, v_inv = 1.0f / sqrtf(v_new);
         float cm[kN], cv[kN], far_m = 0.0f, far_v = 0.0f, least = 1.0f;

@@ -17,10 +17,11 @@
 // the rows that its workgroup takes, in binary32, at most kLnChain of them one
 // after the other; the workgroups' sums are added by a second kernel, in their order.
 //
-// 16384 rows of 4096 in bfloat16 take 53 us forward (5.1 TB/s; a device copy 4.6 to 5.4)
-// and 79 to 82 backward (4.9 to 5.1, with 5 us of the second kernel), 4099 of them 13.2 and 29,
-// 2047 of 16384 in binary16 26 and 52 (the column sums of 256 workgroups are 34 MB there,
-// written and read), 131077 of 128 12 and 24. One row of 4096 is 2.6 us on the card.
+// By itself, over three inputs in rotation: 16384 rows of 4096 in bfloat16 take 54 us forward
+// (5.0 TB/s; a device copy 4.6 to 5.4) and 80 to 83 backward (4.8 to 5.1, with 5 us of the second
+// kernel), 4099 of them 13 and 28, 2047 of 16384 in binary16 27 and 53 (the column sums of 256
+// workgroups are 34 MB there, written and read), 131077 of 128 12 and 23. One row of 4096 is 2.7 us on
+// the card. Wider rows are not worked on yet: 3300 of 20000 in bfloat16 267 and 350.
 // Forward, a lane's reductions and its row's root cost as much as its 16 elements: with the
 // library's square root and division, and each sum gathered by four lanes' reads, 20
 // instructions an element kept the vector units 77% busy (4099 x 4096 14.8 us for 13.2).
