@@ -128,6 +128,7 @@ class Trainer:
         if self.norm is not None:
             _, *grads = pace.pace_layer_norm_backward(states, norm_stats, grad_logits @ head, self.norm[0])
             clipped_norm, factor = pace.pace_grad_norm(grads, self.max_norm, buffers=self.clip)
+            # The default betas do for the few steps here; longer runs with moments in 8 bits want betas=(0.9, 0.95).
             pace.pace_adamw(self.norm, grads, self.norm_state, lr=self.norm_lr, step=self.version + 1, grad_scale=factor)
             more = dict(grad_norm=grads, grad_size=float(clipped_norm))
         self.velocity.mul_(self.momentum).add_(grad_head)
